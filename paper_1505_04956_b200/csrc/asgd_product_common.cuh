@@ -1,0 +1,177 @@
+// Shared by the two kernels of asgd_product: parameters, wrappers of the tensor-core and copy instructions, bounded
+// waits, and the tiles of C that persistent blocks take in turn.
+#pragma once
+
+#include "asgd_experts_common.cuh"
+
+#include <cuda.h>
+
+#include "asgd_stream.cuh"   // mbarrier helpers
+
+namespace {
+
+using namespace asgd::experts;
+using asgd::mbar_expect_tx;
+using asgd::mbar_init;
+using asgd::mbar_try_wait;
+using asgd::smem_u32;
+
+__device__ int g_status;                             // what asgd_experts_sync reports: the smallest (worst) code seen
+constexpr int kKB = 128;                             // numbers (bytes) of a K block: a 128-byte swizzled row
+constexpr size_t kSmemLimit = 227 * 1024;
+
+struct Params {
+  int M, N, K, groups, inner, kblocks;
+  int tiles_n;                                       // tiles of C along a row
+  const float *sa, *sb;
+  long long sa_row, sa_block, sb_row, sb_block, sb_group;
+  int sb_shift;
+  void* c;
+  long long ldc, c_group;
+  int c_type;
+  const int* offsets;
+  unsigned idesc, wait_limit;
+  int withhold;
+};
+
+// ---- tensor-core and copy wrappers ----
+
+__device__ inline void tma_load_3d(void* dst, const CUtensorMap* map, int x, int y, int z, unsigned long long* bar) {
+  asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+               ::"r"(smem_u32(dst)), "l"(map), "r"(x), "r"(y), "r"(z), "r"(smem_u32(bar)) : "memory");
+}
+// K-major rows of 128 bytes, 128-byte swizzle, 8-row groups 1024 bytes apart
+__device__ inline unsigned long long operand_desc(const void* smem) {
+  return (unsigned long long)((smem_u32(smem) & 0x3FFFFu) >> 4) | 1ull << 16 | (unsigned long long)(1024 >> 4) << 32 | 1ull << 46 | 2ull << 61;
+}
+__device__ inline void mma_f8(unsigned d_tmem, unsigned long long a, unsigned long long b, unsigned idesc, bool acc) {
+  asm volatile("{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n}"
+               ::"r"(d_tmem), "l"(a), "l"(b), "r"(idesc), "r"((unsigned)acc) : "memory");
+}
+__device__ inline void commit(unsigned long long* bar) {
+  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
+}
+__device__ inline void arrive(unsigned long long* bar) {
+  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_u32(bar)) : "memory");
+}
+__device__ inline void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ inline void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ inline void copy4(float* dst, const float* src, bool there) {       // asynchronous; zero where not there
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(smem_u32(dst)), "l"(src), "r"(there ? 4 : 0) : "memory");
+}
+__device__ inline void arrive_after_copies(unsigned long long* bar) {
+  asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
+}
+// 16 columns of the warp's 32 accumulator rows
+__device__ inline void tmem_load16(unsigned taddr, float (&v)[16]) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+               : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]), "=f"(v[8]), "=f"(v[9]),
+                 "=f"(v[10]), "=f"(v[11]), "=f"(v[12]), "=f"(v[13]), "=f"(v[14]), "=f"(v[15]) : "r"(taddr) : "memory");
+}
+__device__ inline void tmem_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+
+// A bounded wait that also ends when another warp of the block gave up.
+__device__ inline bool wait(unsigned long long* bar, unsigned parity, unsigned limit, int* abort) {
+  for (unsigned it = 0; it < limit; ++it) {
+    if (mbar_try_wait(bar, parity)) return true;
+    if ((it & 63u) == 63u && *reinterpret_cast<volatile int*>(abort)) return false;
+  }
+  *reinterpret_cast<volatile int*>(abort) = 1;
+  return false;
+}
+
+__device__ inline void store_c(void* c, int type, long long at, float v) {
+  if (type == ASGD_F32) reinterpret_cast<float*>(c)[at] = v;
+  else if (type == ASGD_BF16) reinterpret_cast<__nv_bfloat16*>(c)[at] = __float2bfloat16_rn(v);
+  else reinterpret_cast<__half*>(c)[at] = __float2half_rn(v);
+}
+
+// ---- tiles ----
+
+struct Tile {
+  int g, n0, m0, m_end, kb0, kb1;                    // group, first column and row of C, end of the group's rows, K blocks
+  int k_end;                                         // end of the inner dimension
+  bool bad;                                          // inner groups whose bounds cut a block
+};
+
+__device__ inline void group_bounds(const Params& p, int g, int limit, int& lo, int& hi) {
+  lo = 0; hi = limit;
+  if (p.offsets) {
+    lo = min(max(p.offsets[g], 0), limit);
+    hi = min(max(p.offsets[g + 1], lo), limit);
+  }
+}
+
+// prefix[g]: tiles of the groups before g, for tiles of bm rows.  All threads of the block; ends with a barrier.
+__device__ inline void count_tiles(const Params& p, int bm, int* prefix, int* warp_part) {
+  const int G = max(p.groups, 1), tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
+  const int per = (G + blockDim.x - 1) / blockDim.x;
+  int mine = 0;
+  for (int q = 0; q < per; ++q) {
+    const int g = tid * per + q;
+    if (g >= G) break;
+    int lo = 0, hi = p.M;
+    if (p.groups && !p.inner) group_bounds(p, g, p.M, lo, hi);
+    const int n = (hi - lo + bm - 1) / bm * p.tiles_n;
+    prefix[g] = n;
+    mine += n;
+  }
+  int inc = mine;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) { const int v = __shfl_up_sync(kAll, inc, o); if (lane >= o) inc += v; }
+  if (lane == 31) warp_part[wid] = inc;
+  __syncthreads();
+  int before = 0;
+  for (int w = 0; w < wid; ++w) before += warp_part[w];
+  int run = before + inc - mine;
+  for (int q = 0; q < per; ++q) {
+    const int g = tid * per + q;
+    if (g >= G) break;
+    const int n = prefix[g];
+    prefix[g] = run;
+    run += n;
+    if (g == G - 1) prefix[G] = run;
+  }
+  __syncthreads();
+}
+
+// Tile number `tile` of tiles of bm x bn.  Inside a group the tiles run down bands of `band` tile rows, column after
+// column: neighbouring blocks share operands in L2.
+__device__ inline Tile find_tile(const Params& p, int bm, int bn, int band, const int* prefix, int tile) {
+  Tile t;
+  int a = 0, b = max(p.groups, 1);
+  while (b - a > 1) {                                // the last group that starts at or before the tile
+    const int m = (a + b) >> 1;
+    if (prefix[m] <= tile) a = m; else b = m;
+  }
+  t.g = a;
+  int lo = 0, hi = p.M;
+  if (p.groups && !p.inner) group_bounds(p, a, p.M, lo, hi);
+  const int rows = (hi - lo + bm - 1) / bm;
+  int at = tile - prefix[a], first = 0, high = rows;
+  if (rows > band) {
+    first = at / (band * p.tiles_n) * band;
+    at -= first * p.tiles_n;
+    high = min(band, rows - first);
+  }
+  t.n0 = at / high * bn;
+  t.m0 = lo + (first + at % high) * bm;
+  t.m_end = hi;
+  t.kb0 = 0; t.kb1 = p.kblocks;
+  t.k_end = p.K;
+  t.bad = false;
+  if (p.inner) {
+    group_bounds(p, a, p.K, lo, hi);
+    t.kb0 = lo / kKB;
+    t.kb1 = hi > lo ? (hi + kKB - 1) / kKB : t.kb0;
+    t.k_end = hi;
+    t.bad = hi > lo && (lo % kKB || (hi % kKB && hi != p.K));
+    if (t.bad) t.kb1 = t.kb0;
+  }
+  return t;
+}
+
+// instructions of 32 numbers that K block kb takes (the last block of the inner dimension may be short)
+__device__ inline int steps_of(const Tile& t, int kb) { return min(4, (t.k_end - kb * kKB + 31) >> 5); }
+
+}  // namespace

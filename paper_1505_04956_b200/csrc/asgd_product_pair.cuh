@@ -1,0 +1,312 @@
+// The kernel of asgd_product for many rows of A (per group): a pair of thread blocks on neighbouring SMs takes a tile of
+// 256 x 256 numbers of C.
+//
+// tcgen05.mma of a pair (cta_group::2) multiplies 256 rows of A by 256 rows of B; each SM holds half of either operand
+// (128 rows of A, its rows of C; 128 rows of B, of which both SMs' tensor cores read both halves), so a K block of 128
+// costs an SM 32 KB of shared memory and of L2 traffic where a single SM's 128 x 256 tile would cost 48 KB.
+//
+// Warp roles in each block: 0 issues the TMA loads of the block's halves, which all report to the first block's barrier;
+// 1 and 3, in the first block, issue the products and commit each K block to a barrier in both blocks, which says "the slot
+// is free" to the copies and "the accumulator is full" to the readers; 2 brings the column scales where they differ from
+// column to column; 4 to 11 read the accumulators, a row of C per thread and 128 columns per warp, and add them, scaled,
+// to sums in registers.  Warps 0 to 3 hand most of their registers to these.  A row's scale and, with 128 x 128 blocks of
+// B, the columns' scale are one number per thread, so that a product of the K block costs one multiply-add.
+#pragma once
+
+#include "asgd_product_common.cuh"
+
+namespace {
+
+constexpr int kPairRows = 256, kPairCols = 256;      // of C, per pair
+constexpr int kHalf = 128;                           // rows of either operand per block
+constexpr int kPairThreads = 384;
+constexpr int kPairSlots = 6;                        // even: a slot always meets the same issuing thread, see below
+constexpr int kPairBand = 8;                         // tile rows that neighbouring pairs run down before the next column
+constexpr unsigned kHalfBytes = kHalf * kKB, kPairBytes = 2 * kHalfBytes;      // per block: one operand, a slot
+constexpr int kStageBytes = 32 * 64;                 // per warp: 64 bytes of each of its 32 rows, on the way to C
+enum { P_FULL = 0, P_DONE = kPairSlots, P_SFULL = 2 * kPairSlots, P_SEMPTY = 3 * kPairSlots, P_ACCEMPTY = 4 * kPairSlots,
+       P_DRAIN = P_ACCEMPTY + 2, P_COUNT = P_DRAIN + 2 };
+constexpr size_t kPairSmem = 1024 + (size_t)kPairSlots * kPairBytes + 8 * kStageBytes + (size_t)kPairSlots * kPairCols * 4 +
+                             P_COUNT * 8 + (ASGD_MAX_EXPERTS + 1 + 32) * 4 + 64;
+static_assert(kPairSmem <= kSmemLimit, "shared memory");
+
+__device__ inline unsigned in_first_block(const void* smem) {                  // the same place in the pair's first block
+  unsigned r;
+  asm("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(r) : "r"(smem_u32(smem)));
+  return r;
+}
+__device__ inline unsigned rank_in_pair() {
+  unsigned r;
+  asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+  return r;
+}
+__device__ inline void pair_sync() {
+  asm volatile("barrier.cluster.arrive.release;\nbarrier.cluster.wait.acquire;" ::: "memory");
+}
+// the block's own half; the bytes are counted at a barrier of the pair's first block
+__device__ inline void tma_load_pair(void* dst, const CUtensorMap* map, int x, int y, int z, unsigned bar) {
+  asm volatile("cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+               ::"r"(smem_u32(dst)), "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar) : "memory");
+}
+__device__ inline void mma_f8_pair(unsigned d_tmem, unsigned long long a, unsigned long long b, unsigned idesc, bool acc) {
+  asm volatile("{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::2.kind::f8f6f4 [%0], %1, %2, %3, p;\n}"
+               ::"r"(d_tmem), "l"(a), "l"(b), "r"(idesc), "r"((unsigned)acc) : "memory");
+}
+__device__ inline void commit_pair(unsigned long long* bar) {                  // at the same place in both blocks
+  asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
+               ::"r"(smem_u32(bar)), "h"((unsigned short)3) : "memory");
+}
+// No release at cluster scope: what is handed over is tensor memory (ordered by the tcgen05 fence before), and such a
+// release would wait for the warp's loads in flight, about 1000 cycles of every K block.
+__device__ inline void arrive_cluster(unsigned bar) {
+  asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+__device__ inline void complete_tx(unsigned long long* bar, unsigned bytes) {  // bytes that will not come
+  asm volatile("mbarrier.complete_tx.relaxed.cluster.shared::cta.b64 [%0], %1;" ::"r"(smem_u32(bar)), "r"(bytes) : "memory");
+}
+__device__ inline void store_cluster(unsigned addr, unsigned v) {
+  asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(addr), "r"(v) : "memory");
+}
+// 32 columns of the warp's 32 accumulator rows
+__device__ inline void tmem_load32(unsigned taddr, float (&v)[32]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+      : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]), "=f"(v[8]), "=f"(v[9]), "=f"(v[10]),
+        "=f"(v[11]), "=f"(v[12]), "=f"(v[13]), "=f"(v[14]), "=f"(v[15]), "=f"(v[16]), "=f"(v[17]), "=f"(v[18]), "=f"(v[19]), "=f"(v[20]),
+        "=f"(v[21]), "=f"(v[22]), "=f"(v[23]), "=f"(v[24]), "=f"(v[25]), "=f"(v[26]), "=f"(v[27]), "=f"(v[28]), "=f"(v[29]), "=f"(v[30]), "=f"(v[31])
+      : "r"(taddr) : "memory");
+}
+
+// A warp's 32 rows x 128 columns to C: 64 bytes of every row at a time through the warp's stage (pieces of 16 bytes
+// exchanged by row, so that neither side meets a bank twice), then whole pieces, eight rows per access.
+template <typename T> __device__ __forceinline__ void store_rows(const float (&acc)[128], unsigned char* stage, T* c, long long ldc, int rows, int cols, int lane) {
+  constexpr int per = 64 / (int)sizeof(T), piece = 16 / (int)sizeof(T);        // numbers per pass, per piece
+  const bool whole = ((reinterpret_cast<unsigned long long>(c) | ((unsigned long long)ldc * sizeof(T))) & 15) == 0;
+#pragma unroll
+  for (int c0 = 0; c0 < 128; c0 += per) {
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      float v[piece];
+#pragma unroll
+      for (int i = 0; i < piece; ++i) v[i] = acc[c0 + q * piece + i];
+      *reinterpret_cast<uint4*>(stage + lane * 64 + ((q ^ ((lane >> 1) & 3)) << 4)) = pack16<T>(v);
+    }
+    __syncwarp();
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int r = i * 8 + (lane >> 2), q = lane & 3, at = c0 + q * piece;
+      if (r < rows && at < cols) {
+        const unsigned char* from = stage + r * 64 + ((q ^ ((r >> 1) & 3)) << 4);
+        T* to = c + (long long)r * ldc + at;
+        if (whole && at + piece <= cols) *reinterpret_cast<uint4*>(to) = *reinterpret_cast<const uint4*>(from);
+        else
+          for (int b = 0; b < piece && at + b < cols; ++b) to[b] = reinterpret_cast<const T*>(from)[b];
+      }
+    }
+    __syncwarp();
+  }
+}
+
+// kColumns: the columns have a scale each (rows of B scaled by blocks of 128 along K alone)
+template <bool kColumns> __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
+product_pair_kernel(const Params p, const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b) {
+  constexpr int S = kPairSlots;
+  extern __shared__ __align__(1024) unsigned char smem_dyn[];
+  unsigned char* ring = smem_dyn + ((1024u - (smem_u32(smem_dyn) & 1023u)) & 1023u);
+  unsigned char* stages = ring + (size_t)S * kPairBytes;
+  float* sv = reinterpret_cast<float*>(stages + 8 * kStageBytes);                       // [slot][256] scales of the columns
+  unsigned long long* bars = reinterpret_cast<unsigned long long*>(sv + S * kPairCols);
+  int* prefix = reinterpret_cast<int*>(bars + P_COUNT);
+  int* warp_part = prefix + ASGD_MAX_EXPERTS + 1;
+  int* misc = warp_part + 32;        // [0] tensor memory, [1] abort, [2, 3] K blocks whose copies each block has issued, [4] the other block gave up
+  int* abort = misc + 1;
+  const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
+  const unsigned rank = rank_in_pair();
+  const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
+
+  if (tid == 0) {
+    for (int q = 0; q < S; ++q) { mbar_init(bars + P_FULL + q, 1); mbar_init(bars + P_DONE + q, 1); mbar_init(bars + P_SFULL + q, 32); mbar_init(bars + P_SEMPTY + q, 8); }
+    for (int q = 0; q < 2; ++q) { mbar_init(bars + P_ACCEMPTY + q, 16); mbar_init(bars + P_DRAIN + q, 1); }
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    for (int q = 1; q < 5; ++q) misc[q] = 0;
+  }
+  if (wid == 1) {
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(misc)), "r"(512u) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+  }
+  count_tiles(p, kPairRows, prefix, warp_part);
+  fence_before();
+  __syncthreads();
+  pair_sync();
+  fence_after();
+  const unsigned tmem = (unsigned)misc[0];
+  const int tiles = prefix[max(p.groups, 1)];
+
+  if (wid < 4) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
+    if (wid == 0 && lane == 0) {
+      const unsigned full0 = in_first_block(bars + P_FULL);
+      unsigned it = 0;
+      bool ok = true;
+      for (int tile = pair; tile < tiles && ok; tile += pairs) {
+        const Tile t = find_tile(p, kPairRows, kPairCols, kPairBand, prefix, tile);
+        const int za = 0, zb = p.inner ? 0 : t.g;
+        for (int kb = t.kb0; kb < t.kb1; ++kb, ++it) {
+          const unsigned q = it % S;
+          if (it >= S && !(ok = wait(bars + P_DONE + q, (it / S - 1) & 1, p.wait_limit, abort))) break;
+          unsigned char* to = ring + (size_t)q * kPairBytes;
+          if (rank == 0) mbar_expect_tx(bars + P_FULL + q, 2 * kPairBytes);
+          if (!(p.withhold && it == 0)) {
+            tma_load_pair(to, &map_a, kb * kKB, t.m0 + (int)rank * kHalf, za, full0 + q * 8);
+            tma_load_pair(to + kHalfBytes, &map_b, kb * kKB, t.n0 + (int)rank * kHalf, zb, full0 + q * 8);
+          }
+        }
+      }
+      store_cluster(in_first_block(misc + 2 + rank), it);
+    } else if ((wid == 1 || wid == 3) && lane == 0 && rank == 0) {
+      // Two issuing threads, one per accumulator stage, K blocks in turn: a commit holds the thread that issues it for
+      // several hundred cycles, and the other thread's products fill the gap.  Each meets every phase of the barriers it
+      // waits on (the slots are even in number), as a wait on a parity needs.
+      const unsigned me = (unsigned)wid >> 1;
+      unsigned it = 0;
+      bool ok = true;
+      for (int tile = pair; tile < tiles && ok; tile += pairs) {
+        const Tile t = find_tile(p, kPairRows, kPairCols, kPairBand, prefix, tile);
+        for (int kb = t.kb0; kb < t.kb1; ++kb, ++it) {
+          const unsigned q = it % S, stage = it & 1;
+          if (stage != me) continue;
+          // the operands are there long before the accumulator is free: what can be done is done before that wait
+          if (!(ok = wait(bars + P_FULL + q, (it / S) & 1, p.wait_limit, abort))) break;
+          const unsigned long long da = operand_desc(ring + (size_t)q * kPairBytes), db = operand_desc(ring + (size_t)q * kPairBytes + kHalfBytes);
+          const int steps = steps_of(t, kb);
+          if (it >= 2 && !(ok = wait(bars + P_ACCEMPTY + stage, (it / 2 - 1) & 1, p.wait_limit, abort))) break;
+          fence_after();
+#pragma unroll
+          for (int k4 = 0; k4 < 4; ++k4) if (k4 < steps) mma_f8_pair(tmem + stage * kPairCols, da + 2 * k4, db + 2 * k4, p.idesc, k4 != 0);
+          commit_pair(bars + P_DONE + q);
+        }
+      }
+      if (!ok && it) {                               // products in flight end before the tensor memory is freed
+        commit_pair(bars + P_DRAIN + me);
+        for (unsigned n = 0; n < p.wait_limit && !mbar_try_wait(bars + P_DRAIN + me, 0); ++n) {}
+      }
+    } else if (wid == 2 && kColumns) {
+      unsigned it = 0;
+      bool ok = true;
+      for (int tile = pair; tile < tiles && ok; tile += pairs) {
+        const Tile t = find_tile(p, kPairRows, kPairCols, kPairBand, prefix, tile);
+        const float* from = p.sb + (p.inner ? 0 : t.g * p.sb_group);
+        for (int kb = t.kb0; kb < t.kb1; ++kb, ++it) {
+          const unsigned q = it % S;
+          if (it >= S && !(ok = __all_sync(kAll, wait(bars + P_SEMPTY + q, (it / S - 1) & 1, p.wait_limit, abort)))) break;
+#pragma unroll
+          for (int c = 0; c < kPairCols; c += 32) {
+            const int n = t.n0 + c + lane;
+            copy4(sv + q * kPairCols + c + lane, n < p.N ? from + n * p.sb_row + kb * p.sb_block : p.sb, n < p.N);
+          }
+          arrive_after_copies(bars + P_SFULL + q);
+        }
+      }
+      asm volatile("cp.async.wait_all;" ::: "memory");
+    }
+    __syncwarp();
+  } else {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 232;");
+    const int quarter = wid & 3, half = (wid - 4) >> 2;
+    const unsigned free0 = in_first_block(bars + P_ACCEMPTY);
+    const unsigned at_tmem = tmem + ((unsigned)(quarter * 32) << 16) + half * 128;
+    unsigned char* stage_smem = stages + (wid - 4) * kStageBytes;
+    unsigned it = 0;
+    bool ok = true;
+    for (int tile = pair; tile < tiles && ok; tile += pairs) {
+      const Tile t = find_tile(p, kPairRows, kPairCols, kPairBand, prefix, tile);
+      const int m = t.m0 + (int)rank * kHalf + quarter * 32, n = t.n0 + half * 128;      // the warp's corner
+      const float* sa_at = p.sa + min(m + lane, p.M - 1) * p.sa_row;
+      const float* sb_at = p.sb + (p.inner ? 0 : t.g * p.sb_group) + (long long)(min(n, p.N - 1) >> 7) * p.sb_row;
+      // scales of a K block, loaded two blocks ahead of their use (and multiplied only there: an instruction that needs a
+      // load's result holds the warp until it has come)
+      auto row_scale = [&](int kb) { return __ldg(sa_at + min(kb, t.kb1 - 1) * p.sa_block); };
+      auto col_scale = [&](int kb) { return kColumns ? 1.f : __ldg(sb_at + min(kb, t.kb1 - 1) * p.sb_block); };
+      float acc[128];
+#pragma unroll
+      for (int c = 0; c < 128; ++c) acc[c] = 0.f;
+      float a0 = 0.f, a1 = 0.f, b0 = 0.f, b1 = 0.f;
+      if (t.kb0 < t.kb1) { a0 = row_scale(t.kb0); a1 = row_scale(t.kb0 + 1); b0 = col_scale(t.kb0); b1 = col_scale(t.kb0 + 1); }
+      for (int kb = t.kb0; kb < t.kb1; ++kb, ++it) {
+        const unsigned q = it % S, stage = it & 1;
+        const float a2 = row_scale(kb + 2), b2 = col_scale(kb + 2);
+        ok = (!kColumns || wait(bars + P_SFULL + q, (it / S) & 1, p.wait_limit, abort)) && wait(bars + P_DONE + q, (it / S) & 1, p.wait_limit, abort);
+        if (!(ok = __all_sync(kAll, ok))) break;
+        fence_after();
+        const float s0 = a0 * b0;
+        float v[2][32];
+        tmem_load32(at_tmem + stage * kPairCols, v[0]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          tmem_wait();
+          if (i < 3) tmem_load32(at_tmem + stage * kPairCols + (i + 1) * 32, v[(i + 1) & 1]);
+          else {
+            fence_before();
+            __syncwarp();
+            if (lane == 0) arrive_cluster(free0 + stage * 8);
+          }
+          if (kColumns) {
+            const float4* col = reinterpret_cast<const float4*>(sv + q * kPairCols + half * 128 + i * 32);
+#pragma unroll
+            for (int c = 0; c < 32; c += 4) {
+              const float4 f = col[c / 4];
+              acc[i * 32 + c] = fmaf(v[i & 1][c] * s0, f.x, acc[i * 32 + c]);
+              acc[i * 32 + c + 1] = fmaf(v[i & 1][c + 1] * s0, f.y, acc[i * 32 + c + 1]);
+              acc[i * 32 + c + 2] = fmaf(v[i & 1][c + 2] * s0, f.z, acc[i * 32 + c + 2]);
+              acc[i * 32 + c + 3] = fmaf(v[i & 1][c + 3] * s0, f.w, acc[i * 32 + c + 3]);
+            }
+          } else {
+#pragma unroll
+            for (int c = 0; c < 32; ++c) acc[i * 32 + c] = fmaf(v[i & 1][c], s0, acc[i * 32 + c]);
+          }
+        }
+        if (kColumns) {
+          __syncwarp();
+          if (lane == 0) arrive(bars + P_SEMPTY + q);
+        }
+        a0 = a1; a1 = a2;
+        b0 = b1; b1 = b2;
+      }
+      if (!ok) break;
+      if (t.bad) {
+        if (lane == 0) atomicMin(&g_status, ASGD_EINVAL);
+#pragma unroll
+        for (int c = 0; c < 128; ++c) acc[c] = __int_as_float(0x7fffffff);
+      }
+      const int rows = min(32, t.m_end - m), cols = min(128, p.N - n);
+      if (rows > 0 && cols > 0) {
+        const long long at = (p.inner ? t.g * p.c_group : 0) + m * p.ldc + n;
+        if (p.c_type == ASGD_F32) store_rows(acc, stage_smem, reinterpret_cast<float*>(p.c) + at, p.ldc, rows, cols, lane);
+        else if (p.c_type == ASGD_BF16) store_rows(acc, stage_smem, reinterpret_cast<__nv_bfloat16*>(p.c) + at, p.ldc, rows, cols, lane);
+        else store_rows(acc, stage_smem, reinterpret_cast<__half*>(p.c) + at, p.ldc, rows, cols, lane);
+      }
+    }
+    __syncwarp();
+  }
+  // Both blocks are through.  Where one gave up, the first block settles its barriers: bytes announced that nobody will
+  // send, copies issued that nobody announced; then every copy in flight has landed when the last phases are complete.
+  if (*reinterpret_cast<volatile int*>(abort) && lane == 0) store_cluster(in_first_block(misc + 4), 1);
+  fence_before();
+  pair_sync();
+  fence_after();
+  if (rank == 0 && tid == 0 && *reinterpret_cast<volatile int*>(misc + 4)) {
+    const unsigned mine = (unsigned)misc[2], other = (unsigned)misc[3], last = max(mine, other);
+    for (unsigned i = min(mine, other); i < last; ++i) {
+      if (i < mine) complete_tx(bars + P_FULL + i % S, kPairBytes);
+      else mbar_expect_tx(bars + P_FULL + i % S, kPairBytes);
+    }
+    if (p.withhold && last) complete_tx(bars + P_FULL, ((mine > 0) + (other > 0)) * kPairBytes);
+    for (unsigned q = 0; q < S && q < last; ++q)
+      for (unsigned n = 0; n < p.wait_limit && !mbar_try_wait(bars + P_FULL + q, ((last - 1 - q) / S) & 1); ++n) {}
+    atomicMin(&g_status, ASGD_ETIMEOUT);
+  }
+  pair_sync();
+  if (wid == 1) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u));
+}
+
+}  // namespace
