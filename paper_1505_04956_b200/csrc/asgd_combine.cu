@@ -5,12 +5,16 @@
 // in ascending place, so a sum has one order.
 #include "asgd_experts_common.cuh"
 
+#include <algorithm>
+#include <type_traits>
+
 namespace {
 
 using namespace asgd::experts;
 
-constexpr int kThreads = 128;
-constexpr int kRows = 8;                                   // rows of z a thread has in flight
+constexpr int kThreads = 128;                              // the sum; the gradient takes what fits the row
+constexpr int kMaxThreads = 256;
+constexpr int kMaxRows = 8;                                // rows of z a thread has in flight
 
 struct Args {
   long long T, D, R, ldz, ldy, ld_dy, ld_dz;
@@ -22,100 +26,135 @@ struct Args {
   float* dweights;
 };
 
-// V numbers from column c of a row (c < D); the vector form only where whole vectors are aligned
-template <typename T, int V> __device__ __forceinline__ void load(const T* p, float (&v)[V]) {
-  if constexpr (V == 1) v[0] = Elem<T>::to_f(*p);
-  else unpack16<T>(*reinterpret_cast<const uint4*>(p), v);
-}
-template <typename T, int V> __device__ __forceinline__ void store(T* p, const float (&v)[V]) {
-  if constexpr (V == 1) *p = Elem<T>::from_f(v[0]);
-  else *reinterpret_cast<uint4*>(p) = pack16<T>(v);
+// A piece of a row as it is in memory: 16 bytes where all rows start at 16-byte boundaries, else one number.
+template <typename T, bool kVec> struct Piece {
+  using Word = typename std::conditional<kVec, uint4, T>::type;
+  static constexpr int kN = kVec ? kPer16<T> : 1;
+  static __device__ __forceinline__ void unpack(const Word& w, float (&v)[kN]) {
+    if constexpr (kVec) unpack16<T>(w, v);
+    else v[0] = Elem<T>::to_f(w);
+  }
+  static __device__ __forceinline__ Word pack(const float (&v)[kN]) {
+    if constexpr (kVec) return pack16<T>(v);
+    else return Elem<T>::from_f(v[0]);
+  }
+  static __device__ __forceinline__ Word load(const T* p) { return *reinterpret_cast<const Word*>(p); }
+  static __device__ __forceinline__ void store(T* p, const Word& w) { *reinterpret_cast<Word*>(p) = w; }
+};
+
+// The row of z that an assignment takes, and its factor; row -1: no part
+__device__ __forceinline__ void assignment(const Args& a, long long t, int j, int& row, float& w) {
+  row = -1;
+  w = 0.f;
+  if (j >= a.top_k) return;
+  const int r = a.rows[t * a.top_k + j];
+  if (r < 0 || r >= a.R) return;
+  row = r;
+  w = a.weights ? a.weights[t * a.top_k + j] : 1.f;
 }
 
-template <typename T, int V> __global__ void __launch_bounds__(kThreads) combine_kernel(const Args a, int stretches) {
-  const long long t = blockIdx.x / stretches, c = ((long long)(blockIdx.x % stretches) * kThreads + threadIdx.x) * V;
-  if (c >= a.D) return;
-  const T* z = reinterpret_cast<const T*>(a.z) + c;
-  float acc[V];
+// N: rows met at a time; U: pieces per thread, blockDim apart (what is in flight is N * U pieces)
+template <typename T, bool kVec, int N, int U> __global__ void __launch_bounds__(kThreads) combine_kernel(const Args a) {
+  using P = Piece<T, kVec>;
+  const long long t = blockIdx.x, c0 = ((long long)blockIdx.y * U * kThreads + threadIdx.x) * P::kN;
+  const T* z = reinterpret_cast<const T*>(a.z);
+  float acc[U][P::kN];
 #pragma unroll
-  for (int i = 0; i < V; ++i) acc[i] = 0.f;
-  for (int j0 = 0; j0 < a.top_k; j0 += kRows) {
-    float v[kRows][V], w[kRows];
+  for (int u = 0; u < U; ++u)
 #pragma unroll
-    for (int j = 0; j < kRows; ++j) {
-      const int r = j0 + j < a.top_k ? a.rows[t * a.top_k + j0 + j] : -1;
-      const bool ok = r >= 0 && r < a.R;
-      w[j] = !ok ? 0.f : a.weights ? a.weights[t * a.top_k + j0 + j] : 1.f;
-      if (ok) load<T, V>(z + (long long)r * a.ldz, v[j]);
-      else
+    for (int i = 0; i < P::kN; ++i) acc[u][i] = 0.f;
+  for (int j0 = 0; j0 < a.top_k; j0 += N) {
+    int row[N];
+    float w[N];
 #pragma unroll
-        for (int i = 0; i < V; ++i) v[j][i] = 0.f;
-    }
+    for (int j = 0; j < N; ++j) assignment(a, t, j0 + j, row[j], w[j]);
+    typename P::Word raw[N][U];
 #pragma unroll
-    for (int j = 0; j < kRows; ++j)
+    for (int j = 0; j < N; ++j)
 #pragma unroll
-      for (int i = 0; i < V; ++i) acc[i] = fmaf(w[j], v[j][i], acc[i]);
+      for (int u = 0; u < U; ++u) {
+        const long long c = c0 + (long long)u * kThreads * P::kN;
+        raw[j][u] = typename P::Word{};
+        if (row[j] >= 0 && c < a.D) raw[j][u] = P::load(z + row[j] * a.ldz + c);
+      }
+#pragma unroll
+    for (int j = 0; j < N; ++j)
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        float v[P::kN];
+        P::unpack(raw[j][u], v);
+#pragma unroll
+        for (int i = 0; i < P::kN; ++i) acc[u][i] = fmaf(w[j], v[i], acc[u][i]);
+      }
   }
-  store<T, V>(reinterpret_cast<T*>(a.y) + t * a.ldy + c, acc);
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const long long c = c0 + (long long)u * kThreads * P::kN;
+    if (c < a.D) P::store(reinterpret_cast<T*>(a.y) + t * a.ldy + c, P::pack(acc[u]));
+  }
 }
 
 // Blocks 0..T-1: a token each.  The blocks behind them: 128 grouped rows each, those of nothing become zeros.
-template <typename T, int V> __global__ void __launch_bounds__(kThreads) combine_grad_kernel(const Args a) {
+template <typename T, bool kVec, int N> __global__ void __launch_bounds__(kMaxThreads) combine_grad_kernel(const Args a) {
+  using P = Piece<T, kVec>;
+  T* dz = reinterpret_cast<T*>(a.dz);
   if (blockIdx.x >= a.T) {
     const long long r0 = ((long long)blockIdx.x - a.T) * 128;
     for (int q = 0; q < 128; ++q) {
       const long long r = r0 + q;
       if (r >= a.R || a.source[r] >= 0) continue;
-      T* dz = reinterpret_cast<T*>(a.dz) + r * a.ld_dz;
-      for (long long c = threadIdx.x; c < a.D; c += kThreads) dz[c] = Elem<T>::from_f(0.f);
+      for (long long c = (long long)threadIdx.x * P::kN; c < a.D; c += (long long)blockDim.x * P::kN) P::store(dz + r * a.ld_dz + c, typename P::Word{});
     }
     return;
   }
-  __shared__ float part[kThreads / 32][kRows];
+  __shared__ float part[kMaxThreads / 32][N];
+  const T* z = reinterpret_cast<const T*>(a.z);
   const long long t = blockIdx.x;
   const T* dy = reinterpret_cast<const T*>(a.dy) + t * a.ld_dy;
-  for (int j0 = 0; j0 < a.top_k; j0 += kRows) {
-    long long at[kRows];
-    float w[kRows], dot[kRows];
+  for (int j0 = 0; j0 < a.top_k; j0 += N) {
+    int row[N];
+    float w[N], dot[N];
 #pragma unroll
-    for (int j = 0; j < kRows; ++j) {
-      const int r = j0 + j < a.top_k ? a.rows[t * a.top_k + j0 + j] : -1;
-      at[j] = (r >= 0 && r < a.R) ? r : -1;
-      w[j] = at[j] < 0 ? 0.f : a.weights ? a.weights[t * a.top_k + j0 + j] : 1.f;
-      dot[j] = 0.f;
-    }
-    for (long long c = (long long)threadIdx.x * V; c < a.D; c += (long long)kThreads * V) {
-      float g[V];
-      load<T, V>(dy + c, g);
+    for (int j = 0; j < N; ++j) { assignment(a, t, j0 + j, row[j], w[j]); dot[j] = 0.f; }
+    for (long long c = (long long)threadIdx.x * P::kN; c < a.D; c += (long long)blockDim.x * P::kN) {
+      typename P::Word raw[N];
+      const typename P::Word raw_g = P::load(dy + c);
 #pragma unroll
-      for (int j = 0; j < kRows; ++j) {
-        if (at[j] < 0) continue;
-        if (a.dweights) {
-          float v[V];
-          load<T, V>(reinterpret_cast<const T*>(a.z) + at[j] * a.ldz + c, v);
+      for (int j = 0; j < N; ++j) {
+        raw[j] = typename P::Word{};
+        if (a.dweights && row[j] >= 0) raw[j] = P::load(z + row[j] * a.ldz + c);
+      }
+      float g[P::kN];
+      P::unpack(raw_g, g);
+      if (a.dz)
 #pragma unroll
-          for (int i = 0; i < V; ++i) dot[j] = fmaf(g[i], v[i], dot[j]);
+        for (int j = 0; j < N; ++j) {
+          if (row[j] < 0) continue;
+          float o[P::kN];
+#pragma unroll
+          for (int i = 0; i < P::kN; ++i) o[i] = w[j] * g[i];
+          P::store(dz + row[j] * a.ld_dz + c, P::pack(o));
         }
-        if (a.dz) {
-          float o[V];
 #pragma unroll
-          for (int i = 0; i < V; ++i) o[i] = w[j] * g[i];
-          store<T, V>(reinterpret_cast<T*>(a.dz) + at[j] * a.ld_dz + c, o);
-        }
+      for (int j = 0; j < N; ++j) {
+        float v[P::kN];
+        P::unpack(raw[j], v);
+        if (row[j] >= 0)                             // a row that takes no part adds nothing, whatever dy holds
+#pragma unroll
+          for (int i = 0; i < P::kN; ++i) dot[j] = fmaf(g[i], v[i], dot[j]);
       }
     }
     if (!a.dweights) continue;
 #pragma unroll
-    for (int j = 0; j < kRows; ++j) {
+    for (int j = 0; j < N; ++j) {
 #pragma unroll
       for (int o = 16; o > 0; o >>= 1) dot[j] += __shfl_xor_sync(kAll, dot[j], o);
       if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5][j] = dot[j];
     }
     __syncthreads();
-    if (threadIdx.x < kRows && j0 + (int)threadIdx.x < a.top_k) {
+    if (threadIdx.x < N && j0 + (int)threadIdx.x < a.top_k) {
       float s = 0.f;
-#pragma unroll
-      for (int w2 = 0; w2 < kThreads / 32; ++w2) s += part[w2][threadIdx.x];
+      for (int v = 0; v < (int)blockDim.x / 32; ++v) s += part[v][threadIdx.x];
       a.dweights[t * a.top_k + j0 + threadIdx.x] = s;
     }
     __syncthreads();
@@ -123,6 +162,17 @@ template <typename T, int V> __global__ void __launch_bounds__(kThreads) combine
 }
 
 template <typename T> bool whole(const void* p, long long ld) { return aligned(p, 16) && ld % kPer16<T> == 0; }
+
+// Calls f with the kind of pieces and the rows met at a time, as compile-time constants.
+template <typename F> void with_rows(int top_k, bool vec, F&& f) {
+  auto rows = [&](auto v) {
+    if (top_k <= 2) f(v, std::integral_constant<int, 2>());
+    else if (top_k <= 4) f(v, std::integral_constant<int, 4>());
+    else f(v, std::integral_constant<int, kMaxRows>());
+  };
+  if (vec) rows(std::true_type());
+  else rows(std::false_type());
+}
 
 }  // namespace
 
@@ -139,10 +189,13 @@ extern "C" int asgd_combine(int64_t T, int64_t D, int32_t top_k, const void* z, 
   with_type(type, [&](auto e) {
     using E = decltype(e);
     const bool vec = whole<E>(z, ldz) && whole<E>(y, ldy) && D % kPer16<E> == 0;
-    const long long stretches = ceil_div(D, (long long)kThreads * (vec ? kPer16<E> : 1));
-    if (stretches * T > 0x7fffffffll) { rc = ASGD_EUNSUPPORTED; return; }
-    if (vec) combine_kernel<E, kPer16<E>><<<(unsigned)(stretches * T), kThreads, 0, (cudaStream_t)stream>>>(a, (int)stretches);
-    else combine_kernel<E, 1><<<(unsigned)(stretches * T), kThreads, 0, (cudaStream_t)stream>>>(a, (int)stretches);
+    with_rows(top_k, vec, [&](auto v, auto n) {
+      constexpr bool kVec = decltype(v)::value;
+      constexpr int N = decltype(n)::value, U = 8 / N;
+      const long long stretches = ceil_div(D, (long long)kThreads * U * (kVec ? kPer16<E> : 1));
+      if (stretches > 65535) { rc = ASGD_EUNSUPPORTED; return; }
+      combine_kernel<E, kVec, N, U><<<dim3((unsigned)T, (unsigned)stretches), kThreads, 0, (cudaStream_t)stream>>>(a);
+    });
   });
   if (rc != ASGD_OK) return rc;
   return cudaGetLastError() == cudaSuccess ? ASGD_OK : ASGD_ECUDA;
@@ -165,8 +218,12 @@ extern "C" int asgd_combine_grad(int64_t T, int64_t D, int32_t top_k, const void
   with_type(type, [&](auto e) {
     using E = decltype(e);
     const bool vec = whole<E>(dy, ld_dy) && (!dweights || whole<E>(z, ldz)) && (!dz || whole<E>(dz, ld_dz)) && D % kPer16<E> == 0;
-    if (vec) combine_grad_kernel<E, kPer16<E>><<<(unsigned)blocks, kThreads, 0, (cudaStream_t)stream>>>(a);
-    else combine_grad_kernel<E, 1><<<(unsigned)blocks, kThreads, 0, (cudaStream_t)stream>>>(a);
+    // threads that share the row's pieces evenly: as many turns as 256 threads would take
+    const long long pieces = std::max(1ll, ceil_div(D, vec ? kPer16<E> : 1)), turns = ceil_div(pieces, kMaxThreads);
+    const unsigned threads = (unsigned)ceil_div(ceil_div(pieces, turns), 32) * 32;
+    with_rows(top_k, vec, [&](auto v, auto n) {
+      combine_grad_kernel<E, decltype(v)::value, decltype(n)::value><<<(unsigned)blocks, threads, 0, (cudaStream_t)stream>>>(a);
+    });
   });
   return cudaGetLastError() == cudaSuccess ? ASGD_OK : ASGD_ECUDA;
 }

@@ -42,8 +42,15 @@ long long most_tiles(const Params& p, int bm, int bn) {
   const long long rows = p.inner ? ceil_div(p.M, bm) * p.groups : ceil_div(p.M, bm) + p.groups;
   return rows * ceil_div(p.N, bn);
 }
-template <typename K> bool allow_smem(K kernel, size_t bytes) {
-  return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) == cudaSuccess;
+// Raises a kernel's shared-memory limit, once per device (`done`: a bit per device, of this kernel).
+template <typename K> bool allow_smem(K kernel, size_t bytes, std::atomic<unsigned long long>& done) {
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) return false;
+  const unsigned long long bit = 1ull << (dev & 63);
+  if (dev < 64 && (done.load() & bit)) return true;
+  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) != cudaSuccess) return false;
+  done.fetch_or(bit);
+  return true;
 }
 // fp32 accumulators; formats of the MMA's first and second operand (0 = E4M3, 1 = E5M2); its columns and rows
 unsigned instruction(int type0, int type1, int cols, int rows) {
@@ -61,7 +68,8 @@ template <int BN> int launch_few(const asgd_product_args& a, Params p, cudaStrea
   const long long most = most_tiles(p, BN, kU);
   if (most > 0x7fffffffll) return ASGD_EUNSUPPORTED;
   static_assert(smem_bytes<BN>() <= kSmemLimit, "shared memory");
-  if (!allow_smem(product_few_kernel<BN>, smem_bytes<BN>())) return ASGD_ECUDA;
+  static std::atomic<unsigned long long> done{0};
+  if (!allow_smem(product_few_kernel<BN>, smem_bytes<BN>(), done)) return ASGD_ECUDA;
   product_few_kernel<BN><<<(unsigned)min(most, (long long)kSMs), kThreads, smem_bytes<BN>(), st>>>(p, map_u, map_v);
   return cudaGetLastError() == cudaSuccess ? ASGD_OK : ASGD_ECUDA;
 }
@@ -77,7 +85,8 @@ int launch_pair(const asgd_product_args& a, Params p, cudaStream_t st) {
   const long long most = most_tiles(p, kPairRows, kPairCols);
   if (most > 0x7fffffffll) return ASGD_EUNSUPPORTED;
   const auto kernel = a.b_square ? product_pair_kernel<false> : product_pair_kernel<true>;
-  if (!allow_smem(kernel, kPairSmem)) return ASGD_ECUDA;
+  static std::atomic<unsigned long long> done[2] = {{0}, {0}};
+  if (!allow_smem(kernel, kPairSmem, done[a.b_square])) return ASGD_ECUDA;
   kernel<<<(unsigned)min(most, (long long)(kSMs / 2)) * 2, kPairThreads, kPairSmem, st>>>(p, map_a, map_b);
   return cudaGetLastError() == cudaSuccess ? ASGD_OK : ASGD_ECUDA;
 }

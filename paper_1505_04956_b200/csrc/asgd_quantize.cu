@@ -8,6 +8,8 @@
 // store into the transposed tile in shared memory.
 #include "asgd_experts_common.cuh"
 
+#include <type_traits>
+
 namespace {
 
 using namespace asgd::experts;
@@ -43,91 +45,96 @@ template <typename T> __device__ __forceinline__ const T* input_row(const asgd_q
   return reinterpret_cast<const T*>(a.x) + t * a.ldx;
 }
 
-// V numbers of a row from column c; numbers beyond K are zeros
-template <typename T, int V, bool kVec> __device__ __forceinline__ void load(const T* row, long long c, long long K, float (&v)[V]) {
-  if (kVec && c + V <= K) {
-    if constexpr (sizeof(T) * V == 16) {
-      unpack16<T>(*reinterpret_cast<const uint4*>(row + c), v);
-    } else {
-      static_assert(sizeof(T) * V == 8, "8 or 16 bytes");
-      const uint2 u = *reinterpret_cast<const uint2*>(row + c);
-      const T* e = reinterpret_cast<const T*>(&u);
+// 16 or 8 bytes of a row from column c, as they are in memory; numbers beyond K are zeros
+template <typename T, typename Word, bool kVec> __device__ __forceinline__ Word load(const T* row, int c, int K) {
+  constexpr int V = (int)(sizeof(Word) / sizeof(T));
+  if (kVec && c + V <= K) return *reinterpret_cast<const Word*>(row + c);
+  Word w{};
+  T* e = reinterpret_cast<T*>(&w);
 #pragma unroll
-      for (int i = 0; i < V; ++i) v[i] = Elem<T>::to_f(e[i]);
-    }
-  } else {
-#pragma unroll
-    for (int i = 0; i < V; ++i) v[i] = c + i < K ? Elem<T>::to_f(row[c + i]) : 0.f;
-  }
+  for (int i = 0; i < V; ++i) if (c + i < K) e[i] = row[c + i];
+  return w;
+}
+template <typename T, typename Word> __device__ __forceinline__ float element(const Word& w, int i) {
+  return Elem<T>::to_f(reinterpret_cast<const T*>(&w)[i]);
 }
 
 template <typename T, bool kVec, bool kE5M2> __global__ void __launch_bounds__(kThreads) rows_kernel(const Args p) {
   constexpr int V = kPer16<T>, LB = 128 / V, U = 4;      // numbers per lane, lanes per block, loads in flight per lane
   const asgd_quantize_args& a = p.a;
-  const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
-  const long long span = 32 * V * U, segs = (a.K + span - 1) / span;
+  const int lane = threadIdx.x & 31, K = (int)a.K;
   // the block's warps take neighbouring rows of the same stretch: their scales are neighbours in memory
-  const long long r = (long long)blockIdx.x / segs * kWarps + wid, c0 = (long long)blockIdx.x % segs * span;
+  const long long r = (long long)blockIdx.x * kWarps + (threadIdx.x >> 5);
+  const int c0 = ((int)blockIdx.y * U * 32 + lane) * V;
   if (r >= a.M) return;
   float factor;
   const T* row = input_row<T>(a, r, factor);
-  float v[U][V];
+  uint4 raw[U];
 #pragma unroll
   for (int u = 0; u < U; ++u) {
-    const long long c = c0 + (u * 32 + lane) * V;
-    if (row && c < a.K) load<T, V, kVec>(row, c, a.K, v[u]);
-    else
-#pragma unroll
-      for (int i = 0; i < V; ++i) v[u][i] = 0.f;
+    const int c = c0 + u * 32 * V;
+    raw[u] = make_uint4(0, 0, 0, 0);
+    if (row && c < K) raw[u] = load<T, uint4, kVec>(row, c, K);
   }
   unsigned char* q = reinterpret_cast<unsigned char*>(a.q) + r * a.ldq;
+  float* scale = a.scale + r * a.scale_row;
 #pragma unroll
   for (int u = 0; u < U; ++u) {
-    const long long c = c0 + (u * 32 + lane) * V;
+    const int c = c0 + u * 32 * V;
+    float v[V];
+    unpack16<T>(raw[u], v);
     float m = kTiny;
 #pragma unroll
     for (int i = 0; i < V; ++i) {
-      if (a.weights) v[u][i] = __fmul_rn(v[u][i], factor);
-      m = fmaxf(m, fabsf(v[u][i]));
+      if (a.weights) v[i] = __fmul_rn(v[i], factor);
+      m = fmaxf(m, fabsf(v[i]));
     }
 #pragma unroll
     for (int o = LB / 2; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(kAll, m, o));
     const float inv = __fdiv_rn(p.fmax, m);
-    if (c < a.K) {
-      if ((lane & (LB - 1)) == 0) a.scale[r * a.scale_row + (c >> 7) * a.scale_block] = __fmul_rn(m, p.inv_fmax);
+    if (c < K) {
+      if ((lane & (LB - 1)) == 0) scale[(c >> 7) * a.scale_block] = __fmul_rn(m, p.inv_fmax);
       unsigned w[V / 4];
 #pragma unroll
-      for (int i = 0; i < V; i += 4) w[i / 4] = round4<kE5M2>(v[u][i] * inv, v[u][i + 1] * inv, v[u][i + 2] * inv, v[u][i + 3] * inv);
-      if (kVec && c + V <= a.K) {
+      for (int i = 0; i < V; i += 4) w[i / 4] = round4<kE5M2>(v[i] * inv, v[i + 1] * inv, v[i + 2] * inv, v[i + 3] * inv);
+      if (kVec && c + V <= K) {
         if constexpr (V == 8) *reinterpret_cast<uint2*>(q + c) = make_uint2(w[0], w[1]);
         else *reinterpret_cast<unsigned*>(q + c) = w[0];
       } else {
 #pragma unroll
-        for (int i = 0; i < V; ++i) if (c + i < a.K) q[c + i] = (unsigned char)(w[i / 4] >> (8 * (i & 3)));
+        for (int i = 0; i < V; ++i) if (c + i < K) q[c + i] = (unsigned char)(w[i / 4] >> (8 * (i & 3)));
       }
     }
   }
 }
 
 template <typename T, bool kVec, bool kE5M2> __global__ void __launch_bounds__(kThreads) tile_kernel(const Args p) {
+  using Word = typename std::conditional<sizeof(T) == 4, uint4, uint2>::type;      // 4 numbers
   __shared__ __align__(16) unsigned char tile[128 * 128];       // [column][row], 16-byte pieces exchanged by column / 4
   __shared__ float col_max[kWarps][128];
   __shared__ float whole[kWarps];
   const asgd_quantize_args& a = p.a;
-  const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
-  const long long m0 = (long long)blockIdx.y * 128, k0 = (long long)blockIdx.x * 128;
-  const long long r0 = m0 + 16 * wid, c = k0 + 4 * lane;
-  float v[16][4];
+  const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5, K = (int)a.K;
+  const long long m0 = (long long)blockIdx.y * 128;
+  const int k0 = (int)blockIdx.x * 128;
+  const long long r0 = m0 + 16 * wid;
+  const int c = k0 + 4 * lane;
+  Word raw[16];
+  float factor[16];
 #pragma unroll
   for (int i = 0; i < 16; ++i) {
-    float factor;
-    const T* row = input_row<T>(a, r0 + i, factor);
-    if (row) load<T, 4, kVec>(row, c, a.K, v[i]);
-    else { v[i][0] = v[i][1] = v[i][2] = v[i][3] = 0.f; }
-    if (a.weights)
-#pragma unroll
-      for (int j = 0; j < 4; ++j) v[i][j] = __fmul_rn(v[i][j], factor);
+    const T* row = input_row<T>(a, r0 + i, factor[i]);
+    raw[i] = Word{};
+    if (row && c < K) raw[i] = load<T, Word, kVec>(row, c, K);
   }
+  float v[16][4];
+#pragma unroll
+  for (int i = 0; i < 16; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      v[i][j] = element<T>(raw[i], j);
+      if (a.weights) v[i][j] = __fmul_rn(v[i][j], factor[i]);
+    }
   float one = kTiny;
   if (a.square) {
 #pragma unroll
@@ -143,24 +150,40 @@ template <typename T, bool kVec, bool kE5M2> __global__ void __launch_bounds__(k
     if (threadIdx.x == 0) a.scale[blockIdx.y * a.scale_row + blockIdx.x * a.scale_block] = __fmul_rn(one, p.inv_fmax);
   }
   if (a.q) {
+    float m[16];
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
-      float m = one;
-      if (!a.square) {
+      m[i] = one;
+      if (!a.square)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) m = fmaxf(m, fabsf(v[i][j]));
+        for (int j = 0; j < 4; ++j) m[i] = fmaxf(m[i], fabsf(v[i][j]));
+    }
+    if (!a.square) {
+      // 16 rows' maxima over 32 lanes by halving: each step folds half of the rows onto the other half of the lanes, so
+      // that lane l ends with row l / 2 (16 exchanges instead of 80), and the rows' inverses come from 16 lanes at once
 #pragma unroll
-        for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(kAll, m, o));
-      }
-      const float inv = __fdiv_rn(p.fmax, m);
+      for (int n = 8, o = 16; n > 0; n >>= 1, o >>= 1)
+#pragma unroll
+        for (int i = 0; i < n; ++i) {
+          const bool high = lane & o;
+          const float send = high ? m[i] : m[i + n], keep = high ? m[i + n] : m[i];
+          m[i] = fmaxf(keep, __shfl_xor_sync(kAll, send, o));
+        }
+      m[0] = fmaxf(m[0], __shfl_xor_sync(kAll, m[0], 1));
+      const long long r = r0 + (lane >> 1);
+      if (!(lane & 1) && r < a.M) a.scale[r * a.scale_row + blockIdx.x * a.scale_block] = __fmul_rn(m[0], p.inv_fmax);
+    }
+    const float mine = __fdiv_rn(p.fmax, m[0]);
+    unsigned char* q = reinterpret_cast<unsigned char*>(a.q) + r0 * a.ldq + c;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const float inv = __shfl_sync(kAll, mine, 2 * i);
+      const unsigned w = round4<kE5M2>(v[i][0] * inv, v[i][1] * inv, v[i][2] * inv, v[i][3] * inv);
       if (r0 + i < a.M) {
-        if (!a.square && lane == 0) a.scale[(r0 + i) * a.scale_row + blockIdx.x * a.scale_block] = __fmul_rn(m, p.inv_fmax);
-        unsigned char* q = reinterpret_cast<unsigned char*>(a.q) + (r0 + i) * a.ldq;
-        const unsigned w = round4<kE5M2>(v[i][0] * inv, v[i][1] * inv, v[i][2] * inv, v[i][3] * inv);
-        if (kVec && c + 4 <= a.K) *reinterpret_cast<unsigned*>(q + c) = w;
+        if (kVec && c + 4 <= K) *reinterpret_cast<unsigned*>(q + i * a.ldq) = w;
         else
 #pragma unroll
-          for (int j = 0; j < 4; ++j) if (c + j < a.K) q[c + j] = (unsigned char)(w >> (8 * j));
+          for (int j = 0; j < 4; ++j) if (c + j < K) q[i * a.ldq + j] = (unsigned char)(w >> (8 * j));
       }
     }
   }
@@ -169,21 +192,24 @@ template <typename T, bool kVec, bool kE5M2> __global__ void __launch_bounds__(k
   if (a.square) {
     inv[0] = inv[1] = inv[2] = inv[3] = __fdiv_rn(p.fmax, one);
   } else {
+    float4 m = make_float4(kTiny, kTiny, kTiny, kTiny);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      float m = kTiny;
-#pragma unroll
-      for (int i = 0; i < 16; ++i) m = fmaxf(m, fabsf(v[i][j]));
-      col_max[wid][4 * lane + j] = m;
+    for (int i = 0; i < 16; ++i) {
+      m.x = fmaxf(m.x, fabsf(v[i][0])); m.y = fmaxf(m.y, fabsf(v[i][1]));
+      m.z = fmaxf(m.z, fabsf(v[i][2])); m.w = fmaxf(m.w, fabsf(v[i][3]));
     }
+    *reinterpret_cast<float4*>(&col_max[wid][4 * lane]) = m;
     __syncthreads();
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      float m = kTiny;
+    for (int w = 0; w < kWarps; ++w) {
+      const float4 o = *reinterpret_cast<const float4*>(&col_max[w][4 * lane]);
+      m.x = fmaxf(m.x, o.x); m.y = fmaxf(m.y, o.y); m.z = fmaxf(m.z, o.z); m.w = fmaxf(m.w, o.w);
+    }
+    const float best[4] = {m.x, m.y, m.z, m.w};
 #pragma unroll
-      for (int w = 0; w < kWarps; ++w) m = fmaxf(m, col_max[w][4 * lane + j]);
-      inv[j] = __fdiv_rn(p.fmax, m);
-      if (wid == 0 && c + j < a.K) a.scale_t[(c + j) * a.scale_t_row + blockIdx.y * a.scale_t_block] = __fmul_rn(m, p.inv_fmax);
+    for (int j = 0; j < 4; ++j) {
+      inv[j] = __fdiv_rn(p.fmax, best[j]);
+      if (wid == 0 && c + j < K) a.scale_t[(c + j) * a.scale_t_row + blockIdx.y * a.scale_t_block] = __fmul_rn(best[j], p.inv_fmax);
     }
   }
 #pragma unroll
@@ -201,7 +227,7 @@ template <typename T, bool kVec, bool kE5M2> __global__ void __launch_bounds__(k
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const int col = (int)(threadIdx.x >> 3) + 32 * i, piece = threadIdx.x & 7;
-    if (k0 + col >= a.K) continue;
+    if (k0 + col >= K) continue;
     const uint4 u = *reinterpret_cast<const uint4*>(tile + col * 128 + ((piece ^ ((col >> 2) & 7)) << 4));
     const long long r = m0 + 16 * piece;
     unsigned char* to = qt + (k0 + col) * a.ldqt + r;
@@ -222,9 +248,9 @@ template <typename T> void launch(const Args& p, cudaStream_t st) {
   // vector accesses need every row of the input and of the result to start at a whole vector
   const bool vec = aligned(a.x, V * sizeof(T)) && a.ldx % V == 0 && (!a.q || (aligned(a.q, V) && a.ldq % V == 0));
   if (rows_only) {
-    const long long span = 32 * V * 4, blocks = ceil_div(a.K, span) * ceil_div(a.M, kWarps);
+    const dim3 grid((unsigned)ceil_div(a.M, kWarps), (unsigned)ceil_div(a.K, 32 * V * 4));
     const auto k = vec ? (e5m2 ? rows_kernel<T, true, true> : rows_kernel<T, true, false>) : (e5m2 ? rows_kernel<T, false, true> : rows_kernel<T, false, false>);
-    k<<<(unsigned)blocks, kThreads, 0, st>>>(p);
+    k<<<grid, kThreads, 0, st>>>(p);
   } else {
     const auto k = vec ? (e5m2 ? tile_kernel<T, true, true> : tile_kernel<T, true, false>) : (e5m2 ? tile_kernel<T, false, true> : tile_kernel<T, false, false>);
     k<<<dim3((unsigned)p.row_blocks, (unsigned)p.col_blocks), kThreads, 0, st>>>(p);
@@ -240,7 +266,7 @@ extern "C" int asgd_quantize(const asgd_quantize_args* args, void* stream) {
   if ((a.square != 0 && a.square != 1) || a.per_token < 1) return ASGD_EINVAL;
   if ((a.square && a.source) || (a.weights && !a.source) || a.rows_x < 0 || (!a.source && a.rows_x != a.M)) return ASGD_EINVAL;
   if (a.ldx < a.K || (a.q && a.ldq < a.K) || (a.qt && a.ldqt < a.M)) return ASGD_EINVAL;
-  if (a.M > 0x7fffffffll || a.K > 0x7fffffffll) return ASGD_EUNSUPPORTED;
+  if (a.M > 0x7fffffffll || a.K > 0x7fff0000ll) return ASGD_EUNSUPPORTED;   // column numbers stay inside 32 bits
   if (a.M == 0 || a.K == 0) return ASGD_OK;
   if ((!a.q && !a.qt) || (a.rows_x > 0 && !a.x) || !aligned(a.x, type_bytes(a.x_type))) return ASGD_EINVAL;
   if (((a.q || a.square) && !a.scale) || (a.qt && !a.square && !a.scale_t)) return ASGD_EINVAL;
@@ -251,8 +277,8 @@ extern "C" int asgd_quantize(const asgd_quantize_args* args, void* stream) {
   p.col_blocks = (int)cb;
   p.fmax = a.q_type == ASGD_E4M3 ? 448.f : 57344.f;
   p.inv_fmax = a.q_type == ASGD_E4M3 ? 1.f / 448.f : 1.f / 57344.f;
-  // limits of the grid: 65535 tiles along M, 2^31 - 1 blocks of rows
-  if ((a.qt || a.square) ? cb > 65535 : ceil_div(a.K, 512) * ceil_div(a.M, kWarps) > 0x7fffffffll) return ASGD_EUNSUPPORTED;
+  // limits of the grid: 65535 tiles along M, or 65535 stretches of a row
+  if ((a.qt || a.square) ? cb > 65535 : ceil_div(a.K, 512) > 65535) return ASGD_EUNSUPPORTED;
   with_type(a.x_type, [&](auto e) { launch<decltype(e)>(p, (cudaStream_t)stream); });
   return cudaGetLastError() == cudaSuccess ? ASGD_OK : ASGD_ECUDA;
 }
