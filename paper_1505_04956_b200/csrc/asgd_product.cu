@@ -57,7 +57,8 @@ unsigned instruction(int type0, int type1, int cols, int rows) {
   return 1u << 4 | (type0 == ASGD_E5M2 ? 1u : 0u) << 7 | (type1 == ASGD_E5M2 ? 1u : 0u) << 10 | (unsigned)(cols >> 3) << 17 | (unsigned)(rows >> 4) << 24;
 }
 
-template <int BN> int launch_few(const asgd_product_args& a, Params p, cudaStream_t st) {
+// `split` blocks share a tile (1: a block takes whole tiles in turn)
+template <int BN, bool kSplit> int launch_few(const asgd_product_args& a, Params p, int split, cudaStream_t st) {
   CUtensorMap map_u{}, map_v{};
   if (p.K > 0) {
     if (!encode(&map_u, a.b, p.K, p.N, p.inner ? 1 : max(p.groups, 1), a.ldb, a.b_group, kU)) return ASGD_EINVAL;
@@ -67,11 +68,28 @@ template <int BN> int launch_few(const asgd_product_args& a, Params p, cudaStrea
   p.tiles_n = (int)ceil_div(p.N, kU);
   const long long most = most_tiles(p, BN, kU);
   if (most > 0x7fffffffll) return ASGD_EUNSUPPORTED;
-  static_assert(smem_bytes<BN>() <= kSmemLimit, "shared memory");
   static std::atomic<unsigned long long> done{0};
-  if (!allow_smem(product_few_kernel<BN>, smem_bytes<BN>(), done)) return ASGD_ECUDA;
-  product_few_kernel<BN><<<(unsigned)min(most, (long long)kSMs), kThreads, smem_bytes<BN>(), st>>>(p, map_u, map_v);
-  return cudaGetLastError() == cudaSuccess ? ASGD_OK : ASGD_ECUDA;
+  if (!allow_smem(product_few_kernel<BN, kSplit>, Few<BN>::kSmem, done)) return ASGD_ECUDA;
+  cudaLaunchConfig_t cfg{};
+  cudaLaunchAttribute cluster;
+  cluster.id = cudaLaunchAttributeClusterDimension;
+  cluster.val.clusterDim.x = (unsigned)split;
+  cluster.val.clusterDim.y = cluster.val.clusterDim.z = 1;
+  cfg.gridDim = dim3(kSplit ? (unsigned)(most * split) : (unsigned)min(most, (long long)kSMs));
+  cfg.blockDim = dim3(Few<BN>::kThreads);
+  cfg.dynamicSmemBytes = Few<BN>::kSmem;
+  cfg.stream = st;
+  cfg.attrs = &cluster;
+  cfg.numAttrs = kSplit ? 1 : 0;
+  return cudaLaunchKernelEx(&cfg, product_few_kernel<BN, kSplit>, p, map_u, map_v) == cudaSuccess ? ASGD_OK : ASGD_ECUDA;
+}
+
+template <int BN> int launch_few(const asgd_product_args& a, const Params& p, cudaStream_t st) {
+  // blocks per tile: as many as there are SMs for, of a power of two, with two K blocks each at least
+  const long long most = most_tiles(p, BN, kU);
+  int split = 1;
+  while (split < kMaxSplit && most * split * 2 <= kSMs && p.kblocks >= split * 4) split *= 2;
+  return split > 1 ? launch_few<BN, true>(a, p, split, st) : launch_few<BN, false>(a, p, 1, st);
 }
 
 int launch_pair(const asgd_product_args& a, Params p, cudaStream_t st) {

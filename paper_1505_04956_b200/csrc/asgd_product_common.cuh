@@ -62,6 +62,7 @@ __device__ inline void copy4(float* dst, const float* src, bool there) {       /
 __device__ inline void arrive_after_copies(unsigned long long* bar) {
   asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
 }
+__device__ inline void prefetch_map(const CUtensorMap* map) { asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory"); }
 // 16 columns of the warp's 32 accumulator rows
 __device__ inline void tmem_load16(unsigned taddr, float (&v)[16]) {
   asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
@@ -94,74 +95,73 @@ struct Tile {
   bool bad;                                          // inner groups whose bounds cut a block
 };
 
-__device__ inline void group_bounds(const Params& p, int g, int limit, int& lo, int& hi) {
-  lo = 0; hi = limit;
-  if (p.offsets) {
-    lo = min(max(p.offsets[g], 0), limit);
-    hi = min(max(p.offsets[g + 1], lo), limit);
-  }
-}
-
-// prefix[g]: tiles of the groups before g, for tiles of bm rows.  All threads of the block; ends with a barrier.
-__device__ inline void count_tiles(const Params& p, int bm, int* prefix, int* warp_part) {
+// What the blocks know of the groups, in shared memory: prefix[g], the tiles (of bm rows) of the groups before g, and
+// start[g], the first row (or K number) of group g.  All threads of the block; ends with a barrier.
+struct Groups {
+  int prefix[ASGD_MAX_EXPERTS + 1], start[ASGD_MAX_EXPERTS + 1], warp_part[32];
+};
+__device__ inline void count_tiles(const Params& p, int bm, Groups& gs) {
   const int G = max(p.groups, 1), tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
+  const int limit = p.inner ? p.K : p.M;
+  if (p.groups)
+    for (int g = tid; g <= G; g += blockDim.x) gs.start[g] = min(max(__ldg(p.offsets + g), 0), limit);
+  else if (tid <= 1) gs.start[tid] = tid ? limit : 0;
+  __syncthreads();
   const int per = (G + blockDim.x - 1) / blockDim.x;
   int mine = 0;
   for (int q = 0; q < per; ++q) {
     const int g = tid * per + q;
     if (g >= G) break;
-    int lo = 0, hi = p.M;
-    if (p.groups && !p.inner) group_bounds(p, g, p.M, lo, hi);
-    const int n = (hi - lo + bm - 1) / bm * p.tiles_n;
-    prefix[g] = n;
+    const int rows = p.inner ? p.M : max(gs.start[g + 1] - gs.start[g], 0);
+    const int n = (rows + bm - 1) / bm * p.tiles_n;
+    gs.prefix[g] = n;
     mine += n;
   }
   int inc = mine;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) { const int v = __shfl_up_sync(kAll, inc, o); if (lane >= o) inc += v; }
-  if (lane == 31) warp_part[wid] = inc;
+  if (lane == 31) gs.warp_part[wid] = inc;
   __syncthreads();
   int before = 0;
-  for (int w = 0; w < wid; ++w) before += warp_part[w];
+  for (int w = 0; w < wid; ++w) before += gs.warp_part[w];
   int run = before + inc - mine;
   for (int q = 0; q < per; ++q) {
     const int g = tid * per + q;
     if (g >= G) break;
-    const int n = prefix[g];
-    prefix[g] = run;
+    const int n = gs.prefix[g];
+    gs.prefix[g] = run;
     run += n;
-    if (g == G - 1) prefix[G] = run;
+    if (g == G - 1) gs.prefix[G] = run;
   }
   __syncthreads();
 }
 
 // Tile number `tile` of tiles of bm x bn.  Inside a group the tiles run down bands of `band` tile rows, column after
 // column: neighbouring blocks share operands in L2.
-__device__ inline Tile find_tile(const Params& p, int bm, int bn, int band, const int* prefix, int tile) {
+__device__ inline Tile find_tile(const Params& p, int bm, int bn, int band, const Groups& gs, int tile) {
   Tile t;
   int a = 0, b = max(p.groups, 1);
   while (b - a > 1) {                                // the last group that starts at or before the tile
     const int m = (a + b) >> 1;
-    if (prefix[m] <= tile) a = m; else b = m;
+    if (gs.prefix[m] <= tile) a = m; else b = m;
   }
   t.g = a;
-  int lo = 0, hi = p.M;
-  if (p.groups && !p.inner) group_bounds(p, a, p.M, lo, hi);
-  const int rows = (hi - lo + bm - 1) / bm;
-  int at = tile - prefix[a], first = 0, high = rows;
+  const int lo = gs.start[a], hi = max(gs.start[a + 1], lo);
+  const int first_row = p.inner ? 0 : lo;
+  t.m_end = p.inner ? p.M : hi;
+  const int rows = (t.m_end - first_row + bm - 1) / bm;
+  int at = tile - gs.prefix[a], first = 0, high = rows;
   if (rows > band) {
     first = at / (band * p.tiles_n) * band;
     at -= first * p.tiles_n;
     high = min(band, rows - first);
   }
   t.n0 = at / high * bn;
-  t.m0 = lo + (first + at % high) * bm;
-  t.m_end = hi;
+  t.m0 = first_row + (first + at % high) * bm;
   t.kb0 = 0; t.kb1 = p.kblocks;
   t.k_end = p.K;
   t.bad = false;
   if (p.inner) {
-    group_bounds(p, a, p.K, lo, hi);
     t.kb0 = lo / kKB;
     t.kb1 = hi > lo ? (hi + kKB - 1) / kKB : t.kb0;
     t.k_end = hi;

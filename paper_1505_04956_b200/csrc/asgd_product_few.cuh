@@ -1,13 +1,20 @@
-// The kernel of asgd_product for few rows of A (per group).
+// The kernel of asgd_product for few rows of A (per group), or few tiles of C.
 //
 // A tile is 128 columns of C (rows of B, the weights: the MMA's M, one per epilogue thread) by BN rows of C (rows of
 // A, the tokens: the MMA's N).  Few tokens then cost few columns of the tensor core's tile, and a warp writes 32
-// neighbouring numbers of a row of C.
+// neighbouring numbers of a row of C.  The weights' bytes are the bound; a tile's products alternate between four
+// accumulator stages, so that the copies never wait for the sums.
 //
-// Warp roles: 0 issues the TMA loads (128-byte K blocks of both operands, swizzled, through a ring of slots); 1 issues
-// the products; 2 brings the tokens' scales (asynchronous 4-byte copies into the same ring); 4 to 7 read the
-// accumulators (tcgen05.ld: one column of C per thread) and keep the sums.  Blocks are persistent and take tiles in
-// turn.  Every wait is bounded.
+// With fewer tiles than SMs a cluster of blocks shares a tile: each takes a stretch of the K blocks, leaves its sums in
+// its shared memory (where the ring was), and adds up its share of the tile's rows from all the cluster's, in the
+// blocks' order, so that the result does not depend on timing.
+//
+// Warp roles: 0 issues the TMA loads (128-byte K blocks of both operands, swizzled, through a ring of slots); 1 and 3
+// issue the products, K blocks in turn (a commit holds its thread for several hundred cycles), one commit per K block,
+// which says "the slot is free" and "the accumulator is full"; 2 brings the tokens' scales (asynchronous 4-byte copies
+// into the same ring); the warps from 4 on read the accumulators (tcgen05.ld: one column of C per thread; with 64 or
+// more tokens two warps share a column's rows) and keep the sums.  Blocks are persistent and take tiles in turn.  Every
+// wait is bounded.
 #pragma once
 
 #include "asgd_product_common.cuh"
@@ -15,158 +22,249 @@
 namespace {
 
 constexpr int kU = 128;                              // columns of C per tile
-constexpr int kThreads = 256;
 constexpr int kNoBand = 1 << 30;
+constexpr int kAccStages = 4;
+constexpr int kMaxSplit = 8;                         // blocks that share a tile
 
-template <int BN> __host__ __device__ constexpr int slots() { return BN == 128 ? 6 : BN == 64 ? 8 : 10; }
-template <int BN> __host__ __device__ constexpr unsigned slot_bytes() { return (kU + BN) * kKB; }
-enum { kMaxSlots = 10, B_FULL = 0, B_EMPTY = kMaxSlots, B_SFULL = 2 * kMaxSlots, B_SEMPTY = 3 * kMaxSlots, B_ACCFULL = 4 * kMaxSlots,
-       B_ACCEMPTY = B_ACCFULL + 2, B_DRAIN = B_ACCEMPTY + 2, B_COUNT };
-template <int BN> __host__ __device__ constexpr size_t smem_bytes() {
-  return 1024 + (size_t)slots<BN>() * slot_bytes<BN>() + (size_t)slots<BN>() * BN * 4 + (ASGD_MAX_EXPERTS + 1 + 32) * 4 + B_COUNT * 8 + 64;
+template <int BN> struct Few {
+  static constexpr int kSlots = BN == 128 ? 6 : BN == 64 ? 8 : 10;     // even: a slot always meets the same issuing thread
+  static constexpr unsigned kSlotBytes = (kU + BN) * kKB;
+  static constexpr int kShare = BN >= 64 ? 2 : 1;                       // warps that share a column's rows of C
+  static constexpr int kRows = BN / kShare;
+  static constexpr int kThreads = 128 + 128 * kShare;
+  static constexpr unsigned kCols = kAccStages * BN < 32 ? 32 : kAccStages * BN;
+  enum { FULL = 0, DONE = kSlots, SFULL = 2 * kSlots, SEMPTY = 3 * kSlots, ACCEMPTY = 4 * kSlots, DRAIN = ACCEMPTY + kAccStages, COUNT = DRAIN + 2 };
+  static constexpr size_t kSmem = 1024 + (size_t)kSlots * kSlotBytes + (size_t)kSlots * BN * 4 + COUNT * 8 + sizeof(Groups) + 64;
+  static_assert(kSmem <= kSmemLimit, "shared memory");
+  static_assert((size_t)BN * kU * 4 <= (size_t)kSlots * kSlotBytes, "a block's sums fit where the ring was");
+};
+
+__device__ inline unsigned cluster_rank() {
+  unsigned r;
+  asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+  return r;
+}
+__device__ inline unsigned cluster_size() {
+  unsigned r;
+  asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(r));
+  return r;
+}
+__device__ inline void cluster_sync() {
+  asm volatile("barrier.cluster.arrive.release;\nbarrier.cluster.wait.acquire;" ::: "memory");
+}
+__device__ inline float load_of_block(const float* smem, unsigned rank) {      // the same place in another block of the cluster
+  unsigned a;
+  float v;
+  asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(smem_u32(smem)), "r"(rank));
+  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(a) : "memory");
+  return v;
 }
 
-template <int BN> __global__ void __launch_bounds__(kThreads, 1)
+// kSplit: launched in clusters, a tile per cluster
+template <int BN, bool kSplit> __global__ void __launch_bounds__(Few<BN>::kThreads, 1)
 product_few_kernel(const Params p, const __grid_constant__ CUtensorMap map_u, const __grid_constant__ CUtensorMap map_v) {
-  constexpr int S = slots<BN>();
+  using F = Few<BN>;
+  constexpr int S = F::kSlots;
   extern __shared__ __align__(1024) unsigned char smem_dyn[];
   unsigned char* ring = smem_dyn + ((1024u - (smem_u32(smem_dyn) & 1023u)) & 1023u);
-  float* sv = reinterpret_cast<float*>(ring + (size_t)S * slot_bytes<BN>());           // [slot][BN] scales of the tokens
+  float* sv = reinterpret_cast<float*>(ring + (size_t)S * F::kSlotBytes);              // [slot][BN] scales of the tokens
   unsigned long long* bars = reinterpret_cast<unsigned long long*>(sv + S * BN);
-  int* prefix = reinterpret_cast<int*>(bars + B_COUNT);
-  int* warp_part = prefix + ASGD_MAX_EXPERTS + 1;
-  int* misc = warp_part + 32;                                                            // [0] tensor memory, [1] abort
+  Groups& gs = *reinterpret_cast<Groups*>(bars + F::COUNT);
+  int* misc = reinterpret_cast<int*>(&gs + 1);                                          // [0] tensor memory, [1] abort
+  int* abort = misc + 1;
   const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
-  constexpr unsigned kCols = 2 * BN < 32 ? 32 : 2 * BN;
+  const int rank = kSplit ? (int)cluster_rank() : 0, share = kSplit ? (int)cluster_size() : 1;
+  const int first = (int)blockIdx.x / share, step = (int)gridDim.x / share;
 
   if (tid == 0) {
-    for (int q = 0; q < S; ++q) { mbar_init(bars + B_FULL + q, 1); mbar_init(bars + B_EMPTY + q, 1); mbar_init(bars + B_SFULL + q, 32); mbar_init(bars + B_SEMPTY + q, 4); }
-    for (int q = 0; q < 2; ++q) { mbar_init(bars + B_ACCFULL + q, 1); mbar_init(bars + B_ACCEMPTY + q, 4); }
-    mbar_init(bars + B_DRAIN, 1);
+    prefetch_map(&map_u);
+    prefetch_map(&map_v);
+    for (int q = 0; q < S; ++q) {
+      mbar_init(bars + F::FULL + q, 1); mbar_init(bars + F::DONE + q, 1);
+      mbar_init(bars + F::SFULL + q, 32); mbar_init(bars + F::SEMPTY + q, 4 * F::kShare);
+    }
+    for (int q = 0; q < kAccStages; ++q) mbar_init(bars + F::ACCEMPTY + q, 4 * F::kShare);
+    for (int q = 0; q < 2; ++q) mbar_init(bars + F::DRAIN + q, 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     misc[1] = 0;
   }
   if (wid == 1) {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(misc)), "r"(kCols) : "memory");
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(misc)), "r"(F::kCols) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
-  count_tiles(p, BN, prefix, warp_part);
+  count_tiles(p, BN, gs);
   fence_before();
   __syncthreads();
   fence_after();
   const unsigned tmem = (unsigned)misc[0];
-  const int tiles = prefix[max(p.groups, 1)];
-  int* abort = misc + 1;
+  const int tiles = gs.prefix[max(p.groups, 1)];
+  // a tile's K blocks, or the block's stretch of them
+  auto tile_at = [&](int tile) {
+    Tile t = find_tile(p, BN, kU, kNoBand, gs, tile);
+    if (kSplit) {
+      const int n = t.kb1 - t.kb0, from = t.kb0;
+      t.kb0 = from + n * rank / share;
+      t.kb1 = from + n * (rank + 1) / share;
+    }
+    return t;
+  };
 
   if (wid == 0) {
     if (lane == 0) {
       unsigned it = 0;
       bool ok = true;
-      for (int tile = blockIdx.x; tile < tiles && ok; tile += gridDim.x) {
-        const Tile t = find_tile(p, BN, kU, kNoBand, prefix, tile);
+      for (int tile = first; tile < tiles && ok; tile += step) {
+        const Tile t = tile_at(tile);
         for (int kb = t.kb0; kb < t.kb1; ++kb, ++it) {
           const unsigned q = it % S;
-          if (it >= S && !(ok = wait(bars + B_EMPTY + q, (it / S - 1) & 1, p.wait_limit, abort))) break;
-          unsigned char* to = ring + (size_t)q * slot_bytes<BN>();
-          mbar_expect_tx(bars + B_FULL + q, slot_bytes<BN>());
+          if (it >= S && !(ok = wait(bars + F::DONE + q, (it / S - 1) & 1, p.wait_limit, abort))) break;
+          unsigned char* to = ring + (size_t)q * F::kSlotBytes;
+          mbar_expect_tx(bars + F::FULL + q, F::kSlotBytes);
           if (!(p.withhold && it == 0)) {
-            tma_load_3d(to, &map_u, kb * kKB, t.n0, p.inner ? 0 : t.g, bars + B_FULL + q);
-            tma_load_3d(to + kU * kKB, &map_v, kb * kKB, t.m0, 0, bars + B_FULL + q);
+            tma_load_3d(to, &map_u, kb * kKB, t.n0, p.inner ? 0 : t.g, bars + F::FULL + q);
+            tma_load_3d(to + kU * kKB, &map_v, kb * kKB, t.m0, 0, bars + F::FULL + q);
           }
         }
       }
       if (!ok)                                       // copies in flight land before the block leaves
         for (unsigned q = 0; q < S && q < it; ++q) {
           const unsigned last = (it - 1 - q) / S;    // the slot's last use
-          for (unsigned n = 0; n < p.wait_limit && !mbar_try_wait(bars + B_FULL + q, last & 1); ++n) {}
+          for (unsigned n = 0; n < p.wait_limit && !mbar_try_wait(bars + F::FULL + q, last & 1); ++n) {}
         }
     }
-  } else if (wid == 1) {
+  } else if (wid == 1 || wid == 3) {
     if (lane == 0) {
+      const unsigned me = (unsigned)wid >> 1;
       unsigned it = 0;
       bool ok = true;
-      for (int tile = blockIdx.x; tile < tiles && ok; tile += gridDim.x) {
-        const Tile t = find_tile(p, BN, kU, kNoBand, prefix, tile);
+      for (int tile = first; tile < tiles && ok; tile += step) {
+        const Tile t = tile_at(tile);
         for (int kb = t.kb0; kb < t.kb1; ++kb, ++it) {
-          const unsigned q = it % S, stage = it & 1;
-          if (it >= 2 && !(ok = wait(bars + B_ACCEMPTY + stage, (it / 2 - 1) & 1, p.wait_limit, abort))) break;
-          if (!(ok = wait(bars + B_FULL + q, (it / S) & 1, p.wait_limit, abort))) break;
-          fence_after();
-          const unsigned long long du = operand_desc(ring + (size_t)q * slot_bytes<BN>()), dv = operand_desc(ring + (size_t)q * slot_bytes<BN>() + kU * kKB);
+          if ((it & 1) != me) continue;
+          const unsigned q = it % S, stage = it % kAccStages;
+          if (!(ok = wait(bars + F::FULL + q, (it / S) & 1, p.wait_limit, abort))) break;
+          const unsigned long long du = operand_desc(ring + (size_t)q * F::kSlotBytes), dv = operand_desc(ring + (size_t)q * F::kSlotBytes + kU * kKB);
           const int steps = steps_of(t, kb);
+          if (it >= kAccStages && !(ok = wait(bars + F::ACCEMPTY + stage, (it / kAccStages - 1) & 1, p.wait_limit, abort))) break;
+          fence_after();
 #pragma unroll
           for (int k4 = 0; k4 < 4; ++k4) if (k4 < steps) mma_f8(tmem + stage * BN, du + 2 * k4, dv + 2 * k4, p.idesc, k4 != 0);
-          commit(bars + B_EMPTY + q);
-          commit(bars + B_ACCFULL + stage);
+          commit(bars + F::DONE + q);
         }
       }
       if (!ok && it) {                               // products in flight end before the tensor memory is freed
-        commit(bars + B_DRAIN);
-        for (unsigned n = 0; n < p.wait_limit && !mbar_try_wait(bars + B_DRAIN, 0); ++n) {}
+        commit(bars + F::DRAIN + me);
+        for (unsigned n = 0; n < p.wait_limit && !mbar_try_wait(bars + F::DRAIN + me, 0); ++n) {}
       }
     }
   } else if (wid == 2) {
     unsigned it = 0;
     bool ok = true;
-    for (int tile = blockIdx.x; tile < tiles && ok; tile += gridDim.x) {
-      const Tile t = find_tile(p, BN, kU, kNoBand, prefix, tile);
+    for (int tile = first; tile < tiles && ok; tile += step) {
+      const Tile t = tile_at(tile);
       for (int kb = t.kb0; kb < t.kb1; ++kb, ++it) {
         const unsigned q = it % S;
-        if (it >= S && !(ok = __all_sync(kAll, wait(bars + B_SEMPTY + q, (it / S - 1) & 1, p.wait_limit, abort)))) break;
+        if (it >= S && !(ok = __all_sync(kAll, wait(bars + F::SEMPTY + q, (it / S - 1) & 1, p.wait_limit, abort)))) break;
 #pragma unroll
         for (int c = 0; c < BN; c += 32) {
           const int r = t.m0 + c + lane;
           if (c + lane < BN) copy4(sv + q * BN + c + lane, r < t.m_end ? p.sa + r * p.sa_row + kb * p.sa_block : p.sa, r < t.m_end);
         }
-        arrive_after_copies(bars + B_SFULL + q);
+        arrive_after_copies(bars + F::SFULL + q);
       }
     }
     asm volatile("cp.async.wait_all;" ::: "memory");
-  } else if (wid >= 4) {
-    const int quarter = wid & 3;
+  } else {
+    const int quarter = wid & 3, c_first = ((wid - 4) >> 2) * F::kRows;                  // the warp's columns and rows of C
+    const unsigned at_tmem = tmem + ((unsigned)(quarter * 32) << 16) + c_first;
     unsigned it = 0;
     bool ok = true;
-    for (int tile = blockIdx.x; tile < tiles && ok; tile += gridDim.x) {
-      const Tile t = find_tile(p, BN, kU, kNoBand, prefix, tile);
+    for (int tile = first; tile < tiles && ok; tile += step) {
+      const Tile t = tile_at(tile);
       const int u = t.n0 + quarter * 32 + lane;
       const float* su_at = p.sb + (p.inner ? 0 : t.g * p.sb_group) + (long long)(min(u, p.N - 1) >> p.sb_shift) * p.sb_row;
-      float acc[BN];
+      auto column_scale = [&](int kb) { return __ldg(su_at + min(kb, t.kb1 - 1) * p.sb_block); };
+      float acc[F::kRows];
 #pragma unroll
-      for (int c = 0; c < BN; ++c) acc[c] = 0.f;
-      float su_next = t.kb0 < t.kb1 ? __ldg(su_at + t.kb0 * p.sb_block) : 0.f;
+      for (int c = 0; c < F::kRows; ++c) acc[c] = 0.f;
+      float su = 0.f, su1 = 0.f;                     // loaded two K blocks ahead of their use
+      if (t.kb0 < t.kb1) { su = column_scale(t.kb0); su1 = column_scale(t.kb0 + 1); }
       for (int kb = t.kb0; kb < t.kb1; ++kb, ++it) {
-        const unsigned q = it % S, stage = it & 1;
-        const float su = su_next;
-        if (kb + 1 < t.kb1) su_next = __ldg(su_at + (kb + 1) * p.sb_block);
-        ok = wait(bars + B_SFULL + q, (it / S) & 1, p.wait_limit, abort) && wait(bars + B_ACCFULL + stage, (it / 2) & 1, p.wait_limit, abort);
+        const unsigned q = it % S, stage = it % kAccStages;
+        const float su2 = column_scale(kb + 2);
+        ok = wait(bars + F::SFULL + q, (it / S) & 1, p.wait_limit, abort) && wait(bars + F::DONE + q, (it / S) & 1, p.wait_limit, abort);
         if (!(ok = __all_sync(kAll, ok))) break;
         fence_after();
+        const float4* scale = reinterpret_cast<const float4*>(sv + q * BN + c_first);
+        float v[2][16];
+        tmem_load16(at_tmem + stage * BN, v[0]);
 #pragma unroll
-        for (int c0 = 0; c0 < BN; c0 += 16) {
-          float v[16];
-          tmem_load16(tmem + ((unsigned)(quarter * 32) << 16) + stage * BN + c0, v);
+        for (int c0 = 0; c0 < F::kRows; c0 += 16) {
           tmem_wait();
+          if (c0 + 16 < F::kRows) tmem_load16(at_tmem + stage * BN + c0 + 16, v[(c0 / 16 + 1) & 1]);
+          else {
+            fence_before();
+            __syncwarp();
+            if (lane == 0) arrive(bars + F::ACCEMPTY + stage);
+          }
 #pragma unroll
-          for (int c = 0; c < 16; ++c) acc[c0 + c] = fmaf(v[c] * su, sv[q * BN + c0 + c], acc[c0 + c]);
+          for (int c = 0; c < 16; c += 4) {
+            const float4 f = scale[(c0 + c) / 4];
+            const float* w = v[(c0 / 16) & 1] + c;
+            acc[c0 + c] = fmaf(w[0] * su, f.x, acc[c0 + c]);
+            acc[c0 + c + 1] = fmaf(w[1] * su, f.y, acc[c0 + c + 1]);
+            acc[c0 + c + 2] = fmaf(w[2] * su, f.z, acc[c0 + c + 2]);
+            acc[c0 + c + 3] = fmaf(w[3] * su, f.w, acc[c0 + c + 3]);
+          }
         }
-        fence_before();
         __syncwarp();
-        if (lane == 0) { arrive(bars + B_ACCEMPTY + stage); arrive(bars + B_SEMPTY + q); }
+        if (lane == 0) arrive(bars + F::SEMPTY + q);
+        su = su1;
+        su1 = su2;
       }
       if (!ok) break;
       if (t.bad && lane == 0) atomicMin(&g_status, ASGD_EINVAL);
-      if (u < p.N) {
+      if (kSplit) {
+        // every copy into the ring has been read: the products that read them are complete
+        float* sums = reinterpret_cast<float*>(ring);
+#pragma unroll
+        for (int c = 0; c < F::kRows; ++c) sums[(c_first + c) * kU + quarter * 32 + lane] = t.bad ? __int_as_float(0x7fffffff) : acc[c];
+      } else if (u < p.N) {
         const long long base = (p.inner ? t.g * p.c_group : 0) + u;
 #pragma unroll
-        for (int c = 0; c < BN; ++c)
-          if (t.m0 + c < t.m_end) store_c(p.c, p.c_type, base + (long long)(t.m0 + c) * p.ldc, t.bad ? __int_as_float(0x7fffffff) : acc[c]);
+        for (int c = 0; c < F::kRows; ++c) {
+          const int m = t.m0 + c_first + c;
+          if (m < t.m_end) store_c(p.c, p.c_type, base + (long long)m * p.ldc, t.bad ? __int_as_float(0x7fffffff) : acc[c]);
+        }
       }
     }
   }
+  __syncwarp();
   fence_before();
-  __syncthreads();
+  if (kSplit) {
+    cluster_sync();
+    if (first < tiles && !*reinterpret_cast<volatile int*>(abort)) {
+      const Tile t = find_tile(p, BN, kU, kNoBand, gs, first);
+      const int rows = min(BN, t.m_end - t.m0), cols = min(kU, p.N - t.n0);
+      const float* sums = reinterpret_cast<const float*>(ring);
+      const long long base = (p.inner ? t.g * p.c_group : 0) + t.n0;
+      for (int e = rows * rank / share * kU + tid; e < rows * (rank + 1) / share * kU; e += F::kThreads) {
+        const int u = e % kU;
+        float s[kMaxSplit];
+#pragma unroll
+        for (int r = 0; r < kMaxSplit; ++r) s[r] = r < share ? load_of_block(sums + e, r) : 0.f;
+        float sum = s[0];
+#pragma unroll
+        for (int r = 1; r < kMaxSplit; ++r) if (r < share) sum += s[r];
+        if (u < cols) store_c(p.c, p.c_type, base + (long long)(t.m0 + e / kU) * p.ldc + u, sum);
+      }
+    }
+    cluster_sync();                                  // no block leaves while another reads its sums
+  } else {
+    __syncthreads();
+  }
   fence_after();
-  if (wid == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kCols));
+  if (wid == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(F::kCols));
   if (tid == 0 && *reinterpret_cast<volatile int*>(abort)) atomicMin(&g_status, ASGD_ETIMEOUT);
 }
 

@@ -27,7 +27,7 @@ constexpr int kStageBytes = 32 * 64;                 // per warp: 64 bytes of ea
 enum { P_FULL = 0, P_DONE = kPairSlots, P_SFULL = 2 * kPairSlots, P_SEMPTY = 3 * kPairSlots, P_ACCEMPTY = 4 * kPairSlots,
        P_DRAIN = P_ACCEMPTY + 2, P_COUNT = P_DRAIN + 2 };
 constexpr size_t kPairSmem = 1024 + (size_t)kPairSlots * kPairBytes + 8 * kStageBytes + (size_t)kPairSlots * kPairCols * 4 +
-                             P_COUNT * 8 + (ASGD_MAX_EXPERTS + 1 + 32) * 4 + 64;
+                             P_COUNT * 8 + sizeof(Groups) + 64;
 static_assert(kPairSmem <= kSmemLimit, "shared memory");
 
 __device__ inline unsigned in_first_block(const void* smem) {                  // the same place in the pair's first block
@@ -116,15 +116,16 @@ product_pair_kernel(const Params p, const __grid_constant__ CUtensorMap map_a, c
   unsigned char* stages = ring + (size_t)S * kPairBytes;
   float* sv = reinterpret_cast<float*>(stages + 8 * kStageBytes);                       // [slot][256] scales of the columns
   unsigned long long* bars = reinterpret_cast<unsigned long long*>(sv + S * kPairCols);
-  int* prefix = reinterpret_cast<int*>(bars + P_COUNT);
-  int* warp_part = prefix + ASGD_MAX_EXPERTS + 1;
-  int* misc = warp_part + 32;        // [0] tensor memory, [1] abort, [2, 3] K blocks whose copies each block has issued, [4] the other block gave up
+  Groups& gs = *reinterpret_cast<Groups*>(bars + P_COUNT);
+  int* misc = reinterpret_cast<int*>(&gs + 1);        // [0] tensor memory, [1] abort, [2, 3] K blocks whose copies each block has issued, [4] the other block gave up
   int* abort = misc + 1;
   const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
   const unsigned rank = rank_in_pair();
   const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
 
   if (tid == 0) {
+    prefetch_map(&map_a);
+    prefetch_map(&map_b);
     for (int q = 0; q < S; ++q) { mbar_init(bars + P_FULL + q, 1); mbar_init(bars + P_DONE + q, 1); mbar_init(bars + P_SFULL + q, 32); mbar_init(bars + P_SEMPTY + q, 8); }
     for (int q = 0; q < 2; ++q) { mbar_init(bars + P_ACCEMPTY + q, 16); mbar_init(bars + P_DRAIN + q, 1); }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -134,13 +135,13 @@ product_pair_kernel(const Params p, const __grid_constant__ CUtensorMap map_a, c
     asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(misc)), "r"(512u) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
   }
-  count_tiles(p, kPairRows, prefix, warp_part);
+  count_tiles(p, kPairRows, gs);
   fence_before();
   __syncthreads();
   pair_sync();
   fence_after();
   const unsigned tmem = (unsigned)misc[0];
-  const int tiles = prefix[max(p.groups, 1)];
+  const int tiles = gs.prefix[max(p.groups, 1)];
 
   if (wid < 4) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
@@ -149,7 +150,7 @@ product_pair_kernel(const Params p, const __grid_constant__ CUtensorMap map_a, c
       unsigned it = 0;
       bool ok = true;
       for (int tile = pair; tile < tiles && ok; tile += pairs) {
-        const Tile t = find_tile(p, kPairRows, kPairCols, kPairBand, prefix, tile);
+        const Tile t = find_tile(p, kPairRows, kPairCols, kPairBand, gs, tile);
         const int za = 0, zb = p.inner ? 0 : t.g;
         for (int kb = t.kb0; kb < t.kb1; ++kb, ++it) {
           const unsigned q = it % S;
@@ -171,7 +172,7 @@ product_pair_kernel(const Params p, const __grid_constant__ CUtensorMap map_a, c
       unsigned it = 0;
       bool ok = true;
       for (int tile = pair; tile < tiles && ok; tile += pairs) {
-        const Tile t = find_tile(p, kPairRows, kPairCols, kPairBand, prefix, tile);
+        const Tile t = find_tile(p, kPairRows, kPairCols, kPairBand, gs, tile);
         for (int kb = t.kb0; kb < t.kb1; ++kb, ++it) {
           const unsigned q = it % S, stage = it & 1;
           if (stage != me) continue;
@@ -194,7 +195,7 @@ product_pair_kernel(const Params p, const __grid_constant__ CUtensorMap map_a, c
       unsigned it = 0;
       bool ok = true;
       for (int tile = pair; tile < tiles && ok; tile += pairs) {
-        const Tile t = find_tile(p, kPairRows, kPairCols, kPairBand, prefix, tile);
+        const Tile t = find_tile(p, kPairRows, kPairCols, kPairBand, gs, tile);
         const float* from = p.sb + (p.inner ? 0 : t.g * p.sb_group);
         for (int kb = t.kb0; kb < t.kb1; ++kb, ++it) {
           const unsigned q = it % S;
@@ -219,7 +220,7 @@ product_pair_kernel(const Params p, const __grid_constant__ CUtensorMap map_a, c
     unsigned it = 0;
     bool ok = true;
     for (int tile = pair; tile < tiles && ok; tile += pairs) {
-      const Tile t = find_tile(p, kPairRows, kPairCols, kPairBand, prefix, tile);
+      const Tile t = find_tile(p, kPairRows, kPairCols, kPairBand, gs, tile);
       const int m = t.m0 + (int)rank * kHalf + quarter * 32, n = t.n0 + half * 128;      // the warp's corner
       const float* sa_at = p.sa + min(m + lane, p.M - 1) * p.sa_row;
       const float* sb_at = p.sb + (p.inner ? 0 : t.g * p.sb_group) + (long long)(min(n, p.N - 1) >> 7) * p.sb_row;
