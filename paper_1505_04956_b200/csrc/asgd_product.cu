@@ -18,23 +18,33 @@ std::atomic<int> g_withhold{0};
 
 // ---- host ----
 
-// rows of 128-byte K blocks of an 8-bit matrix [outer][rows][cols]; what lies beyond is read as zeros
-bool encode(CUtensorMap* map, const void* base, long long cols, long long rows, long long outer, long long ld, long long outer_stride, unsigned box_rows) {
+PFN_cuTensorMapEncodeTiled encoder() {
   static std::atomic<PFN_cuTensorMapEncodeTiled> known{nullptr};
   PFN_cuTensorMapEncodeTiled f = known.load();
   if (!f) {
     void* fn = nullptr;
     cudaDriverEntryPointQueryResult q;
-    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &q) != cudaSuccess || !fn) return false;
+    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &q) != cudaSuccess || !fn) return nullptr;
     f = (PFN_cuTensorMapEncodeTiled)fn;
     known.store(f);
   }
+  return f;
+}
+// a matrix [outer][rows][cols]; strides in bytes; what lies beyond is read as zeros and not written
+bool encode(CUtensorMap* map, CUtensorMapDataType type, CUtensorMapSwizzle swizzle, const void* base, long long cols, long long rows, long long outer,
+            long long row_bytes, long long outer_bytes, unsigned box_cols, unsigned box_rows) {
+  const PFN_cuTensorMapEncodeTiled f = encoder();
+  if (!f) return false;
   cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)outer};
-  cuuint64_t strides[2] = {(cuuint64_t)ld, (cuuint64_t)(outer > 1 ? outer_stride : ld)};
-  cuuint32_t box[3] = {kKB, box_rows, 1};
+  cuuint64_t strides[2] = {(cuuint64_t)row_bytes, (cuuint64_t)(outer > 1 ? outer_bytes : row_bytes)};
+  cuuint32_t box[3] = {box_cols, box_rows, 1};
   cuuint32_t estr[3] = {1, 1, 1};
-  return f(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
-           CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+  return f(map, type, 3, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
+           CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+// 128-byte K blocks of an 8-bit operand
+bool encode(CUtensorMap* map, const void* base, long long cols, long long rows, long long outer, long long ld, long long outer_stride, unsigned box_rows) {
+  return encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, CU_TENSOR_MAP_SWIZZLE_128B, base, cols, rows, outer, ld, outer_stride, kKB, box_rows);
 }
 
 // the most tiles of bm x bn there can be: what the offsets say is known on the device alone
@@ -102,10 +112,18 @@ int launch_pair(const asgd_product_args& a, Params p, cudaStream_t st) {
   p.tiles_n = (int)ceil_div(p.N, kPairCols);
   const long long most = most_tiles(p, kPairRows, kPairCols);
   if (most > 0x7fffffffll) return ASGD_EUNSUPPORTED;
+  // C by tensor map where its rows (and groups) start at 16-byte boundaries
+  CUtensorMap map_c{};
+  const long long size = (long long)type_bytes(a.c_type), outer = p.inner ? p.groups : 1;
+  p.c_by_map = aligned(a.c, 16) && a.ldc * size % 16 == 0 && (outer == 1 || (a.c_group > 0 && a.c_group * size % 16 == 0));
+  if (p.c_by_map) {
+    const CUtensorMapDataType type = a.c_type == ASGD_F32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : a.c_type == ASGD_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
+    p.c_by_map = encode(&map_c, type, CU_TENSOR_MAP_SWIZZLE_64B, a.c, p.N, p.M, outer, a.ldc * size, a.c_group * size, (unsigned)(64 / size), 32);
+  }
   const auto kernel = a.b_square ? product_pair_kernel<false> : product_pair_kernel<true>;
   static std::atomic<unsigned long long> done[2] = {{0}, {0}};
   if (!allow_smem(kernel, kPairSmem, done[a.b_square])) return ASGD_ECUDA;
-  kernel<<<(unsigned)min(most, (long long)(kSMs / 2)) * 2, kPairThreads, kPairSmem, st>>>(p, map_a, map_b);
+  kernel<<<(unsigned)min(most, (long long)(kSMs / 2)) * 2, kPairThreads, kPairSmem, st>>>(p, map_a, map_b, map_c);
   return cudaGetLastError() == cudaSuccess ? ASGD_OK : ASGD_ECUDA;
 }
 
@@ -130,7 +148,7 @@ extern "C" int asgd_product(const asgd_product_args* args, void* stream) {
   p.sa = a.a_scale; p.sa_row = a.a_scale_row; p.sa_block = a.a_scale_block;
   p.sb = a.b_scale; p.sb_row = a.b_scale_row; p.sb_block = a.b_scale_block; p.sb_group = a.b_scale_group;
   p.sb_shift = a.b_square ? 7 : 0;
-  p.c = a.c; p.ldc = a.ldc; p.c_group = a.c_group; p.c_type = a.c_type;
+  p.c = a.c; p.ldc = a.ldc; p.c_group = a.c_group; p.c_type = a.c_type; p.c_by_map = 0;
   p.offsets = a.offsets;
   p.idesc = 0;
   p.wait_limit = g_wait_limit.load();

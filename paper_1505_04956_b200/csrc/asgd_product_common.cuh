@@ -28,7 +28,7 @@ struct Params {
   int sb_shift;
   void* c;
   long long ldc, c_group;
-  int c_type;
+  int c_type, c_by_map;                              // c_by_map: a tensor map of C is there
   const int* offsets;
   unsigned idesc, wait_limit;
   int withhold;

@@ -11,8 +11,8 @@
 //
 // Warp roles: 0 issues the TMA loads (128-byte K blocks of both operands, swizzled, through a ring of slots); 1 and 3
 // issue the products, K blocks in turn (a commit holds its thread for several hundred cycles), one commit per K block,
-// which says "the slot is free" and "the accumulator is full"; 2 brings the tokens' scales (asynchronous 4-byte copies
-// into the same ring); the warps from 4 on read the accumulators (tcgen05.ld: one column of C per thread; with 64 or
+// which says "the slot is free" and "the accumulator is full"; 2 brings the scales (asynchronous 4-byte copies; a load
+// into registers would hold the reading warps); the warps from 4 on read the accumulators (tcgen05.ld: one column of C per thread; with 64 or
 // more tokens two warps share a column's rows) and keep the sums.  Blocks are persistent and take tiles in turn.  Every
 // wait is bounded.
 #pragma once
@@ -34,7 +34,8 @@ template <int BN> struct Few {
   static constexpr int kThreads = 128 + 128 * kShare;
   static constexpr unsigned kCols = kAccStages * BN < 32 ? 32 : kAccStages * BN;
   enum { FULL = 0, DONE = kSlots, SFULL = 2 * kSlots, SEMPTY = 3 * kSlots, ACCEMPTY = 4 * kSlots, DRAIN = ACCEMPTY + kAccStages, COUNT = DRAIN + 2 };
-  static constexpr size_t kSmem = 1024 + (size_t)kSlots * kSlotBytes + (size_t)kSlots * BN * 4 + COUNT * 8 + sizeof(Groups) + 64;
+  static constexpr int kScales = BN + kU;                               // of a slot: the tokens', then the columns'
+  static constexpr size_t kSmem = 1024 + (size_t)kSlots * kSlotBytes + (size_t)kSlots * kScales * 4 + COUNT * 8 + sizeof(Groups) + 64;
   static_assert(kSmem <= kSmemLimit, "shared memory");
   static_assert((size_t)BN * kU * 4 <= (size_t)kSlots * kSlotBytes, "a block's sums fit where the ring was");
 };
@@ -52,11 +53,14 @@ __device__ inline unsigned cluster_size() {
 __device__ inline void cluster_sync() {
   asm volatile("barrier.cluster.arrive.release;\nbarrier.cluster.wait.acquire;" ::: "memory");
 }
-__device__ inline float load_of_block(const float* smem, unsigned rank) {      // the same place in another block of the cluster
+__device__ inline unsigned in_block(const void* smem, unsigned rank) {         // the same place in another block of the cluster
   unsigned a;
-  float v;
   asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(smem_u32(smem)), "r"(rank));
-  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(a) : "memory");
+  return a;
+}
+__device__ inline float4 load_cluster4(unsigned addr) {
+  float4 v;
+  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
   return v;
 }
 
@@ -67,8 +71,8 @@ product_few_kernel(const Params p, const __grid_constant__ CUtensorMap map_u, co
   constexpr int S = F::kSlots;
   extern __shared__ __align__(1024) unsigned char smem_dyn[];
   unsigned char* ring = smem_dyn + ((1024u - (smem_u32(smem_dyn) & 1023u)) & 1023u);
-  float* sv = reinterpret_cast<float*>(ring + (size_t)S * F::kSlotBytes);              // [slot][BN] scales of the tokens
-  unsigned long long* bars = reinterpret_cast<unsigned long long*>(sv + S * BN);
+  float* scales = reinterpret_cast<float*>(ring + (size_t)S * F::kSlotBytes);          // [slot][kScales]
+  unsigned long long* bars = reinterpret_cast<unsigned long long*>(scales + S * F::kScales);
   Groups& gs = *reinterpret_cast<Groups*>(bars + F::COUNT);
   int* misc = reinterpret_cast<int*>(&gs + 1);                                          // [0] tensor memory, [1] abort
   int* abort = misc + 1;
@@ -162,13 +166,20 @@ product_few_kernel(const Params p, const __grid_constant__ CUtensorMap map_u, co
     bool ok = true;
     for (int tile = first; tile < tiles && ok; tile += step) {
       const Tile t = tile_at(tile);
+      const float* from = p.sb + (p.inner ? 0 : t.g * p.sb_group);
       for (int kb = t.kb0; kb < t.kb1; ++kb, ++it) {
         const unsigned q = it % S;
         if (it >= S && !(ok = __all_sync(kAll, wait(bars + F::SEMPTY + q, (it / S - 1) & 1, p.wait_limit, abort)))) break;
+        float* to = scales + q * F::kScales;
+#pragma unroll
+        for (int c = 0; c < kU; c += 32) {
+          const int n = min(t.n0 + c + lane, p.N - 1);
+          copy4(to + BN + c + lane, from + (n >> p.sb_shift) * p.sb_row + kb * p.sb_block, true);
+        }
 #pragma unroll
         for (int c = 0; c < BN; c += 32) {
           const int r = t.m0 + c + lane;
-          if (c + lane < BN) copy4(sv + q * BN + c + lane, r < t.m_end ? p.sa + r * p.sa_row + kb * p.sa_block : p.sa, r < t.m_end);
+          if (c + lane < BN) copy4(to + c + lane, r < t.m_end ? p.sa + r * p.sa_row + kb * p.sa_block : p.sa, r < t.m_end);
         }
         arrive_after_copies(bars + F::SFULL + q);
       }
@@ -182,20 +193,16 @@ product_few_kernel(const Params p, const __grid_constant__ CUtensorMap map_u, co
     for (int tile = first; tile < tiles && ok; tile += step) {
       const Tile t = tile_at(tile);
       const int u = t.n0 + quarter * 32 + lane;
-      const float* su_at = p.sb + (p.inner ? 0 : t.g * p.sb_group) + (long long)(min(u, p.N - 1) >> p.sb_shift) * p.sb_row;
-      auto column_scale = [&](int kb) { return __ldg(su_at + min(kb, t.kb1 - 1) * p.sb_block); };
       float acc[F::kRows];
 #pragma unroll
       for (int c = 0; c < F::kRows; ++c) acc[c] = 0.f;
-      float su = 0.f, su1 = 0.f;                     // loaded two K blocks ahead of their use
-      if (t.kb0 < t.kb1) { su = column_scale(t.kb0); su1 = column_scale(t.kb0 + 1); }
       for (int kb = t.kb0; kb < t.kb1; ++kb, ++it) {
         const unsigned q = it % S, stage = it % kAccStages;
-        const float su2 = column_scale(kb + 2);
         ok = wait(bars + F::SFULL + q, (it / S) & 1, p.wait_limit, abort) && wait(bars + F::DONE + q, (it / S) & 1, p.wait_limit, abort);
         if (!(ok = __all_sync(kAll, ok))) break;
         fence_after();
-        const float4* scale = reinterpret_cast<const float4*>(sv + q * BN + c_first);
+        const float su = scales[q * F::kScales + BN + quarter * 32 + lane];
+        const float4* scale = reinterpret_cast<const float4*>(scales + q * F::kScales + c_first);
         float v[2][16];
         tmem_load16(at_tmem + stage * BN, v[0]);
 #pragma unroll
@@ -219,8 +226,6 @@ product_few_kernel(const Params p, const __grid_constant__ CUtensorMap map_u, co
         }
         __syncwarp();
         if (lane == 0) arrive(bars + F::SEMPTY + q);
-        su = su1;
-        su1 = su2;
       }
       if (!ok) break;
       if (t.bad && lane == 0) atomicMin(&g_status, ASGD_EINVAL);
@@ -246,17 +251,23 @@ product_few_kernel(const Params p, const __grid_constant__ CUtensorMap map_u, co
     if (first < tiles && !*reinterpret_cast<volatile int*>(abort)) {
       const Tile t = find_tile(p, BN, kU, kNoBand, gs, first);
       const int rows = min(BN, t.m_end - t.m0), cols = min(kU, p.N - t.n0);
-      const float* sums = reinterpret_cast<const float*>(ring);
       const long long base = (p.inner ? t.g * p.c_group : 0) + t.n0;
-      for (int e = rows * rank / share * kU + tid; e < rows * (rank + 1) / share * kU; e += F::kThreads) {
-        const int u = e % kU;
-        float s[kMaxSplit];
+      unsigned from[kMaxSplit];
 #pragma unroll
-        for (int r = 0; r < kMaxSplit; ++r) s[r] = r < share ? load_of_block(sums + e, r) : 0.f;
-        float sum = s[0];
+      for (int r = 0; r < kMaxSplit; ++r) from[r] = in_block(ring, r < share ? r : 0);
+      // four neighbouring columns per thread and turn
+      for (int e = rows * rank / share * (kU / 4) + tid; e < rows * (rank + 1) / share * (kU / 4); e += F::kThreads) {
+        float4 s[kMaxSplit];
 #pragma unroll
-        for (int r = 1; r < kMaxSplit; ++r) if (r < share) sum += s[r];
-        if (u < cols) store_c(p.c, p.c_type, base + (long long)(t.m0 + e / kU) * p.ldc + u, sum);
+        for (int r = 0; r < kMaxSplit; ++r) if (r < share) s[r] = load_cluster4(from[r] + e * 16);
+        float4 sum = s[0];
+#pragma unroll
+        for (int r = 1; r < kMaxSplit; ++r) if (r < share) { sum.x += s[r].x; sum.y += s[r].y; sum.z += s[r].z; sum.w += s[r].w; }
+        const int u = e % (kU / 4) * 4;
+        const float v[4] = {sum.x, sum.y, sum.z, sum.w};
+        const long long at = base + (long long)(t.m0 + e / (kU / 4)) * p.ldc + u;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) if (u + i < cols) store_c(p.c, p.c_type, at + i, v[i]);
       }
     }
     cluster_sync();                                  // no block leaves while another reads its sums

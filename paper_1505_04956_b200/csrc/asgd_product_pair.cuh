@@ -7,8 +7,8 @@
 //
 // Warp roles in each block: 0 issues the TMA loads of the block's halves, which all report to the first block's barrier;
 // 1 and 3, in the first block, issue the products and commit each K block to a barrier in both blocks, which says "the slot
-// is free" to the copies and "the accumulator is full" to the readers; 2 brings the column scales where they differ from
-// column to column; 4 to 11 read the accumulators, a row of C per thread and 128 columns per warp, and add them, scaled,
+// is free" to the copies and "the accumulator is full" to the readers; 2 brings the scales (asynchronous 4-byte copies; a load
+// into registers would hold the reading warps); 4 to 11 read the accumulators, a row of C per thread and 128 columns per warp, and add them, scaled,
 // to sums in registers.  Warps 0 to 3 hand most of their registers to these.  A row's scale and, with 128 x 128 blocks of
 // B, the columns' scale are one number per thread, so that a product of the K block costs one multiply-add.
 #pragma once
@@ -23,10 +23,12 @@ constexpr int kPairThreads = 384;
 constexpr int kPairSlots = 6;                        // even: a slot always meets the same issuing thread, see below
 constexpr int kPairBand = 8;                         // tile rows that neighbouring pairs run down before the next column
 constexpr unsigned kHalfBytes = kHalf * kKB, kPairBytes = 2 * kHalfBytes;      // per block: one operand, a slot
-constexpr int kStageBytes = 32 * 64;                 // per warp: 64 bytes of each of its 32 rows, on the way to C
+constexpr int kPieceBytes = 32 * 64;                 // per warp, on the way to C: 64 bytes of each of its 32 rows
+constexpr int kStagePieces = 1, kStageBytes = kStagePieces * kPieceBytes;
+constexpr int kScales = kHalf + kPairCols;           // of a slot: the block's rows', then the columns' (256, or two blocks')
 enum { P_FULL = 0, P_DONE = kPairSlots, P_SFULL = 2 * kPairSlots, P_SEMPTY = 3 * kPairSlots, P_ACCEMPTY = 4 * kPairSlots,
        P_DRAIN = P_ACCEMPTY + 2, P_COUNT = P_DRAIN + 2 };
-constexpr size_t kPairSmem = 1024 + (size_t)kPairSlots * kPairBytes + 8 * kStageBytes + (size_t)kPairSlots * kPairCols * 4 +
+constexpr size_t kPairSmem = 1024 + (size_t)kPairSlots * kPairBytes + 8 * kStageBytes + (size_t)kPairSlots * kScales * 4 +
                              P_COUNT * 8 + sizeof(Groups) + 64;
 static_assert(kPairSmem <= kSmemLimit, "shared memory");
 
@@ -77,45 +79,118 @@ __device__ inline void tmem_load32(unsigned taddr, float (&v)[32]) {
       : "r"(taddr) : "memory");
 }
 
-// A warp's 32 rows x 128 columns to C: 64 bytes of every row at a time through the warp's stage (pieces of 16 bytes
-// exchanged by row, so that neither side meets a bank twice), then whole pieces, eight rows per access.
-template <typename T> __device__ __forceinline__ void store_rows(const float (&acc)[128], unsigned char* stage, T* c, long long ldc, int rows, int cols, int lane) {
-  constexpr int per = 64 / (int)sizeof(T), piece = 16 / (int)sizeof(T);        // numbers per pass, per piece
-  const bool whole = ((reinterpret_cast<unsigned long long>(c) | ((unsigned long long)ldc * sizeof(T))) & 15) == 0;
+// 16 columns of 32 accumulator rows, a thread's share: rows lane / 4 + 8 i, columns 8 g + 2 (lane % 4) + e as v[(g * 4 + i) * 2 + e]
+__device__ inline void tmem_load_fragments(unsigned taddr, float (&v)[16]) {
+  asm volatile("tcgen05.ld.sync.aligned.16x256b.x2.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+               : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[8]), "=f"(v[9]), "=f"(v[10]), "=f"(v[11]) : "r"(taddr) : "memory");
+  asm volatile("tcgen05.ld.sync.aligned.16x256b.x2.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+               : "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]), "=f"(v[12]), "=f"(v[13]), "=f"(v[14]), "=f"(v[15]) : "r"(taddr + (16u << 16)) : "memory");
+}
+__device__ inline void tma_store_3d(const CUtensorMap* map, int x, int y, int z, const void* src) {
+  asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.bulk_group [%0, {%1, %2, %3}], [%4];" ::"l"(map), "r"(x), "r"(y), "r"(z), "r"(smem_u32(src)) : "memory");
+}
+
+// Two sums at a time: x * s + acc, x * (a * f) + acc.  The packed form takes the multiply-add pipe for as long as two
+// scalar ones and half of the issue slots: with scalar ones the reading warps kept the issuing threads of the products
+// (same schedulers) from theirs.
+__device__ __forceinline__ unsigned long long pair_of(float x, float y) {
+  unsigned long long r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(x), "f"(y));
+  return r;
+}
+__device__ __forceinline__ void fma2(float& acc0, float& acc1, float x0, float x1, unsigned long long s) {
+  unsigned long long r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(pair_of(x0, x1)), "l"(s), "l"(pair_of(acc0, acc1)));
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(acc0), "=f"(acc1) : "l"(r));
+}
+__device__ __forceinline__ unsigned long long mul2(unsigned long long a, unsigned long long b) {
+  unsigned long long r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+
+template <typename T> __device__ __forceinline__ unsigned pack32(float a, float b) {       // two 16-bit numbers
+  const T v[2] = {Elem<T>::from_f(a), Elem<T>::from_f(b)};
+  return *reinterpret_cast<const unsigned*>(v);
+}
+
+// Where a warp's 32 rows x 128 columns go.  map: the copies out of shared memory run on while the warp goes on, for
+// whole warps' rows and where C's rows start at 16-byte boundaries; else the warp writes C itself.
+struct Out {
+  const CUtensorMap* map;
+  bool by_map;
+  int n, m, z;                                       // the corner, the group
+  long long ldc, at;                                 // elements from C to the corner
+  int rows, cols;                                    // how many there are
+};
+
+// 64 bytes of every row make a piece of the warp's stage, with parts of 16 bytes exchanged by row (the 64-byte swizzle),
+// so that no access meets a bank more than twice.
+template <typename T, bool kFragments> __device__ __forceinline__ void store_rows(const float (&acc)[128], unsigned char* stage, T* c, const Out& o, int lane) {
+  constexpr int per = 64 / (int)sizeof(T), part = 16 / (int)sizeof(T);         // numbers of a row in a piece, in a part
+  T* corner = c + o.at;
+  const bool whole = ((reinterpret_cast<unsigned long long>(corner) | ((unsigned long long)o.ldc * sizeof(T))) & 15) == 0;
 #pragma unroll
-  for (int c0 = 0; c0 < 128; c0 += per) {
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      float v[piece];
-#pragma unroll
-      for (int i = 0; i < piece; ++i) v[i] = acc[c0 + q * piece + i];
-      *reinterpret_cast<uint4*>(stage + lane * 64 + ((q ^ ((lane >> 1) & 3)) << 4)) = pack16<T>(v);
-    }
+  for (int first = 0; first < 128; first += per) {
+    unsigned char* piece = stage + first / per % kStagePieces * kPieceBytes;
+    // the copy before last, out of the same place, has read it
+    if (lane == 0) asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(kStagePieces - 1) : "memory");
     __syncwarp();
+    if constexpr (!kFragments) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int r = i * 8 + (lane >> 2), q = lane & 3, at = c0 + q * piece;
-      if (r < rows && at < cols) {
-        const unsigned char* from = stage + r * 64 + ((q ^ ((r >> 1) & 3)) << 4);
-        T* to = c + (long long)r * ldc + at;
-        if (whole && at + piece <= cols) *reinterpret_cast<uint4*>(to) = *reinterpret_cast<const uint4*>(from);
-        else
-          for (int b = 0; b < piece && at + b < cols; ++b) to[b] = reinterpret_cast<const T*>(from)[b];
+      for (int q = 0; q < 4; ++q) {
+        float v[part];
+#pragma unroll
+        for (int i = 0; i < part; ++i) v[i] = acc[first + q * part + i];
+        *reinterpret_cast<uint4*>(piece + lane * 64 + ((q ^ ((lane >> 1) & 3)) << 4)) = pack16<T>(v);
       }
+    } else {
+#pragma unroll
+      for (int g = 0; g < per / 8; ++g)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float x = acc[((first / 8 + g) * 4 + i) * 2], y = acc[((first / 8 + g) * 4 + i) * 2 + 1];
+          const int r = (lane >> 2) + 8 * i, byte = (8 * g + 2 * (lane & 3)) * (int)sizeof(T);
+          unsigned char* at = piece + r * 64 + (((byte >> 4) ^ ((r >> 1) & 3)) << 4) + (byte & 15);
+          if constexpr (sizeof(T) == 4) *reinterpret_cast<float2*>(at) = make_float2(x, y);
+          else *reinterpret_cast<unsigned*>(at) = pack32<T>(x, y);
+        }
     }
-    __syncwarp();
+    if (o.by_map) {
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      __syncwarp();
+      if (lane == 0) {
+        if (first < o.cols) tma_store_3d(o.map, o.n + first, o.m, o.z, piece);
+        asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+      }
+    } else {
+      __syncwarp();
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int r = i * 8 + (lane >> 2), q = lane & 3, at = first + q * part;
+        if (r < o.rows && at < o.cols) {
+          const unsigned char* from = piece + r * 64 + ((q ^ ((r >> 1) & 3)) << 4);
+          T* to = corner + (long long)r * o.ldc + at;
+          if (whole && at + part <= o.cols) *reinterpret_cast<uint4*>(to) = *reinterpret_cast<const uint4*>(from);
+          else
+            for (int b = 0; b < part && at + b < o.cols; ++b) to[b] = reinterpret_cast<const T*>(from)[b];
+        }
+      }
+      __syncwarp();
+    }
   }
 }
 
 // kColumns: the columns have a scale each (rows of B scaled by blocks of 128 along K alone)
 template <bool kColumns> __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
-product_pair_kernel(const Params p, const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b) {
+product_pair_kernel(const Params p, const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
+                    const __grid_constant__ CUtensorMap map_c) {
   constexpr int S = kPairSlots;
   extern __shared__ __align__(1024) unsigned char smem_dyn[];
   unsigned char* ring = smem_dyn + ((1024u - (smem_u32(smem_dyn) & 1023u)) & 1023u);
   unsigned char* stages = ring + (size_t)S * kPairBytes;
-  float* sv = reinterpret_cast<float*>(stages + 8 * kStageBytes);                       // [slot][256] scales of the columns
-  unsigned long long* bars = reinterpret_cast<unsigned long long*>(sv + S * kPairCols);
+  float* scales = reinterpret_cast<float*>(stages + 8 * kStageBytes);                   // [slot][kScales]
+  unsigned long long* bars = reinterpret_cast<unsigned long long*>(scales + S * kScales);
   Groups& gs = *reinterpret_cast<Groups*>(bars + P_COUNT);
   int* misc = reinterpret_cast<int*>(&gs + 1);        // [0] tensor memory, [1] abort, [2, 3] K blocks whose copies each block has issued, [4] the other block gave up
   int* abort = misc + 1;
@@ -126,6 +201,7 @@ product_pair_kernel(const Params p, const __grid_constant__ CUtensorMap map_a, c
   if (tid == 0) {
     prefetch_map(&map_a);
     prefetch_map(&map_b);
+    if (p.c_by_map) prefetch_map(&map_c);
     for (int q = 0; q < S; ++q) { mbar_init(bars + P_FULL + q, 1); mbar_init(bars + P_DONE + q, 1); mbar_init(bars + P_SFULL + q, 32); mbar_init(bars + P_SEMPTY + q, 8); }
     for (int q = 0; q < 2; ++q) { mbar_init(bars + P_ACCEMPTY + q, 16); mbar_init(bars + P_DRAIN + q, 1); }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -144,7 +220,7 @@ product_pair_kernel(const Params p, const __grid_constant__ CUtensorMap map_a, c
   const int tiles = gs.prefix[max(p.groups, 1)];
 
   if (wid < 4) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
     if (wid == 0 && lane == 0) {
       const unsigned full0 = in_first_block(bars + P_FULL);
       unsigned it = 0;
@@ -191,7 +267,7 @@ product_pair_kernel(const Params p, const __grid_constant__ CUtensorMap map_a, c
         commit_pair(bars + P_DRAIN + me);
         for (unsigned n = 0; n < p.wait_limit && !mbar_try_wait(bars + P_DRAIN + me, 0); ++n) {}
       }
-    } else if (wid == 2 && kColumns) {
+    } else if (wid == 2) {
       unsigned it = 0;
       bool ok = true;
       for (int tile = pair; tile < tiles && ok; tile += pairs) {
@@ -200,10 +276,21 @@ product_pair_kernel(const Params p, const __grid_constant__ CUtensorMap map_a, c
         for (int kb = t.kb0; kb < t.kb1; ++kb, ++it) {
           const unsigned q = it % S;
           if (it >= S && !(ok = __all_sync(kAll, wait(bars + P_SEMPTY + q, (it / S - 1) & 1, p.wait_limit, abort)))) break;
+          float* to = scales + q * kScales;
 #pragma unroll
-          for (int c = 0; c < kPairCols; c += 32) {
-            const int n = t.n0 + c + lane;
-            copy4(sv + q * kPairCols + c + lane, n < p.N ? from + n * p.sb_row + kb * p.sb_block : p.sb, n < p.N);
+          for (int c = 0; c < kHalf; c += 32) {
+            const int m = t.m0 + (int)rank * kHalf + c + lane;
+            copy4(to + c + lane, m < t.m_end ? p.sa + m * p.sa_row + kb * p.sa_block : p.sa, m < t.m_end);
+          }
+          if (kColumns) {
+#pragma unroll
+            for (int c = 0; c < kPairCols; c += 32) {
+              const int n = t.n0 + c + lane;
+              copy4(to + kHalf + c + lane, n < p.N ? from + n * p.sb_row + kb * p.sb_block : p.sb, n < p.N);
+            }
+          } else if (lane < 2) {
+            const int n = t.n0 + 128 * lane;
+            copy4(to + kHalf + lane, n < p.N ? from + (n >> 7) * p.sb_row + kb * p.sb_block : p.sb, n < p.N);
           }
           arrive_after_copies(bars + P_SFULL + q);
         }
@@ -212,7 +299,7 @@ product_pair_kernel(const Params p, const __grid_constant__ CUtensorMap map_a, c
     }
     __syncwarp();
   } else {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 232;");
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 224;");
     const int quarter = wid & 3, half = (wid - 4) >> 2;
     const unsigned free0 = in_first_block(bars + P_ACCEMPTY);
     const unsigned at_tmem = tmem + ((unsigned)(quarter * 32) << 16) + half * 128;
@@ -222,56 +309,66 @@ product_pair_kernel(const Params p, const __grid_constant__ CUtensorMap map_a, c
     for (int tile = pair; tile < tiles && ok; tile += pairs) {
       const Tile t = find_tile(p, kPairRows, kPairCols, kPairBand, gs, tile);
       const int m = t.m0 + (int)rank * kHalf + quarter * 32, n = t.n0 + half * 128;      // the warp's corner
-      const float* sa_at = p.sa + min(m + lane, p.M - 1) * p.sa_row;
-      const float* sb_at = p.sb + (p.inner ? 0 : t.g * p.sb_group) + (long long)(min(n, p.N - 1) >> 7) * p.sb_row;
-      // scales of a K block, loaded two blocks ahead of their use (and multiplied only there: an instruction that needs a
-      // load's result holds the warp until it has come)
-      auto row_scale = [&](int kb) { return __ldg(sa_at + min(kb, t.kb1 - 1) * p.sa_block); };
-      auto col_scale = [&](int kb) { return kColumns ? 1.f : __ldg(sb_at + min(kb, t.kb1 - 1) * p.sb_block); };
       float acc[128];
 #pragma unroll
       for (int c = 0; c < 128; ++c) acc[c] = 0.f;
-      float a0 = 0.f, a1 = 0.f, b0 = 0.f, b1 = 0.f;
-      if (t.kb0 < t.kb1) { a0 = row_scale(t.kb0); a1 = row_scale(t.kb0 + 1); b0 = col_scale(t.kb0); b1 = col_scale(t.kb0 + 1); }
       for (int kb = t.kb0; kb < t.kb1; ++kb, ++it) {
         const unsigned q = it % S, stage = it & 1;
-        const float a2 = row_scale(kb + 2), b2 = col_scale(kb + 2);
-        ok = (!kColumns || wait(bars + P_SFULL + q, (it / S) & 1, p.wait_limit, abort)) && wait(bars + P_DONE + q, (it / S) & 1, p.wait_limit, abort);
+        ok = wait(bars + P_SFULL + q, (it / S) & 1, p.wait_limit, abort) && wait(bars + P_DONE + q, (it / S) & 1, p.wait_limit, abort);
         if (!(ok = __all_sync(kAll, ok))) break;
         fence_after();
-        const float s0 = a0 * b0;
-        float v[2][32];
-        tmem_load32(at_tmem + stage * kPairCols, v[0]);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          tmem_wait();
-          if (i < 3) tmem_load32(at_tmem + stage * kPairCols + (i + 1) * 32, v[(i + 1) & 1]);
-          else {
-            fence_before();
-            __syncwarp();
-            if (lane == 0) arrive_cluster(free0 + stage * 8);
-          }
-          if (kColumns) {
-            const float4* col = reinterpret_cast<const float4*>(sv + q * kPairCols + half * 128 + i * 32);
-#pragma unroll
-            for (int c = 0; c < 32; c += 4) {
-              const float4 f = col[c / 4];
-              acc[i * 32 + c] = fmaf(v[i & 1][c] * s0, f.x, acc[i * 32 + c]);
-              acc[i * 32 + c + 1] = fmaf(v[i & 1][c + 1] * s0, f.y, acc[i * 32 + c + 1]);
-              acc[i * 32 + c + 2] = fmaf(v[i & 1][c + 2] * s0, f.z, acc[i * 32 + c + 2]);
-              acc[i * 32 + c + 3] = fmaf(v[i & 1][c + 3] * s0, f.w, acc[i * 32 + c + 3]);
-            }
-          } else {
+        const float* of_rows = scales + q * kScales + quarter * 32;
+        const float* of_cols = scales + q * kScales + kHalf;
+        const unsigned from = at_tmem + stage * kPairCols;
+        auto hand_back = [&]() {                     // the warp's part of the accumulator has been read
+          fence_before();
+          __syncwarp();
+          if (lane == 0) arrive_cluster(free0 + stage * 8);
+        };
+        if constexpr (!kColumns) {
+          float s0, v[2][32];
+          auto add = [&](int i) {
 #pragma unroll
             for (int c = 0; c < 32; ++c) acc[i * 32 + c] = fmaf(v[i & 1][c], s0, acc[i * 32 + c]);
+          };
+          // the reads as early as the registers allow: the accumulator goes back before the last two adds
+          tmem_load32(from, v[0]);
+          tmem_load32(from + 32, v[1]);
+          s0 = of_rows[lane] * of_cols[half];
+          tmem_wait();
+          add(0);
+          tmem_load32(from + 64, v[0]);
+          add(1);
+          tmem_load32(from + 96, v[1]);
+          tmem_wait();
+          hand_back();
+          add(2);
+          add(3);
+        } else {
+          // fragments of 32 rows x 16 columns: a thread needs 32 columns' scales of a K block where a row per thread
+          // would need 128 (every broadcast read of 16 bytes takes four cycles of the shared memory's path)
+          float v[2][16], a0[4];
+          tmem_load_fragments(from, v[0]);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) a0[i] = of_rows[(lane >> 2) + 8 * i];
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            tmem_wait();
+            if (j < 7) tmem_load_fragments(from + (j + 1) * 16, v[(j + 1) & 1]);
+            else hand_back();
+#pragma unroll
+            for (int g = 0; g < 2; ++g) {
+              const float2 f = *reinterpret_cast<const float2*>(of_cols + half * 128 + 2 * (lane & 3) + j * 16 + g * 8);
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                const int e = (g * 4 + i) * 2;
+                fma2(acc[j * 16 + e], acc[j * 16 + e + 1], v[j & 1][e], v[j & 1][e + 1], mul2(pair_of(a0[i], a0[i]), pair_of(f.x, f.y)));
+              }
+            }
           }
         }
-        if (kColumns) {
-          __syncwarp();
-          if (lane == 0) arrive(bars + P_SEMPTY + q);
-        }
-        a0 = a1; a1 = a2;
-        b0 = b1; b1 = b2;
+        __syncwarp();
+        if (lane == 0) arrive(bars + P_SEMPTY + q);
       }
       if (!ok) break;
       if (t.bad) {
@@ -279,14 +376,20 @@ product_pair_kernel(const Params p, const __grid_constant__ CUtensorMap map_a, c
 #pragma unroll
         for (int c = 0; c < 128; ++c) acc[c] = __int_as_float(0x7fffffff);
       }
-      const int rows = min(32, t.m_end - m), cols = min(128, p.N - n);
-      if (rows > 0 && cols > 0) {
-        const long long at = (p.inner ? t.g * p.c_group : 0) + m * p.ldc + n;
-        if (p.c_type == ASGD_F32) store_rows(acc, stage_smem, reinterpret_cast<float*>(p.c) + at, p.ldc, rows, cols, lane);
-        else if (p.c_type == ASGD_BF16) store_rows(acc, stage_smem, reinterpret_cast<__nv_bfloat16*>(p.c) + at, p.ldc, rows, cols, lane);
-        else store_rows(acc, stage_smem, reinterpret_cast<__half*>(p.c) + at, p.ldc, rows, cols, lane);
+      Out o;
+      o.map = &map_c;
+      o.rows = min(32, t.m_end - m); o.cols = min(128, p.N - n);
+      o.n = n; o.m = m; o.z = p.inner ? t.g : 0;
+      o.ldc = p.ldc;
+      o.at = o.z * p.c_group + m * p.ldc + n;
+      o.by_map = p.c_by_map && o.rows == 32;
+      if (o.rows > 0 && o.cols > 0) {
+        if (p.c_type == ASGD_F32) store_rows<float, kColumns>(acc, stage_smem, reinterpret_cast<float*>(p.c), o, lane);
+        else if (p.c_type == ASGD_BF16) store_rows<__nv_bfloat16, kColumns>(acc, stage_smem, reinterpret_cast<__nv_bfloat16*>(p.c), o, lane);
+        else store_rows<__half, kColumns>(acc, stage_smem, reinterpret_cast<__half*>(p.c), o, lane);
       }
     }
+    if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
     __syncwarp();
   }
   // Both blocks are through.  Where one gave up, the first block settles its barriers: bytes announced that nobody will
