@@ -6,7 +6,9 @@
 // cores fill the other accumulator stage.
 #include <cudaTypedefs.h>
 
+#include <algorithm>
 #include <atomic>
+#include <cmath>
 
 #include "asgd_product_few.cuh"
 #include "asgd_product_pair.cuh"
@@ -94,11 +96,17 @@ template <int BN, bool kSplit> int launch_few(const asgd_product_args& a, Params
   return cudaLaunchKernelEx(&cfg, product_few_kernel<BN, kSplit>, p, map_u, map_v) == cudaSuccess ? ASGD_OK : ASGD_ECUDA;
 }
 
+// Blocks per tile of the few-rows kernel: a power of two, with two K blocks each at least, whose clusters are on the SMs
+// all at once: of 8 blocks with an SM each 14 fit for certain (a cluster stays inside one of the GPU's partitions; two
+// more and 1024 x 4096 with 200 rows takes 17.5 us instead of 11), of 4 blocks 32, of 2 blocks 74.
+int split_of(const Params& p, int bn) {
+  const long long most = most_tiles(p, bn, kU);
+  for (const int split : {8, 4, 2})
+    if (most <= (split == 8 ? 14 : split == 4 ? 32 : kSMs / 2) && p.kblocks >= split * 2) return split;
+  return 1;
+}
 template <int BN> int launch_few(const asgd_product_args& a, const Params& p, cudaStream_t st) {
-  // blocks per tile: as many as there are SMs for, of a power of two, with two K blocks each at least
-  const long long most = most_tiles(p, BN, kU);
-  int split = 1;
-  while (split < kMaxSplit && most * split * 2 <= kSMs && p.kblocks >= split * 4) split *= 2;
+  const int split = split_of(p, BN);
   return split > 1 ? launch_few<BN, true>(a, p, split, st) : launch_few<BN, false>(a, p, 1, st);
 }
 
@@ -125,6 +133,32 @@ int launch_pair(const asgd_product_args& a, Params p, cudaStream_t st) {
   if (!allow_smem(kernel, kPairSmem, done[a.b_square])) return ASGD_ECUDA;
   kernel<<<(unsigned)min(most, (long long)(kSMs / 2)) * 2, kPairThreads, kPairSmem, st>>>(p, map_a, map_b, map_c);
   return cudaGetLastError() == cudaSuccess ? ASGD_OK : ASGD_ECUDA;
+}
+
+// Which kernel: the one whose blocks are through first, by the K blocks the busiest of them meets and the time of one.
+// Microseconds of a K block, measured where operands come from L2 (4096 x 4096 x 4096; the pair with a scale per column
+// from weight gradients of 2048 x 2048): tiles of 16, 32, 64 and 128 rows 0.29, 0.31, 0.43 and 0.66, the pair 0.50, with
+// scales per column 0.85; about 1 us a tile for its beginning and end.
+enum Kernel { FEW16, FEW32, FEW64, FEW128, PAIR };
+Kernel choose(const Params& p) {
+  static const int rows_of[5] = {16, 32, 64, 128, kPairRows};
+  const double block_us[5] = {0.29, 0.31, 0.43, 0.66, p.sb_shift ? 0.50 : 0.85};
+  const int groups = max(p.groups, 1);
+  const double kblocks = p.inner ? std::ceil((double)p.kblocks / groups) : p.kblocks;
+  Kernel best = FEW16;
+  double best_us = 0;
+  for (int k = FEW16; k <= PAIR; ++k) {
+    const int bm = rows_of[k];
+    // tile rows: a group's last one is half full on average, and a group with rows has one at least
+    const double tile_rows = p.inner ? (double)ceil_div(p.M, bm) * groups
+                             : groups > 1 ? std::max(std::min((double)p.M, (double)groups), (double)p.M / bm + 0.5 * groups) : (double)ceil_div(p.M, bm);
+    const double tiles = std::ceil(tile_rows) * (double)ceil_div(p.N, k == PAIR ? kPairCols : kU);
+    const int split = k == PAIR ? 1 : split_of(p, bm);
+    const double turns = std::ceil(tiles * split / (k == PAIR ? kSMs / 2 : kSMs));
+    const double us = turns * (std::ceil(kblocks / split) * block_us[k] + 1.0) + (split > 1 ? 1.0 : 0.0);
+    if (k == FEW16 || us < best_us) { best = (Kernel)k; best_us = us; }
+  }
+  return best;
 }
 
 }  // namespace
@@ -154,12 +188,13 @@ extern "C" int asgd_product(const asgd_product_args* args, void* stream) {
   p.wait_limit = g_wait_limit.load();
   p.withhold = g_withhold.load();
   cudaStream_t st = (cudaStream_t)stream;
-  const long long rows = a.groups && !a.inner ? ceil_div(a.M, a.groups) : a.M;     // rows of a group, on average
-  if (rows <= 16) return launch_few<16>(a, p, st);
-  if (rows <= 32) return launch_few<32>(a, p, st);
-  if (rows <= 64) return launch_few<64>(a, p, st);
-  if (rows <= 128) return launch_few<128>(a, p, st);
-  return launch_pair(a, p, st);
+  switch (choose(p)) {
+    case FEW16: return launch_few<16>(a, p, st);
+    case FEW32: return launch_few<32>(a, p, st);
+    case FEW64: return launch_few<64>(a, p, st);
+    case FEW128: return launch_few<128>(a, p, st);
+    default: return launch_pair(a, p, st);
+  }
 }
 
 extern "C" int asgd_experts_sync(void* stream) {
