@@ -59,8 +59,25 @@ template <typename T, typename Word> __device__ __forceinline__ float element(co
   return Elem<T>::to_f(reinterpret_cast<const T*>(&w)[i]);
 }
 
-template <typename T, bool kVec, bool kE5M2> __global__ void __launch_bounds__(kThreads) rows_kernel(const Args p) {
-  constexpr int V = kPer16<T>, LB = 128 / V, U = 4;      // numbers per lane, lanes per block, loads in flight per lane
+// largest magnitude of the numbers in 16 bytes (a NaN is passed over)
+template <typename T> __device__ __forceinline__ float largest(const uint4& w) {
+  if constexpr (sizeof(T) == 4) {
+    const float* v = reinterpret_cast<const float*>(&w);
+    return fmaxf(fmaxf(fabsf(v[0]), fabsf(v[1])), fmaxf(fabsf(v[2]), fabsf(v[3])));
+  } else {                                               // two at a time
+    using T2 = typename std::conditional<std::is_same<T, __half>::value, __half2, __nv_bfloat162>::type;
+    const T2* v = reinterpret_cast<const T2*>(&w);
+    const T2 m = __hmax2(__hmax2(__habs2(v[0]), __habs2(v[1])), __hmax2(__habs2(v[2]), __habs2(v[3])));
+    return fmaxf(Elem<T>::to_f(m.x), Elem<T>::to_f(m.y));
+  }
+}
+
+// A warp takes a stretch of a row: four 16-byte pieces per lane, all loaded before the first is used.  The four blocks a
+// lane has a part in are reduced together: each exchange between lanes folds half of the maxima onto half of the lanes,
+// so that a lane ends with one block's maximum, divides once, and hands the result round (9 exchanges and one division
+// where four separate reductions take 16 to 20 and four).
+template <typename T, bool kVec, bool kE5M2, bool kWeights> __global__ void __launch_bounds__(kThreads) rows_kernel(const Args p) {
+  constexpr int V = kPer16<T>, LB = 128 / V, U = 4;      // numbers per piece, lanes per block, pieces per lane
   const asgd_quantize_args& a = p.a;
   const int lane = threadIdx.x & 31, K = (int)a.K;
   // the block's warps take neighbouring rows of the same stretch: their scales are neighbours in memory
@@ -69,41 +86,67 @@ template <typename T, bool kVec, bool kE5M2> __global__ void __launch_bounds__(k
   if (r >= a.M) return;
   float factor;
   const T* row = input_row<T>(a, r, factor);
+  const bool whole = kVec && ((int)blockIdx.y + 1) * (U * 32 * V) <= K;
   uint4 raw[U];
 #pragma unroll
   for (int u = 0; u < U; ++u) {
     const int c = c0 + u * 32 * V;
     raw[u] = make_uint4(0, 0, 0, 0);
-    if (row && c < K) raw[u] = load<T, uint4, kVec>(row, c, K);
+    if (row) {
+      if (whole) raw[u] = *reinterpret_cast<const uint4*>(row + c);
+      else if (c < K) raw[u] = load<T, uint4, kVec>(row, c, K);
+    }
+  }
+  float m[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    if (kWeights) {
+      float v[V];
+      unpack16<T>(raw[u], v);
+      m[u] = 0.f;
+#pragma unroll
+      for (int i = 0; i < V; ++i) m[u] = fmaxf(m[u], fabsf(__fmul_rn(v[i], factor)));
+    } else {
+      m[u] = largest<T>(raw[u]);
+    }
+  }
+  constexpr int O1 = LB / 2, O2 = LB / 4;
+#pragma unroll
+  for (int u = 0; u < 2; ++u) {
+    const bool high = lane & O1;
+    const float got = __shfl_xor_sync(kAll, high ? m[u] : m[u + 2], O1);
+    m[u] = fmaxf(high ? m[u + 2] : m[u], got);
+  }
+  {
+    const bool high = lane & O2;
+    const float got = __shfl_xor_sync(kAll, high ? m[0] : m[1], O2);
+    m[0] = fmaxf(high ? m[1] : m[0], got);
+  }
+#pragma unroll
+  for (int o = O2 / 2; o > 0; o >>= 1) m[0] = fmaxf(m[0], __shfl_xor_sync(kAll, m[0], o));
+  const float best = fmaxf(m[0], kTiny), mine = __fdiv_rn(p.fmax, best);
+  if ((lane & (O2 - 1)) == 0) {                          // the block this lane ended with
+    const int c = (int)blockIdx.y * U * 32 * V + (((lane & O1) ? 2 : 0) + ((lane & O2) ? 1 : 0)) * 32 * V + (LB == 16 ? (lane & 16) * V : 0);
+    if (c < K) a.scale[r * a.scale_row + (c >> 7) * a.scale_block] = __fmul_rn(best, p.inv_fmax);
   }
   unsigned char* q = reinterpret_cast<unsigned char*>(a.q) + r * a.ldq;
-  float* scale = a.scale + r * a.scale_row;
 #pragma unroll
   for (int u = 0; u < U; ++u) {
     const int c = c0 + u * 32 * V;
+    const float inv = __shfl_sync(kAll, mine, (LB == 16 ? lane & 16 : 0) | ((u & 2) ? O1 : 0) | ((u & 1) ? O2 : 0));
     float v[V];
     unpack16<T>(raw[u], v);
-    float m = kTiny;
+    unsigned w[V / 4];
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-      if (a.weights) v[i] = __fmul_rn(v[i], factor);
-      m = fmaxf(m, fabsf(v[i]));
-    }
+    for (int i = 0; i < V; ++i) v[i] = (kWeights ? __fmul_rn(v[i], factor) : v[i]) * inv;
 #pragma unroll
-    for (int o = LB / 2; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(kAll, m, o));
-    const float inv = __fdiv_rn(p.fmax, m);
-    if (c < K) {
-      if ((lane & (LB - 1)) == 0) scale[(c >> 7) * a.scale_block] = __fmul_rn(m, p.inv_fmax);
-      unsigned w[V / 4];
+    for (int i = 0; i < V; i += 4) w[i / 4] = round4<kE5M2>(v[i], v[i + 1], v[i + 2], v[i + 3]);
+    if (whole || (kVec && c + V <= K)) {
+      if constexpr (V == 8) *reinterpret_cast<uint2*>(q + c) = make_uint2(w[0], w[1]);
+      else *reinterpret_cast<unsigned*>(q + c) = w[0];
+    } else {
 #pragma unroll
-      for (int i = 0; i < V; i += 4) w[i / 4] = round4<kE5M2>(v[i] * inv, v[i + 1] * inv, v[i + 2] * inv, v[i + 3] * inv);
-      if (kVec && c + V <= K) {
-        if constexpr (V == 8) *reinterpret_cast<uint2*>(q + c) = make_uint2(w[0], w[1]);
-        else *reinterpret_cast<unsigned*>(q + c) = w[0];
-      } else {
-#pragma unroll
-        for (int i = 0; i < V; ++i) if (c + i < K) q[c + i] = (unsigned char)(w[i / 4] >> (8 * (i & 3)));
-      }
+      for (int i = 0; i < V; ++i) if (c + i < K) q[c + i] = (unsigned char)(w[i / 4] >> (8 * (i & 3)));
     }
   }
 }
@@ -249,7 +292,9 @@ template <typename T> void launch(const Args& p, cudaStream_t st) {
   const bool vec = aligned(a.x, V * sizeof(T)) && a.ldx % V == 0 && (!a.q || (aligned(a.q, V) && a.ldq % V == 0));
   if (rows_only) {
     const dim3 grid((unsigned)ceil_div(a.M, kWarps), (unsigned)ceil_div(a.K, 32 * V * 4));
-    const auto k = vec ? (e5m2 ? rows_kernel<T, true, true> : rows_kernel<T, true, false>) : (e5m2 ? rows_kernel<T, false, true> : rows_kernel<T, false, false>);
+    const bool w = a.weights != nullptr;
+    const auto k = vec ? (e5m2 ? (w ? rows_kernel<T, true, true, true> : rows_kernel<T, true, true, false>) : (w ? rows_kernel<T, true, false, true> : rows_kernel<T, true, false, false>))
+                       : (e5m2 ? (w ? rows_kernel<T, false, true, true> : rows_kernel<T, false, true, false>) : (w ? rows_kernel<T, false, false, true> : rows_kernel<T, false, false, false>));
     k<<<grid, kThreads, 0, st>>>(p);
   } else {
     const auto k = vec ? (e5m2 ? tile_kernel<T, true, true> : tile_kernel<T, true, false>) : (e5m2 ? tile_kernel<T, false, true> : tile_kernel<T, false, false>);

@@ -2,24 +2,35 @@
 // The contract is in include/asgd_experts.h.
 //
 // A warp owns a token: lane l holds the experts l, l + 32, ... in registers, so the row is read once, coalesced at any
-// stride.  Keys become unsigned numbers of the same order, and each choice is two warp-wide integer reductions (the
-// largest key, then the lowest index that has it).  The plan is a stable counting sort by expert.  A block's tokens are
-// a chunk of 64; inside a chunk each expert has a 64-bit word with a bit per token that chose it, so an assignment's
-// rank among the chunk's is the population count below its bit.  Chunk counts are then summed along the chunks and the
-// experts, and the ranks moved by those sums: integers only, so the plan does not depend on timing.
+// stride.  Keys become unsigned numbers of the same order and each lane sorts its own; a choice is then a warp-wide
+// integer maximum of the lanes' first keys, a vote for the lane that has it, and a shift of that lane's list.  16-bit
+// logits that are themselves the keys leave room for the place in the list in the key's low bits, so that equal keys
+// need no second look.  Only the chosen logits are turned into weights.  Instructions and their latency are the bound,
+// not the bytes.
+//
+// The plan is a stable counting sort by expert.  A block's tokens are a chunk (of 64 at most); inside a chunk each
+// expert has a 64-bit word with a bit per token that chose it, so an assignment's rank among the chunk's is the
+// population count below its bit.  Chunk counts are then summed along the chunks and the experts, and the ranks moved by
+// those sums: integers only, so the plan does not depend on timing.
 #include "asgd_experts_common.cuh"
+
+#include <algorithm>
+#include <type_traits>
 
 namespace {
 
 using namespace asgd::experts;
 
-constexpr int kChunk = 64;                   // tokens of a chunk (bits of an expert's word)
-constexpr int kThreads = 256;                // threads of a block when there are many chunks
+constexpr int kMaxChunk = 64;                // tokens of a chunk (bits of an expert's word)
+constexpr int kThreads = 256, kWarps = kThreads / 32;
 constexpr int kThreadsOne = 1024;            // the one block of a single chunk: two tokens per warp, latency counts
+constexpr int kFillBlocks = 2 * kSMs;        // blocks at least that write the rows of nothing
 
 struct RouteArgs {
   asgd_route_config c;
-  long long T, ld, chunks, source_len;
+  long long T, ld, source_len;
+  int chunk, chunks;                         // tokens of a chunk, chunks
+  unsigned group_magic;                      // e / (experts of a group) = umulhi(e, group_magic); 0: groups of one
   const void* logits;
   const float* bias;
   int* ids;
@@ -39,10 +50,9 @@ __device__ __forceinline__ unsigned ordered(float v) {
 __device__ __forceinline__ float from_ordered(unsigned u) {
   return __uint_as_float((u >> 31) ? (u & 0x7fffffffu) : ~u);
 }
-__device__ __forceinline__ float warp_max(float v) {
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(kAll, v, o));
-  return v;
+__device__ __forceinline__ float warp_max(float v) {               // by one integer reduction; NaNs are passed over
+  const unsigned u = __reduce_max_sync(kAll, v == v ? ordered(v) : 0u);
+  return u ? from_ordered(u) : v;
 }
 __device__ __forceinline__ float warp_sum(float v) {
 #pragma unroll
@@ -50,32 +60,26 @@ __device__ __forceinline__ float warp_sum(float v) {
   return v;
 }
 
-// Scores of the row in registers.  Softmax over all E (entries beyond E are -inf logits); a logit equal to the largest
-// counts exactly 1, so that rows of +inf have finite scores.
-template <int S> __device__ __forceinline__ void scores(const float (&x)[S], float (&p)[S], int score) {
-  if (score == ASGD_SCORE_SIGMOID) {
-#pragma unroll
-    for (int j = 0; j < S; ++j) p[j] = __fdiv_rn(1.f, __fadd_rn(1.f, expf(-x[j])));
-    return;
-  }
+__device__ __forceinline__ float sigmoid(float x) { return __fdiv_rn(1.f, __fadd_rn(1.f, expf(-x))); }
+
+// Softmax of the row in registers: its largest logit and the sum.  A logit equal to the largest counts exactly 1, so
+// that rows of +inf have finite scores; entries beyond the row are -inf.
+struct Softmax {
+  float m, sum;
+  __device__ __forceinline__ float part(float x) const { return x == m ? 1.f : expf(x - m); }
+  __device__ __forceinline__ float score(float x) const { return __fdiv_rn(part(x), sum); }
+};
+template <int S> __device__ __forceinline__ Softmax softmax(const float (&x)[S]) {
+  Softmax f;
   float m = x[0];
 #pragma unroll
   for (int j = 1; j < S; ++j) m = fmaxf(m, x[j]);
-  m = warp_max(m);
+  f.m = warp_max(m);
   float sum = 0.f;
 #pragma unroll
-  for (int j = 0; j < S; ++j) { p[j] = (x[j] == m) ? 1.f : expf(x[j] - m); sum += p[j]; }
-  sum = warp_sum(sum);
-#pragma unroll
-  for (int j = 0; j < S; ++j) p[j] = __fdiv_rn(p[j], sum);
-}
-
-// p[e] of the row, known to every lane
-template <int S> __device__ __forceinline__ float pick(const float (&p)[S], int e) {
-  float v = 0.f;
-#pragma unroll
-  for (int j = 0; j < S; ++j) v = (e >> 5) == j ? p[j] : v;
-  return __shfl_sync(kAll, v, e & 31);
+  for (int j = 0; j < S; ++j) sum += f.part(x[j]);
+  f.sum = warp_sum(sum);
+  return f;
 }
 
 template <int S, typename T> __device__ __forceinline__ void load_row(const T* row, int E, int lane, float (&x)[S]) {
@@ -86,71 +90,148 @@ template <int S, typename T> __device__ __forceinline__ void load_row(const T* r
   }
 }
 
+// a <-> b so that the larger key (the first of equals) is in a
+__device__ __forceinline__ void order2(unsigned& a, unsigned& b) {
+  const unsigned hi = max(a, b);
+  b = min(a, b);
+  a = hi;
+}
+__device__ __forceinline__ void order2(unsigned& a, unsigned& b, int& ia, int& ib) {
+  const bool swap = b > a || (b == a && ib < ia);
+  const unsigned ka = a, kb = b;
+  const int ja = ia, jb = ib;
+  a = swap ? kb : ka; b = swap ? ka : kb;
+  ia = swap ? jb : ja; ib = swap ? ja : jb;
+}
+// A lane's S keys, descending (odd-even merge sort); kPlaces: with the places they came from, equal keys in their order
+template <int S, bool kPlaces> __device__ __forceinline__ void sort_keys(unsigned (&key)[S], int (&place)[S]) {
+#pragma unroll
+  for (int p = 1; p < S; p *= 2)
+#pragma unroll
+    for (int k = p; k >= 1; k /= 2)
+#pragma unroll
+      for (int j = k % p; j + k < S; j += 2 * k)
+#pragma unroll
+        for (int i = 0; i < k; ++i)
+          if (i + j + k < S && (i + j) / (2 * p) == (i + j + k) / (2 * p)) {
+            if (kPlaces) order2(key[i + j], key[i + j + k], place[i + j], place[i + j + k]);
+            else order2(key[i + j], key[i + j + k]);
+          }
+}
+
+// Takes all experts but those of the best groups_kept groups out (their keys become 0).
+template <int S> __device__ __forceinline__ void keep_groups(const RouteArgs& a, int lane, unsigned (&key)[S]) {
+  const asgd_route_config& c = a.c;
+  int group[S];
+#pragma unroll
+  for (int j = 0; j < S; ++j) group[j] = a.group_magic ? (int)__umulhi((unsigned)(j * 32 + lane), a.group_magic) : j * 32 + lane;
+  unsigned mine = 0;                                                   // lane g: the ordered score of group g
+  for (int g = 0; g < c.groups; ++g) {
+    unsigned m1 = 0, m2 = 0;                                           // this lane's two largest keys of the group
+#pragma unroll
+    for (int j = 0; j < S; ++j) {
+      const unsigned k = group[j] == g ? key[j] : 0u;
+      m2 = max(m2, min(m1, k));
+      m1 = max(m1, k);
+    }
+    unsigned best = __reduce_max_sync(kAll, m1);
+    if (c.group_top == 2 && best) {
+      const unsigned holders = __ballot_sync(kAll, m1 == best);
+      const unsigned second = __reduce_max_sync(kAll, (lane == __ffs(holders) - 1) ? m2 : m1);
+      if (second) best = ordered(__fadd_rn(from_ordered(best), from_ordered(second)));
+    }
+    if (lane == g) mine = best;
+  }
+  unsigned kept = 0;
+  for (int i = 0; i < c.groups_kept; ++i) {
+    const unsigned best = __reduce_max_sync(kAll, (kept >> lane) & 1u ? 0u : mine);
+    if (!best) break;
+    kept |= 1u << (__ffs(__ballot_sync(kAll, mine == best && !((kept >> lane) & 1u))) - 1);
+  }
+#pragma unroll
+  for (int j = 0; j < S; ++j) if (!((kept >> (group[j] & 31)) & 1u)) key[j] = 0u;
+}
+
 // The choice of one token: lane j < top_k returns its j-th expert (or -1) and weight.
-template <int S> __device__ __forceinline__ void choose(const asgd_route_config& c, const float (&x)[S], const float* bias, int lane, int& id, float& weight) {
-  const int E = c.experts;
-  float p[S];
-  scores<S>(x, p, c.score);
-  const bool by_logit = bias == nullptr && c.group_top == 1;
+template <int S, bool k16> __device__ __forceinline__ void choose(const RouteArgs& a, const float (&x)[S], int lane, int& id, float& weight) {
+  const asgd_route_config& c = a.c;
+  const int E = c.experts, K = c.top_k;
+  const bool by_logit = a.bias == nullptr && c.group_top == 1, sigmoid_scores = c.score == ASGD_SCORE_SIGMOID;
+  Softmax f{0.f, 1.f};
+  if (!sigmoid_scores) f = softmax<S>(x);
   unsigned key[S];
 #pragma unroll
   for (int j = 0; j < S; ++j) {
     const int e = j * 32 + lane;
-    const float v = by_logit ? x[j] : (bias && e < E) ? __fadd_rn(p[j], bias[e]) : p[j];
+    float v = x[j];
+    if (!by_logit) {
+      v = sigmoid_scores ? sigmoid(x[j]) : f.score(x[j]);
+      if (a.bias && e < E) v = __fadd_rn(v, a.bias[e]);
+    }
     key[j] = (e < E && x[j] > -INFINITY && v > -INFINITY) ? ordered(v) : 0u;
   }
-  if (c.groups_kept < c.groups) {
-    const int per = E / c.groups;
-    unsigned mine = 0;                                                 // lane g: the ordered score of group g
-    for (int g = 0; g < c.groups; ++g) {
-      unsigned m1 = 0, m2 = 0;                                         // this lane's two largest keys of the group
-#pragma unroll
-      for (int j = 0; j < S; ++j) {
-        const int e = j * 32 + lane;
-        const unsigned k = (e >= g * per && e < (g + 1) * per) ? key[j] : 0u;
-        m2 = max(m2, min(m1, k));
-        m1 = max(m1, k);
-      }
-      unsigned best = __reduce_max_sync(kAll, m1);
-      if (c.group_top == 2 && best) {
-        const unsigned holders = __ballot_sync(kAll, m1 == best);
-        const unsigned second = __reduce_max_sync(kAll, (lane == __ffs(holders) - 1) ? m2 : m1);
-        if (second) best = ordered(__fadd_rn(from_ordered(best), from_ordered(second)));
-      }
-      if (lane == g) mine = best;
-    }
-    unsigned kept = 0;
-    for (int i = 0; i < c.groups_kept; ++i) {
-      const unsigned best = __reduce_max_sync(kAll, (kept >> lane) & 1u ? 0u : mine);
-      if (!best) break;
-      kept |= 1u << (__ffs(__ballot_sync(kAll, mine == best && !((kept >> lane) & 1u))) - 1);
-    }
-#pragma unroll
-    for (int j = 0; j < S; ++j) {
-      const int e = j * 32 + lane;
-      if (e < E && !((kept >> (e / per)) & 1u)) key[j] = 0u;
-    }
-  }
+  if (c.groups_kept < c.groups) keep_groups<S>(a, lane, key);
   id = -1;
-  weight = 0.f;
-  float sum = 0.f;
-  for (int i = 0; i < c.top_k; ++i) {
-    unsigned m = key[0];
+  float chosen = 0.f;                                                  // lane j: the j-th choice's logit
+  int place[S];
+  if (k16 && by_logit) {
+    // The keys are 16-bit numbers (their last 13 bits are zero, or one for negative ones): the place goes there, the
+    // first place highest.
 #pragma unroll
-    for (int j = 1; j < S; ++j) m = max(m, key[j]);
-    const unsigned best = __reduce_max_sync(kAll, m);
-    if (!best) break;
-    unsigned at = 0xffffffffu;
+    for (int j = 0; j < S; ++j) key[j] = key[j] ? (key[j] & ~31u) | (unsigned)(31 - j) : 0u;
+    sort_keys<S, false>(key, place);
+    for (int i = 0; i < K; ++i) {
+      const unsigned best = __reduce_max_sync(kAll, key[0]);
+      if (!best) break;
+      const int from = __ffs(__ballot_sync(kAll, key[0] == best)) - 1;
+      if (lane == i) { id = (31 - (int)(best & 31u)) * 32 + from; chosen = from_ordered((best >> 31) ? best & ~31u : best | 31u); }
+      if (lane == from) {
 #pragma unroll
-    for (int j = S - 1; j >= 0; --j) at = key[j] == best ? (unsigned)(j * 32 + lane) : at;
-    const int e = (int)__reduce_min_sync(kAll, at);
+        for (int j = 0; j + 1 < S; ++j) key[j] = key[j + 1];
+        key[S - 1] = 0u;
+      }
+    }
+  } else {
 #pragma unroll
-    for (int j = 0; j < S; ++j) if (e == j * 32 + lane) key[j] = 0u;
-    const float s = pick<S>(p, e);
-    sum += s;
-    if (lane == i) { id = e; weight = s; }
+    for (int j = 0; j < S; ++j) place[j] = j;
+    sort_keys<S, true>(key, place);
+    for (int i = 0; i < K; ++i) {
+      const unsigned best = __reduce_max_sync(kAll, key[0]);
+      if (!best) break;
+      unsigned holders = __ballot_sync(kAll, key[0] == best);
+      if (holders & (holders - 1)) {                                   // equal keys: the lowest expert, so the first place first
+        const unsigned mine = key[0] == best ? (unsigned)place[0] : 32u, first = __reduce_min_sync(kAll, mine);
+        holders = __ballot_sync(kAll, mine == first);
+      }
+      const int from = __ffs(holders) - 1, at = __shfl_sync(kAll, place[0], from);
+      if (lane == i) id = at * 32 + from;
+      if (!by_logit) {
+        float v = x[0];
+#pragma unroll
+        for (int j = 1; j < S; ++j) v = at == j ? x[j] : v;
+        v = __shfl_sync(kAll, v, from);
+        if (lane == i) chosen = v;
+      } else if (lane == i) {
+        chosen = from_ordered(best);
+      }
+      if (lane == from) {
+#pragma unroll
+        for (int j = 0; j + 1 < S; ++j) { key[j] = key[j + 1]; place[j] = place[j + 1]; }
+        key[S - 1] = 0u;
+      }
+    }
   }
-  if (id >= 0) weight = c.renormalise ? c.scale * weight / (sum + 1e-20f) : c.scale * weight;
+  const float s = id < 0 ? 0.f : sigmoid_scores ? sigmoid(chosen) : f.score(chosen);
+  weight = 0.f;
+  if (c.renormalise) {
+    // the chosen scores' sum: lanes beyond top_k hold zeros
+    float sum = s;
+    for (int o = 1; o < K; o <<= 1) sum += __shfl_xor_sync(kAll, sum, o);
+    sum = __shfl_sync(kAll, sum, 0);
+    if (id >= 0) weight = c.scale * s / (sum + 1e-20f);
+  } else if (id >= 0) {
+    weight = c.scale * s;
+  }
 }
 
 // exclusive sums over the E padded counts of the block's shared array, in place; returns the total.  All threads.
@@ -178,37 +259,39 @@ __device__ int scan_padded(int* cnt, int E, int align, int* warp_part) {
   return total;
 }
 
-// -1 for the rows of nothing: experts e = first, first + step, ... and the tail behind the last expert
-__device__ void fill_nothing(const RouteArgs& a, const int* first_row, const int* count, int total, int first, int step) {
-  const int E = a.c.experts;
+// -1 for the rows of nothing: the experts' padding, a warp each in turn, and the tail behind the last expert
+__device__ void fill_nothing(const RouteArgs& a, const int* first_row, const int* count, int total, int block, int blocks) {
+  const int E = a.c.experts, lane = threadIdx.x & 31, nw = blockDim.x >> 5;
   if (a.c.align > 1)
-    for (int e = first; e < E; e += step) {
+    for (int e = block * nw + (int)(threadIdx.x >> 5); e < E; e += blocks * nw) {
       const int to = e + 1 < E ? first_row[e + 1] : total;
-      for (int r = first_row[e] + count[e] + (int)threadIdx.x; r < to; r += blockDim.x) a.source[r] = -1;
+      for (int r = first_row[e] + count[e] + lane; r < to; r += 32) a.source[r] = -1;
     }
-  for (long long r = total + (long long)first * blockDim.x + threadIdx.x; r < a.source_len; r += (long long)step * blockDim.x) a.source[r] = -1;
+  for (long long r = total + (long long)block * blockDim.x + threadIdx.x; r < a.source_len; r += (long long)blocks * blockDim.x) a.source[r] = -1;
 }
 
-template <int S, typename T> __global__ void route_kernel(const RouteArgs a) {
+template <int S, typename T> __global__ void __launch_bounds__(S <= 8 ? kThreadsOne : 512) route_kernel(const RouteArgs a) {
   __shared__ unsigned long long word[ASGD_MAX_EXPERTS];
   __shared__ int first_row[ASGD_MAX_EXPERTS], count[ASGD_MAX_EXPERTS], warp_part[32];
+  __shared__ int ids[kMaxChunk * ASGD_MAX_TOP_K];
   const int E = a.c.experts, K = a.c.top_k, lane = threadIdx.x & 31, wid = threadIdx.x >> 5, nw = blockDim.x >> 5;
   const bool plan = a.offsets != nullptr;
-  const long long t0 = (long long)blockIdx.x * kChunk;
-  const int nt = (int)min((long long)kChunk, a.T - t0);
+  const long long t0 = (long long)blockIdx.x * a.chunk;
+  const int nt = (int)min((long long)a.chunk, a.T - t0);
   if (plan) {
     for (int e = threadIdx.x; e < E; e += blockDim.x) word[e] = 0;
     __syncthreads();
   }
+  float x[S];
   for (int q = wid; q < nt; q += nw) {
-    float x[S];
     load_row<S, T>(reinterpret_cast<const T*>(a.logits) + (t0 + q) * a.ld, E, lane, x);
     int id;
     float w;
-    choose<S>(a.c, x, a.bias, lane, id, w);
+    choose<S, sizeof(T) == 2>(a, x, lane, id, w);
     if (lane < K) {
       a.ids[(t0 + q) * K + lane] = id;
       a.weights[(t0 + q) * K + lane] = w;
+      ids[q * K + lane] = id;
       if (plan && id >= 0) atomicOr(&word[id], 1ull << q);
     }
   }
@@ -227,38 +310,45 @@ template <int S, typename T> __global__ void route_kernel(const RouteArgs a) {
     for (int e = threadIdx.x; e < E; e += blockDim.x) a.offsets[e] = first_row[e];
     if (threadIdx.x == 0) a.offsets[E] = total;
   }
-  for (int i = threadIdx.x; i < nt * K; i += blockDim.x) {
-    const long long at = t0 * K + i;
-    const int id = a.ids[at], q = i / K;                               // written by this block before the barrier above
-    int r = -1;
-    if (id >= 0) {
-      r = __popcll(word[id] & ((1ull << q) - 1ull));
-      if (one) { r += first_row[id]; a.source[r] = (int)at; }
+  for (int q = wid; q < nt; q += nw)
+    if (lane < K) {
+      const long long at = (t0 + q) * K + lane;
+      const int id = ids[q * K + lane];
+      int r = -1;
+      if (id >= 0) {
+        r = __popcll(word[id] & ((1ull << q) - 1ull));
+        if (one) { r += first_row[id]; a.source[r] = (int)at; }
+      }
+      a.rows[at] = r;
     }
-    a.rows[at] = r;
-  }
   if (one) fill_nothing(a, first_row, count, total, 0, 1);
 }
 
 // per expert (a warp each): counts of the chunks before, and the total
-__global__ void chunk_sums_kernel(const RouteArgs a) {
+__global__ void __launch_bounds__(128) chunk_sums_kernel(const RouteArgs a) {
   const int e = (int)(blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5)), lane = threadIdx.x & 31;
   if (e >= a.c.experts) return;
   int* h = a.hist + (long long)e * a.chunks;
   int run = 0;
-  for (long long c0 = 0; c0 < a.chunks; c0 += 32) {
-    const int n = c0 + lane < a.chunks ? h[c0 + lane] : 0;
-    int inc = n;
+  for (int c0 = 0; c0 < a.chunks; c0 += 256) {
+    int n[8];
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) { const int v = __shfl_up_sync(kAll, inc, o); if (lane >= o) inc += v; }
-    if (c0 + lane < a.chunks) h[c0 + lane] = run + inc - n;
-    run += __shfl_sync(kAll, inc, 31);
+    for (int i = 0; i < 8; ++i) { const int c = c0 + i * 32 + lane; n[i] = c < a.chunks ? h[c] : 0; }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int c = c0 + i * 32 + lane;
+      int inc = n[i];
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) { const int v = __shfl_up_sync(kAll, inc, o); if (lane >= o) inc += v; }
+      if (c < a.chunks) h[c] = run + inc - n[i];
+      run += __shfl_sync(kAll, inc, 31);
+    }
   }
   if (lane == 0) a.totals[e] = run;
 }
 
-// ranks inside a chunk -> grouped rows, and the way back
-__global__ void place_kernel(const RouteArgs a) {
+// ranks inside a chunk -> grouped rows, and the way back; more blocks than chunks where there is much to fill
+__global__ void __launch_bounds__(kThreads) place_kernel(const RouteArgs a) {
   __shared__ int first_row[ASGD_MAX_EXPERTS], count[ASGD_MAX_EXPERTS], warp_part[32];
   const int E = a.c.experts, K = a.c.top_k;
   for (int e = threadIdx.x; e < E; e += blockDim.x) first_row[e] = count[e] = a.totals[e];
@@ -268,15 +358,15 @@ __global__ void place_kernel(const RouteArgs a) {
     for (int e = threadIdx.x; e < E; e += blockDim.x) a.offsets[e] = first_row[e];
     if (threadIdx.x == 0) a.offsets[E] = total;
   }
-  const long long t0 = (long long)blockIdx.x * kChunk;
-  const int nt = (int)min((long long)kChunk, a.T - t0);
-  for (int i = threadIdx.x; i < nt * K; i += blockDim.x) {
-    const long long at = t0 * K + i;
-    const int id = a.ids[at];
-    if (id < 0) continue;
-    const int r = a.rows[at] + first_row[id] + a.hist[(long long)id * a.chunks + blockIdx.x];
-    a.rows[at] = r;
-    a.source[r] = (int)at;
+  if (blockIdx.x < a.chunks) {
+    const long long from = (long long)blockIdx.x * a.chunk * K, to = min(from + (long long)a.chunk * K, a.T * K);
+    for (long long at = from + threadIdx.x; at < to; at += blockDim.x) {
+      const int id = a.ids[at];
+      if (id < 0) continue;
+      const int r = a.rows[at] + first_row[id] + a.hist[(long long)id * a.chunks + blockIdx.x];
+      a.rows[at] = r;
+      a.source[r] = (int)at;
+    }
   }
   fill_nothing(a, first_row, count, total, (int)blockIdx.x, (int)gridDim.x);
 }
@@ -296,49 +386,46 @@ struct GradArgs {
   void* dlogits;
 };
 
+// sum over the lanes that hold a choice, known to all (lanes from top_k on hold zeros)
+__device__ __forceinline__ float choice_sum(float v, int K) {
+  for (int o = 1; o < K; o <<= 1) v += __shfl_xor_sync(kAll, v, o);
+  return __shfl_sync(kAll, v, 0);
+}
+
 template <int S, typename T> __global__ void __launch_bounds__(kThreads) route_grad_kernel(const GradArgs a) {
   const int E = a.c.experts, K = a.c.top_k, lane = threadIdx.x & 31;
-  const long long t = (long long)blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5);
+  const bool sigmoid_scores = a.c.score == ASGD_SCORE_SIGMOID;
+  const long long t = (long long)blockIdx.x * kWarps + (threadIdx.x >> 5);
   if (t >= a.T) return;
-  float x[S], p[S];
-  load_row<S, T>(reinterpret_cast<const T*>(a.logits) + t * a.ld, E, lane, x);
+  const T* row = reinterpret_cast<const T*>(a.logits) + t * a.ld;
+  T* out = reinterpret_cast<T*>(a.dlogits) + t * a.ld_out;
+  // lane j: the j-th choice
   int id = -1;
-  float dw = 0.f;
+  float dw = 0.f, chosen = 0.f;
   if (lane < K) { id = a.ids[t * K + lane]; dw = a.dweights[t * K + lane]; }
   const bool ok = id >= 0 && id < E;
-  scores<S>(x, p, a.c.score);
-  // lane j: score of the j-th choice
-  float s = 0.f;
-  for (int i = 0; i < K; ++i) {
-    const int e = __shfl_sync(kAll, ok ? id : 0, i);
-    const float v = pick<S>(p, e);
-    if (lane == i) s = v;
-  }
-  if (!ok) { s = 0.f; dw = 0.f; }
-  float ds;
+  float x[S];
+  load_row<S, T>(row, E, lane, x);
+  if (ok) chosen = Elem<T>::to_f(row[id]);
+  Softmax f{0.f, 1.f};
+  if (!sigmoid_scores) f = softmax<S>(x);
+  const float s = !ok ? 0.f : sigmoid_scores ? sigmoid(chosen) : f.score(chosen);
+  float ds = 0.f;
   if (a.c.renormalise) {
-    const float total = warp_sum(s) + 1e-20f;
-    ds = a.c.scale * (dw - warp_sum(dw * s) / total) / total;
-  } else {
+    const float total = choice_sum(s, K) + 1e-20f, dot = choice_sum(ok ? dw * s : 0.f, K);
+    if (ok) ds = a.c.scale * (dw - dot / total) / total;
+  } else if (ok) {
     ds = a.c.scale * dw;
   }
-  if (!ok) ds = 0.f;
-  const float dot = warp_sum(ds * s);
-  float g[S];
-#pragma unroll
-  for (int j = 0; j < S; ++j) g[j] = 0.f;
-  for (int i = 0; i < K; ++i) {
-    const int e = __shfl_sync(kAll, ok ? id : -1, i);
-    const float v = __shfl_sync(kAll, ds, i);
-#pragma unroll
-    for (int j = 0; j < S; ++j) if (e == j * 32 + lane) g[j] += v;
-  }
-  T* out = reinterpret_cast<T*>(a.dlogits) + t * a.ld_out;
+  // every expert's gradient as of one that was not chosen, then the chosen ones' over it
+  const float dot = sigmoid_scores ? 0.f : choice_sum(ds * s, K), per = dot / f.sum;
 #pragma unroll
   for (int j = 0; j < S; ++j) {
     const int e = j * 32 + lane;
-    if (e < E) out[e] = Elem<T>::from_f(a.c.score == ASGD_SCORE_SIGMOID ? g[j] * p[j] * (1.f - p[j]) : p[j] * (g[j] - dot));
+    if (e < E) out[e] = Elem<T>::from_f(sigmoid_scores ? 0.f : -f.part(x[j]) * per);
   }
+  __syncwarp();
+  if (ok) out[id] = Elem<T>::from_f(sigmoid_scores ? ds * s * (1.f - s) : s * (ds - dot));
 }
 
 // Calls f with the registers a lane needs for E experts, as a compile-time number.
@@ -365,9 +452,20 @@ bool config_ok(const asgd_route_config* c) {
 bool config_supported(const asgd_route_config* c) {
   return c->experts <= ASGD_MAX_EXPERTS && c->groups <= ASGD_MAX_EXPERT_GROUPS && c->top_k <= ASGD_MAX_TOP_K;
 }
+// Tokens of a chunk: one block where it does all (few tokens, little to fill); else as many per warp (eight warps) as keep
+// some 32 warps on every SM, so that short batches spread over the GPU.
+int chunk_of(const asgd_route_config* c, long long T) {
+  if (T <= kMaxChunk && (long long)c->experts * (c->align - 1) <= 4096) return kMaxChunk;
+  long long per_warp = ceil_div(T, (long long)kSMs * 32);
+  int n = 1;
+  while (n < per_warp && n < kMaxChunk / kWarps) n *= 2;
+  return n * kWarps;
+}
+bool one_block(const asgd_route_config* c, long long T) { return chunk_of(c, T) == kMaxChunk && T <= kMaxChunk; }
+// (a plan that takes more than one block has two chunks at least, the second one empty if need be)
+int chunks_of(const asgd_route_config* c, long long T) { return one_block(c, T) ? 1 : (int)std::max(2ll, ceil_div(T, chunk_of(c, T))); }
 size_t workspace_bytes(const asgd_route_config* c, long long T) {
-  if (T <= kChunk) return 0;
-  return ((size_t)ceil_div(T, kChunk) + 1) * (size_t)c->experts * sizeof(int);
+  return one_block(c, T) ? 0 : ((size_t)chunks_of(c, T) + 1) * (size_t)c->experts * sizeof(int);
 }
 
 }  // namespace
@@ -398,7 +496,11 @@ extern "C" int asgd_route(const asgd_route_config* cfg, int64_t T, const void* l
   cudaStream_t st = (cudaStream_t)stream;
   RouteArgs a;
   a.c = *cfg;
-  a.T = T; a.ld = ld; a.chunks = ceil_div(T, kChunk); a.source_len = source_len;
+  a.T = T; a.ld = ld; a.source_len = source_len;
+  a.chunk = chunk_of(cfg, T);
+  a.chunks = chunks_of(cfg, T);
+  const unsigned per = (unsigned)(cfg->experts / cfg->groups);
+  a.group_magic = per > 1 ? (unsigned)((1ull << 32) / per + 1) : 0;    // exact for numbers below 2^16
   a.logits = logits; a.bias = bias; a.ids = ids; a.weights = weights;
   a.offsets = plan ? offsets : nullptr; a.rows = rows; a.source = source;
   a.hist = (int*)workspace;
@@ -407,16 +509,17 @@ extern "C" int asgd_route(const asgd_route_config* cfg, int64_t T, const void* l
     if (plan) empty_plan_kernel<<<1, kThreads, 0, st>>>(a);
     return cudaGetLastError() == cudaSuccess ? ASGD_OK : ASGD_ECUDA;
   }
+  const bool one = one_block(cfg, T);
   with_slots(cfg->experts, [&](auto s) {
     with_type(type, [&](auto e) {
-      // the widest instance needs more registers than 1024 threads have
-      const int threads = a.chunks > 1 ? kThreads : decltype(s)::value > 8 ? 512 : kThreadsOne;
+      // the widest instances need more registers than 1024 threads have
+      const int threads = !one ? kThreads : decltype(s)::value > 8 ? 512 : kThreadsOne;
       route_kernel<decltype(s)::value, decltype(e)><<<(unsigned)a.chunks, threads, 0, st>>>(a);
     });
   });
-  if (plan && a.chunks > 1) {
+  if (plan && !one) {
     chunk_sums_kernel<<<(unsigned)ceil_div(cfg->experts, 4), 128, 0, st>>>(a);
-    place_kernel<<<(unsigned)a.chunks, kThreads, 0, st>>>(a);
+    place_kernel<<<(unsigned)std::max(a.chunks, cfg->align > 1 ? kFillBlocks : 1), kThreads, 0, st>>>(a);
   }
   return cudaGetLastError() == cudaSuccess ? ASGD_OK : ASGD_ECUDA;
 }
