@@ -1,8 +1,8 @@
 // The experts' rows back into token order, and the gradient.  The contract is in include/asgd_experts.h.
 //
-// HBM is the bound: every row of z is read once (and written once in the gradient), a token's row of y or dy once.  A
-// thread block takes a token (the sum: a stretch of a token's row), threads take 16-byte pieces; the rows of z are met
-// in ascending place, so a sum has one order.
+// HBM is the bound: every row of z is read once (and written once in the gradient), a token's row of y or dy once.  In
+// the sum a thread block takes a stretch of a token's row, a thread 16-byte pieces of it, and the rows of z are met in
+// ascending place; in the gradient a warp takes an assignment.  Every sum has one order.
 #include "asgd_experts_common.cuh"
 
 #include <algorithm>
@@ -12,8 +12,8 @@ namespace {
 
 using namespace asgd::experts;
 
-constexpr int kThreads = 128;                              // the sum; the gradient takes what fits the row
-constexpr int kMaxThreads = 256;
+constexpr int kThreads = 128;                              // of the sum
+constexpr int kGradThreads = 256;
 constexpr int kMaxRows = 8;                                // rows of z a thread has in flight
 
 struct Args {
@@ -94,71 +94,70 @@ template <typename T, bool kVec, int N, int U> __global__ void __launch_bounds__
   }
 }
 
-// Blocks 0..T-1: a token each.  The blocks behind them: 128 grouped rows each, those of nothing become zeros.
-template <typename T, bool kVec, int N> __global__ void __launch_bounds__(kMaxThreads) combine_grad_kernel(const Args a) {
+// W warps take an assignment (one where there are many): its row of z and its token's row of dy, U pieces of each in
+// flight per thread.  A token's assignments are neighbours, so its row of dy comes from HBM once and from the caches after
+// that; what a thread holds is small, and it is the bytes in flight that the rate needs (a token per block with all its rows
+// in registers: 91 us where this takes 67, on 5003 x 6 rows of 2560 bf16 numbers).  The blocks behind the assignments' take
+// 128 grouped rows each; those of nothing become zeros.
+template <typename T, bool kVec, int W> __global__ void __launch_bounds__(kGradThreads, kVec ? 4 : 3) combine_grad_kernel(const Args a, long long fill_from) {
   using P = Piece<T, kVec>;
+  constexpr int U = kVec ? 4 : 8, kAcross = 32 * W;
   T* dz = reinterpret_cast<T*>(a.dz);
-  if (blockIdx.x >= a.T) {
-    const long long r0 = ((long long)blockIdx.x - a.T) * 128;
+  if (blockIdx.x >= fill_from) {
+    const long long r0 = ((long long)blockIdx.x - fill_from) * 128;
     for (int q = 0; q < 128; ++q) {
       const long long r = r0 + q;
       if (r >= a.R || a.source[r] >= 0) continue;
-      for (long long c = (long long)threadIdx.x * P::kN; c < a.D; c += (long long)blockDim.x * P::kN) P::store(dz + r * a.ld_dz + c, typename P::Word{});
+      for (long long c = (long long)threadIdx.x * P::kN; c < a.D; c += (long long)kGradThreads * P::kN) P::store(dz + r * a.ld_dz + c, typename P::Word{});
     }
     return;
   }
-  __shared__ float part[kMaxThreads / 32][N];
-  const T* z = reinterpret_cast<const T*>(a.z);
-  const long long t = blockIdx.x;
-  const T* dy = reinterpret_cast<const T*>(a.dy) + t * a.ld_dy;
-  for (int j0 = 0; j0 < a.top_k; j0 += N) {
-    int row[N];
-    float w[N], dot[N];
+  __shared__ float part[kGradThreads / 32];
+  const int of = threadIdx.x / kAcross, at = threadIdx.x % kAcross;      // assignment of the block, thread of the assignment
+  const long long i = (long long)blockIdx.x * (kGradThreads / kAcross) + of, t = i / a.top_k;
+  int row = -1;
+  float w = 0.f, dot = 0.f;
+  if (t < a.T) assignment(a, t, (int)(i - t * a.top_k), row, w);
+  if (row >= 0) {
+    const T* dy = reinterpret_cast<const T*>(a.dy) + t * a.ld_dy;
+    const T* z = reinterpret_cast<const T*>(a.z) + row * a.ldz;
+    T* out = dz + row * a.ld_dz;
+    for (long long c0 = at * P::kN; c0 < a.D; c0 += U * kAcross * P::kN) {
+      typename P::Word g[U], v[U];
 #pragma unroll
-    for (int j = 0; j < N; ++j) { assignment(a, t, j0 + j, row[j], w[j]); dot[j] = 0.f; }
-    for (long long c = (long long)threadIdx.x * P::kN; c < a.D; c += (long long)blockDim.x * P::kN) {
-      typename P::Word raw[N];
-      const typename P::Word raw_g = P::load(dy + c);
-#pragma unroll
-      for (int j = 0; j < N; ++j) {
-        raw[j] = typename P::Word{};
-        if (a.dweights && row[j] >= 0) raw[j] = P::load(z + row[j] * a.ldz + c);
-      }
-      float g[P::kN];
-      P::unpack(raw_g, g);
-      if (a.dz)
-#pragma unroll
-        for (int j = 0; j < N; ++j) {
-          if (row[j] < 0) continue;
-          float o[P::kN];
-#pragma unroll
-          for (int i = 0; i < P::kN; ++i) o[i] = w[j] * g[i];
-          P::store(dz + row[j] * a.ld_dz + c, P::pack(o));
+      for (int u = 0; u < U; ++u) {
+        const long long c = c0 + u * kAcross * P::kN;
+        g[u] = v[u] = typename P::Word{};
+        if (c < a.D) {
+          g[u] = P::load(dy + c);
+          if (a.dweights) v[u] = P::load(z + c);
         }
+      }
 #pragma unroll
-      for (int j = 0; j < N; ++j) {
-        float v[P::kN];
-        P::unpack(raw[j], v);
-        if (row[j] >= 0)                             // a row that takes no part adds nothing, whatever dy holds
+      for (int u = 0; u < U; ++u) {
+        const long long c = c0 + u * kAcross * P::kN;
+        float x[P::kN], y[P::kN];
+        P::unpack(g[u], x);
+        P::unpack(v[u], y);
+        if (c < a.D) {
 #pragma unroll
-          for (int i = 0; i < P::kN; ++i) dot[j] = fmaf(g[i], v[i], dot[j]);
+          for (int e = 0; e < P::kN; ++e) { dot = fmaf(x[e], y[e], dot); y[e] = w * x[e]; }
+          if (a.dz) P::store(out + c, P::pack(y));
+        }
       }
     }
-    if (!a.dweights) continue;
-#pragma unroll
-    for (int j = 0; j < N; ++j) {
-#pragma unroll
-      for (int o = 16; o > 0; o >>= 1) dot[j] += __shfl_xor_sync(kAll, dot[j], o);
-      if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5][j] = dot[j];
-    }
-    __syncthreads();
-    if (threadIdx.x < N && j0 + (int)threadIdx.x < a.top_k) {
-      float s = 0.f;
-      for (int v = 0; v < (int)blockDim.x / 32; ++v) s += part[v][threadIdx.x];
-      a.dweights[t * a.top_k + j0 + threadIdx.x] = s;
-    }
-    __syncthreads();
   }
+  if (!a.dweights) return;
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) dot += __shfl_xor_sync(kAll, dot, o);
+  if (W > 1) {
+    if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = dot;
+    __syncthreads();
+    dot = 0.f;
+#pragma unroll
+    for (int q = 0; q < W; ++q) dot += part[of * W + q];
+  }
+  if (at == 0 && t < a.T) a.dweights[i] = dot;
 }
 
 template <typename T> bool whole(const void* p, long long ld) { return aligned(p, 16) && ld % kPer16<T> == 0; }
@@ -191,7 +190,7 @@ extern "C" int asgd_combine(int64_t T, int64_t D, int32_t top_k, const void* z, 
     const bool vec = whole<E>(z, ldz) && whole<E>(y, ldy) && D % kPer16<E> == 0;
     with_rows(top_k, vec, [&](auto v, auto n) {
       constexpr bool kVec = decltype(v)::value;
-      constexpr int N = decltype(n)::value, U = 8 / N;
+      constexpr int N = decltype(n)::value, U = (kVec ? 8 : 32) / N;
       const long long stretches = ceil_div(D, (long long)kThreads * U * (kVec ? kPer16<E> : 1));
       if (stretches > 65535) { rc = ASGD_EUNSUPPORTED; return; }
       combine_kernel<E, kVec, N, U><<<dim3((unsigned)T, (unsigned)stretches), kThreads, 0, (cudaStream_t)stream>>>(a);
@@ -212,18 +211,18 @@ extern "C" int asgd_combine_grad(int64_t T, int64_t D, int32_t top_k, const void
   Args a{};
   a.T = T; a.D = D; a.R = R; a.ldz = ldz; a.ld_dy = ld_dy; a.ld_dz = ld_dz; a.top_k = top_k;
   a.z = z; a.dy = dy; a.rows = rows; a.weights = weights; a.source = source; a.dz = dz; a.dweights = dweights;
-  const long long blocks = T + (dz && source ? ceil_div(R, 128) : 0);
+  // a warp per assignment where that keeps the SMs full, else four
+  const long long assignments = T * top_k;
+  const int warps = assignments >= kSMs * 32 ? 1 : 4;
+  const long long fill_from = ceil_div(assignments * warps, kGradThreads / 32), blocks = fill_from + (dz && source ? ceil_div(R, 128) : 0);
   if (blocks > 0x7fffffffll) return ASGD_EUNSUPPORTED;
   if (blocks == 0) return ASGD_OK;
   with_type(type, [&](auto e) {
     using E = decltype(e);
     const bool vec = whole<E>(dy, ld_dy) && (!dweights || whole<E>(z, ldz)) && (!dz || whole<E>(dz, ld_dz)) && D % kPer16<E> == 0;
-    // threads that share the row's pieces evenly: as many turns as 256 threads would take
-    const long long pieces = std::max(1ll, ceil_div(D, vec ? kPer16<E> : 1)), turns = ceil_div(pieces, kMaxThreads);
-    const unsigned threads = (unsigned)ceil_div(ceil_div(pieces, turns), 32) * 32;
-    with_rows(top_k, vec, [&](auto v, auto n) {
-      combine_grad_kernel<E, decltype(v)::value, decltype(n)::value><<<(unsigned)blocks, threads, 0, (cudaStream_t)stream>>>(a);
-    });
+    const auto kernel = vec ? (warps == 1 ? combine_grad_kernel<E, true, 1> : combine_grad_kernel<E, true, 4>)
+                            : (warps == 1 ? combine_grad_kernel<E, false, 1> : combine_grad_kernel<E, false, 4>);
+    kernel<<<(unsigned)blocks, kGradThreads, 0, (cudaStream_t)stream>>>(a, fill_from);
   });
   return cudaGetLastError() == cudaSuccess ? ASGD_OK : ASGD_ECUDA;
 }
