@@ -1,8 +1,8 @@
 // Routing of tokens to experts: choice and weights, their gradient, and the plan that groups the assignments by expert.
 // The contract is in include/asgd_experts.h.
 //
-// A warp owns a token: lane l holds the experts l, l + 32, ... in registers, so the row is read once, coalesced at any
-// stride.  Keys become unsigned numbers of the same order and each lane sorts its own; a choice is then a warp-wide
+// A warp, or with few experts L = 8 or 16 lanes of one, own a token: lane l holds the experts l, l + L, ... in registers, so
+// the row is read once, coalesced at any stride.  Keys become unsigned numbers of the same order and each lane sorts its own; a choice is then a warp-wide
 // integer maximum of the lanes' first keys, a vote for the lane that has it, and a shift of that lane's list.  16-bit
 // logits that are themselves the keys leave room for the place in the list in the key's low bits, so that equal keys
 // need no second look.  Only the chosen logits are turned into weights.  Instructions and their latency are the bound,
@@ -50,14 +50,41 @@ __device__ __forceinline__ unsigned ordered(float v) {
 __device__ __forceinline__ float from_ordered(unsigned u) {
   return __uint_as_float((u >> 31) ? (u & 0x7fffffffu) : ~u);
 }
-__device__ __forceinline__ float warp_max(float v) {               // by one integer reduction; NaNs are passed over
-  const unsigned u = __reduce_max_sync(kAll, v == v ? ordered(v) : 0u);
-  return u ? from_ordered(u) : v;
-}
-__device__ __forceinline__ float warp_sum(float v) {
+// The L lanes of a token: maxima (one instruction for a whole warp), votes, sums.  Every lane of the warp takes part.
+template <int L> __device__ __forceinline__ unsigned lanes_max(unsigned v) {
+  if (L == 32) return __reduce_max_sync(kAll, v);
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(kAll, v, o);
+  for (int o = L / 2; o > 0; o >>= 1) v = max(v, __shfl_xor_sync(kAll, v, o));
   return v;
+}
+template <int L> __device__ __forceinline__ unsigned lanes_min(unsigned v) {
+  if (L == 32) return __reduce_min_sync(kAll, v);
+#pragma unroll
+  for (int o = L / 2; o > 0; o >>= 1) v = min(v, __shfl_xor_sync(kAll, v, o));
+  return v;
+}
+template <int L> __device__ __forceinline__ unsigned lanes_ballot(bool p) {       // bit l: the token's lane l
+  const unsigned b = __ballot_sync(kAll, p);
+  return L == 32 ? b : (b >> (threadIdx.x & 31 & ~(L - 1))) & ((1u << (L & 31)) - 1u);
+}
+template <int L> __device__ __forceinline__ float lanes_max(float v) {            // NaNs are passed over
+  if (L == 32) {
+    const unsigned u = __reduce_max_sync(kAll, v == v ? ordered(v) : 0u);
+    return u ? from_ordered(u) : v;
+  }
+#pragma unroll
+  for (int o = L / 2; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(kAll, v, o));
+  return v;
+}
+template <int L> __device__ __forceinline__ float lanes_sum(float v) {
+#pragma unroll
+  for (int o = L / 2; o > 0; o >>= 1) v += __shfl_xor_sync(kAll, v, o);
+  return v;
+}
+// sum over the lanes that hold a choice (those from top_k on hold zeros), known to the token's lanes
+template <int L> __device__ __forceinline__ float choice_sum(float v, int K) {
+  for (int o = 1; o < K; o <<= 1) v += __shfl_xor_sync(kAll, v, o);
+  return __shfl_sync(kAll, v, 0, L);
 }
 
 __device__ __forceinline__ float sigmoid(float x) { return __fdiv_rn(1.f, __fadd_rn(1.f, expf(-x))); }
@@ -69,23 +96,23 @@ struct Softmax {
   __device__ __forceinline__ float part(float x) const { return x == m ? 1.f : expf(x - m); }
   __device__ __forceinline__ float score(float x) const { return __fdiv_rn(part(x), sum); }
 };
-template <int S> __device__ __forceinline__ Softmax softmax(const float (&x)[S]) {
+template <int S, int L> __device__ __forceinline__ Softmax softmax(const float (&x)[S]) {
   Softmax f;
   float m = x[0];
 #pragma unroll
   for (int j = 1; j < S; ++j) m = fmaxf(m, x[j]);
-  f.m = warp_max(m);
+  f.m = lanes_max<L>(m);
   float sum = 0.f;
 #pragma unroll
   for (int j = 0; j < S; ++j) sum += f.part(x[j]);
-  f.sum = warp_sum(sum);
+  f.sum = lanes_sum<L>(sum);
   return f;
 }
 
-template <int S, typename T> __device__ __forceinline__ void load_row(const T* row, int E, int lane, float (&x)[S]) {
+template <int S, int L, typename T> __device__ __forceinline__ void load_row(const T* row, int E, int lane, float (&x)[S]) {
 #pragma unroll
   for (int j = 0; j < S; ++j) {
-    const int e = j * 32 + lane;
+    const int e = j * L + lane;
     x[j] = (e < E) ? Elem<T>::to_f(row[e]) : -INFINITY;
   }
 }
@@ -120,12 +147,12 @@ template <int S, bool kPlaces> __device__ __forceinline__ void sort_keys(unsigne
 }
 
 // Takes all experts but those of the best groups_kept groups out (their keys become 0).
-template <int S> __device__ __forceinline__ void keep_groups(const RouteArgs& a, int lane, unsigned (&key)[S]) {
+template <int S, int L> __device__ __forceinline__ void keep_groups(const RouteArgs& a, int lane, unsigned (&key)[S]) {
   const asgd_route_config& c = a.c;
   int group[S];
 #pragma unroll
-  for (int j = 0; j < S; ++j) group[j] = a.group_magic ? (int)__umulhi((unsigned)(j * 32 + lane), a.group_magic) : j * 32 + lane;
-  unsigned mine = 0;                                                   // lane g: the ordered score of group g
+  for (int j = 0; j < S; ++j) group[j] = a.group_magic ? (int)__umulhi((unsigned)(j * L + lane), a.group_magic) : j * L + lane;
+  unsigned mine = 0;                                                   // lane g: the ordered score of group g (groups <= L)
   for (int g = 0; g < c.groups; ++g) {
     unsigned m1 = 0, m2 = 0;                                           // this lane's two largest keys of the group
 #pragma unroll
@@ -134,35 +161,36 @@ template <int S> __device__ __forceinline__ void keep_groups(const RouteArgs& a,
       m2 = max(m2, min(m1, k));
       m1 = max(m1, k);
     }
-    unsigned best = __reduce_max_sync(kAll, m1);
-    if (c.group_top == 2 && best) {
-      const unsigned holders = __ballot_sync(kAll, m1 == best);
-      const unsigned second = __reduce_max_sync(kAll, (lane == __ffs(holders) - 1) ? m2 : m1);
+    unsigned best = lanes_max<L>(m1);
+    if (c.group_top == 2) {
+      const unsigned holders = lanes_ballot<L>(m1 == best);
+      const unsigned second = lanes_max<L>((lane == __ffs(holders) - 1) ? m2 : m1);
       if (second) best = ordered(__fadd_rn(from_ordered(best), from_ordered(second)));
     }
     if (lane == g) mine = best;
   }
   unsigned kept = 0;
   for (int i = 0; i < c.groups_kept; ++i) {
-    const unsigned best = __reduce_max_sync(kAll, (kept >> lane) & 1u ? 0u : mine);
-    if (!best) break;
-    kept |= 1u << (__ffs(__ballot_sync(kAll, mine == best && !((kept >> lane) & 1u))) - 1);
+    const bool taken = (kept >> lane) & 1u;
+    const unsigned best = lanes_max<L>(taken ? 0u : mine);
+    const unsigned holders = lanes_ballot<L>(best && mine == best && !taken);
+    kept |= holders & (0u - holders);                                  // the lowest of them, if any
   }
 #pragma unroll
   for (int j = 0; j < S; ++j) if (!((kept >> (group[j] & 31)) & 1u)) key[j] = 0u;
 }
 
 // The choice of one token: lane j < top_k returns its j-th expert (or -1) and weight.
-template <int S, bool k16> __device__ __forceinline__ void choose(const RouteArgs& a, const float (&x)[S], int lane, int& id, float& weight) {
+template <int S, int L, bool k16> __device__ __forceinline__ void choose(const RouteArgs& a, const float (&x)[S], int lane, int& id, float& weight) {
   const asgd_route_config& c = a.c;
   const int E = c.experts, K = c.top_k;
   const bool by_logit = a.bias == nullptr && c.group_top == 1, sigmoid_scores = c.score == ASGD_SCORE_SIGMOID;
   Softmax f{0.f, 1.f};
-  if (!sigmoid_scores) f = softmax<S>(x);
+  if (!sigmoid_scores) f = softmax<S, L>(x);
   unsigned key[S];
 #pragma unroll
   for (int j = 0; j < S; ++j) {
-    const int e = j * 32 + lane;
+    const int e = j * L + lane;
     float v = x[j];
     if (!by_logit) {
       v = sigmoid_scores ? sigmoid(x[j]) : f.score(x[j]);
@@ -170,7 +198,7 @@ template <int S, bool k16> __device__ __forceinline__ void choose(const RouteArg
     }
     key[j] = (e < E && x[j] > -INFINITY && v > -INFINITY) ? ordered(v) : 0u;
   }
-  if (c.groups_kept < c.groups) keep_groups<S>(a, lane, key);
+  if (c.groups_kept < c.groups) keep_groups<S, L>(a, lane, key);
   id = -1;
   float chosen = 0.f;                                                  // lane j: the j-th choice's logit
   int place[S];
@@ -181,53 +209,46 @@ template <int S, bool k16> __device__ __forceinline__ void choose(const RouteArg
     for (int j = 0; j < S; ++j) key[j] = key[j] ? (key[j] & ~31u) | (unsigned)(31 - j) : 0u;
     sort_keys<S, false>(key, place);
     for (int i = 0; i < K; ++i) {
-      const unsigned best = __reduce_max_sync(kAll, key[0]);
-      if (!best) break;
-      const int from = __ffs(__ballot_sync(kAll, key[0] == best)) - 1;
-      if (lane == i) { id = (31 - (int)(best & 31u)) * 32 + from; chosen = from_ordered((best >> 31) ? best & ~31u : best | 31u); }
-      if (lane == from) {
+      const unsigned best = lanes_max<L>(key[0]);
+      const int from = __ffs(lanes_ballot<L>(key[0] == best)) - 1;
+      if (lane == i && best) { id = (31 - (int)(best & 31u)) * L + from; chosen = from_ordered((best >> 31) ? best & ~31u : best | 31u); }
+      const bool pop = lane == from;
 #pragma unroll
-        for (int j = 0; j + 1 < S; ++j) key[j] = key[j + 1];
-        key[S - 1] = 0u;
-      }
+      for (int j = 0; j + 1 < S; ++j) key[j] = pop ? key[j + 1] : key[j];
+      key[S - 1] = pop ? 0u : key[S - 1];
     }
   } else {
 #pragma unroll
     for (int j = 0; j < S; ++j) place[j] = j;
     sort_keys<S, true>(key, place);
     for (int i = 0; i < K; ++i) {
-      const unsigned best = __reduce_max_sync(kAll, key[0]);
-      if (!best) break;
-      unsigned holders = __ballot_sync(kAll, key[0] == best);
-      if (holders & (holders - 1)) {                                   // equal keys: the lowest expert, so the first place first
-        const unsigned mine = key[0] == best ? (unsigned)place[0] : 32u, first = __reduce_min_sync(kAll, mine);
-        holders = __ballot_sync(kAll, mine == first);
+      const unsigned best = lanes_max<L>(key[0]);
+      unsigned holders = lanes_ballot<L>(key[0] == best);
+      // equal keys (of any of the warp's tokens): the lowest expert, so the first place first
+      if (__any_sync(kAll, (holders & (holders - 1)) && best)) {
+        const unsigned mine = key[0] == best ? (unsigned)place[0] : 32u, first = lanes_min<L>(mine);
+        holders = lanes_ballot<L>(mine == first);
       }
-      const int from = __ffs(holders) - 1, at = __shfl_sync(kAll, place[0], from);
-      if (lane == i) id = at * 32 + from;
+      const int from = __ffs(holders) - 1, at = __shfl_sync(kAll, place[0], from, L);
+      if (lane == i && best) id = at * L + from;
+      float v = from_ordered(best);
       if (!by_logit) {
-        float v = x[0];
+        v = x[0];
 #pragma unroll
         for (int j = 1; j < S; ++j) v = at == j ? x[j] : v;
-        v = __shfl_sync(kAll, v, from);
-        if (lane == i) chosen = v;
-      } else if (lane == i) {
-        chosen = from_ordered(best);
+        v = __shfl_sync(kAll, v, from, L);
       }
-      if (lane == from) {
+      if (lane == i) chosen = v;
+      const bool pop = lane == from;
 #pragma unroll
-        for (int j = 0; j + 1 < S; ++j) { key[j] = key[j + 1]; place[j] = place[j + 1]; }
-        key[S - 1] = 0u;
-      }
+      for (int j = 0; j + 1 < S; ++j) { key[j] = pop ? key[j + 1] : key[j]; place[j] = pop ? place[j + 1] : place[j]; }
+      key[S - 1] = pop ? 0u : key[S - 1];
     }
   }
   const float s = id < 0 ? 0.f : sigmoid_scores ? sigmoid(chosen) : f.score(chosen);
   weight = 0.f;
   if (c.renormalise) {
-    // the chosen scores' sum: lanes beyond top_k hold zeros
-    float sum = s;
-    for (int o = 1; o < K; o <<= 1) sum += __shfl_xor_sync(kAll, sum, o);
-    sum = __shfl_sync(kAll, sum, 0);
+    const float sum = choice_sum<L>(s, K);
     if (id >= 0) weight = c.scale * s / (sum + 1e-20f);
   } else if (id >= 0) {
     weight = c.scale * s;
@@ -270,7 +291,7 @@ __device__ void fill_nothing(const RouteArgs& a, const int* first_row, const int
   for (long long r = total + (long long)block * blockDim.x + threadIdx.x; r < a.source_len; r += (long long)blocks * blockDim.x) a.source[r] = -1;
 }
 
-template <int S, typename T> __global__ void __launch_bounds__(S <= 8 ? kThreadsOne : 512) route_kernel(const RouteArgs a) {
+template <int S, int L, typename T> __global__ void __launch_bounds__(S <= 8 ? kThreadsOne : 512) route_kernel(const RouteArgs a) {
   __shared__ unsigned long long word[ASGD_MAX_EXPERTS];
   __shared__ int first_row[ASGD_MAX_EXPERTS], count[ASGD_MAX_EXPERTS], warp_part[32];
   __shared__ int ids[kMaxChunk * ASGD_MAX_TOP_K];
@@ -282,16 +303,19 @@ template <int S, typename T> __global__ void __launch_bounds__(S <= 8 ? kThreads
     for (int e = threadIdx.x; e < E; e += blockDim.x) word[e] = 0;
     __syncthreads();
   }
-  float x[S];
-  for (int q = wid; q < nt; q += nw) {
-    load_row<S, T>(reinterpret_cast<const T*>(a.logits) + (t0 + q) * a.ld, E, lane, x);
+  const int l = lane % L, sub = lane / L;                              // lane of the token, token of the warp
+  for (int q0 = wid * (32 / L); q0 < nt; q0 += nw * (32 / L)) {
+    const int q = q0 + sub;
+    const bool there = q < nt;
+    float x[S];
+    load_row<S, L, T>(reinterpret_cast<const T*>(a.logits) + (t0 + q) * a.ld, there ? E : 0, l, x);
     int id;
     float w;
-    choose<S, sizeof(T) == 2>(a, x, lane, id, w);
-    if (lane < K) {
-      a.ids[(t0 + q) * K + lane] = id;
-      a.weights[(t0 + q) * K + lane] = w;
-      ids[q * K + lane] = id;
+    choose<S, L, sizeof(T) == 2>(a, x, l, id, w);
+    if (there && l < K) {
+      a.ids[(t0 + q) * K + l] = id;
+      a.weights[(t0 + q) * K + l] = w;
+      ids[q * K + l] = id;
       if (plan && id >= 0) atomicOr(&word[id], 1ull << q);
     }
   }
@@ -386,56 +410,61 @@ struct GradArgs {
   void* dlogits;
 };
 
-// sum over the lanes that hold a choice, known to all (lanes from top_k on hold zeros)
-__device__ __forceinline__ float choice_sum(float v, int K) {
-  for (int o = 1; o < K; o <<= 1) v += __shfl_xor_sync(kAll, v, o);
-  return __shfl_sync(kAll, v, 0);
-}
-
-template <int S, typename T> __global__ void __launch_bounds__(kThreads) route_grad_kernel(const GradArgs a) {
-  const int E = a.c.experts, K = a.c.top_k, lane = threadIdx.x & 31;
+template <int S, int L, typename T> __global__ void __launch_bounds__(kThreads) route_grad_kernel(const GradArgs a) {
+  const int K = a.c.top_k, lane = threadIdx.x % L;
   const bool sigmoid_scores = a.c.score == ASGD_SCORE_SIGMOID;
-  const long long t = (long long)blockIdx.x * kWarps + (threadIdx.x >> 5);
-  if (t >= a.T) return;
+  const long long t = (long long)blockIdx.x * (kThreads / L) + threadIdx.x / L;
+  const int E = t < a.T ? a.c.experts : 0;                             // lanes beyond the tokens go along with nothing
   const T* row = reinterpret_cast<const T*>(a.logits) + t * a.ld;
   T* out = reinterpret_cast<T*>(a.dlogits) + t * a.ld_out;
   // lane j: the j-th choice
   int id = -1;
   float dw = 0.f, chosen = 0.f;
-  if (lane < K) { id = a.ids[t * K + lane]; dw = a.dweights[t * K + lane]; }
+  if (lane < K && t < a.T) { id = a.ids[t * K + lane]; dw = a.dweights[t * K + lane]; }
   const bool ok = id >= 0 && id < E;
   float x[S];
-  load_row<S, T>(row, E, lane, x);
+  load_row<S, L, T>(row, E, lane, x);
   if (ok) chosen = Elem<T>::to_f(row[id]);
   Softmax f{0.f, 1.f};
-  if (!sigmoid_scores) f = softmax<S>(x);
+  if (!sigmoid_scores) f = softmax<S, L>(x);
   const float s = !ok ? 0.f : sigmoid_scores ? sigmoid(chosen) : f.score(chosen);
   float ds = 0.f;
   if (a.c.renormalise) {
-    const float total = choice_sum(s, K) + 1e-20f, dot = choice_sum(ok ? dw * s : 0.f, K);
+    const float total = choice_sum<L>(s, K) + 1e-20f, dot = choice_sum<L>(ok ? dw * s : 0.f, K);
     if (ok) ds = a.c.scale * (dw - dot / total) / total;
   } else if (ok) {
     ds = a.c.scale * dw;
   }
   // every expert's gradient as of one that was not chosen, then the chosen ones' over it
-  const float dot = sigmoid_scores ? 0.f : choice_sum(ds * s, K), per = dot / f.sum;
+  const float dot = sigmoid_scores ? 0.f : choice_sum<L>(ds * s, K), per = dot / f.sum;
 #pragma unroll
   for (int j = 0; j < S; ++j) {
-    const int e = j * 32 + lane;
+    const int e = j * L + lane;
     if (e < E) out[e] = Elem<T>::from_f(sigmoid_scores ? 0.f : -f.part(x[j]) * per);
   }
   __syncwarp();
   if (ok) out[id] = Elem<T>::from_f(sigmoid_scores ? ds * s * (1.f - s) : s * (ds - dot));
 }
 
-// Calls f with the registers a lane needs for E experts, as a compile-time number.
-template <typename F> void with_slots(int E, F&& f) {
-  if (E <= 32) f(std::integral_constant<int, 1>());
-  else if (E <= 64) f(std::integral_constant<int, 2>());
-  else if (E <= 128) f(std::integral_constant<int, 4>());
-  else if (E <= 256) f(std::integral_constant<int, 8>());
-  else if (E <= 512) f(std::integral_constant<int, 16>());
-  else f(std::integral_constant<int, 32>());
+// Calls f with the numbers a lane holds and the lanes of a token, as compile-time numbers: as few lanes as have room for
+// the choices and the groups and hold eight numbers at most, for most of the instructions are the same whatever the
+// lanes hold (gradient of 32768 x 64 logits: 13 us with 32 lanes a token, 9.6 with 8; 65536 x 64,
+// 2 chosen: 38.7 and 29.6 us).
+template <int N> using Int = std::integral_constant<int, N>;
+template <typename F> void with_shape(const asgd_route_config& c, F&& f) {
+  const int E = c.experts, need = std::max(c.top_k, c.groups_kept < c.groups ? c.groups : 1);
+  if (E <= 64 && need <= 8) {
+    if (E <= 16) f(Int<2>(), Int<8>());
+    else if (E <= 32) f(Int<4>(), Int<8>());
+    else f(Int<8>(), Int<8>());
+  } else if (E <= 128 && need <= 16) {
+    if (E <= 64) f(Int<4>(), Int<16>());
+    else f(Int<8>(), Int<16>());
+  } else if (E <= 64) f(Int<2>(), Int<32>());
+  else if (E <= 128) f(Int<4>(), Int<32>());
+  else if (E <= 256) f(Int<8>(), Int<32>());
+  else if (E <= 512) f(Int<16>(), Int<32>());
+  else f(Int<32>(), Int<32>());
 }
 
 bool config_ok(const asgd_route_config* c) {
@@ -510,11 +539,11 @@ extern "C" int asgd_route(const asgd_route_config* cfg, int64_t T, const void* l
     return cudaGetLastError() == cudaSuccess ? ASGD_OK : ASGD_ECUDA;
   }
   const bool one = one_block(cfg, T);
-  with_slots(cfg->experts, [&](auto s) {
+  with_shape(*cfg, [&](auto s, auto l) {
     with_type(type, [&](auto e) {
       // the widest instances need more registers than 1024 threads have
       const int threads = !one ? kThreads : decltype(s)::value > 8 ? 512 : kThreadsOne;
-      route_kernel<decltype(s)::value, decltype(e)><<<(unsigned)a.chunks, threads, 0, st>>>(a);
+      route_kernel<decltype(s)::value, decltype(l)::value, decltype(e)><<<(unsigned)a.chunks, threads, 0, st>>>(a);
     });
   });
   if (plan && !one) {
@@ -531,9 +560,12 @@ extern "C" int asgd_route_grad(const asgd_route_config* cfg, int64_t T, const vo
   if (T == 0) return ASGD_OK;
   if (!logits || !ids || !dweights || !dlogits || !aligned(logits, type_bytes(type)) || !aligned(dlogits, type_bytes(type))) return ASGD_EINVAL;
   GradArgs a{*cfg, T, ld, ld_out, logits, ids, dweights, dlogits};
-  with_slots(cfg->experts, [&](auto s) {
+  asgd_route_config shape = *cfg;
+  shape.groups = shape.groups_kept = 1;                                // groups have no part in the gradient
+  with_shape(shape, [&](auto s, auto l) {
     with_type(type, [&](auto e) {
-      route_grad_kernel<decltype(s)::value, decltype(e)><<<(unsigned)ceil_div(T, kThreads / 32), kThreads, 0, (cudaStream_t)stream>>>(a);
+      constexpr int L = decltype(l)::value;
+      route_grad_kernel<decltype(s)::value, L, decltype(e)><<<(unsigned)ceil_div(T, kThreads / L), kThreads, 0, (cudaStream_t)stream>>>(a);
     });
   });
   return cudaGetLastError() == cudaSuccess ? ASGD_OK : ASGD_ECUDA;
