@@ -136,21 +136,17 @@ __device__ inline void count_tiles(const Params& p, int bm, Groups& gs) {
   __syncthreads();
 }
 
-// Tile number `tile` of tiles of bm x bn.  Inside a group the tiles run down bands of `band` tile rows, column after
-// column: neighbouring blocks share operands in L2.
-__device__ inline Tile find_tile(const Params& p, int bm, int bn, int band, const Groups& gs, int tile) {
+// Tile number `tile` of tiles of bm x bn, of group g that has `before` tiles before it and the rows (or K numbers) lo to
+// hi.  Inside a group the tiles run down bands of `band` tile rows, column after column: neighbouring blocks share
+// operands in L2.
+__device__ inline Tile make_tile(const Params& p, int bm, int bn, int band, int g, int before, int lo, int hi, int tile) {
   Tile t;
-  int a = 0, b = max(p.groups, 1);
-  while (b - a > 1) {                                // the last group that starts at or before the tile
-    const int m = (a + b) >> 1;
-    if (gs.prefix[m] <= tile) a = m; else b = m;
-  }
-  t.g = a;
-  const int lo = gs.start[a], hi = max(gs.start[a + 1], lo);
+  t.g = g;
+  hi = max(hi, lo);
   const int first_row = p.inner ? 0 : lo;
   t.m_end = p.inner ? p.M : hi;
   const int rows = (t.m_end - first_row + bm - 1) / bm;
-  int at = tile - gs.prefix[a], first = 0, high = rows;
+  int at = tile - before, first = 0, high = rows;
   if (rows > band) {
     first = at / (band * p.tiles_n) * band;
     at -= first * p.tiles_n;
@@ -170,6 +166,36 @@ __device__ inline Tile find_tile(const Params& p, int bm, int bn, int band, cons
   }
   return t;
 }
+// by one thread: the last group that starts at or before the tile
+__device__ inline Tile find_tile(const Params& p, int bm, int bn, int band, const Groups& gs, int tile) {
+  int a = 0, b = max(p.groups, 1);
+  while (b - a > 1) {
+    const int m = (a + b) >> 1;
+    if (gs.prefix[m] <= tile) a = m; else b = m;
+  }
+  return make_tile(p, bm, bn, band, a, gs.prefix[a], gs.start[a], gs.start[a + 1], tile);
+}
+// By a whole warp, 32 groups at a look: a search step by step through shared memory that the tensor cores keep busy takes
+// some 250 cycles a step.  With at most 32 groups the lanes keep them in registers.
+struct LaneGroups {
+  int prefix, start, next;
+  __device__ inline LaneGroups(const Params& p, const Groups& gs, int lane) {
+    const int G = max(p.groups, 1), g = min(lane, G - 1);
+    prefix = lane < G ? gs.prefix[g] : 0x7fffffff;
+    start = gs.start[g];
+    next = gs.start[g + 1];
+  }
+  __device__ inline Tile find(const Params& p, int bm, int bn, int band, const Groups& gs, int tile, int lane) const {
+    const int G = max(p.groups, 1);
+    if (G <= 32) {
+      const int a = 31 - __clz(__ballot_sync(kAll, prefix <= tile));
+      return make_tile(p, bm, bn, band, a, __shfl_sync(kAll, prefix, a), __shfl_sync(kAll, start, a), __shfl_sync(kAll, next, a), tile);
+    }
+    int a = -1;
+    for (int g = 0; g < G; g += 32) a += __popc(__ballot_sync(kAll, g + lane < G && gs.prefix[min(g + lane, G - 1)] <= tile));
+    return make_tile(p, bm, bn, band, a, gs.prefix[a], gs.start[a], gs.start[a + 1], tile);
+  }
+};
 
 // instructions of 32 numbers that K block kb takes (the last block of the inner dimension may be short)
 __device__ inline int steps_of(const Tile& t, int kb) { return min(4, (t.k_end - kb * kKB + 31) >> 5); }

@@ -20,17 +20,23 @@ namespace {
 constexpr int kPairRows = 256, kPairCols = 256;      // of C, per pair
 constexpr int kHalf = 128;                           // rows of either operand per block
 constexpr int kPairThreads = 384;
-constexpr int kPairSlots = 6;                        // even: a slot always meets the same issuing thread, see below
+constexpr int kPairSlots = 5;
 constexpr int kPairBand = 8;                         // tile rows that neighbouring pairs run down before the next column
 constexpr unsigned kHalfBytes = kHalf * kKB, kPairBytes = 2 * kHalfBytes;      // per block: one operand, a slot
 constexpr int kPieceBytes = 32 * 64;                 // per warp, on the way to C: 64 bytes of each of its 32 rows
-constexpr int kStagePieces = 1, kStageBytes = kStagePieces * kPieceBytes;
+constexpr int kStagePieces = 2, kStageBytes = kStagePieces * kPieceBytes;
 constexpr int kScales = kHalf + kPairCols;           // of a slot: the block's rows', then the columns' (256, or two blocks')
-enum { P_FULL = 0, P_DONE = kPairSlots, P_SFULL = 2 * kPairSlots, P_SEMPTY = 3 * kPairSlots, P_ACCEMPTY = 4 * kPairSlots,
+enum { P_FULL = 0 /* [issuing thread][slot] */, P_DONE = 2 * kPairSlots, P_SFULL = 3 * kPairSlots, P_SEMPTY = 4 * kPairSlots, P_ACCEMPTY = 5 * kPairSlots,
        P_DRAIN = P_ACCEMPTY + 2, P_COUNT = P_DRAIN + 2 };
 constexpr size_t kPairSmem = 1024 + (size_t)kPairSlots * kPairBytes + 8 * kStageBytes + (size_t)kPairSlots * kScales * 4 +
                              P_COUNT * 8 + sizeof(Groups) + 64;
 static_assert(kPairSmem <= kSmemLimit, "shared memory");
+
+// K block number `it` of a block's work: its full barrier (each issuing thread has its own, so that it meets every phase of
+// what it waits on: a wait on a parity cannot tell a phase from the one two before) and the phase
+__device__ inline unsigned full_of(unsigned it) { return P_FULL + (it & 1) * kPairSlots + it % kPairSlots; }
+__device__ inline unsigned full_phase(unsigned it) { return it / (2 * kPairSlots) & 1; }
+static_assert(kPairSlots % 2 == 1, "a slot meets the issuing threads in turn");
 
 __device__ inline unsigned in_first_block(const void* smem) {                  // the same place in the pair's first block
   unsigned r;
@@ -202,7 +208,8 @@ product_pair_kernel(const Params p, const __grid_constant__ CUtensorMap map_a, c
     prefetch_map(&map_a);
     prefetch_map(&map_b);
     if (p.c_by_map) prefetch_map(&map_c);
-    for (int q = 0; q < S; ++q) { mbar_init(bars + P_FULL + q, 1); mbar_init(bars + P_DONE + q, 1); mbar_init(bars + P_SFULL + q, 32); mbar_init(bars + P_SEMPTY + q, 8); }
+    for (int q = 0; q < 2 * S; ++q) mbar_init(bars + P_FULL + q, 1);
+    for (int q = 0; q < S; ++q) { mbar_init(bars + P_DONE + q, 1); mbar_init(bars + P_SFULL + q, 32); mbar_init(bars + P_SEMPTY + q, 8); }
     for (int q = 0; q < 2; ++q) { mbar_init(bars + P_ACCEMPTY + q, 16); mbar_init(bars + P_DRAIN + q, 1); }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     for (int q = 1; q < 5; ++q) misc[q] = 0;
@@ -222,7 +229,7 @@ product_pair_kernel(const Params p, const __grid_constant__ CUtensorMap map_a, c
   if (wid < 4) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
     if (wid == 0 && lane == 0) {
-      const unsigned full0 = in_first_block(bars + P_FULL);
+      const unsigned bars0 = in_first_block(bars);
       unsigned it = 0;
       bool ok = true;
       for (int tile = pair; tile < tiles && ok; tile += pairs) {
@@ -232,28 +239,30 @@ product_pair_kernel(const Params p, const __grid_constant__ CUtensorMap map_a, c
           const unsigned q = it % S;
           if (it >= S && !(ok = wait(bars + P_DONE + q, (it / S - 1) & 1, p.wait_limit, abort))) break;
           unsigned char* to = ring + (size_t)q * kPairBytes;
-          if (rank == 0) mbar_expect_tx(bars + P_FULL + q, 2 * kPairBytes);
+          if (rank == 0) mbar_expect_tx(bars + full_of(it), 2 * kPairBytes);
+          const unsigned full = bars0 + full_of(it) * 8;
           if (!(p.withhold && it == 0)) {
-            tma_load_pair(to, &map_a, kb * kKB, t.m0 + (int)rank * kHalf, za, full0 + q * 8);
-            tma_load_pair(to + kHalfBytes, &map_b, kb * kKB, t.n0 + (int)rank * kHalf, zb, full0 + q * 8);
+            tma_load_pair(to, &map_a, kb * kKB, t.m0 + (int)rank * kHalf, za, full);
+            tma_load_pair(to + kHalfBytes, &map_b, kb * kKB, t.n0 + (int)rank * kHalf, zb, full);
           }
         }
       }
       store_cluster(in_first_block(misc + 2 + rank), it);
     } else if ((wid == 1 || wid == 3) && lane == 0 && rank == 0) {
       // Two issuing threads, one per accumulator stage, K blocks in turn: a commit holds the thread that issues it for
-      // several hundred cycles, and the other thread's products fill the gap.  Each meets every phase of the barriers it
-      // waits on (the slots are even in number), as a wait on a parity needs.
+      // several hundred cycles, and the other thread's products fill the gap.
       const unsigned me = (unsigned)wid >> 1;
       unsigned it = 0;
       bool ok = true;
       for (int tile = pair; tile < tiles && ok; tile += pairs) {
-        const Tile t = find_tile(p, kPairRows, kPairCols, kPairBand, gs, tile);
+        Tile t;                                      // the K blocks alone
+        t.kb0 = 0; t.kb1 = p.kblocks; t.k_end = p.K;
+        if (p.inner) t = find_tile(p, kPairRows, kPairCols, kPairBand, gs, tile);
         for (int kb = t.kb0; kb < t.kb1; ++kb, ++it) {
           const unsigned q = it % S, stage = it & 1;
           if (stage != me) continue;
           // the operands are there long before the accumulator is free: what can be done is done before that wait
-          if (!(ok = wait(bars + P_FULL + q, (it / S) & 1, p.wait_limit, abort))) break;
+          if (!(ok = wait(bars + full_of(it), full_phase(it), p.wait_limit, abort))) break;
           const unsigned long long da = operand_desc(ring + (size_t)q * kPairBytes), db = operand_desc(ring + (size_t)q * kPairBytes + kHalfBytes);
           const int steps = steps_of(t, kb);
           if (it >= 2 && !(ok = wait(bars + P_ACCEMPTY + stage, (it / 2 - 1) & 1, p.wait_limit, abort))) break;
@@ -268,10 +277,11 @@ product_pair_kernel(const Params p, const __grid_constant__ CUtensorMap map_a, c
         for (unsigned n = 0; n < p.wait_limit && !mbar_try_wait(bars + P_DRAIN + me, 0); ++n) {}
       }
     } else if (wid == 2) {
+      const LaneGroups lg(p, gs, lane);
       unsigned it = 0;
       bool ok = true;
       for (int tile = pair; tile < tiles && ok; tile += pairs) {
-        const Tile t = find_tile(p, kPairRows, kPairCols, kPairBand, gs, tile);
+        const Tile t = lg.find(p, kPairRows, kPairCols, kPairBand, gs, tile, lane);
         const float* from = p.sb + (p.inner ? 0 : t.g * p.sb_group);
         for (int kb = t.kb0; kb < t.kb1; ++kb, ++it) {
           const unsigned q = it % S;
@@ -304,10 +314,11 @@ product_pair_kernel(const Params p, const __grid_constant__ CUtensorMap map_a, c
     const unsigned free0 = in_first_block(bars + P_ACCEMPTY);
     const unsigned at_tmem = tmem + ((unsigned)(quarter * 32) << 16) + half * 128;
     unsigned char* stage_smem = stages + (wid - 4) * kStageBytes;
+    const LaneGroups lg(p, gs, lane);
     unsigned it = 0;
     bool ok = true;
     for (int tile = pair; tile < tiles && ok; tile += pairs) {
-      const Tile t = find_tile(p, kPairRows, kPairCols, kPairBand, gs, tile);
+      const Tile t = lg.find(p, kPairRows, kPairCols, kPairBand, gs, tile, lane);
       const int m = t.m0 + (int)rank * kHalf + quarter * 32, n = t.n0 + half * 128;      // the warp's corner
       float acc[128];
 #pragma unroll
@@ -401,12 +412,12 @@ product_pair_kernel(const Params p, const __grid_constant__ CUtensorMap map_a, c
   if (rank == 0 && tid == 0 && *reinterpret_cast<volatile int*>(misc + 4)) {
     const unsigned mine = (unsigned)misc[2], other = (unsigned)misc[3], last = max(mine, other);
     for (unsigned i = min(mine, other); i < last; ++i) {
-      if (i < mine) complete_tx(bars + P_FULL + i % S, kPairBytes);
-      else mbar_expect_tx(bars + P_FULL + i % S, kPairBytes);
+      if (i < mine) complete_tx(bars + full_of(i), kPairBytes);
+      else mbar_expect_tx(bars + full_of(i), kPairBytes);
     }
-    if (p.withhold && last) complete_tx(bars + P_FULL, ((mine > 0) + (other > 0)) * kPairBytes);
-    for (unsigned q = 0; q < S && q < last; ++q)
-      for (unsigned n = 0; n < p.wait_limit && !mbar_try_wait(bars + P_FULL + q, ((last - 1 - q) / S) & 1); ++n) {}
+    if (p.withhold && last) complete_tx(bars + full_of(0), ((mine > 0) + (other > 0)) * kPairBytes);
+    for (unsigned i = last > 2 * S ? last - 2 * S : 0; i < last; ++i)          // every barrier's last use
+      for (unsigned n = 0; n < p.wait_limit && !mbar_try_wait(bars + full_of(i), full_phase(i)); ++n) {}
     atomicMin(&g_status, ASGD_ETIMEOUT);
   }
   pair_sync();
