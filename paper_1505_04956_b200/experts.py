@@ -22,6 +22,7 @@ from .binding import ASGD_OK, AsgdError
 F32, BF16, F16, E4M3, E5M2 = 0, 1, 2, 3, 4
 SCORES = {"softmax": 0, "sigmoid": 1}
 BLOCK = 128
+_FORMS = {"rows": (True, False, 0), "columns": (False, True, 0), "both": (True, True, 0), "blocks": (True, False, 1), "blocks both": (True, True, 1)}
 
 _FLOAT = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
 _EIGHT = {torch.float8_e4m3fn: E4M3, torch.float8_e5m2: E5M2}
@@ -90,29 +91,35 @@ def _need(ok, what, *values):
         raise ValueError(what % values if values else what)
 
 
+def _wrong(t, types, name, dims):
+    _need(t.is_cuda, "%s must be a CUDA tensor: the library has no host path", name)
+    _need(t.dim() == dims, "%s must have %d dimensions", name, dims)
+    _need(t.dtype in types, "%s: dtype %s is not supported", name, t.dtype)
+    _need(False, "%s: the last dimension must be contiguous", name)
+
+
+# A call takes as long on the host as on the device when the tensors are small, so every attribute of a tensor is read once.
 def _matrix(t, types, name, dims=2):
-    """A CUDA tensor of one of the types whose last dimension is contiguous; returns its type's number."""
-    number = types.get(t.dtype)
-    if not (t.is_cuda and number is not None and t.dim() == dims and (t.stride(-1) == 1 or t.shape[-1] <= 1)):
-        _need(t.is_cuda, "%s must be a CUDA tensor: the library has no host path", name)
-        _need(t.dim() == dims, "%s must have %d dimensions", name, dims)
-        _need(number is not None, "%s: dtype %s is not supported", name, t.dtype)
-        _need(False, "%s: the last dimension must be contiguous", name)
-    return number
+    """A CUDA tensor of one of the types whose last dimension is contiguous: its type's number, shape and strides."""
+    number, shape, strides = types.get(t.dtype), t.shape, t.stride()
+    if not (number is not None and t.is_cuda and len(shape) == dims and (strides[-1] == 1 or shape[-1] <= 1)):
+        _wrong(t, types, name, dims)
+    return number, shape, strides
 
 
 def _flat(t, dtype, shape, name):
-    _need(t.is_cuda and t.dtype == dtype and t.shape == shape and t.is_contiguous(),
-          "%s must be a contiguous CUDA tensor of %s with shape %s", name, dtype, shape)
+    """Its address."""
+    if not (t.is_cuda and t.dtype == dtype and t.shape == shape and t.is_contiguous()):
+        raise ValueError("%s must be a contiguous CUDA tensor of %s with shape %s" % (name, dtype, tuple(shape)))
+    return t.data_ptr()
 
 
-def _ld(t, unit=1):
+def _ld(shape, strides, unit=1):
     """Elements from one row to the next; for a single row, which has no say, a multiple of `unit`."""
-    return t.stride(-2) if t.shape[-2] > 1 else -(-t.shape[-1] // unit) * unit
+    return strides[-2] if shape[-2] > 1 else -(-shape[-1] // unit) * unit
 
 
-def _new(shape, strides, dtype, dev):
-    return torch.empty_strided(shape, strides, dtype=dtype, device=dev)
+_new = torch.empty_strided
 
 
 def _handle(t):
@@ -145,25 +152,22 @@ def asgd_route(logits, top_k, *, score="softmax", bias=None, groups=1, groups_ke
     if stream is not None:
         return _on(stream, asgd_route, logits, top_k, score=score, bias=bias, groups=groups, groups_kept=groups_kept, group_top=group_top,
                    renormalise=renormalise, scale=scale, align=align, plan=plan)
-    type_ = _matrix(logits, _FLOAT, "logits")
-    T, E = logits.shape
-    if bias is not None:
-        _flat(bias, torch.float32, (E,), "bias")
+    type_, (T, E), strides = _matrix(logits, _FLOAT, "logits")
+    bias_ptr = None if bias is None else _flat(bias, torch.float32, (E,), "bias")
     cfg, need = _route_config(E, top_k, score, groups, groups_kept, group_top, renormalise, scale, align, T)
-    dev = logits.device
-    ids = _new((T, top_k), (top_k, 1), torch.int32, dev)
-    weights = _new((T, top_k), (top_k, 1), torch.float32, dev)
-    bias_ptr = bias.data_ptr() if bias is not None else None
+    dev, ints, ld = logits.device, torch.int32, _ld((T, E), strides)
+    ids = _new((T, top_k), (top_k, 1), dtype=ints, device=dev)
+    weights = _new((T, top_k), (top_k, 1), dtype=torch.float32, device=dev)
     if not plan:
-        _chk(_load().asgd_route(cfg, T, logits.data_ptr(), type_, _ld(logits), bias_ptr, ids.data_ptr(), weights.data_ptr(), None, None, None, 0,
+        _chk(_load().asgd_route(cfg, T, logits.data_ptr(), type_, ld, bias_ptr, ids.data_ptr(), weights.data_ptr(), None, None, None, 0,
                                 None, 0, _handle(logits)), "asgd_route")
         return ids, weights
     n = T * top_k + E * (align - 1)
-    offsets = _new((E + 1,), (1,), torch.int32, dev)
-    rows = _new((T, top_k), (top_k, 1), torch.int32, dev)
-    source = _new((n,), (1,), torch.int32, dev)
-    work = _new((need,), (1,), torch.uint8, dev) if need else None
-    _chk(_load().asgd_route(cfg, T, logits.data_ptr(), type_, _ld(logits), bias_ptr, ids.data_ptr(), weights.data_ptr(), offsets.data_ptr(),
+    offsets = _new((E + 1,), (1,), dtype=ints, device=dev)
+    rows = _new((T, top_k), (top_k, 1), dtype=ints, device=dev)
+    source = _new((n,), (1,), dtype=ints, device=dev)
+    work = _new((need,), (1,), dtype=torch.uint8, device=dev) if need else None
+    _chk(_load().asgd_route(cfg, T, logits.data_ptr(), type_, ld, bias_ptr, ids.data_ptr(), weights.data_ptr(), offsets.data_ptr(),
                             rows.data_ptr(), source.data_ptr(), n, work.data_ptr() if need else None, need, _handle(logits)), "asgd_route")
     return ids, weights, offsets, rows, source
 
@@ -172,27 +176,26 @@ def asgd_route_grad(logits, ids, dweights, *, score="softmax", renormalise=True,
     """Gradient [T, E] (of the logits' type) of the weights that asgd_route gave for `ids`, from dweights [T, top_k]."""
     if stream is not None:
         return _on(stream, asgd_route_grad, logits, ids, dweights, score=score, renormalise=renormalise, scale=scale)
-    type_ = _matrix(logits, _FLOAT, "logits")
-    T, E = logits.shape
+    type_, (T, E), strides = _matrix(logits, _FLOAT, "logits")
     _need(ids.dim() == 2 and ids.shape[0] == T, "ids must have shape [T, top_k]")
     top_k = ids.shape[1]
-    _flat(ids, torch.int32, (T, top_k), "ids")
-    _flat(dweights, torch.float32, (T, top_k), "dweights")
+    ids_ptr = _flat(ids, torch.int32, (T, top_k), "ids")
+    dw_ptr = _flat(dweights, torch.float32, (T, top_k), "dweights")
     cfg, _ = _route_config(E, top_k, score, 1, 1, 1, renormalise, scale, 1, T)
-    out = _new((T, E), (E, 1), logits.dtype, logits.device)
-    _chk(_load().asgd_route_grad(cfg, T, logits.data_ptr(), type_, _ld(logits), ids.data_ptr(), dweights.data_ptr(), out.data_ptr(), E,
-                                 _handle(logits)), "asgd_route_grad")
+    out = _new((T, E), (E, 1), dtype=logits.dtype, device=logits.device)
+    _chk(_load().asgd_route_grad(cfg, T, logits.data_ptr(), type_, _ld((T, E), strides), ids_ptr, dw_ptr, out.data_ptr(), E, _handle(logits)),
+         "asgd_route_grad")
     return out
 
 
 def _eight(rows, cols, dtype, dev):
     """An 8-bit matrix whose rows start at multiples of 16 bytes."""
-    return _new((rows, cols), (-(-cols // 16) * 16, 1), dtype, dev)
+    return _new((rows, cols), (-(-cols // 16) * 16, 1), dtype=dtype, device=dev)
 
 
 def _scales(rows, cols, dev):
     """Scales [rows, blocks of cols], block after block in memory."""
-    return _new((rows, -(-cols // BLOCK)), (1, rows), torch.float32, dev)
+    return _new((rows, -(-cols // BLOCK)), (1, rows), dtype=torch.float32, device=dev)
 
 
 def asgd_quantize(x, *, form="rows", dtype=torch.float8_e4m3fn, source=None, per_token=1, weights=None, stream=None):
@@ -206,41 +209,49 @@ def asgd_quantize(x, *, form="rows", dtype=torch.float8_e4m3fn, source=None, per
     if there are any, and zeros where source[r] < 0."""
     if stream is not None:
         return _on(stream, asgd_quantize, x, form=form, dtype=dtype, source=source, per_token=per_token, weights=weights)
-    x_type = _matrix(x, _FLOAT, "x")
-    _need(form in ("rows", "columns", "both", "blocks", "blocks both"), "form %r is not known", form)
-    _need(dtype in _EIGHT, "dtype %s is not supported", dtype)
-    T, K = x.shape
-    M = T
-    square = form.startswith("blocks")
+    x_type, (T, K), strides = _matrix(x, _FLOAT, "x")
+    q_type = _EIGHT.get(dtype)
+    _need(form in _FORMS, "form %r is not known", form)
+    _need(q_type is not None, "dtype %s is not supported", dtype)
+    by_rows, by_columns, square = _FORMS[form]
+    M, source_ptr, weights_ptr = T, None, None
     if source is not None:
         _need(not square, "blocks of 128 x 128 are not gathered")
         M = source.numel()
-        _flat(source, torch.int32, (M,), "source")
+        source_ptr = _flat(source, torch.int32, (M,), "source")
     if weights is not None:
         _need(source is not None, "weights need a source")
         _need(weights.is_cuda and weights.dtype == torch.float32 and weights.is_contiguous() and weights.numel() == T * per_token,
               "weights must be contiguous fp32 on the GPU, T * per_token of them")
-    dev = x.device
-    q = scale = qt = scale_t = None
-    if form != "columns":
+        weights_ptr = weights.data_ptr()
+    dev, blocks = x.device, -(-K // BLOCK)
+    args = [M, K, x.data_ptr(), _ld((T, K), strides), T, x_type, q_type, square, int(per_token), source_ptr, weights_ptr]
+    out = ()
+    if by_rows:
         q = _eight(M, K, dtype, dev)
-        blocks = -(-K // BLOCK)
-        scale = _new((-(-M // BLOCK), blocks), (blocks, 1), torch.float32, dev) if square else _scales(M, K, dev)
-    if form in ("columns", "both", "blocks both"):
+        scale = _new((-(-M // BLOCK), blocks), (blocks, 1), dtype=torch.float32, device=dev) if square else _scales(M, K, dev)
+        args += [q.data_ptr(), -(-K // 16) * 16, scale.data_ptr(), blocks if square else 1, 1 if square else M]
+        out = (q, scale)
+    else:
+        args += [None, 0, None, 0, 0]
+    if by_columns:
         qt = _eight(K, M, dtype, dev)
-        scale_t = None if square else _scales(K, M, dev)
-    a = QuantizeArgs(M, K, x.data_ptr(), _ld(x), T, x_type, _EIGHT[dtype], 1 if square else 0, int(per_token),
-                     source.data_ptr() if source is not None else None, weights.data_ptr() if weights is not None else None,
-                     *((q.data_ptr(), q.stride(0), scale.data_ptr(), scale.stride(0), scale.stride(1)) if q is not None else (None, 0, None, 0, 0)),
-                     *((qt.data_ptr(), qt.stride(0)) if qt is not None else (None, 0)),
-                     *((scale_t.data_ptr(), scale_t.stride(0), scale_t.stride(1)) if scale_t is not None else (None, 0, 0)))
-    _chk(_load().asgd_quantize(C.byref(a), _handle(x)), "asgd_quantize")
-    return tuple(t for t in (q, scale, qt, scale_t) if t is not None)
+        out += (qt,)
+        args += [qt.data_ptr(), -(-M // 16) * 16]
+        if not square:
+            scale_t = _scales(K, M, dev)
+            args += [scale_t.data_ptr(), 1, K]
+            out += (scale_t,)
+    _chk(_load().asgd_quantize(C.byref(QuantizeArgs(*args)), _handle(x)), "asgd_quantize")
+    return out
 
 
 def _scale_of(s, name, shape, other=None):
-    _need(s.is_cuda and s.dtype == torch.float32, "%s must be fp32 on the GPU", name)
-    _need(s.shape == shape or s.shape == other, "%s has shape %s, not %s", name, tuple(s.shape), shape)
+    """Scales of one of two shapes: the shape and the strides."""
+    found = s.shape
+    if not ((found == shape or found == other) and s.dtype == torch.float32 and s.is_cuda):
+        raise ValueError("%s must be fp32 on the GPU with shape %s, not %s of shape %s" % (name, tuple(shape), s.dtype, tuple(found)))
+    return found, s.stride()
 
 
 def asgd_product(a, a_scale, b, b_scale, *, offsets=None, out_dtype=torch.bfloat16, out=None, stream=None):
@@ -250,28 +261,33 @@ def asgd_product(a, a_scale, b, b_scale, *, offsets=None, out_dtype=torch.bfloat
     they are in `out` (undefined without one)."""
     if stream is not None:
         return _on(stream, asgd_product, a, a_scale, b, b_scale, offsets=offsets, out_dtype=out_dtype, out=out)
-    a_type, b_type = _matrix(a, _EIGHT, "a"), _matrix(b, _EIGHT, "b", 2 if offsets is None else 3)
-    M, K = a.shape
-    N, kb = b.shape[-2], -(-K // BLOCK)
-    _need(b.shape[-1] == K, "a and b differ in their last dimension")
-    G = 0
-    lead = ()
-    if offsets is not None:
-        G = b.shape[0]
-        lead = (G,)
+    grouped = offsets is not None
+    a_type, a_shape, a_strides = _matrix(a, _EIGHT, "a")
+    b_type, b_shape, b_strides = _matrix(b, _EIGHT, "b", 3 if grouped else 2)
+    (M, K), N, kb = a_shape, b_shape[-2], -(-a_shape[1] // BLOCK)
+    _need(b_shape[-1] == K, "a and b differ in their last dimension")
+    G, offsets_ptr = 0, None
+    if grouped:
+        G = b_shape[0]
         _need(G > 0, "b holds no group")
-        _flat(offsets, torch.int32, (G + 1,), "offsets")
-    _scale_of(a_scale, "a_scale", (M, kb))
-    _scale_of(b_scale, "b_scale", lead + (-(-N // BLOCK), kb), lead + (N, kb))
-    c = _new((M, N), (N, 1), out_dtype, a.device) if out is None else out
-    c_type = _matrix(c, _FLOAT, "out")
-    _need(c.shape == (M, N), "out must have shape (%d, %d)", M, N)
-    args = ProductArgs(M, N, K, a.data_ptr(), _ld(a, 16), a_scale.data_ptr(), a_scale.stride(0), a_scale.stride(1),
-                       b.data_ptr(), _ld(b, 16), b.stride(0) if G > 1 else 0,
-                       b_scale.data_ptr(), b_scale.stride(-2), b_scale.stride(-1), b_scale.stride(0) if G > 1 else 0,
-                       c.data_ptr(), _ld(c), 0, offsets.data_ptr() if G else None, G, 0, a_type, b_type, c_type, 1 if b_scale.shape[-2] != N else 0)
+        offsets_ptr = _flat(offsets, torch.int32, (G + 1,), "offsets")
+    _, sa = _scale_of(a_scale, "a_scale", (M, kb))
+    square = -(-N // BLOCK)
+    s_shape, sb = _scale_of(b_scale, "b_scale", (G, square, kb), (G, N, kb)) if grouped else _scale_of(b_scale, "b_scale", (square, kb), (N, kb))
+    if out is None:
+        out, c_type, ldc = _new((M, N), (N, 1), dtype=out_dtype, device=a.device), _FLOAT.get(out_dtype), N
+        _need(c_type is not None, "out_dtype %s is not supported", out_dtype)
+    else:
+        c_type, c_shape, c_strides = _matrix(out, _FLOAT, "out")
+        _need(c_shape == (M, N), "out must have shape (%d, %d)", M, N)
+        ldc = _ld(c_shape, c_strides)
+    many = G > 1
+    args = ProductArgs(M, N, K, a.data_ptr(), _ld(a_shape, a_strides, 16), a_scale.data_ptr(), sa[0], sa[1],
+                       b.data_ptr(), _ld(b_shape, b_strides, 16), b_strides[0] if many else 0,
+                       b_scale.data_ptr(), sb[-2], sb[-1], sb[0] if many else 0,
+                       out.data_ptr(), ldc, 0, offsets_ptr, G, 0, a_type, b_type, c_type, 1 if s_shape[-2] != N else 0)
     _chk(_load().asgd_product(C.byref(args), _handle(a)), "asgd_product")
-    return c
+    return out
 
 
 def asgd_product_inner(a, a_scale, b, b_scale, offsets, *, out_dtype=torch.float32, out=None, stream=None):
@@ -279,39 +295,42 @@ def asgd_product_inner(a, a_scale, b, b_scale, offsets, *, out_dtype=torch.float
     gradients.  a [M, K], a_scale [M, ceil(K / 128)], b [N, K], b_scale [N, ceil(K / 128)]."""
     if stream is not None:
         return _on(stream, asgd_product_inner, a, a_scale, b, b_scale, offsets, out_dtype=out_dtype, out=out)
-    a_type, b_type = _matrix(a, _EIGHT, "a"), _matrix(b, _EIGHT, "b")
-    M, K = a.shape
-    N, kb = b.shape[0], -(-K // BLOCK)
-    _need(b.shape[1] == K, "a and b differ in their last dimension")
+    a_type, a_shape, a_strides = _matrix(a, _EIGHT, "a")
+    b_type, b_shape, b_strides = _matrix(b, _EIGHT, "b")
+    (M, K), N, kb = a_shape, b_shape[0], -(-a_shape[1] // BLOCK)
+    _need(b_shape[1] == K, "a and b differ in their last dimension")
     G = offsets.numel() - 1
     _need(G > 0, "offsets hold no group")
-    _flat(offsets, torch.int32, (G + 1,), "offsets")
-    _scale_of(a_scale, "a_scale", (M, kb))
-    _scale_of(b_scale, "b_scale", (N, kb))
-    c = _new((G, M, N), (M * N, N, 1), out_dtype, a.device) if out is None else out
-    c_type = _matrix(c, _FLOAT, "out", 3)
-    _need(c.shape == (G, M, N), "out must have shape (%d, %d, %d)", G, M, N)
-    args = ProductArgs(M, N, K, a.data_ptr(), _ld(a, 16), a_scale.data_ptr(), a_scale.stride(0), a_scale.stride(1),
-                       b.data_ptr(), _ld(b, 16), 0, b_scale.data_ptr(), b_scale.stride(0), b_scale.stride(1), 0,
-                       c.data_ptr(), _ld(c), c.stride(0), offsets.data_ptr(), G, 1, a_type, b_type, c_type, 0)
+    offsets_ptr = _flat(offsets, torch.int32, (G + 1,), "offsets")
+    _, sa = _scale_of(a_scale, "a_scale", (M, kb))
+    _, sb = _scale_of(b_scale, "b_scale", (N, kb))
+    if out is None:
+        out, c_type, ldc, c_group = _new((G, M, N), (M * N, N, 1), dtype=out_dtype, device=a.device), _FLOAT.get(out_dtype), N, M * N
+        _need(c_type is not None, "out_dtype %s is not supported", out_dtype)
+    else:
+        c_type, c_shape, c_strides = _matrix(out, _FLOAT, "out", 3)
+        _need(c_shape == (G, M, N), "out must have shape (%d, %d, %d)", G, M, N)
+        ldc, c_group = _ld(c_shape, c_strides), c_strides[0]
+    args = ProductArgs(M, N, K, a.data_ptr(), _ld(a_shape, a_strides, 16), a_scale.data_ptr(), sa[0], sa[1],
+                       b.data_ptr(), _ld(b_shape, b_strides, 16), 0, b_scale.data_ptr(), sb[0], sb[1], 0,
+                       out.data_ptr(), ldc, c_group, offsets_ptr, G, 1, a_type, b_type, c_type, 0)
     _chk(_load().asgd_product(C.byref(args), _handle(a)), "asgd_product")
-    return c
+    return out
 
 
 def asgd_combine(z, rows, weights=None, *, stream=None):
     """y[t] = sum_j weights[t, j] * z[rows[t, j]] of z's type; rows [T, top_k] int32 (negative: no part)."""
     if stream is not None:
         return _on(stream, asgd_combine, z, rows, weights)
-    type_ = _matrix(z, _FLOAT, "z")
-    _need(rows.dim() == 2, "rows must have shape [T, top_k]")
-    T, top_k = rows.shape
-    _flat(rows, torch.int32, (T, top_k), "rows")
-    if weights is not None:
-        _flat(weights, torch.float32, (T, top_k), "weights")
-    R, D = z.shape
-    y = _new((T, D), (D, 1), z.dtype, z.device)
-    _chk(_load().asgd_combine(T, D, top_k, z.data_ptr(), type_, R, _ld(z), rows.data_ptr(), weights.data_ptr() if weights is not None else None,
-                              y.data_ptr(), D, _handle(z)), "asgd_combine")
+    type_, (R, D), strides = _matrix(z, _FLOAT, "z")
+    shape = rows.shape
+    _need(len(shape) == 2, "rows must have shape [T, top_k]")
+    T, top_k = shape
+    rows_ptr = _flat(rows, torch.int32, shape, "rows")
+    weights_ptr = None if weights is None else _flat(weights, torch.float32, shape, "weights")
+    y = _new((T, D), (D, 1), dtype=z.dtype, device=z.device)
+    _chk(_load().asgd_combine(T, D, top_k, z.data_ptr(), type_, R, _ld((R, D), strides), rows_ptr, weights_ptr, y.data_ptr(), D, _handle(z)),
+         "asgd_combine")
     return y
 
 
@@ -320,24 +339,21 @@ def asgd_combine_grad(dy, z, rows, weights=None, source=None, *, need_dz=True, n
     takes are undefined) and dweights [T, top_k]; None for what is not needed."""
     if stream is not None:
         return _on(stream, asgd_combine_grad, dy, z, rows, weights, source, need_dz=need_dz, need_dweights=need_dweights)
-    type_ = _matrix(dy, _FLOAT, "dy")
-    _matrix(z, _FLOAT, "z")
-    _need(z.dtype == dy.dtype, "dy and z differ in type")
-    T, D = dy.shape
-    R = z.shape[0]
-    _need(z.shape[1] == D, "dy and z differ in their last dimension")
-    _need(rows.dim() == 2 and rows.shape[0] == T, "rows must have shape [T, top_k]")
-    top_k = rows.shape[1]
-    _flat(rows, torch.int32, (T, top_k), "rows")
-    if weights is not None:
-        _flat(weights, torch.float32, (T, top_k), "weights")
-    if source is not None:
-        _flat(source, torch.int32, (R,), "source")
-    dz = _new((R, D), (D, 1), dy.dtype, dy.device) if need_dz else None
-    dw = _new((T, top_k), (top_k, 1), torch.float32, dy.device) if need_dweights else None
-    _chk(_load().asgd_combine_grad(T, D, top_k, dy.data_ptr(), type_, _ld(dy), z.data_ptr(), R, _ld(z), rows.data_ptr(),
-                                   weights.data_ptr() if weights is not None else None, source.data_ptr() if source is not None else None,
-                                   dz.data_ptr() if need_dz else None, D, dw.data_ptr() if need_dweights else None, _handle(dy)), "asgd_combine_grad")
+    type_, (T, D), strides = _matrix(dy, _FLOAT, "dy")
+    z_type, (R, z_D), z_strides = _matrix(z, _FLOAT, "z")
+    _need(z_type == type_, "dy and z differ in type")
+    _need(z_D == D, "dy and z differ in their last dimension")
+    shape = rows.shape
+    _need(len(shape) == 2 and shape[0] == T, "rows must have shape [T, top_k]")
+    top_k = shape[1]
+    rows_ptr = _flat(rows, torch.int32, shape, "rows")
+    weights_ptr = None if weights is None else _flat(weights, torch.float32, shape, "weights")
+    source_ptr = None if source is None else _flat(source, torch.int32, (R,), "source")
+    dz = _new((R, D), (D, 1), dtype=dy.dtype, device=dy.device) if need_dz else None
+    dw = _new((T, top_k), (top_k, 1), dtype=torch.float32, device=dy.device) if need_dweights else None
+    _chk(_load().asgd_combine_grad(T, D, top_k, dy.data_ptr(), type_, _ld((T, D), strides), z.data_ptr(), R, _ld((R, D), z_strides), rows_ptr,
+                                   weights_ptr, source_ptr, dz.data_ptr() if need_dz else None, D, dw.data_ptr() if need_dweights else None,
+                                   _handle(dy)), "asgd_combine_grad")
     return dz, dw
 
 
