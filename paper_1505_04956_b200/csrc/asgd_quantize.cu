@@ -77,7 +77,7 @@ template <typename T> __device__ __forceinline__ float largest(const uint4& w) {
 // part in are reduced together: each exchange between lanes folds half of the maxima onto half of the lanes, so that a
 // lane ends with one block's maximum, divides once, and hands the result round (with eight pieces 16 exchanges and one
 // division where eight separate reductions take 32 to 40 and eight).  The instructions issued are the bound for gathered
-// rows that come from L2: 8192 x 4096 rows gathered four times 107 us with separate reductions, 57 with four pieces.
+// rows that come from L2: 8192 x 4096 numbers gathered four times took 107 us with separate reductions.
 template <typename T, bool kVec, bool kE5M2, bool kWeights, int U> __global__ void __launch_bounds__(kThreads) rows_kernel(const Args p) {
   constexpr int V = kPer16<T>, LB = 128 / V;             // numbers per piece, lanes per block
   const asgd_quantize_args& a = p.a;
@@ -350,9 +350,10 @@ template <typename T> void launch(const Args& p, cudaStream_t st) {
   // vector accesses need every row of the input and of the result to start at a whole vector
   const bool vec = aligned(a.x, V * sizeof(T)) && a.ldx % V == 0 && (!a.q || (aligned(a.q, V) && a.ldq % V == 0));
   if (rows_only) {
-    // eight pieces per lane where they leave enough warps, a row is that long and pieces are loaded whole (8192 rows of 4095
-    // bf16 numbers, one by one: 67 us with eight, 56 with four)
-    if (vec && a.K >= 32 * V * 8 && a.M >= 4 * kSMs) launch_rows<T, 8>(p, vec, st);
+    // eight pieces per lane for gathered rows, which L2 feeds faster than they are rounded (8192 x 4096 bf16 numbers four
+    // times: 53 us, with four pieces 57), where they leave enough warps, a row is that long and pieces are loaded whole; rows
+    // in order come from HBM and are faster with more warps (once: 17.2 us with four pieces, 18.3 with eight)
+    if (vec && a.source && a.K >= 32 * V * 8 && a.M >= 4 * kSMs) launch_rows<T, 8>(p, vec, st);
     else launch_rows<T, 4>(p, vec, st);
   } else {
     const dim3 grid((unsigned)p.row_blocks, (unsigned)p.col_blocks);

@@ -30,7 +30,7 @@ constexpr int kFillBlocks = 2 * kSMs;        // blocks at least that write the r
 struct RouteArgs {
   asgd_route_config c;
   long long T, ld, source_len;
-  int chunk, chunks;                         // tokens of a chunk, chunks
+  int chunk, chunks, stride;                 // tokens of a chunk, chunks, numbers of an expert in hist (a multiple of 4)
   int group_lanes;                           // log2 of the lanes a group's keys are shared by
   unsigned group_magic;                      // e / (experts of a group) = umulhi(e, group_magic); 0: groups of one
   const void* logits;
@@ -40,7 +40,7 @@ struct RouteArgs {
   int* offsets;
   int* rows;
   int* source;
-  int* hist;                                 // [E][chunks] assignments per expert and chunk, then those in the chunks before
+  int* hist;                                 // [E][stride] assignments per expert and chunk, then those in the chunks before
   int* totals;                               // [E]
 };
 
@@ -381,7 +381,7 @@ template <int S, int L, typename T> __global__ void __launch_bounds__(S <= 8 ? k
   for (int e = threadIdx.x; e < E; e += blockDim.x) {
     const int n = __popcll(word[e]);
     if (one) { count[e] = n; first_row[e] = n; }
-    else a.hist[(long long)e * a.chunks + blockIdx.x] = n;
+    else a.hist[(long long)e * a.stride + blockIdx.x] = n;
   }
   if (one) {
     __syncthreads();
@@ -403,25 +403,31 @@ template <int S, int L, typename T> __global__ void __launch_bounds__(S <= 8 ? k
   if (one) fill_nothing(a, first_row, count, total, 0, 1);
 }
 
-// per expert (a warp each): counts of the chunks before, and the total
+// per expert (a warp each, a lane eight neighbouring chunks at a time): counts of the chunks before, and the total
 __global__ void __launch_bounds__(128) chunk_sums_kernel(const RouteArgs a) {
   const int e = (int)(blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5)), lane = threadIdx.x & 31;
   if (e >= a.c.experts) return;
-  int* h = a.hist + (long long)e * a.chunks;
+  int4* h = reinterpret_cast<int4*>(a.hist + (long long)e * a.stride);
   int run = 0;
   for (int c0 = 0; c0 < a.chunks; c0 += 256) {
+    const int c = c0 + lane * 8;
     int n[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) { const int c = c0 + i * 32 + lane; n[i] = c < a.chunks ? h[c] : 0; }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const int c = c0 + i * 32 + lane;
-      int inc = n[i];
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) { const int v = __shfl_up_sync(kAll, inc, o); if (lane >= o) inc += v; }
-      if (c < a.chunks) h[c] = run + inc - n[i];
-      run += __shfl_sync(kAll, inc, 31);
+    for (int i = 0; i < 8; i += 4) {
+      const int4 v = c + i < a.stride ? h[(c + i) / 4] : make_int4(0, 0, 0, 0);
+      n[i] = v.x; n[i + 1] = v.y; n[i + 2] = v.z; n[i + 3] = v.w;
     }
+    int mine = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) { const int v = c + i < a.chunks ? n[i] : 0; n[i] = mine; mine += v; }
+    int inc = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) { const int v = __shfl_up_sync(kAll, inc, o); if (lane >= o) inc += v; }
+    const int before = run + inc - mine;
+#pragma unroll
+    for (int i = 0; i < 8; i += 4)
+      if (c + i < a.stride) h[(c + i) / 4] = make_int4(before + n[i], before + n[i + 1], before + n[i + 2], before + n[i + 3]);
+    run += __shfl_sync(kAll, inc, 31);
   }
   if (lane == 0) a.totals[e] = run;
 }
@@ -442,7 +448,7 @@ __global__ void __launch_bounds__(kThreads) place_kernel(const RouteArgs a) {
     for (long long at = from + threadIdx.x; at < to; at += blockDim.x) {
       const int id = a.ids[at];
       if (id < 0) continue;
-      const int r = a.rows[at] + first_row[id] + a.hist[(long long)id * a.chunks + blockIdx.x];
+      const int r = a.rows[at] + first_row[id] + a.hist[(long long)id * a.stride + blockIdx.x];
       a.rows[at] = r;
       a.source[r] = (int)at;
     }
@@ -545,7 +551,7 @@ bool one_block(const asgd_route_config* c, long long T) { return chunk_of(c, T) 
 // (a plan that takes more than one block has two chunks at least, the second one empty if need be)
 int chunks_of(const asgd_route_config* c, long long T) { return one_block(c, T) ? 1 : (int)std::max(2ll, ceil_div(T, chunk_of(c, T))); }
 size_t workspace_bytes(const asgd_route_config* c, long long T) {
-  return one_block(c, T) ? 0 : ((size_t)chunks_of(c, T) + 1) * (size_t)c->experts * sizeof(int);
+  return one_block(c, T) ? 0 : ((size_t)ceil_div(chunks_of(c, T), 4) * 4 + 1) * (size_t)c->experts * sizeof(int);
 }
 
 }  // namespace
@@ -586,7 +592,8 @@ extern "C" int asgd_route(const asgd_route_config* cfg, int64_t T, const void* l
   a.logits = logits; a.bias = bias; a.ids = ids; a.weights = weights;
   a.offsets = plan ? offsets : nullptr; a.rows = rows; a.source = source;
   a.hist = (int*)workspace;
-  a.totals = a.hist + (want ? (size_t)a.chunks * cfg->experts : 0);
+  a.stride = (int)ceil_div(a.chunks, 4) * 4;
+  a.totals = a.hist + (want ? (size_t)a.stride * cfg->experts : 0);
   if (T == 0) {
     if (plan) empty_plan_kernel<<<1, kThreads, 0, st>>>(a);
     return cudaGetLastError() == cudaSuccess ? ASGD_OK : ASGD_ECUDA;
