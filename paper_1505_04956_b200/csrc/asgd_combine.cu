@@ -55,6 +55,7 @@ __device__ __forceinline__ void assignment(const Args& a, long long t, int j, in
 
 // N: rows met at a time; U: pieces per thread, blockDim apart (what is in flight is N * U pieces)
 template <typename T, bool kVec, int N, int U> __global__ void __launch_bounds__(kThreads) combine_kernel(const Args a) {
+  wait_for_stream();
   using P = Piece<T, kVec>;
   const long long t = blockIdx.x, c0 = ((long long)blockIdx.y * U * kThreads + threadIdx.x) * P::kN;
   const T* z = reinterpret_cast<const T*>(a.z);
@@ -100,6 +101,7 @@ template <typename T, bool kVec, int N, int U> __global__ void __launch_bounds__
 // in registers: 91 us where this takes 67, on 5003 x 6 rows of 2560 bf16 numbers).  The blocks behind the assignments' take
 // 128 grouped rows each; those of nothing become zeros.
 template <typename T, bool kVec, int W> __global__ void __launch_bounds__(kGradThreads, kVec ? 4 : 3) combine_grad_kernel(const Args a, long long fill_from) {
+  wait_for_stream();
   using P = Piece<T, kVec>;
   constexpr int U = kVec ? 4 : 8, kAcross = 32 * W;
   T* dz = reinterpret_cast<T*>(a.dz);
@@ -193,11 +195,10 @@ extern "C" int asgd_combine(int64_t T, int64_t D, int32_t top_k, const void* z, 
       constexpr int N = decltype(n)::value, U = (kVec ? 8 : 32) / N;
       const long long stretches = ceil_div(D, (long long)kThreads * U * (kVec ? kPer16<E> : 1));
       if (stretches > 65535) { rc = ASGD_EUNSUPPORTED; return; }
-      combine_kernel<E, kVec, N, U><<<dim3((unsigned)T, (unsigned)stretches), kThreads, 0, (cudaStream_t)stream>>>(a);
+      if (!launch_after(combine_kernel<E, kVec, N, U>, dim3((unsigned)T, (unsigned)stretches), kThreads, 0, (cudaStream_t)stream, a)) rc = ASGD_ECUDA;
     });
   });
-  if (rc != ASGD_OK) return rc;
-  return cudaGetLastError() == cudaSuccess ? ASGD_OK : ASGD_ECUDA;
+  return rc;
 }
 
 extern "C" int asgd_combine_grad(int64_t T, int64_t D, int32_t top_k, const void* dy, int32_t type, int64_t ld_dy, const void* z, int64_t R,
@@ -217,12 +218,13 @@ extern "C" int asgd_combine_grad(int64_t T, int64_t D, int32_t top_k, const void
   const long long fill_from = ceil_div(assignments * warps, kGradThreads / 32), blocks = fill_from + (dz && source ? ceil_div(R, 128) : 0);
   if (blocks > 0x7fffffffll) return ASGD_EUNSUPPORTED;
   if (blocks == 0) return ASGD_OK;
+  bool ok = false;
   with_type(type, [&](auto e) {
     using E = decltype(e);
     const bool vec = whole<E>(dy, ld_dy) && (!dweights || whole<E>(z, ldz)) && (!dz || whole<E>(dz, ld_dz)) && D % kPer16<E> == 0;
     const auto kernel = vec ? (warps == 1 ? combine_grad_kernel<E, true, 1> : combine_grad_kernel<E, true, 4>)
                             : (warps == 1 ? combine_grad_kernel<E, false, 1> : combine_grad_kernel<E, false, 4>);
-    kernel<<<(unsigned)blocks, kGradThreads, 0, (cudaStream_t)stream>>>(a, fill_from);
+    ok = launch_after(kernel, dim3((unsigned)blocks), kGradThreads, 0, (cudaStream_t)stream, a, fill_from);
   });
-  return cudaGetLastError() == cudaSuccess ? ASGD_OK : ASGD_ECUDA;
+  return ok ? ASGD_OK : ASGD_ECUDA;
 }

@@ -50,6 +50,25 @@ template <typename T> __device__ __forceinline__ uint4 pack16(const float (&v)[k
   return u;
 }
 
+// A launch that may begin while the kernel before it in the stream ends: blocks come up as SMs fall free, and wait (first
+// thing, wait_for_stream) until all that was before is complete and visible.
+template <typename... P, typename... A> inline bool launch_after(void (*kernel)(P...), dim3 grid, unsigned threads, size_t smem, cudaStream_t st, A&&... args) {
+  cudaLaunchAttribute early;
+  early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  early.val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cfg.attrs = &early;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kernel, P(args)...) == cudaSuccess;
+}
+// (in a kernel that another one of the same call follows) the next kernel's blocks may come up as soon as there is room
+__device__ __forceinline__ void let_next_come() { asm volatile("griddepcontrol.launch_dependents;"); }
+__device__ __forceinline__ void wait_for_stream() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+
 // Calls f with a value of the C++ type of a floating element type.
 template <typename F> inline void with_type(int type, F&& f) {
   if (type == ASGD_F32) f(float());

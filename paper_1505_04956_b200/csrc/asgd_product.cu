@@ -83,16 +83,18 @@ template <int BN, bool kSplit> int launch_few(const asgd_product_args& a, Params
   static std::atomic<unsigned long long> done{0};
   if (!allow_smem(product_few_kernel<BN, kSplit>, Few<BN>::kSmem, done)) return ASGD_ECUDA;
   cudaLaunchConfig_t cfg{};
-  cudaLaunchAttribute cluster;
-  cluster.id = cudaLaunchAttributeClusterDimension;
-  cluster.val.clusterDim.x = (unsigned)split;
-  cluster.val.clusterDim.y = cluster.val.clusterDim.z = 1;
+  cudaLaunchAttribute attrs[2];
+  attrs[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;    // see launch_after
+  attrs[0].val.programmaticStreamSerializationAllowed = 1;
+  attrs[1].id = cudaLaunchAttributeClusterDimension;
+  attrs[1].val.clusterDim.x = (unsigned)split;
+  attrs[1].val.clusterDim.y = attrs[1].val.clusterDim.z = 1;
   cfg.gridDim = dim3(kSplit ? (unsigned)(most * split) : (unsigned)min(most, (long long)kSMs));
   cfg.blockDim = dim3(Few<BN>::kThreads);
   cfg.dynamicSmemBytes = Few<BN>::kSmem;
   cfg.stream = st;
-  cfg.attrs = &cluster;
-  cfg.numAttrs = kSplit ? 1 : 0;
+  cfg.attrs = attrs;
+  cfg.numAttrs = kSplit ? 2 : 1;
   return cudaLaunchKernelEx(&cfg, product_few_kernel<BN, kSplit>, p, map_u, map_v) == cudaSuccess ? ASGD_OK : ASGD_ECUDA;
 }
 
@@ -131,8 +133,8 @@ int launch_pair(const asgd_product_args& a, Params p, cudaStream_t st) {
   const auto kernel = a.b_square ? product_pair_kernel<false> : product_pair_kernel<true>;
   static std::atomic<unsigned long long> done[2] = {{0}, {0}};
   if (!allow_smem(kernel, kPairSmem, done[a.b_square])) return ASGD_ECUDA;
-  kernel<<<(unsigned)min(most, (long long)(kSMs / 2)) * 2, kPairThreads, kPairSmem, st>>>(p, map_a, map_b, map_c);
-  return cudaGetLastError() == cudaSuccess ? ASGD_OK : ASGD_ECUDA;
+  const dim3 grid((unsigned)min(most, (long long)(kSMs / 2)) * 2);
+  return launch_after(kernel, grid, kPairThreads, kPairSmem, st, p, map_a, map_b, map_c) ? ASGD_OK : ASGD_ECUDA;
 }
 
 // Which kernel: the one whose blocks are through first, by the K blocks the busiest of them meets and the time of one.

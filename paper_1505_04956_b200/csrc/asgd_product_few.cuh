@@ -96,6 +96,7 @@ product_few_kernel(const Params p, const __grid_constant__ CUtensorMap map_u, co
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(misc)), "r"(F::kCols) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
+  wait_for_stream();                                 // what comes before reads nothing of the call's but its arguments
   count_tiles(p, BN, gs);
   fence_before();
   __syncthreads();

@@ -218,6 +218,7 @@ product_pair_kernel(const Params p, const __grid_constant__ CUtensorMap map_a, c
     asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(misc)), "r"(512u) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
   }
+  wait_for_stream();                                 // what comes before reads nothing of the call's but its arguments
   count_tiles(p, kPairRows, gs);
   fence_before();
   __syncthreads();

@@ -79,6 +79,7 @@ template <typename T> __device__ __forceinline__ float largest(const uint4& w) {
 // division where eight separate reductions take 32 to 40 and eight).  The instructions issued are the bound for gathered
 // rows that come from L2: 8192 x 4096 numbers gathered four times took 107 us with separate reductions.
 template <typename T, bool kVec, bool kE5M2, bool kWeights, int U> __global__ void __launch_bounds__(kThreads) rows_kernel(const Args p) {
+  wait_for_stream();
   constexpr int V = kPer16<T>, LB = 128 / V;             // numbers per piece, lanes per block
   const asgd_quantize_args& a = p.a;
   const int lane = threadIdx.x & 31, K = (int)a.K;
@@ -178,6 +179,7 @@ __device__ __forceinline__ float4 max4(float4 a, float4 b) { return make_float4(
 // The numbers stay in registers as they came (16-bit ones packed), and are taken apart once for the rows' rounding and
 // once for the columns': more blocks per SM are worth more than the second unpacking (loads' latency is the bound).
 template <typename T, bool kVec, bool kE5M2, bool kWeights> __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 3 : 2) tile_kernel(const Args p) {
+  wait_for_stream();
   using Word = typename std::conditional<sizeof(T) == 4, uint4, uint2>::type;      // 4 numbers
   __shared__ __align__(16) unsigned char tile[128 * 128];       // [column][row], 16-byte pieces exchanged by column / 4
   __shared__ float4 col_max[kWarps][32];
@@ -336,13 +338,15 @@ template <typename F> void with_flags(bool vec, bool e5m2, bool weights, F&& f) 
   if (vec) second(std::true_type());
   else second(std::false_type());
 }
-template <typename T, int U> void launch_rows(const Args& p, bool vec, cudaStream_t st) {
+template <typename T, int U> bool launch_rows(const Args& p, bool vec, cudaStream_t st) {
   const dim3 grid((unsigned)ceil_div(p.a.M, kWarps), (unsigned)ceil_div(p.a.K, 32 * kPer16<T> * U));
+  bool ok = false;
   with_flags(vec, p.a.q_type == ASGD_E5M2, p.a.weights != nullptr, [&](auto kv, auto ke, auto kw) {
-    rows_kernel<T, decltype(kv)::value, decltype(ke)::value, decltype(kw)::value, U><<<grid, kThreads, 0, st>>>(p);
+    ok = launch_after(rows_kernel<T, decltype(kv)::value, decltype(ke)::value, decltype(kw)::value, U>, grid, kThreads, 0, st, p);
   });
+  return ok;
 }
-template <typename T> void launch(const Args& p, cudaStream_t st) {
+template <typename T> bool launch(const Args& p, cudaStream_t st) {
   const asgd_quantize_args& a = p.a;
   const bool e5m2 = a.q_type == ASGD_E5M2, w = a.weights != nullptr;
   const bool rows_only = !a.qt && !a.square;
@@ -353,13 +357,15 @@ template <typename T> void launch(const Args& p, cudaStream_t st) {
     // eight pieces per lane for gathered rows, which L2 feeds faster than they are rounded (8192 x 4096 bf16 numbers four
     // times: 53 us, with four pieces 57), where they leave enough warps, a row is that long and pieces are loaded whole; rows
     // in order come from HBM and are faster with more warps (once: 17.2 us with four pieces, 18.3 with eight)
-    if (vec && a.source && a.K >= 32 * V * 8 && a.M >= 4 * kSMs) launch_rows<T, 8>(p, vec, st);
-    else launch_rows<T, 4>(p, vec, st);
+    if (vec && a.source && a.K >= 32 * V * 8 && a.M >= 4 * kSMs) return launch_rows<T, 8>(p, vec, st);
+    return launch_rows<T, 4>(p, vec, st);
   } else {
     const dim3 grid((unsigned)p.row_blocks, (unsigned)p.col_blocks);
+    bool ok = false;
     with_flags(vec, e5m2, w, [&](auto kv, auto ke, auto kw) {
-      tile_kernel<T, decltype(kv)::value, decltype(ke)::value, decltype(kw)::value><<<grid, kThreads, 0, st>>>(p);
+      ok = launch_after(tile_kernel<T, decltype(kv)::value, decltype(ke)::value, decltype(kw)::value>, grid, kThreads, 0, st, p);
     });
+    return ok;
   }
 }
 
@@ -393,6 +399,7 @@ extern "C" int asgd_quantize(const asgd_quantize_args* args, void* stream) {
   p.inv_fmax = a.q_type == ASGD_E4M3 ? 1.f / 448.f : 1.f / 57344.f;
   // limits of the grid: 65535 tiles along M, or 65535 stretches of a row
   if ((a.qt || a.square) ? cb > 65535 : ceil_div(a.K, 512) > 65535) return ASGD_EUNSUPPORTED;
-  with_type(a.x_type, [&](auto e) { launch<decltype(e)>(p, (cudaStream_t)stream); });
-  return cudaGetLastError() == cudaSuccess ? ASGD_OK : ASGD_ECUDA;
+  bool ok = false;
+  with_type(a.x_type, [&](auto e) { ok = launch<decltype(e)>(p, (cudaStream_t)stream); });
+  return ok ? ASGD_OK : ASGD_ECUDA;
 }

@@ -341,6 +341,8 @@ __device__ void fill_nothing(const RouteArgs& a, const int* first_row, const int
 }
 
 template <int S, int L, typename T> __global__ void __launch_bounds__(S <= 8 ? kThreadsOne : 512) route_kernel(const RouteArgs a) {
+  wait_for_stream();
+  if (a.chunks > 1) let_next_come();
   // 48 KB: the warps' scratch of the choices, then the plan's arrays in its place
   __shared__ unsigned long long word[ASGD_MAX_EXPERTS];
   __shared__ int ids[kMaxChunk * ASGD_MAX_TOP_K];
@@ -405,6 +407,8 @@ template <int S, int L, typename T> __global__ void __launch_bounds__(S <= 8 ? k
 
 // per expert (a warp each, a lane eight neighbouring chunks at a time): counts of the chunks before, and the total
 __global__ void __launch_bounds__(128) chunk_sums_kernel(const RouteArgs a) {
+  wait_for_stream();
+  let_next_come();
   const int e = (int)(blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5)), lane = threadIdx.x & 31;
   if (e >= a.c.experts) return;
   int4* h = reinterpret_cast<int4*>(a.hist + (long long)e * a.stride);
@@ -434,6 +438,7 @@ __global__ void __launch_bounds__(128) chunk_sums_kernel(const RouteArgs a) {
 
 // ranks inside a chunk -> grouped rows, and the way back; more blocks than chunks where there is much to fill
 __global__ void __launch_bounds__(kThreads) place_kernel(const RouteArgs a) {
+  wait_for_stream();
   __shared__ int first_row[ASGD_MAX_EXPERTS], count[ASGD_MAX_EXPERTS], warp_part[32];
   const int E = a.c.experts, K = a.c.top_k;
   for (int e = threadIdx.x; e < E; e += blockDim.x) first_row[e] = count[e] = a.totals[e];
@@ -472,6 +477,7 @@ struct GradArgs {
 };
 
 template <int S, int L, typename T> __global__ void __launch_bounds__(kThreads) route_grad_kernel(const GradArgs a) {
+  wait_for_stream();
   const int K = a.c.top_k, lane = threadIdx.x % L;
   const bool sigmoid_scores = a.c.score == ASGD_SCORE_SIGMOID;
   const long long t = (long long)blockIdx.x * (kThreads / L) + threadIdx.x / L;
@@ -599,18 +605,19 @@ extern "C" int asgd_route(const asgd_route_config* cfg, int64_t T, const void* l
     return cudaGetLastError() == cudaSuccess ? ASGD_OK : ASGD_ECUDA;
   }
   const bool one = one_block(cfg, T);
+  bool ok = false;
   with_shape(*cfg, [&](auto s, auto l) {
     with_type(type, [&](auto e) {
       // the widest instances need more registers than 1024 threads have
       const int threads = !one ? kThreads : decltype(s)::value > 8 ? 512 : kThreadsOne;
-      route_kernel<decltype(s)::value, decltype(l)::value, decltype(e)><<<(unsigned)a.chunks, threads, 0, st>>>(a);
+      ok = launch_after(route_kernel<decltype(s)::value, decltype(l)::value, decltype(e)>, dim3((unsigned)a.chunks), threads, 0, st, a);
     });
   });
   if (plan && !one) {
-    chunk_sums_kernel<<<(unsigned)ceil_div(cfg->experts, 4), 128, 0, st>>>(a);
-    place_kernel<<<(unsigned)std::max(a.chunks, cfg->align > 1 ? kFillBlocks : 1), kThreads, 0, st>>>(a);
+    ok = ok && launch_after(chunk_sums_kernel, dim3((unsigned)ceil_div(cfg->experts, 4)), 128, 0, st, a) &&
+         launch_after(place_kernel, dim3((unsigned)std::max(a.chunks, cfg->align > 1 ? kFillBlocks : 1)), kThreads, 0, st, a);
   }
-  return cudaGetLastError() == cudaSuccess ? ASGD_OK : ASGD_ECUDA;
+  return ok ? ASGD_OK : ASGD_ECUDA;
 }
 
 extern "C" int asgd_route_grad(const asgd_route_config* cfg, int64_t T, const void* logits, int32_t type, int64_t ld, const int32_t* ids,
@@ -622,11 +629,12 @@ extern "C" int asgd_route_grad(const asgd_route_config* cfg, int64_t T, const vo
   GradArgs a{*cfg, T, ld, ld_out, logits, ids, dweights, dlogits};
   asgd_route_config shape = *cfg;
   shape.groups = shape.groups_kept = 1;                                // groups have no part in the gradient
+  bool ok = false;
   with_shape(shape, [&](auto s, auto l) {
     with_type(type, [&](auto e) {
       constexpr int L = decltype(l)::value;
-      route_grad_kernel<decltype(s)::value, L, decltype(e)><<<(unsigned)ceil_div(T, kThreads / L), kThreads, 0, (cudaStream_t)stream>>>(a);
+      ok = launch_after(route_grad_kernel<decltype(s)::value, L, decltype(e)>, dim3((unsigned)ceil_div(T, kThreads / L)), kThreads, 0, (cudaStream_t)stream, a);
     });
   });
-  return cudaGetLastError() == cudaSuccess ? ASGD_OK : ASGD_ECUDA;
+  return ok ? ASGD_OK : ASGD_ECUDA;
 }
