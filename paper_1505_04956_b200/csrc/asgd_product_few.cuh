@@ -3,11 +3,13 @@
 // A tile is 128 columns of C (rows of B, the weights: the MMA's M, one per epilogue thread) by BN rows of C (rows of
 // A, the tokens: the MMA's N).  Few tokens then cost few columns of the tensor core's tile, and a warp writes 32
 // neighbouring numbers of a row of C.  The weights' bytes are the bound; a tile's products alternate between four
-// accumulator stages, so that the copies never wait for the sums.
+// accumulator stages, so that the copies never wait for the sums (256 rows over 64 experts of 2048 x 2048, some 55 of them
+// with rows: 43 us, about 5.5 TB/s of weights; with two stages and two commits a K block 60).
 //
 // With fewer tiles than SMs a cluster of blocks shares a tile: each takes a stretch of the K blocks, leaves its sums in
 // its shared memory (where the ring was), and adds up its share of the tile's rows from all the cluster's, in the
-// blocks' order, so that the result does not depend on timing.
+// blocks' order, so that the result does not depend on timing (5 rows by 4096 x 4096: 8.5 us
+// in clusters of four; an earlier form with a block per tile took 22).
 //
 // Warp roles: 0 issues the TMA loads (128-byte K blocks of both operands, swizzled, through a ring of slots); 1 and 3
 // issue the products, K blocks in turn (a commit holds its thread for several hundred cycles), one commit per K block,

@@ -7,7 +7,8 @@
 // keys, as a rule) is gathered, one key per lane in the experts' order, and ranked by counting.  Where more than 32 keys
 // reach the bound, and where 8 lanes own a token, each lane sorts its keys, and a choice is the largest of the lanes' first
 // ones, a vote for the lane that has it, and a shift of that lane's list.  Only the chosen logits are turned into weights.
-// Instructions and their latency are the bound, not the bytes.
+// Instructions and their latency are the bound, not the bytes: 16384 tokens among 128 experts 14 us (and 7 for the plan),
+// 65536 among 256 in groups 116; each lane's keys sorted instead of pruned took 17 and 180.
 //
 // The plan is a stable counting sort by expert.  A block's tokens are a chunk (of 64 at most); inside a chunk each
 // expert has a 64-bit word with a bit per token that chose it, so an assignment's rank among the chunk's is the
