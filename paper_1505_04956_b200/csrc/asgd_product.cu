@@ -140,11 +140,11 @@ int launch_pair(const asgd_product_args& a, Params p, cudaStream_t st) {
 // Which kernel: the one whose blocks are through first, by the K blocks the busiest of them meets and the time of one.
 // Microseconds of a K block, measured where operands come from L2 (4096 x 4096 x 4096; the pair with a scale per column
 // from weight gradients of 2048 x 2048): tiles of 16, 32, 64 and 128 rows 0.29, 0.31, 0.43 and 0.66, the pair 0.50, with
-// scales per column 0.85; about 1 us a tile for its beginning and end.
+// scales per column 0.80; about 1 us a tile for its beginning and end.
 enum Kernel { FEW16, FEW32, FEW64, FEW128, PAIR };
 Kernel choose(const Params& p) {
   static const int rows_of[5] = {16, 32, 64, 128, kPairRows};
-  const double block_us[5] = {0.29, 0.31, 0.43, 0.66, p.sb_shift ? 0.50 : 0.85};
+  const double block_us[5] = {0.29, 0.31, 0.43, 0.66, p.sb_shift ? 0.50 : 0.80};
   const int groups = max(p.groups, 1);
   const double kblocks = p.inner ? std::ceil((double)p.kblocks / groups) : p.kblocks;
   Kernel best = FEW16;

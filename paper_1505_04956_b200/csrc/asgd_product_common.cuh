@@ -59,6 +59,9 @@ __device__ inline void fence_after() { asm volatile("tcgen05.fence::after_thread
 __device__ inline void copy4(float* dst, const float* src, bool there) {       // asynchronous; zero where not there
   asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(smem_u32(dst)), "l"(src), "r"(there ? 4 : 0) : "memory");
 }
+__device__ inline void copy16(float* dst, const float* src, int bytes) {       // the first `bytes` of 16, zeros for the others
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_u32(dst)), "l"(src), "r"(bytes) : "memory");
+}
 __device__ inline void arrive_after_copies(unsigned long long* bar) {
   asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
 }
@@ -86,6 +89,44 @@ __device__ inline void store_c(void* c, int type, long long at, float v) {
   else if (type == ASGD_BF16) reinterpret_cast<__nv_bfloat16*>(c)[at] = __float2bfloat16_rn(v);
   else reinterpret_cast<__half*>(c)[at] = __float2half_rn(v);
 }
+
+// ---- scales ----
+
+// The scales of kRows rows, K block after K block, brought by a warp: zeros from row `end` on.  Where neighbouring rows'
+// scales are neighbours in memory and start at 16-byte boundaries, a lane takes four at a time; addresses are worked out
+// once a tile.  (One copy and one address per scale held up the products: a gradient of 2048 x 2048 over 16384 rows, with
+// 384 scales a K block, took 125 us.)
+template <int kRows> struct ScaleRows {
+  const float *at, *any;
+  long long part, block;                             // from a lane's copy to its next one, from a K block to the next
+  int left;                                          // rows from the lane's first on
+  bool wide;
+  __device__ __forceinline__ void start(const float* scales, long long row, long long block_, int kb, int first, int end, int lane) {
+    const float* from = scales + first * row + kb * block_;
+    any = scales;
+    block = block_;
+    wide = row == 1 && ((reinterpret_cast<unsigned long long>(from) | (unsigned long long)block * 4) & 15) == 0;
+    const int unit = wide ? 4 : 1;
+    at = from + lane * unit * row;
+    part = 32 * unit * row;
+    left = min(end - first, kRows) - lane * unit;
+  }
+  __device__ __forceinline__ void copy(float* to, int lane) {
+    if (wide) {
+#pragma unroll
+      for (int c = 0; c < kRows; c += 128)
+        if (c + 128 <= kRows || c + 4 * lane < kRows) {
+          const int n = min(max(left - c, 0), 4);
+          copy16(to + c + 4 * lane, n ? at + c / 128 * part : any, 4 * n);
+        }
+    } else {
+#pragma unroll
+      for (int c = 0; c < kRows; c += 32)
+        if (c + 32 <= kRows || c + lane < kRows) copy4(to + c + lane, left > c ? at + c / 32 * part : any, left > c);
+    }
+    at += block;
+  }
+};
 
 // ---- tiles ----
 

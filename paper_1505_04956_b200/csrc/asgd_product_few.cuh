@@ -170,20 +170,16 @@ product_few_kernel(const Params p, const __grid_constant__ CUtensorMap map_u, co
     for (int tile = first; tile < tiles && ok; tile += step) {
       const Tile t = tile_at(tile);
       const float* from = p.sb + (p.inner ? 0 : t.g * p.sb_group);
+      ScaleRows<kU> cols;
+      ScaleRows<BN> rows;
+      cols.start(from + (t.n0 >> p.sb_shift) * p.sb_row, p.sb_shift ? 0 : p.sb_row, p.sb_block, t.kb0, 0, p.sb_shift ? kU : p.N - t.n0, lane);
+      rows.start(p.sa, p.sa_row, p.sa_block, t.kb0, t.m0, t.m_end, lane);
       for (int kb = t.kb0; kb < t.kb1; ++kb, ++it) {
         const unsigned q = it % S;
         if (it >= S && !(ok = __all_sync(kAll, wait(bars + F::SEMPTY + q, (it / S - 1) & 1, p.wait_limit, abort)))) break;
         float* to = scales + q * F::kScales;
-#pragma unroll
-        for (int c = 0; c < kU; c += 32) {
-          const int n = min(t.n0 + c + lane, p.N - 1);
-          copy4(to + BN + c + lane, from + (n >> p.sb_shift) * p.sb_row + kb * p.sb_block, true);
-        }
-#pragma unroll
-        for (int c = 0; c < BN; c += 32) {
-          const int r = t.m0 + c + lane;
-          if (c + lane < BN) copy4(to + c + lane, r < t.m_end ? p.sa + r * p.sa_row + kb * p.sa_block : p.sa, r < t.m_end);
-        }
+        cols.copy(to + BN, lane);
+        rows.copy(to, lane);
         arrive_after_copies(bars + F::SFULL + q);
       }
     }

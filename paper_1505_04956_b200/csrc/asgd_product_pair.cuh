@@ -20,7 +20,9 @@
 // read the rows of A twice and shared memory is then the bound).  8192 x 8192 x 8192: 515 us (2.13 PFLOP/s; 615 us where the
 // power limit holds the clock near 1.4 GHz), 32 groups of 16384 rows by 2744 x 2064: 142 us (184), of which a fifth is rows of
 // tiles that no group fills and a sixth the way of C through shared memory.  With a scale per column the readers' arithmetic
-// is the pace, some 1500 cycles a K block: weight gradients of 16 groups, 16384 rows, 2048 x 2048, 149 us.
+// is the pace, some 1500 cycles a K block (870 without it): weight gradients of 16 groups, 16384 rows, 2048 x 2048, 133 us.
+// C straight from registers, 32 bytes a thread, took 541 us where the way through shared memory took 525 (8192^3), and
+// 166 where that took 149 (weight gradient).
 #pragma once
 
 #include "asgd_product_common.cuh"
@@ -294,24 +296,23 @@ product_pair_kernel(const Params p, const __grid_constant__ CUtensorMap map_a, c
       for (int tile = pair; tile < tiles && ok; tile += pairs) {
         const Tile t = lg.find(p, kPairRows, kPairCols, kPairBand, gs, tile, lane);
         const float* from = p.sb + (p.inner ? 0 : t.g * p.sb_group);
+        ScaleRows<kHalf> rows;
+        ScaleRows<kPairCols> cols;
+        rows.start(p.sa, p.sa_row, p.sa_block, t.kb0, t.m0 + (int)rank * kHalf, t.m_end, lane);
+        if (kColumns) cols.start(from, p.sb_row, p.sb_block, t.kb0, t.n0, p.N, lane);
+        const int n = t.n0 + 128 * lane;             // two blocks of columns
+        const bool there = n < p.N;
+        const float* of_block = there ? from + (n >> 7) * p.sb_row + t.kb0 * p.sb_block : p.sb;
         for (int kb = t.kb0; kb < t.kb1; ++kb, ++it) {
           const unsigned q = it % S;
           if (it >= S && !(ok = __all_sync(kAll, wait(bars + P_SEMPTY + q, (it / S - 1) & 1, p.wait_limit, abort)))) break;
           float* to = scales + q * kScales;
-#pragma unroll
-          for (int c = 0; c < kHalf; c += 32) {
-            const int m = t.m0 + (int)rank * kHalf + c + lane;
-            copy4(to + c + lane, m < t.m_end ? p.sa + m * p.sa_row + kb * p.sa_block : p.sa, m < t.m_end);
-          }
+          rows.copy(to, lane);
           if (kColumns) {
-#pragma unroll
-            for (int c = 0; c < kPairCols; c += 32) {
-              const int n = t.n0 + c + lane;
-              copy4(to + kHalf + c + lane, n < p.N ? from + n * p.sb_row + kb * p.sb_block : p.sb, n < p.N);
-            }
-          } else if (lane < 2) {
-            const int n = t.n0 + 128 * lane;
-            copy4(to + kHalf + lane, n < p.N ? from + (n >> 7) * p.sb_row + kb * p.sb_block : p.sb, n < p.N);
+            cols.copy(to + kHalf, lane);
+          } else {
+            if (lane < 2) copy4(to + kHalf + lane, of_block, there);
+            if (there) of_block += p.sb_block;
           }
           arrive_after_copies(bars + P_SFULL + q);
         }
