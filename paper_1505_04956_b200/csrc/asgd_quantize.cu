@@ -23,6 +23,8 @@ struct Args {
   int per_shift;
   int row_blocks, col_blocks;                        // blocks of 128 along K and along M
   float fmax, inv_fmax;
+  const char *lo, *hi;                               // where x begins and ends
+  int q_wide;                                        // rows of q start at vectors (for rows of x that do not)
 };
 
 template <bool kE5M2> __device__ __forceinline__ unsigned short round2(float x, float y) {
@@ -56,6 +58,50 @@ template <typename T, typename Word, bool kVec> __device__ __forceinline__ Word 
   for (int i = 0; i < V; ++i) if (c + i < K) e[i] = row[c + i];
   return w;
 }
+
+// Rows of 16-bit numbers that do not start at vectors: the two aligned vectors that hold the numbers from column c on, put
+// together.  (8192 rows of 4095 bf16 numbers: 25 us; number by number 56; 4096 numbers at vectors 17.  fp32 numbers are read
+// one by one: 47 us both ways where this took 64.)  Vectors that reach beyond x, at its very ends, are not read.
+__device__ __forceinline__ uint2 join(const uint2& a, const uint2& b, unsigned skip) {      // bytes skip.. of the two
+  const unsigned w0 = skip & 4 ? a.y : a.x, w1 = skip & 4 ? b.x : a.y, w2 = skip & 4 ? b.y : b.x, bits = (skip & 3) * 8;
+  return make_uint2(__funnelshift_r(w0, w1, bits), __funnelshift_r(w1, w2, bits));
+}
+__device__ __forceinline__ uint4 join(const uint4& a, const uint4& b, unsigned skip) {
+  unsigned w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+#pragma unroll
+  for (int i = 0; i < 6; ++i) w[i] = skip & 8 ? w[i + 2] : w[i];
+#pragma unroll
+  for (int i = 0; i < 5; ++i) w[i] = skip & 4 ? w[i + 1] : w[i];
+  const unsigned bits = (skip & 3) * 8;
+  return make_uint4(__funnelshift_r(w[0], w[1], bits), __funnelshift_r(w[1], w[2], bits), __funnelshift_r(w[2], w[3], bits), __funnelshift_r(w[3], w[4], bits));
+}
+template <typename T, typename Word> struct Unaligned {
+  Word a, b;
+  bool ok;
+  __device__ __forceinline__ void start(const Args& p, const T* row, int c, bool there) {
+    const char* at = reinterpret_cast<const char*>(row + c);
+    const unsigned skip = (unsigned)reinterpret_cast<unsigned long long>(at) & (sizeof(Word) - 1);
+    const Word* from = reinterpret_cast<const Word*>(at - skip);
+    ok = there && at - skip >= p.lo && at - skip + (skip ? 2 : 1) * sizeof(Word) <= p.hi;
+    a = b = Word{};
+    if (ok) {
+      a = from[0];
+      if (skip) b = from[1];
+    }
+  }
+  __device__ __forceinline__ Word get(const T* row, int c, int K, bool there) const {
+    constexpr int V = (int)(sizeof(Word) / sizeof(T));
+    if (!there) return Word{};
+    if (!ok) return load<T, Word, false>(row, c, K);
+    Word w = join(a, b, (unsigned)reinterpret_cast<unsigned long long>(row + c) & (sizeof(Word) - 1));
+    if (c + V > K) {
+      T* e = reinterpret_cast<T*>(&w);
+#pragma unroll
+      for (int i = 0; i < V; ++i) if (c + i >= K) e[i] = Elem<T>::from_f(0.f);
+    }
+    return w;
+  }
+};
 template <typename T, typename Word> __device__ __forceinline__ float element(const Word& w, int i) {
   return Elem<T>::to_f(reinterpret_cast<const T*>(&w)[i]);
 }
@@ -92,14 +138,22 @@ template <typename T, bool kVec, bool kE5M2, bool kWeights, int U> __global__ vo
   const T* row = reinterpret_cast<const T*>(a.x) + from * a.ldx;
   const bool whole = kVec && ((int)blockIdx.y + 1) * (U * 32 * V) <= K;
   uint4 raw[U];
+  if constexpr (kVec || sizeof(T) == 4) {
 #pragma unroll
-  for (int u = 0; u < U; ++u) {
-    const int c = c0 + u * 32 * V;
-    raw[u] = make_uint4(0, 0, 0, 0);
-    if (from >= 0) {
-      if (whole) raw[u] = *reinterpret_cast<const uint4*>(row + c);
-      else if (c < K) raw[u] = load<T, uint4, kVec>(row, c, K);
+    for (int u = 0; u < U; ++u) {
+      const int c = c0 + u * 32 * V;
+      raw[u] = make_uint4(0, 0, 0, 0);
+      if (from >= 0) {
+        if (whole) raw[u] = *reinterpret_cast<const uint4*>(row + c);
+        else if (c < K) raw[u] = load<T, uint4, kVec>(row, c, K);
+      }
     }
+  } else {
+    Unaligned<T, uint4> two[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) two[u].start(p, row, c0 + u * 32 * V, from >= 0 && c0 + u * 32 * V < K);
+#pragma unroll
+    for (int u = 0; u < U; ++u) raw[u] = two[u].get(row, c0 + u * 32 * V, K, from >= 0 && c0 + u * 32 * V < K);
   }
   float m[U];
 #pragma unroll
@@ -142,7 +196,7 @@ template <typename T, bool kVec, bool kE5M2, bool kWeights, int U> __global__ vo
     for (int i = 0; i < V; ++i) v[i] = (kWeights ? __fmul_rn(v[i], factor) : v[i]) * inv;
 #pragma unroll
     for (int i = 0; i < V; i += 4) w[i / 4] = round4<kE5M2>(v[i], v[i + 1], v[i + 2], v[i + 3]);
-    if (whole || (kVec && c + V <= K)) {
+    if (whole || ((kVec || p.q_wide) && c + V <= K)) {
       if constexpr (V == 8) *reinterpret_cast<uint2*>(q + c) = make_uint2(w[0], w[1]);
       else *reinterpret_cast<unsigned*>(q + c) = w[0];
     } else {
@@ -181,6 +235,7 @@ __device__ __forceinline__ float4 max4(float4 a, float4 b) { return make_float4(
 template <typename T, bool kVec, bool kE5M2, bool kWeights> __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 3 : 2) tile_kernel(const Args p) {
   wait_for_stream();
   using Word = typename std::conditional<sizeof(T) == 4, uint4, uint2>::type;      // 4 numbers
+  constexpr int kAtOnce = 8;                                    // rows in flight where they do not start at vectors (four: 50 us, eight: 48)
   __shared__ __align__(16) unsigned char tile[128 * 128];       // [column][row], 16-byte pieces exchanged by column / 4
   __shared__ float4 col_max[kWarps][32];
   __shared__ float whole_max[kWarps];
@@ -203,12 +258,25 @@ template <typename T, bool kVec, bool kE5M2, bool kWeights> __global__ void __la
       raw[i] = Word{};
       if ((there >> i) & 1u) raw[i] = *reinterpret_cast<const Word*>(x + t * a.ldx + c);
     }
-  } else {
+  } else if constexpr (kVec || sizeof(T) == 4) {
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
       const long long t = __shfl_sync(kAll, from, i);
       raw[i] = Word{};
       if (((there >> i) & 1u) && c < K) raw[i] = load<T, Word, kVec>(x + t * a.ldx, c, K);
+    }
+  } else {
+#pragma unroll
+    for (int i0 = 0; i0 < 16; i0 += kAtOnce) {
+      Unaligned<T, Word> two[kAtOnce];
+      const T* row[kAtOnce];
+#pragma unroll
+      for (int i = 0; i < kAtOnce; ++i) {
+        row[i] = x + __shfl_sync(kAll, from, i0 + i) * a.ldx;
+        two[i].start(p, row[i], c, ((there >> (i0 + i)) & 1u) && c < K);
+      }
+#pragma unroll
+      for (int i = 0; i < kAtOnce; ++i) raw[i0 + i] = two[i].get(row[i], c, K, ((there >> (i0 + i)) & 1u) && c < K);
     }
   }
   float factor[kWeights ? 16 : 1];
@@ -267,7 +335,7 @@ template <typename T, bool kVec, bool kE5M2, bool kWeights> __global__ void __la
       const float inv = __shfl_sync(kAll, mine, 2 * i);
       const unsigned w = round4<kE5M2>(value(i, 0) * inv, value(i, 1) * inv, value(i, 2) * inv, value(i, 3) * inv);
       if (r0 + i < a.M) {
-        if (kVec && c + 4 <= K) *reinterpret_cast<unsigned*>(q) = w;
+        if ((kVec || p.q_wide) && c + 4 <= K) *reinterpret_cast<unsigned*>(q) = w;
         else
 #pragma unroll
           for (int j = 0; j < 4; ++j) if (c + j < K) q[j] = (unsigned char)(w >> (8 * j));
@@ -342,17 +410,22 @@ template <typename T, int U> bool launch_rows(const Args& p, bool vec, cudaStrea
   const dim3 grid((unsigned)ceil_div(p.a.M, kWarps), (unsigned)ceil_div(p.a.K, 32 * kPer16<T> * U));
   bool ok = false;
   with_flags(vec, p.a.q_type == ASGD_E5M2, p.a.weights != nullptr, [&](auto kv, auto ke, auto kw) {
-    ok = launch_after(rows_kernel<T, decltype(kv)::value, decltype(ke)::value, decltype(kw)::value, U>, grid, kThreads, 0, st, p);
+    if constexpr (decltype(kv)::value || U == 4)         // eight pieces for whole vectors alone
+      ok = launch_after(rows_kernel<T, decltype(kv)::value, decltype(ke)::value, decltype(kw)::value, U>, grid, kThreads, 0, st, p);
   });
   return ok;
 }
-template <typename T> bool launch(const Args& p, cudaStream_t st) {
-  const asgd_quantize_args& a = p.a;
+template <typename T> bool launch(const Args& given, cudaStream_t st) {
+  const asgd_quantize_args& a = given.a;
   const bool e5m2 = a.q_type == ASGD_E5M2, w = a.weights != nullptr;
   const bool rows_only = !a.qt && !a.square;
   const int V = rows_only ? kPer16<T> : 4;
   // vector accesses need every row of the input and of the result to start at a whole vector
-  const bool vec = aligned(a.x, V * sizeof(T)) && a.ldx % V == 0 && (!a.q || (aligned(a.q, V) && a.ldq % V == 0));
+  const bool q_wide = !a.q || (aligned(a.q, V) && a.ldq % V == 0), vec = aligned(a.x, V * sizeof(T)) && a.ldx % V == 0 && q_wide;
+  Args p = given;
+  p.q_wide = q_wide;
+  p.lo = reinterpret_cast<const char*>(a.x);
+  p.hi = a.rows_x > 0 ? p.lo + ((a.rows_x - 1) * a.ldx + a.K) * (long long)sizeof(T) : p.lo;
   if (rows_only) {
     // eight pieces per lane for gathered rows, which L2 feeds faster than they are rounded (8192 x 4096 bf16 numbers four
     // times: 53 us, with four pieces 57), where they leave enough warps, a row is that long and pieces are loaded whole; rows

@@ -365,6 +365,22 @@ def test_quantize_strides_and_order():
         pkg.asgd_quantize(big.t())
 
 
+@pytest.mark.parametrize("dtype", [F32, BF, F16])
+@pytest.mark.parametrize("K", [1, 7, 130, 1031])
+def test_quantize_rows_that_start_anywhere(K, dtype):
+    M, per = 37, 2
+    big = _numbers(1, 8 + M * K, dtype, K)[0]
+    source = torch.randperm(M * per, generator=_gen(K), device="cuda").to(torch.int32)
+    wide = torch.zeros(M, -(-K // 16) * 16, dtype=dtype, device="cuda")
+    for first in (0, 1, 2, 3, 5, 8):
+        x = big[first:first + M * K].view(M, K)          # up to the storage's very end with first = 8
+        wide[:, :K] = x
+        for kw in (dict(form="both"), dict(form="blocks both"), dict(source=source, per_token=per), dict(form="both", source=source, per_token=per)):
+            for got, want in zip(pkg.asgd_quantize(x, **kw), pkg.asgd_quantize(wide[:, :K], **kw)):
+                one = got.element_size() == 1
+                assert torch.equal(got.view(torch.uint8) if one else got, want.view(torch.uint8) if one else want)
+
+
 def test_quantize_infinity_nan_and_tiny():
     x = torch.ones(4, 256, device="cuda")
     x[0, 3] = math.inf
