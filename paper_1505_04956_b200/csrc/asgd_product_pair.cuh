@@ -20,7 +20,7 @@
 // read the rows of A twice and shared memory is then the bound).  8192 x 8192 x 8192: 515 us (2.13 PFLOP/s; 615 us where the
 // power limit holds the clock near 1.4 GHz), 32 groups of 16384 rows by 2744 x 2064: 142 us (184), of which a fifth is rows of
 // tiles that no group fills and a sixth the way of C through shared memory.  With a scale per column the readers' arithmetic
-// is the pace, some 1500 cycles a K block (870 without it): weight gradients of 16 groups, 16384 rows, 2048 x 2048, 133 us.
+// is the pace, some 1500 cycles a K block (870 without it): weight gradients of 16 groups, 16384 rows, 2048 x 2048, 131 us.
 // C straight from registers, 32 bytes a thread, took 541 us where the way through shared memory took 525 (8192^3), and
 // 166 where that took 149 (weight gradient).
 #pragma once
@@ -371,21 +371,27 @@ product_pair_kernel(const Params p, const __grid_constant__ CUtensorMap map_a, c
           // fragments of 32 rows x 16 columns: a thread needs 32 columns' scales of a K block where a row per thread
           // would need 128 (every broadcast read of 16 bytes takes four cycles of the shared memory's path)
           float v[2][16], a0[4];
+          float2 f[2][2];                            // the columns' scales, read one step ahead
+          const float* cols = of_cols + half * 128 + 2 * (lane & 3);
+          f[0][0] = *reinterpret_cast<const float2*>(cols);
+          f[0][1] = *reinterpret_cast<const float2*>(cols + 8);
           tmem_load_fragments(from, v[0]);
 #pragma unroll
           for (int i = 0; i < 4; ++i) a0[i] = of_rows[(lane >> 2) + 8 * i];
 #pragma unroll
           for (int j = 0; j < 8; ++j) {
             tmem_wait();
-            if (j < 7) tmem_load_fragments(from + (j + 1) * 16, v[(j + 1) & 1]);
-            else hand_back();
+            if (j < 7) {
+              tmem_load_fragments(from + (j + 1) * 16, v[(j + 1) & 1]);
+              f[(j + 1) & 1][0] = *reinterpret_cast<const float2*>(cols + (j + 1) * 16);
+              f[(j + 1) & 1][1] = *reinterpret_cast<const float2*>(cols + (j + 1) * 16 + 8);
+            } else hand_back();
 #pragma unroll
             for (int g = 0; g < 2; ++g) {
-              const float2 f = *reinterpret_cast<const float2*>(of_cols + half * 128 + 2 * (lane & 3) + j * 16 + g * 8);
 #pragma unroll
               for (int i = 0; i < 4; ++i) {
                 const int e = (g * 4 + i) * 2;
-                fma2(acc[j * 16 + e], acc[j * 16 + e + 1], v[j & 1][e], v[j & 1][e + 1], mul2(pair_of(a0[i], a0[i]), pair_of(f.x, f.y)));
+                fma2(acc[j * 16 + e], acc[j * 16 + e + 1], v[j & 1][e], v[j & 1][e + 1], mul2(pair_of(a0[i], a0[i]), pair_of(f[j & 1][g].x, f[j & 1][g].y)));
               }
             }
           }
