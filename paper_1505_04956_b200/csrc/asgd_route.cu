@@ -8,7 +8,7 @@
 // reach the bound, and where 8 lanes own a token, each lane sorts its keys, and a choice is the largest of the lanes' first
 // ones, a vote for the lane that has it, and a shift of that lane's list.  Only the chosen logits are turned into weights.
 // Instructions and their latency are the bound, not the bytes: 16384 tokens among 128 experts 14 us (and 7 for the plan),
-// 65536 among 256 in groups 116; each lane's keys sorted instead of pruned took 17 and 180.
+// 65536 among 256 in groups 115; each lane's keys sorted instead of pruned took 17 and 180.
 //
 // The plan is a stable counting sort by expert.  A block's tokens are a chunk (of 64 at most); inside a chunk each
 // expert has a 64-bit word with a bit per token that chose it, so an assignment's rank among the chunk's is the
@@ -545,14 +545,24 @@ bool config_ok(const asgd_route_config* c) {
 bool config_supported(const asgd_route_config* c) {
   return c->experts <= ASGD_MAX_EXPERTS && c->groups <= ASGD_MAX_EXPERT_GROUPS && c->top_k <= ASGD_MAX_TOP_K;
 }
-// Tokens of a chunk: one block where it does all (few tokens, little to fill); else as many per warp (eight warps) as keep
-// some 32 warps on every SM, so that short batches spread over the GPU.
+// Tokens of a chunk: one block where it does all (few tokens, little to fill).  Else the number with the shortest way
+// through: the waves of blocks (an SM holds four, of the widest instances two), by a block's turns of its eight warps and
+// some one and a half more for its beginning and end; of equal ones the smallest, so that short batches spread over the GPU.
+// (41270 tokens among 256 experts in groups: 74 us in chunks of 40, 90 in chunks of 64, which leave a half-empty wave.)
 int chunk_of(const asgd_route_config* c, long long T) {
   if (T <= kMaxChunk && (long long)c->experts * (c->align - 1) <= 4096) return kMaxChunk;
-  long long per_warp = ceil_div(T, (long long)kSMs * 32);
-  int n = 1;
-  while (n < per_warp && n < kMaxChunk / kWarps) n *= 2;
-  return n * kWarps;
+  int at_once = 0;
+  long long blocks = 0, least = 0;
+  with_shape(*c, [&](auto s, auto l) {
+    at_once = kWarps * (32 / decltype(l)::value);
+    blocks = kSMs * (decltype(s)::value <= 8 ? 4 : 2);
+  });
+  int best = 0;
+  for (int n = kWarps; n <= kMaxChunk; n += n < at_once ? n : at_once) {
+    const long long cost = ceil_div(ceil_div(T, n), blocks) * (2 * ceil_div(n, at_once) + 3);
+    if (!best || cost < least) { best = n; least = cost; }
+  }
+  return best;
 }
 bool one_block(const asgd_route_config* c, long long T) { return chunk_of(c, T) == kMaxChunk && T <= kMaxChunk; }
 // (a plan that takes more than one block has two chunks at least, the second one empty if need be)

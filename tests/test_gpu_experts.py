@@ -226,6 +226,22 @@ def test_route_plan_over_many_chunks():
     assert torch.equal(source.long(), want)
 
 
+@pytest.mark.parametrize("T, E, K", [(41273, 70, 2), (41273, 24, 2), (18969, 300, 1)])
+def test_route_plan_over_more_blocks_than_run_at_once(T, E, K):
+    x = torch.rand(T, E, generator=_gen(T + E), device="cuda").argsort(dim=1).float()          # a permutation a row: no ties
+    ids, w, offsets, rows, source = pkg.asgd_route(x, K, align=8)
+    assert torch.equal(ids.long(), torch.topk(x, K).indices)
+    flat = ids.reshape(-1).long()
+    pad = (torch.bincount(flat, minlength=E) + 7) // 8 * 8
+    assert torch.equal(offsets.long(), torch.cat([torch.zeros(1, dtype=torch.long, device="cuda"), pad.cumsum(0)]))
+    order = torch.sort(flat, stable=True).indices
+    want = torch.full((source.numel(),), -1, dtype=torch.long, device="cuda")
+    first = torch.cat([torch.zeros(1, dtype=torch.long, device="cuda"), torch.bincount(flat, minlength=E).cumsum(0)])
+    want[offsets[flat[order]].long() + torch.arange(T * K, device="cuda") - first[flat[order]]] = order
+    assert torch.equal(source.long(), want)
+    assert torch.equal(source.long()[rows.reshape(-1).long()], torch.arange(T * K, device="cuda"))
+
+
 @pytest.mark.parametrize("T, E, top_k, score, dtype, renormalise", [
     (1, 4, 2, "softmax", F32, True), (67, 60, 6, "sigmoid", F32, True), (33, 129, 8, "softmax", BF, True), (33, 129, 8, "softmax", F32, False),
     (20, 256, 1, "sigmoid", F16, False), (9, 1000, 32, "softmax", F32, True), (12, 32, 32, "softmax", F32, True)])
