@@ -231,8 +231,10 @@ template <> struct ColMax<__nv_bfloat16> : ColMax16<__nv_bfloat16, __nv_bfloat16
 __device__ __forceinline__ float4 max4(float4 a, float4 b) { return make_float4(fmaxf(a.x, b.x), fmaxf(a.y, b.y), fmaxf(a.z, b.z), fmaxf(a.w, b.w)); }
 
 // The numbers stay in registers as they came (16-bit ones packed), and are taken apart once for the rows' rounding and
-// once for the columns': more blocks per SM are worth more than the second unpacking (loads' latency is the bound).
-template <typename T, bool kVec, bool kE5M2, bool kWeights> __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 3 : 2) tile_kernel(const Args p) {
+// once for the columns': more blocks per SM are worth more than the second unpacking (loads' latency is the bound).  Blocks
+// per SM: as many as spill nothing to speak of (8192 x 4096 both ways: bf16 30 us with four, 33 with three; fp32 42 with two,
+// 45 with three).
+template <typename T, bool kVec, bool kE5M2, bool kWeights> __global__ void __launch_bounds__(kThreads, sizeof(T) == 4 ? 2 : kVec && !kWeights ? 4 : 3) tile_kernel(const Args p) {
   wait_for_stream();
   using Word = typename std::conditional<sizeof(T) == 4, uint4, uint2>::type;      // 4 numbers
   constexpr int kAtOnce = 8;                                    // rows in flight where they do not start at vectors (four: 50 us, eight: 48)
