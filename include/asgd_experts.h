@@ -102,7 +102,8 @@ int asgd_route_grad(const asgd_route_config *cfg, int64_t T, const void *logits,
  *   qt       [K][ldqt] out or NULL: the transposed matrix rounded in its own blocks, 128 neighbours along M, with
  *            scales scale_t[c * scale_t_row + b * scale_t_block], b < ceil(M / 128); with `square` the transpose of q,
  *            whose scales are those of q (scale_t is not used)
- * Nothing is written between K and ldq.  ld* >= the row's length.
+ * Nothing is written between K and ldq.  ld* >= the row's length.  K above 2^25 - 512 without qt
+ * and square, M above 2^23 - 128 with either, are ASGD_EUNSUPPORTED.
  */
 typedef struct asgd_quantize_args {
   int64_t M, K;            /* rows and columns of the result; M <= 2^31 - 1, K <= 2^31 - 1                  */
@@ -170,6 +171,7 @@ int asgd_product(const asgd_product_args *args, void *stream);
  * factors 1 without weights; rows outside 0..R-1 take no part), y and z of `type`.
  * Gradient: dz[rows[t][j]] = weights[t][j] * dy[t] (dz may be NULL), dweights[t][j] = <dy[t], z[rows[t][j]]> (may be
  * NULL), 0 where the row takes no part; the rows of dz whose source (see asgd_route; may be NULL) is negative become 0.
+ * D above 2^22 may be ASGD_EUNSUPPORTED.
  */
 int asgd_combine(int64_t T, int64_t D, int32_t top_k, const void *z, int32_t type, int64_t R, int64_t ldz,
                  const int32_t *rows, const float *weights, void *y, int64_t ldy, void *stream);

@@ -3,7 +3,7 @@
 // HBM is the bound: every row of z is read once (and written once in the gradient), a token's row of y or dy once.  In
 // the sum a thread block takes a stretch of a token's row, a thread 16-byte pieces of it, and the rows of z are met in
 // ascending place; in the gradient a warp takes an assignment.  Every sum has one order.  8192 tokens of four rows of 4096 bf16 numbers:
-// 61 us, 5.5 TB/s; with the numbers unpacked as they came, eight rows always, 153.
+// 55 us, 6.1 TB/s; with the numbers unpacked as they came, eight rows always, 153.
 #include "asgd_experts_common.cuh"
 
 #include <algorithm>
@@ -13,7 +13,6 @@ namespace {
 
 using namespace asgd::experts;
 
-constexpr int kThreads = 128;                              // of the sum
 constexpr int kGradThreads = 256;
 constexpr int kMaxRows = 8;                                // rows of z a thread has in flight
 
@@ -54,8 +53,15 @@ __device__ __forceinline__ void assignment(const Args& a, long long t, int j, in
   w = a.weights ? a.weights[t * a.top_k + j] : 1.f;
 }
 
-// N: rows met at a time; U: pieces per thread, blockDim apart (what is in flight is N * U pieces)
-template <typename T, bool kVec, int N, int U> __global__ void __launch_bounds__(kThreads) combine_kernel(const Args a) {
+// N: rows met at a time; U: pieces per thread, blockDim apart (what is in flight is N * U pieces).  Small blocks, that are
+// through soon and make room for the next ones' loads: 64 threads with four pieces each (32 with eight, where eight rows
+// are met; 32 narrow ones).  8192 tokens, 4096 bf16 numbers, of 1, 2, 4 and 8 rows: 26, 35, 55 and 92 us; with 128 threads
+// and eight pieces 31, 41, 61 and 103; 32 threads with four pieces 36, 36, 70, for then blocks come up too slowly.
+template <bool kVec, int N> struct Shape {
+  static constexpr int kThreads = kVec && N == 8 ? 32 : 64, U = (kVec ? (N == 8 ? 8 : 4) : 32) / N;
+};
+template <typename T, bool kVec, int N> __global__ void __launch_bounds__(Shape<kVec, N>::kThreads) combine_kernel(const Args a) {
+  constexpr int kThreads = Shape<kVec, N>::kThreads, U = Shape<kVec, N>::U;
   wait_for_stream();
   using P = Piece<T, kVec>;
   const long long t = blockIdx.x, c0 = ((long long)blockIdx.y * U * kThreads + threadIdx.x) * P::kN;
@@ -193,10 +199,10 @@ extern "C" int asgd_combine(int64_t T, int64_t D, int32_t top_k, const void* z, 
     const bool vec = whole<E>(z, ldz) && whole<E>(y, ldy) && D % kPer16<E> == 0;
     with_rows(top_k, vec, [&](auto v, auto n) {
       constexpr bool kVec = decltype(v)::value;
-      constexpr int N = decltype(n)::value, U = (kVec ? 8 : 32) / N;
-      const long long stretches = ceil_div(D, (long long)kThreads * U * (kVec ? kPer16<E> : 1));
+      constexpr int N = decltype(n)::value, kThreads = Shape<kVec, N>::kThreads;
+      const long long stretches = ceil_div(D, (long long)kThreads * Shape<kVec, N>::U * (kVec ? kPer16<E> : 1));
       if (stretches > 65535) { rc = ASGD_EUNSUPPORTED; return; }
-      if (!launch_after(combine_kernel<E, kVec, N, U>, dim3((unsigned)T, (unsigned)stretches), kThreads, 0, (cudaStream_t)stream, a)) rc = ASGD_ECUDA;
+      if (!launch_after(combine_kernel<E, kVec, N>, dim3((unsigned)T, (unsigned)stretches), kThreads, 0, (cudaStream_t)stream, a)) rc = ASGD_ECUDA;
     });
   });
   return rc;
