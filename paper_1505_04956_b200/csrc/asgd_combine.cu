@@ -13,7 +13,8 @@ namespace {
 
 using namespace asgd::experts;
 
-constexpr int kGradThreads = 256;
+constexpr int kGradThreads = 128, kGradWarps = kGradThreads / 32;
+constexpr int kFillRows = 4;                               // grouped rows a warp looks at for those of nothing
 constexpr int kMaxRows = 8;                                // rows of z a thread has in flight
 
 struct Args {
@@ -105,23 +106,25 @@ template <typename T, bool kVec, int N> __global__ void __launch_bounds__(Shape<
 // W warps take an assignment (one where there are many): its row of z and its token's row of dy, U pieces of each in
 // flight per thread.  A token's assignments are neighbours, so its row of dy comes from HBM once and from the caches after
 // that; what a thread holds is small, and it is the bytes in flight that the rate needs (a token per block with all its rows
-// in registers: 91 us where this takes 67, on 5003 x 6 rows of 2560 bf16 numbers).  The blocks behind the assignments' take
-// 128 grouped rows each; those of nothing become zeros.
-template <typename T, bool kVec, int W> __global__ void __launch_bounds__(kGradThreads, kVec ? 4 : 3) combine_grad_kernel(const Args a, long long fill_from) {
+// in registers: 91 us where this takes 54, 6.2 TB/s, on 5003 x 6 rows of 2560 bf16 numbers).  The warps behind the assignments'
+// take four grouped rows each, for those of nothing become zeros: a block with 128 rows, one after the other, was a tail of
+// some 12 us in every call (64 assignments 10 us, now 2.3).
+template <typename T, bool kVec, int W> __global__ void __launch_bounds__(kGradThreads, kVec ? 10 : 6) combine_grad_kernel(const Args a, long long fill_from) {
   wait_for_stream();
   using P = Piece<T, kVec>;
-  constexpr int U = kVec ? 4 : 8, kAcross = 32 * W;
+  constexpr int U = kVec ? 2 : 8, kAcross = 32 * W;
   T* dz = reinterpret_cast<T*>(a.dz);
   if (blockIdx.x >= fill_from) {
-    const long long r0 = ((long long)blockIdx.x - fill_from) * 128;
-    for (int q = 0; q < 128; ++q) {
-      const long long r = r0 + q;
-      if (r >= a.R || a.source[r] >= 0) continue;
-      for (long long c = (long long)threadIdx.x * P::kN; c < a.D; c += (long long)kGradThreads * P::kN) P::store(dz + r * a.ld_dz + c, typename P::Word{});
+    const int lane = threadIdx.x & 31;
+    const long long r0 = (((long long)blockIdx.x - fill_from) * kGradWarps + (threadIdx.x >> 5)) * kFillRows, mine = r0 + lane;
+    unsigned nothing = __ballot_sync(kAll, lane < kFillRows && mine < a.R && a.source[mine] < 0);
+    for (; nothing; nothing &= nothing - 1) {
+      T* out = dz + (r0 + __ffs(nothing) - 1) * a.ld_dz;
+      for (long long c = (long long)lane * P::kN; c < a.D; c += 32 * P::kN) P::store(out + c, typename P::Word{});
     }
     return;
   }
-  __shared__ float part[kGradThreads / 32];
+  __shared__ float part[kGradWarps];
   const int of = threadIdx.x / kAcross, at = threadIdx.x % kAcross;      // assignment of the block, thread of the assignment
   const long long i = (long long)blockIdx.x * (kGradThreads / kAcross) + of, t = i / a.top_k;
   int row = -1;
@@ -222,7 +225,7 @@ extern "C" int asgd_combine_grad(int64_t T, int64_t D, int32_t top_k, const void
   // a warp per assignment where that keeps the SMs full, else four
   const long long assignments = T * top_k;
   const int warps = assignments >= kSMs * 32 ? 1 : 4;
-  const long long fill_from = ceil_div(assignments * warps, kGradThreads / 32), blocks = fill_from + (dz && source ? ceil_div(R, 128) : 0);
+  const long long fill_from = ceil_div(assignments * warps, kGradWarps), blocks = fill_from + (dz && source ? ceil_div(R, kGradWarps * kFillRows) : 0);
   if (blocks > 0x7fffffffll) return ASGD_EUNSUPPORTED;
   if (blocks == 0) return ASGD_OK;
   bool ok = false;
