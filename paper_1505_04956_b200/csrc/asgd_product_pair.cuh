@@ -148,10 +148,16 @@ template <typename T, bool kFragments> __device__ __forceinline__ void store_row
   constexpr int per = 64 / (int)sizeof(T), part = 16 / (int)sizeof(T);         // numbers of a row in a piece, in a part
   T* corner = c + o.at;
   const bool whole = ((reinterpret_cast<unsigned long long>(corner) | ((unsigned long long)o.ldc * sizeof(T))) & 15) == 0;
+  // Rows that the warp writes itself add no groups of copies, so the count below says nothing of the tile before: all of
+  // its copies have read the stage first.
+  if (!o.by_map) {
+    if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+    __syncwarp();
+  }
 #pragma unroll
   for (int first = 0; first < 128; first += per) {
     unsigned char* piece = stage + first / per % kStagePieces * kPieceBytes;
-    // the copy before last, out of the same place, has read it
+    // the copy before last, out of the same place, has read it (a piece that is copied is a group of its own)
     if (lane == 0) asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(kStagePieces - 1) : "memory");
     __syncwarp();
     if constexpr (!kFragments) {
