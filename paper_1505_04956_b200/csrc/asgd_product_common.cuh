@@ -97,13 +97,13 @@ __device__ inline void store_c(void* c, int type, long long at, float v) {
 // once a tile.  (One copy and one address per scale held up the products: a gradient of 2048 x 2048 over 16384 rows, with
 // 384 scales a K block, took 125 us.)
 template <int kRows> struct ScaleRows {
-  const float *at, *any;
+  const float *at, *any;                             // any: for copies of no bytes, which need an aligned address too
   long long part, block;                             // from a lane's copy to its next one, from a K block to the next
   int left;                                          // rows from the lane's first on
   bool wide;
   __device__ __forceinline__ void start(const float* scales, long long row, long long block_, int kb, int first, int end, int lane) {
     const float* from = scales + first * row + kb * block_;
-    any = scales;
+    any = reinterpret_cast<const float*>(reinterpret_cast<unsigned long long>(scales) & ~15ull);
     block = block_;
     wide = row == 1 && ((reinterpret_cast<unsigned long long>(from) | (unsigned long long)block * 4) & 15) == 0;
     const int unit = wide ? 4 : 1;

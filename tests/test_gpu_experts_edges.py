@@ -37,3 +37,32 @@ def test_inner_groups_without_rows_between_full_ones(G, R, M, N, out, fa):
                 _check_product(c[g], a64[:, s], b64[:, s], at[g + 1] - at[g], out)
         assert torch.equal(c, first)
     pkg.asgd_experts_sync()
+
+
+# ---------------------------------------------------------------------------------------------------------------
+# products: scales and groups that start anywhere
+# ---------------------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("M, N, K, G", [(37, 136, 512, 3), (203, 264, 512, 4), (1900, 520, 256, 3), (2700, 1100, 1024, 3)])
+@pytest.mark.parametrize("first", [0, 1, 2, 3])
+def test_scales_and_groups_that_start_anywhere(M, N, K, G, first):
+    # the scales lie `first` numbers behind a 16-byte boundary, block after block a whole number of 16 bytes apart, and the
+    # groups start at rows of every remainder by 4: a tile's scales are aligned where the array of them is not
+    a, sa = _operand(M, K, E4, 1)
+    b, sb = _operand(N, K, E4, 2, True, (G,))
+    store = torch.zeros(K // 128 * 4096 + 8, device="cuda")
+    moved = store[first:first + K // 128 * 4096].view(K // 128, 4096)[:, :M].t()
+    moved.copy_(sa)
+    assert moved.data_ptr() % 16 == 4 * first
+    for start in range(4):
+        at = torch.linspace(start, M, G + 1).to(torch.int32)
+        at[1:-1] = at[1:-1] // 4 * 4 + (4 - first) % 4
+        offsets = at.cuda()
+        got = pkg.asgd_product(a, moved, b, sb, offsets=offsets, out=torch.zeros(M, N, device="cuda"))
+        want = pkg.asgd_product(a, sa, b, sb, offsets=offsets, out=torch.zeros(M, N, device="cuda"))
+        assert torch.equal(got, want)
+        a64, b64, rows = _values64(a, sa), _values64(b, sb), at.tolist()
+        for g in range(G):
+            s = slice(rows[g], rows[g + 1])
+            _check_product(got[s], a64[s], b64[g], K, F32)
+    pkg.asgd_experts_sync()
