@@ -36,6 +36,8 @@ enum { ASGD_SCORE_SOFTMAX = 0, ASGD_SCORE_SIGMOID = 1 };
 #define ASGD_MAX_EXPERTS 1024
 #define ASGD_MAX_EXPERT_GROUPS 32
 #define ASGD_MAX_TOP_K 32
+#define ASGD_PRODUCT_MAX 2147483392ll  /* 2^31 - 256: rows, columns and inner numbers of a product              */
+#define ASGD_QUANTIZE_MAX 2147418112ll /* 2^31 - 65536: numbers of a row that is rounded                        */
 #define ASGD_BLOCK 128 /* numbers that share a scale, along a row (and rows that do, in a 128 x 128 block) */
 
 /*
@@ -106,7 +108,7 @@ int asgd_route_grad(const asgd_route_config *cfg, int64_t T, const void *logits,
  * and square, M above 2^23 - 128 with either, are ASGD_EUNSUPPORTED.
  */
 typedef struct asgd_quantize_args {
-  int64_t M, K;            /* rows and columns of the result; M <= 2^31 - 1, K <= 2^31 - 1                  */
+  int64_t M, K;            /* rows and columns of the result; M <= 2^31 - 1, K <= ASGD_QUANTIZE_MAX         */
   const void *x;           /* [rows_x][ldx] of x_type, or of M rows without `source`                        */
   int64_t ldx;
   int64_t rows_x;          /* rows of x (equal to M without source)                                         */
@@ -146,7 +148,7 @@ int asgd_quantize(const asgd_quantize_args *args, void *stream);
  * or fp16, aligned to its element.  ASGD_EINVAL otherwise.
  */
 typedef struct asgd_product_args {
-  int64_t M, N, K;         /* each <= 2^31 - 1 */
+  int64_t M, N, K;         /* each <= ASGD_PRODUCT_MAX (ASGD_EUNSUPPORTED above) */
   const void *a;
   int64_t lda;
   const float *a_scale;

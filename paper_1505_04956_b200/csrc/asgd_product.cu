@@ -49,6 +49,8 @@ bool encode(CUtensorMap* map, const void* base, long long cols, long long rows, 
   return encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, CU_TENSOR_MAP_SWIZZLE_128B, base, cols, rows, outer, ld, outer_stride, kKB, box_rows);
 }
 
+constexpr long long kMostTiles = 0x7fffffffll - 2 * kSMs;    // a block's next tile number stays inside 32 bits
+
 // the most tiles of bm x bn there can be: what the offsets say is known on the device alone
 long long most_tiles(const Params& p, int bm, int bn) {
   const long long rows = p.inner ? ceil_div(p.M, bm) * p.groups : ceil_div(p.M, bm) + p.groups;
@@ -79,7 +81,7 @@ template <int BN, bool kSplit> int launch_few(const asgd_product_args& a, Params
   p.idesc = instruction(a.b_type, a.a_type, BN, kU);
   p.tiles_n = (int)ceil_div(p.N, kU);
   const long long most = most_tiles(p, BN, kU);
-  if (most > 0x7fffffffll) return ASGD_EUNSUPPORTED;
+  if (most > kMostTiles) return ASGD_EUNSUPPORTED;
   static std::atomic<unsigned long long> done{0};
   if (!allow_smem(product_few_kernel<BN, kSplit>, Few<BN>::kSmem, done)) return ASGD_ECUDA;
   cudaLaunchConfig_t cfg{};
@@ -121,7 +123,7 @@ int launch_pair(const asgd_product_args& a, Params p, cudaStream_t st) {
   p.idesc = instruction(a.a_type, a.b_type, kPairCols, kPairRows);
   p.tiles_n = (int)ceil_div(p.N, kPairCols);
   const long long most = most_tiles(p, kPairRows, kPairCols);
-  if (most > 0x7fffffffll) return ASGD_EUNSUPPORTED;
+  if (most > kMostTiles) return ASGD_EUNSUPPORTED;
   // C by tensor map where its rows (and groups) start at 16-byte boundaries
   CUtensorMap map_c{};
   const long long size = (long long)type_bytes(a.c_type), outer = p.inner ? p.groups : 1;
@@ -172,7 +174,8 @@ extern "C" int asgd_product(const asgd_product_args* args, void* stream) {
   if (!eight_bit_type(a.a_type) || !eight_bit_type(a.b_type) || !float_type(a.c_type)) return ASGD_EINVAL;
   if ((a.groups > 0) != (a.offsets != nullptr) || (a.inner && !a.groups)) return ASGD_EINVAL;
   if (a.lda < a.K || a.ldb < a.K || a.ldc < a.N || (a.K > 0 && (a.lda % 16 || a.ldb % 16))) return ASGD_EINVAL;
-  if (a.M > 0x7fffffffll || a.N > 0x7fffffffll || a.K > 0x7fffff00ll || a.groups > ASGD_MAX_EXPERTS) return ASGD_EUNSUPPORTED;
+  // row, column and inner numbers of whole tiles (256 at most) stay inside 32 bits
+  if (std::max({a.M, a.N, a.K}) > ASGD_PRODUCT_MAX || a.groups > ASGD_MAX_EXPERTS) return ASGD_EUNSUPPORTED;
   if (a.M == 0 || a.N == 0) return ASGD_OK;
   if (!a.c || !aligned(a.c, type_bytes(a.c_type))) return ASGD_EINVAL;
   if (a.K > 0 && (!a.a || !a.b || !a.a_scale || !a.b_scale || !aligned(a.a, 16) || !aligned(a.b, 16) || !aligned(a.a_scale, 4) || !aligned(a.b_scale, 4))) return ASGD_EINVAL;

@@ -306,7 +306,7 @@ product_pair_kernel(const Params p, const __grid_constant__ CUtensorMap map_a, c
         ScaleRows<kPairCols> cols;
         rows.start(p.sa, p.sa_row, p.sa_block, t.kb0, t.m0 + (int)rank * kHalf, t.m_end, lane);
         if (kColumns) cols.start(from, p.sb_row, p.sb_block, t.kb0, t.n0, p.N, lane);
-        const int n = t.n0 + 128 * lane;             // two blocks of columns
+        const int n = t.n0 + 128 * min(lane, 1);     // two blocks of columns
         const bool there = n < p.N;
         const float* of_block = there ? from + (n >> 7) * p.sb_row + t.kb0 * p.sb_block : p.sb;
         for (int kb = t.kb0; kb < t.kb1; ++kb, ++it) {

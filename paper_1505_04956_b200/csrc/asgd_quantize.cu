@@ -456,7 +456,7 @@ extern "C" int asgd_quantize(const asgd_quantize_args* args, void* stream) {
   if ((a.square != 0 && a.square != 1) || a.per_token < 1) return ASGD_EINVAL;
   if ((a.square && a.source) || (a.weights && !a.source) || a.rows_x < 0 || (!a.source && a.rows_x != a.M)) return ASGD_EINVAL;
   if (a.ldx < a.K || (a.q && a.ldq < a.K) || (a.qt && a.ldqt < a.M)) return ASGD_EINVAL;
-  if (a.M > 0x7fffffffll || a.K > 0x7fff0000ll) return ASGD_EUNSUPPORTED;   // column numbers stay inside 32 bits
+  if (a.M > 0x7fffffffll || a.K > ASGD_QUANTIZE_MAX) return ASGD_EUNSUPPORTED;   // column numbers stay inside 32 bits
   if (a.M == 0 || a.K == 0) return ASGD_OK;
   if ((!a.q && !a.qt) || (a.rows_x > 0 && !a.x) || !aligned(a.x, type_bytes(a.x_type))) return ASGD_EINVAL;
   if (((a.q || a.square) && !a.scale) || (a.qt && !a.square && !a.scale_t)) return ASGD_EINVAL;

@@ -66,3 +66,35 @@ def test_scales_and_groups_that_start_anywhere(M, N, K, G, first):
             s = slice(rows[g], rows[g + 1])
             _check_product(got[s], a64[s], b64[g], K, F32)
     pkg.asgd_experts_sync()
+
+
+# ---------------------------------------------------------------------------------------------------------------
+# products: the most rows and columns
+# ---------------------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("by_groups", [False, True])
+def test_products_of_the_most_rows_and_columns(by_groups):
+    n = 2 ** 31 - 256                                    # 34 GB of rows of 16 numbers
+    long = torch.zeros(n, 16, dtype=torch.uint8, device="cuda")
+    scale = torch.ones(n, 1, device="cuda")
+    a, sa = _operand(300, 16, E4, 1)
+    long[-300:] = a.view(torch.uint8)
+    scale[-300:] = sa
+    b, sb = _operand(1, 16, E4, 2)
+    a64, b64 = _values64(a, sa), _values64(b, sb)
+    out = torch.full((n, 1), 5.0, device="cuda")
+    if by_groups:
+        offsets = torch.tensor([0, 7, 7, n], dtype=torch.int32, device="cuda")
+        pkg.asgd_product(long.view(E4), scale, b.view(torch.uint8).expand(3, 1, 16).contiguous().view(E4), sb.expand(3, 1, 1), offsets=offsets, out=out)
+    else:
+        pkg.asgd_product(long.view(E4), scale, b, sb, out=out)
+    pkg.asgd_experts_sync()
+    _check_product(out[-300:], a64, b64, 16, F32)
+    assert int(out[:-300].count_nonzero()) == 0
+    if by_groups:
+        return
+    out.fill_(5.0)
+    pkg.asgd_product(b, sb, long.view(E4), scale, out=out.view(1, n))
+    pkg.asgd_experts_sync()
+    _check_product(out.view(1, n)[:, -300:], b64, a64, 16, F32)
+    assert int(out[:-300].count_nonzero()) == 0
