@@ -12,7 +12,8 @@
  *     read before the call returns.  Nothing is allocated; outputs and workspaces are the caller's.
  *   - Every function returns 0 (ASGD_OK) or a negative asgd_status and enqueues its work on `stream` (a cudaStream_t,
  *     NULL = default stream); nothing is launched when it returns an error, except ASGD_ECUDA.
- *   - The functions keep no state between calls and may be used from several threads and streams at a time.
+ *   - The functions keep no state between calls (but for the report that asgd_experts_sync takes) and may be used from
+ *     several threads and streams at a time.
  *   - Sums, softmax statistics and scores are fp32 whatever the inputs' type; results do not depend on timing.
  *   - Tensors are row-major with a leading dimension (elements from one row to the next); a size of zero rows is no
  *     error: nothing is written but what does not depend on rows.
@@ -183,7 +184,9 @@ int asgd_combine_grad(int64_t T, int64_t D, int32_t top_k, const void *dy, int32
 
 /* Wait for the stream and return what asgd_product calls on this device have reported since the last asgd_experts_sync:
  * ASGD_OK, ASGD_EINVAL (offsets, see above) or ASGD_ETIMEOUT (a bounded wait on the kernel's own copies or products ran
- * out; the outputs of that call are not to be used). */
+ * out; the outputs of that call are not to be used); of several the last named.  This is the one state between calls:
+ * there is one report per device, shared by all of its streams, and the call that takes it clears it (no report that comes
+ * meanwhile is lost).  With several streams in use, wait for all of them, then call this once for all. */
 int asgd_experts_sync(void *stream);
 /* Failure drill of asgd_product's bounded waits, as asgd_set_wait_drill: later launches of this process give a wait up
  * after wait_limit polls, and with withhold = 1 the first copy of every block is announced but never issued.

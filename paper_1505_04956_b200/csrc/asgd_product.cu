@@ -9,6 +9,7 @@
 #include <algorithm>
 #include <atomic>
 #include <cmath>
+#include <mutex>
 
 #include "asgd_product_few.cuh"
 #include "asgd_product_pair.cuh"
@@ -17,6 +18,13 @@ namespace {
 
 std::atomic<unsigned> g_wait_limit{asgd::DEFAULT_WAIT_LIMIT};
 std::atomic<int> g_withhold{0};
+
+// What has been reported becomes the answer, in one exchange: a report that comes while it is taken is for the next one.
+__device__ int g_taken;
+__global__ void take_status_kernel() {
+  wait_for_stream();
+  g_taken = atomicExch(&g_status, 0);
+}
 
 // ---- host ----
 
@@ -203,12 +211,14 @@ extern "C" int asgd_product(const asgd_product_args* args, void* stream) {
 }
 
 extern "C" int asgd_experts_sync(void* stream) {
-  if (cudaStreamSynchronize((cudaStream_t)stream) != cudaSuccess) return ASGD_ECUDA;
+  const cudaStream_t st = (cudaStream_t)stream;
+  if (cudaStreamSynchronize(st) != cudaSuccess) return ASGD_ECUDA;
+  static std::mutex turn;                              // g_taken holds one answer at a time
+  const std::lock_guard<std::mutex> mine(turn);
   int status = 0;
-  const int none = 0;
-  if (cudaMemcpyFromSymbol(&status, g_status, sizeof(int)) != cudaSuccess) return ASGD_ECUDA;
-  if (status && cudaMemcpyToSymbol(g_status, &none, sizeof(int)) != cudaSuccess) return ASGD_ECUDA;
-  return status;
+  if (!launch_after(take_status_kernel, dim3(1), 1, 0, st)) return ASGD_ECUDA;
+  if (cudaMemcpyFromSymbolAsync(&status, g_taken, sizeof(int), 0, cudaMemcpyDeviceToHost, st) != cudaSuccess) return ASGD_ECUDA;
+  return cudaStreamSynchronize(st) == cudaSuccess ? status : ASGD_ECUDA;
 }
 
 extern "C" int asgd_product_set_wait_drill(uint32_t wait_limit, int32_t withhold) {

@@ -358,7 +358,8 @@ def asgd_combine_grad(dy, z, rows, weights=None, source=None, *, need_dz=True, n
 
 
 def asgd_experts_sync(stream=None):
-    """Wait for the stream; raise what asgd_product calls on this device have reported since the last call."""
+    """Wait for the stream; raise what asgd_product calls on this device have reported since the last call (one report per
+    device, whatever the streams: where there are several, wait for all of them first)."""
     s = stream if stream is not None else torch.cuda.current_stream()
     _chk(_load().asgd_experts_sync(C.c_void_p(s.cuda_stream)), "asgd_experts_sync")
 

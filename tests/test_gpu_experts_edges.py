@@ -4,6 +4,7 @@ import pytest
 import torch
 
 import paper_1505_04956_b200 as pkg
+from paper_1505_04956_b200 import binding
 
 from .test_gpu_experts import BF, E4, E5, F16, F32, _check_product, _loads, _operand, _values64
 
@@ -98,3 +99,47 @@ def test_products_of_the_most_rows_and_columns(by_groups):
     pkg.asgd_experts_sync()
     _check_product(out.view(1, n)[:, -300:], b64, a64, 16, F32)
     assert int(out[:-300].count_nonzero()) == 0
+
+
+# ---------------------------------------------------------------------------------------------------------------
+# reports
+# ---------------------------------------------------------------------------------------------------------------
+
+def test_no_report_is_lost_while_another_is_taken():
+    # a wait that runs out on one stream, while calls on another stream report offsets that cut a block and are taken one
+    # after the other: whichever call takes it, the timeout (the worse status) is seen
+    a, sa = _operand(8, 1024, E4, 1)
+    b, sb = _operand(512, 1024, E4, 2, True)
+    u, su = _operand(16, 400, E4, 3)
+    cut = torch.tensor([0, 100, 400], dtype=torch.int32, device="cuda")
+    side = torch.cuda.Stream()
+    pkg.asgd_product(a, sa, b, sb)
+    pkg.asgd_product_inner(u, su, u, su, cut[::2].contiguous())
+    torch.cuda.synchronize()
+    try:
+        pkg.asgd_experts_sync()
+    except binding.AsgdError:
+        pass
+
+    def take(stream=None):
+        try:
+            pkg.asgd_experts_sync(stream)
+            return binding.ASGD_OK
+        except binding.AsgdError as err:
+            return err.status
+    for _ in range(40):
+        try:
+            pkg.asgd_product_set_wait_drill(2000, True)
+            pkg.asgd_product(a, sa, b, sb, stream=side)
+        finally:
+            pkg.asgd_product_set_wait_drill()
+        seen, turns = [], 0
+        while not side.query():
+            pkg.asgd_product_inner(u, su, u, su, cut)
+            seen.append(take())
+            turns += 1
+            assert turns < 10 ** 6
+        seen.append(take(side))
+        assert binding.ASGD_ETIMEOUT in seen             # (each of the call's blocks reports: more than one may see it)
+        assert all(s == binding.ASGD_EINVAL for s in seen[:-1] if s != binding.ASGD_ETIMEOUT)
+    assert take() == binding.ASGD_OK
