@@ -2,7 +2,7 @@
 
 The functions carry the C names and marshal arguments: they check shapes and types, take outputs from torch's
 allocator and pass strides on.  Every number is computed in the library's kernels, on the current CUDA stream or the
-one given.
+one given; a call's tensors are on the current device (that of the stream, where one is given).
 
     ids, weights, offsets, rows, source = asgd_route(logits, 8, score="sigmoid", bias=balance, align=128)
     xq, xs = asgd_quantize(x, source=source, per_token=8)                 # tokens in the experts' order, 8 bits
@@ -91,26 +91,39 @@ def _need(ok, what, *values):
         raise ValueError(what % values if values else what)
 
 
-def _wrong(t, types, name, dims):
-    _need(t.is_cuda, "%s must be a CUDA tensor: the library has no host path", name)
+_current_device = getattr(torch._C, "_cuda_getDevice", None)               # (none where torch knows no CUDA)
+
+
+def _wrong(t, on, types, name, dims):
+    _need(t.get_device() >= 0, "%s must be a CUDA tensor: the library has no host path", name)
+    _need(t.get_device() == on, "%s is on cuda:%d, where cuda:%d is wanted", name, t.get_device(), on)
     _need(t.dim() == dims, "%s must have %d dimensions", name, dims)
     _need(t.dtype in types, "%s: dtype %s is not supported", name, t.dtype)
     _need(False, "%s: the last dimension must be contiguous", name)
 
 
 # A call takes as long on the host as on the device when the tensors are small, so every attribute of a tensor is read once.
-def _matrix(t, types, name, dims=2):
-    """A CUDA tensor of one of the types whose last dimension is contiguous: its type's number, shape and strides."""
+def _first(t, types, name):
+    """A call's first matrix: the number of its device, where all of the call's tensors have to be, and what _matrix gives.
+    The device has to be the current one, for that is where the library launches."""
+    on, number, shape, strides = t.get_device(), types.get(t.dtype), t.shape, t.stride()
+    if not (on >= 0 and on == _current_device() and number is not None and len(shape) == 2 and (strides[-1] == 1 or shape[-1] <= 1)):
+        _wrong(t, _current_device() if on >= 0 else on, types, name, 2)
+    return on, number, shape, strides
+
+
+def _matrix(t, on, types, name, dims=2):
+    """A tensor on device `on` of one of the types whose last dimension is contiguous: its type's number, shape and strides."""
     number, shape, strides = types.get(t.dtype), t.shape, t.stride()
-    if not (number is not None and t.is_cuda and len(shape) == dims and (strides[-1] == 1 or shape[-1] <= 1)):
-        _wrong(t, types, name, dims)
+    if not (number is not None and t.get_device() == on and len(shape) == dims and (strides[-1] == 1 or shape[-1] <= 1)):
+        _wrong(t, on, types, name, dims)
     return number, shape, strides
 
 
-def _flat(t, dtype, shape, name):
+def _flat(t, on, dtype, shape, name):
     """Its address."""
-    if not (t.is_cuda and t.dtype == dtype and t.shape == shape and t.is_contiguous()):
-        raise ValueError("%s must be a contiguous CUDA tensor of %s with shape %s" % (name, dtype, tuple(shape)))
+    if not (t.get_device() == on and t.dtype == dtype and t.shape == shape and t.is_contiguous()):
+        raise ValueError("%s must be a contiguous tensor of %s with shape %s on cuda:%d" % (name, dtype, tuple(shape), on))
     return t.data_ptr()
 
 
@@ -122,9 +135,9 @@ def _ld(shape, strides, unit=1):
 _new = torch.empty_strided
 
 
-def _handle(t):
-    """The current stream of the tensor's device, as the C functions take it."""
-    return torch._C._cuda_getCurrentRawStream(t.get_device())
+def _handle(on):
+    """The current stream of the device, as the C functions take it."""
+    return torch._C._cuda_getCurrentRawStream(on)
 
 
 def _on(stream, call, *args, **kw):
@@ -152,15 +165,15 @@ def asgd_route(logits, top_k, *, score="softmax", bias=None, groups=1, groups_ke
     if stream is not None:
         return _on(stream, asgd_route, logits, top_k, score=score, bias=bias, groups=groups, groups_kept=groups_kept, group_top=group_top,
                    renormalise=renormalise, scale=scale, align=align, plan=plan)
-    type_, (T, E), strides = _matrix(logits, _FLOAT, "logits")
-    bias_ptr = None if bias is None else _flat(bias, torch.float32, (E,), "bias")
+    on, type_, (T, E), strides = _first(logits, _FLOAT, "logits")
+    bias_ptr = None if bias is None else _flat(bias, on, torch.float32, (E,), "bias")
     cfg, need = _route_config(E, top_k, score, groups, groups_kept, group_top, renormalise, scale, align, T)
     dev, ints, ld = logits.device, torch.int32, _ld((T, E), strides)
     ids = _new((T, top_k), (top_k, 1), dtype=ints, device=dev)
     weights = _new((T, top_k), (top_k, 1), dtype=torch.float32, device=dev)
     if not plan:
         _chk(_load().asgd_route(cfg, T, logits.data_ptr(), type_, ld, bias_ptr, ids.data_ptr(), weights.data_ptr(), None, None, None, 0,
-                                None, 0, _handle(logits)), "asgd_route")
+                                None, 0, _handle(on)), "asgd_route")
         return ids, weights
     n = T * top_k + E * (align - 1)
     offsets = _new((E + 1,), (1,), dtype=ints, device=dev)
@@ -168,7 +181,7 @@ def asgd_route(logits, top_k, *, score="softmax", bias=None, groups=1, groups_ke
     source = _new((n,), (1,), dtype=ints, device=dev)
     work = _new((need,), (1,), dtype=torch.uint8, device=dev) if need else None
     _chk(_load().asgd_route(cfg, T, logits.data_ptr(), type_, ld, bias_ptr, ids.data_ptr(), weights.data_ptr(), offsets.data_ptr(),
-                            rows.data_ptr(), source.data_ptr(), n, work.data_ptr() if need else None, need, _handle(logits)), "asgd_route")
+                            rows.data_ptr(), source.data_ptr(), n, work.data_ptr() if need else None, need, _handle(on)), "asgd_route")
     return ids, weights, offsets, rows, source
 
 
@@ -176,14 +189,14 @@ def asgd_route_grad(logits, ids, dweights, *, score="softmax", renormalise=True,
     """Gradient [T, E] (of the logits' type) of the weights that asgd_route gave for `ids`, from dweights [T, top_k]."""
     if stream is not None:
         return _on(stream, asgd_route_grad, logits, ids, dweights, score=score, renormalise=renormalise, scale=scale)
-    type_, (T, E), strides = _matrix(logits, _FLOAT, "logits")
+    on, type_, (T, E), strides = _first(logits, _FLOAT, "logits")
     _need(ids.dim() == 2 and ids.shape[0] == T, "ids must have shape [T, top_k]")
     top_k = ids.shape[1]
-    ids_ptr = _flat(ids, torch.int32, (T, top_k), "ids")
-    dw_ptr = _flat(dweights, torch.float32, (T, top_k), "dweights")
+    ids_ptr = _flat(ids, on, torch.int32, (T, top_k), "ids")
+    dw_ptr = _flat(dweights, on, torch.float32, (T, top_k), "dweights")
     cfg, _ = _route_config(E, top_k, score, 1, 1, 1, renormalise, scale, 1, T)
     out = _new((T, E), (E, 1), dtype=logits.dtype, device=logits.device)
-    _chk(_load().asgd_route_grad(cfg, T, logits.data_ptr(), type_, _ld((T, E), strides), ids_ptr, dw_ptr, out.data_ptr(), E, _handle(logits)),
+    _chk(_load().asgd_route_grad(cfg, T, logits.data_ptr(), type_, _ld((T, E), strides), ids_ptr, dw_ptr, out.data_ptr(), E, _handle(on)),
          "asgd_route_grad")
     return out
 
@@ -209,7 +222,7 @@ def asgd_quantize(x, *, form="rows", dtype=torch.float8_e4m3fn, source=None, per
     if there are any, and zeros where source[r] < 0."""
     if stream is not None:
         return _on(stream, asgd_quantize, x, form=form, dtype=dtype, source=source, per_token=per_token, weights=weights)
-    x_type, (T, K), strides = _matrix(x, _FLOAT, "x")
+    on, x_type, (T, K), strides = _first(x, _FLOAT, "x")
     q_type = _EIGHT.get(dtype)
     _need(form in _FORMS, "form %r is not known", form)
     _need(q_type is not None, "dtype %s is not supported", dtype)
@@ -218,11 +231,11 @@ def asgd_quantize(x, *, form="rows", dtype=torch.float8_e4m3fn, source=None, per
     if source is not None:
         _need(not square, "blocks of 128 x 128 are not gathered")
         M = source.numel()
-        source_ptr = _flat(source, torch.int32, (M,), "source")
+        source_ptr = _flat(source, on, torch.int32, (M,), "source")
     if weights is not None:
         _need(source is not None, "weights need a source")
-        _need(weights.is_cuda and weights.dtype == torch.float32 and weights.is_contiguous() and weights.numel() == T * per_token,
-              "weights must be contiguous fp32 on the GPU, T * per_token of them")
+        _need(weights.get_device() == on and weights.dtype == torch.float32 and weights.is_contiguous() and weights.numel() == T * per_token,
+              "weights must be contiguous fp32 on the device of x, T * per_token of them")
         weights_ptr = weights.data_ptr()
     dev, blocks = x.device, -(-K // BLOCK)
     args = [M, K, x.data_ptr(), _ld((T, K), strides), T, x_type, q_type, square, int(per_token), source_ptr, weights_ptr]
@@ -242,15 +255,15 @@ def asgd_quantize(x, *, form="rows", dtype=torch.float8_e4m3fn, source=None, per
             scale_t = _scales(K, M, dev)
             args += [scale_t.data_ptr(), 1, K]
             out += (scale_t,)
-    _chk(_load().asgd_quantize(C.byref(QuantizeArgs(*args)), _handle(x)), "asgd_quantize")
+    _chk(_load().asgd_quantize(C.byref(QuantizeArgs(*args)), _handle(on)), "asgd_quantize")
     return out
 
 
-def _scale_of(s, name, shape, other=None):
+def _scale_of(s, on, name, shape, other=None):
     """Scales of one of two shapes: the shape and the strides."""
     found = s.shape
-    if not ((found == shape or found == other) and s.dtype == torch.float32 and s.is_cuda):
-        raise ValueError("%s must be fp32 on the GPU with shape %s, not %s of shape %s" % (name, tuple(shape), s.dtype, tuple(found)))
+    if not ((found == shape or found == other) and s.dtype == torch.float32 and s.get_device() == on):
+        raise ValueError("%s must be fp32 on cuda:%d with shape %s, not %s of shape %s" % (name, on, tuple(shape), s.dtype, tuple(found)))
     return found, s.stride()
 
 
@@ -262,23 +275,23 @@ def asgd_product(a, a_scale, b, b_scale, *, offsets=None, out_dtype=torch.bfloat
     if stream is not None:
         return _on(stream, asgd_product, a, a_scale, b, b_scale, offsets=offsets, out_dtype=out_dtype, out=out)
     grouped = offsets is not None
-    a_type, a_shape, a_strides = _matrix(a, _EIGHT, "a")
-    b_type, b_shape, b_strides = _matrix(b, _EIGHT, "b", 3 if grouped else 2)
+    on, a_type, a_shape, a_strides = _first(a, _EIGHT, "a")
+    b_type, b_shape, b_strides = _matrix(b, on, _EIGHT, "b", 3 if grouped else 2)
     (M, K), N, kb = a_shape, b_shape[-2], -(-a_shape[1] // BLOCK)
     _need(b_shape[-1] == K, "a and b differ in their last dimension")
     G, offsets_ptr = 0, None
     if grouped:
         G = b_shape[0]
         _need(G > 0, "b holds no group")
-        offsets_ptr = _flat(offsets, torch.int32, (G + 1,), "offsets")
-    _, sa = _scale_of(a_scale, "a_scale", (M, kb))
+        offsets_ptr = _flat(offsets, on, torch.int32, (G + 1,), "offsets")
+    _, sa = _scale_of(a_scale, on, "a_scale", (M, kb))
     square = -(-N // BLOCK)
-    s_shape, sb = _scale_of(b_scale, "b_scale", (G, square, kb), (G, N, kb)) if grouped else _scale_of(b_scale, "b_scale", (square, kb), (N, kb))
+    s_shape, sb = _scale_of(b_scale, on, "b_scale", (G, square, kb), (G, N, kb)) if grouped else _scale_of(b_scale, on, "b_scale", (square, kb), (N, kb))
     if out is None:
         out, c_type, ldc = _new((M, N), (N, 1), dtype=out_dtype, device=a.device), _FLOAT.get(out_dtype), N
         _need(c_type is not None, "out_dtype %s is not supported", out_dtype)
     else:
-        c_type, c_shape, c_strides = _matrix(out, _FLOAT, "out")
+        c_type, c_shape, c_strides = _matrix(out, on, _FLOAT, "out")
         _need(c_shape == (M, N), "out must have shape (%d, %d)", M, N)
         ldc = _ld(c_shape, c_strides)
     many = G > 1
@@ -286,7 +299,7 @@ def asgd_product(a, a_scale, b, b_scale, *, offsets=None, out_dtype=torch.bfloat
                        b.data_ptr(), _ld(b_shape, b_strides, 16), b_strides[0] if many else 0,
                        b_scale.data_ptr(), sb[-2], sb[-1], sb[0] if many else 0,
                        out.data_ptr(), ldc, 0, offsets_ptr, G, 0, a_type, b_type, c_type, 1 if s_shape[-2] != N else 0)
-    _chk(_load().asgd_product(C.byref(args), _handle(a)), "asgd_product")
+    _chk(_load().asgd_product(C.byref(args), _handle(on)), "asgd_product")
     return out
 
 
@@ -295,26 +308,26 @@ def asgd_product_inner(a, a_scale, b, b_scale, offsets, *, out_dtype=torch.float
     gradients.  a [M, K], a_scale [M, ceil(K / 128)], b [N, K], b_scale [N, ceil(K / 128)]."""
     if stream is not None:
         return _on(stream, asgd_product_inner, a, a_scale, b, b_scale, offsets, out_dtype=out_dtype, out=out)
-    a_type, a_shape, a_strides = _matrix(a, _EIGHT, "a")
-    b_type, b_shape, b_strides = _matrix(b, _EIGHT, "b")
+    on, a_type, a_shape, a_strides = _first(a, _EIGHT, "a")
+    b_type, b_shape, b_strides = _matrix(b, on, _EIGHT, "b")
     (M, K), N, kb = a_shape, b_shape[0], -(-a_shape[1] // BLOCK)
     _need(b_shape[1] == K, "a and b differ in their last dimension")
     G = offsets.numel() - 1
     _need(G > 0, "offsets hold no group")
-    offsets_ptr = _flat(offsets, torch.int32, (G + 1,), "offsets")
-    _, sa = _scale_of(a_scale, "a_scale", (M, kb))
-    _, sb = _scale_of(b_scale, "b_scale", (N, kb))
+    offsets_ptr = _flat(offsets, on, torch.int32, (G + 1,), "offsets")
+    _, sa = _scale_of(a_scale, on, "a_scale", (M, kb))
+    _, sb = _scale_of(b_scale, on, "b_scale", (N, kb))
     if out is None:
         out, c_type, ldc, c_group = _new((G, M, N), (M * N, N, 1), dtype=out_dtype, device=a.device), _FLOAT.get(out_dtype), N, M * N
         _need(c_type is not None, "out_dtype %s is not supported", out_dtype)
     else:
-        c_type, c_shape, c_strides = _matrix(out, _FLOAT, "out", 3)
+        c_type, c_shape, c_strides = _matrix(out, on, _FLOAT, "out", 3)
         _need(c_shape == (G, M, N), "out must have shape (%d, %d, %d)", G, M, N)
         ldc, c_group = _ld(c_shape, c_strides), c_strides[0]
     args = ProductArgs(M, N, K, a.data_ptr(), _ld(a_shape, a_strides, 16), a_scale.data_ptr(), sa[0], sa[1],
                        b.data_ptr(), _ld(b_shape, b_strides, 16), 0, b_scale.data_ptr(), sb[0], sb[1], 0,
                        out.data_ptr(), ldc, c_group, offsets_ptr, G, 1, a_type, b_type, c_type, 0)
-    _chk(_load().asgd_product(C.byref(args), _handle(a)), "asgd_product")
+    _chk(_load().asgd_product(C.byref(args), _handle(on)), "asgd_product")
     return out
 
 
@@ -322,14 +335,14 @@ def asgd_combine(z, rows, weights=None, *, stream=None):
     """y[t] = sum_j weights[t, j] * z[rows[t, j]] of z's type; rows [T, top_k] int32 (negative: no part)."""
     if stream is not None:
         return _on(stream, asgd_combine, z, rows, weights)
-    type_, (R, D), strides = _matrix(z, _FLOAT, "z")
+    on, type_, (R, D), strides = _first(z, _FLOAT, "z")
     shape = rows.shape
     _need(len(shape) == 2, "rows must have shape [T, top_k]")
     T, top_k = shape
-    rows_ptr = _flat(rows, torch.int32, shape, "rows")
-    weights_ptr = None if weights is None else _flat(weights, torch.float32, shape, "weights")
+    rows_ptr = _flat(rows, on, torch.int32, shape, "rows")
+    weights_ptr = None if weights is None else _flat(weights, on, torch.float32, shape, "weights")
     y = _new((T, D), (D, 1), dtype=z.dtype, device=z.device)
-    _chk(_load().asgd_combine(T, D, top_k, z.data_ptr(), type_, R, _ld((R, D), strides), rows_ptr, weights_ptr, y.data_ptr(), D, _handle(z)),
+    _chk(_load().asgd_combine(T, D, top_k, z.data_ptr(), type_, R, _ld((R, D), strides), rows_ptr, weights_ptr, y.data_ptr(), D, _handle(on)),
          "asgd_combine")
     return y
 
@@ -339,21 +352,21 @@ def asgd_combine_grad(dy, z, rows, weights=None, source=None, *, need_dz=True, n
     takes are undefined) and dweights [T, top_k]; None for what is not needed."""
     if stream is not None:
         return _on(stream, asgd_combine_grad, dy, z, rows, weights, source, need_dz=need_dz, need_dweights=need_dweights)
-    type_, (T, D), strides = _matrix(dy, _FLOAT, "dy")
-    z_type, (R, z_D), z_strides = _matrix(z, _FLOAT, "z")
+    on, type_, (T, D), strides = _first(dy, _FLOAT, "dy")
+    z_type, (R, z_D), z_strides = _matrix(z, on, _FLOAT, "z")
     _need(z_type == type_, "dy and z differ in type")
     _need(z_D == D, "dy and z differ in their last dimension")
     shape = rows.shape
     _need(len(shape) == 2 and shape[0] == T, "rows must have shape [T, top_k]")
     top_k = shape[1]
-    rows_ptr = _flat(rows, torch.int32, shape, "rows")
-    weights_ptr = None if weights is None else _flat(weights, torch.float32, shape, "weights")
-    source_ptr = None if source is None else _flat(source, torch.int32, (R,), "source")
+    rows_ptr = _flat(rows, on, torch.int32, shape, "rows")
+    weights_ptr = None if weights is None else _flat(weights, on, torch.float32, shape, "weights")
+    source_ptr = None if source is None else _flat(source, on, torch.int32, (R,), "source")
     dz = _new((R, D), (D, 1), dtype=dy.dtype, device=dy.device) if need_dz else None
     dw = _new((T, top_k), (top_k, 1), dtype=torch.float32, device=dy.device) if need_dweights else None
     _chk(_load().asgd_combine_grad(T, D, top_k, dy.data_ptr(), type_, _ld((T, D), strides), z.data_ptr(), R, _ld((R, D), z_strides), rows_ptr,
                                    weights_ptr, source_ptr, dz.data_ptr() if need_dz else None, D, dw.data_ptr() if need_dweights else None,
-                                   _handle(dy)), "asgd_combine_grad")
+                                   _handle(on)), "asgd_combine_grad")
     return dz, dw
 
 
@@ -361,7 +374,8 @@ def asgd_experts_sync(stream=None):
     """Wait for the stream; raise what asgd_product calls on this device have reported since the last call (one report per
     device, whatever the streams: where there are several, wait for all of them first)."""
     s = stream if stream is not None else torch.cuda.current_stream()
-    _chk(_load().asgd_experts_sync(C.c_void_p(s.cuda_stream)), "asgd_experts_sync")
+    with torch.cuda.device(s.device):
+        _chk(_load().asgd_experts_sync(C.c_void_p(s.cuda_stream)), "asgd_experts_sync")
 
 
 def asgd_product_set_wait_drill(wait_limit: int = 1 << 22, withhold: bool = False):

@@ -2,6 +2,7 @@
 import ctypes as C
 
 import pytest
+import torch
 
 from paper_1505_04956_b200 import binding, experts
 
@@ -20,3 +21,76 @@ def test_product_refuses_sizes_whose_tiles_pass_32_bits(bad, grouped):
 def test_quantize_refuses_rows_whose_blocks_pass_32_bits():
     wide = 1 << 31
     assert experts._load().asgd_quantize(C.byref(_q(M=1, rows_x=1, K=wide - 65535, ldx=wide, ldq=wide, square=1)), None) == EUNSUPPORTED
+
+
+# ---------------------------------------------------------------------------------------------------------------
+# devices
+# ---------------------------------------------------------------------------------------------------------------
+
+class _On:
+    """Stands for a CUDA tensor of a device."""
+    is_cuda = True
+
+    def __init__(self, device, dtype, *shape):
+        self.index, self.dtype, self.shape, self.device = device, dtype, torch.Size(shape), torch.device("cuda", device)
+
+    def get_device(self):
+        return self.index
+
+    def dim(self):
+        return len(self.shape)
+
+    def numel(self):
+        return self.shape.numel()
+
+    def stride(self):
+        out = [1]
+        for n in self.shape[:0:-1]:
+            out.insert(0, out[0] * n)
+        return tuple(out)
+
+    def is_contiguous(self):
+        return True
+
+    def data_ptr(self):
+        return 1 << 20
+
+
+F32, I32, E4 = torch.float32, torch.int32, torch.float8_e4m3fn
+_CALLS = [
+    ("asgd_route", [(F32, 4, 8), None], dict(top_k=2, bias=(F32, 8))),
+    ("asgd_route_grad", [(F32, 4, 8), (I32, 4, 2), (F32, 4, 2)], {}),
+    ("asgd_quantize", [(F32, 4, 8)], dict(source=(I32, 8), per_token=2, weights=(F32, 4, 2))),
+    ("asgd_product", [(E4, 4, 128), (F32, 4, 1), (E4, 3, 32, 128), (F32, 3, 1, 1)], dict(offsets=(I32, 4), out=(F32, 4, 32))),
+    ("asgd_product_inner", [(E4, 4, 256), (F32, 4, 2), (E4, 32, 256), (F32, 32, 2), (I32, 4)], dict(out=(F32, 3, 4, 32))),
+    ("asgd_combine", [(F32, 8, 16), (I32, 4, 2), (F32, 4, 2)], {}),
+    ("asgd_combine_grad", [(F32, 4, 16), (F32, 8, 16), (I32, 4, 2), (F32, 4, 2), (I32, 8)], {}),
+]
+
+
+@pytest.mark.parametrize("name, args, kw", _CALLS)
+def test_tensors_of_another_device_are_refused(name, args, kw, monkeypatch):
+    class Reached(Exception):
+        pass
+
+    def library():
+        raise Reached
+    monkeypatch.setattr(experts, "_load", library)
+    monkeypatch.setattr(experts, "_route_config", lambda *a: (None, 0))
+    monkeypatch.setattr(experts, "_new", lambda shape, strides, dtype, device: _On(device.index, dtype, *shape))
+    monkeypatch.setattr(experts, "_handle", lambda where: 0, raising=False)
+    monkeypatch.setattr(experts, "_current_device", lambda: 0, raising=False)
+    tensors = [i for i, a in enumerate(args) if a] + [k for k, a in kw.items() if isinstance(a, tuple)]
+
+    def call(devices):
+        make = lambda key, a: _On(devices.get(key, 0), *a) if isinstance(a, tuple) else a          # noqa: E731
+        fn = getattr(experts, name)
+        given = {k: make(k, a) for k, a in kw.items()}
+        return fn(*[make(i, a) for i, a in enumerate(args) if a], **given)
+    with pytest.raises(Reached):                         # all on the current device: the library is called
+        call({})
+    with pytest.raises(ValueError):                      # all on another one
+        call({t: 1 for t in tensors})
+    for t in tensors:                                    # one of them elsewhere
+        with pytest.raises(ValueError):
+            call({t: 1})
