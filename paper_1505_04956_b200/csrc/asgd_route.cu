@@ -511,7 +511,8 @@ template <int S, int L, typename T> __global__ void __launch_bounds__(kThreads) 
     if (e < E) out[e] = Elem<T>::from_f(sigmoid_scores ? 0.f : -f.part(x[j]) * per);
   }
   __syncwarp();
-  if (ok) out[id] = Elem<T>::from_f(sigmoid_scores ? ds * s * (1.f - s) : s * (ds - dot));
+  // 1 - s as a sigmoid of its own: the difference loses all of it from logits of 17 on
+  if (ok) out[id] = Elem<T>::from_f(sigmoid_scores ? ds * s * sigmoid(-chosen) : s * (ds - dot));
 }
 
 // Calls f with the numbers a lane holds and the lanes of a token, as compile-time numbers: 8 lanes where they have room

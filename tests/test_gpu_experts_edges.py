@@ -6,7 +6,7 @@ import torch
 import paper_1505_04956_b200 as pkg
 from paper_1505_04956_b200 import binding
 
-from .test_gpu_experts import BF, E4, E5, F16, F32, _check_product, _loads, _operand, _values64
+from .test_gpu_experts import BF, E4, E5, F16, F32, HALF_STEP, SMALLEST, U, _check_product, _close, _gen, _loads, _operand, _values64
 
 pytestmark = pytest.mark.gpu
 
@@ -143,3 +143,24 @@ def test_no_report_is_lost_while_another_is_taken():
         assert binding.ASGD_ETIMEOUT in seen             # (each of the call's blocks reports: more than one may see it)
         assert all(s == binding.ASGD_EINVAL for s in seen[:-1] if s != binding.ASGD_ETIMEOUT)
     assert take() == binding.ASGD_OK
+
+
+# ---------------------------------------------------------------------------------------------------------------
+# routing
+# ---------------------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", [F32, BF, F16])
+@pytest.mark.parametrize("E, top_k", [(12, 12), (40, 8), (200, 16), (1000, 32)])
+def test_sigmoid_gradient_of_large_logits(E, top_k, dtype):
+    # dx = scale * dw * s * (1 - s), relative to itself: both sigmoids (exponential 4 u, sum and reciprocal 1 u each), three
+    # products and the factor scale * dw stay below 32 u
+    g = _gen(E)
+    T = 60
+    size = 10 + 20 * torch.rand(T, E, generator=g, device="cuda")
+    x = torch.where(torch.rand(T, E, generator=g, device="cuda") < 0.5, size, -size).to(dtype)
+    ids = torch.rand(T, E, generator=g, device="cuda").argsort(dim=1)[:, :top_k].to(torch.int32).contiguous()
+    dw = torch.randn(T, top_k, generator=g, device="cuda")
+    got = pkg.asgd_route_grad(x, ids, dw, score="sigmoid", renormalise=False, scale=1.5)
+    z = x.double()
+    want = torch.zeros_like(z).scatter(1, ids.long(), 1.5 * dw.double()) / ((1 + torch.exp(-z)) * (1 + torch.exp(z)))
+    _close(got, want, (32 * U + HALF_STEP[dtype]) * want.abs() + SMALLEST[dtype])
