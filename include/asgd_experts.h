@@ -9,7 +9,8 @@
  *
  * General rules (those of asgd.h where they apply)
  *   - Every pointer is DEVICE memory of the current device, except the argument structures, which are HOST and are
- *     read before the call returns.  Nothing is allocated; outputs and workspaces are the caller's.
+ *     read before the call returns.  Nothing is allocated; outputs and workspaces are the caller's.  Arrays are aligned
+ *     to their element (ASGD_EINVAL otherwise), and to more where it is said.
  *   - Every function returns 0 (ASGD_OK) or a negative asgd_status and enqueues its work on `stream` (a cudaStream_t,
  *     NULL = default stream); nothing is launched when it returns an error, except ASGD_ECUDA.
  *   - The functions keep no state between calls (but for the report that asgd_experts_sync takes) and may be used from

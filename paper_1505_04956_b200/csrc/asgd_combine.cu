@@ -192,7 +192,7 @@ extern "C" int asgd_combine(int64_t T, int64_t D, int32_t top_k, const void* z, 
   if (T < 0 || D < 0 || R < 0 || top_k < 1 || !float_type(type) || ldz < D || ldy < D) return ASGD_EINVAL;
   if (T > 0x7fffffffll || R > 0x7fffffffll || top_k > ASGD_MAX_TOP_K) return ASGD_EUNSUPPORTED;
   if (T == 0 || D == 0) return ASGD_OK;
-  if ((R > 0 && !z) || !rows || !y || !aligned(z, type_bytes(type)) || !aligned(y, type_bytes(type))) return ASGD_EINVAL;
+  if ((R > 0 && !z) || !rows || !y || !aligned(z, type_bytes(type)) || !aligned(y, type_bytes(type)) || !aligned_words(rows, weights)) return ASGD_EINVAL;
   Args a{};
   a.T = T; a.D = D; a.R = R; a.ldz = ldz; a.ldy = ldy; a.top_k = top_k;
   a.z = z; a.rows = rows; a.weights = weights; a.y = y;
@@ -219,6 +219,7 @@ extern "C" int asgd_combine_grad(int64_t T, int64_t D, int32_t top_k, const void
   if (!dz && !dweights) return ASGD_OK;
   if (T > 0 && (!rows || (D > 0 && !dy) || (D > 0 && R > 0 && dweights && !z))) return ASGD_EINVAL;
   if (!aligned(dy, type_bytes(type)) || !aligned(z, type_bytes(type)) || !aligned(dz, type_bytes(type))) return ASGD_EINVAL;
+  if (!aligned_words(rows, weights, source, dweights)) return ASGD_EINVAL;
   Args a{};
   a.T = T; a.D = D; a.R = R; a.ldz = ldz; a.ld_dy = ld_dy; a.ld_dz = ld_dz; a.top_k = top_k;
   a.z = z; a.dy = dy; a.rows = rows; a.weights = weights; a.source = source; a.dz = dz; a.dweights = dweights;

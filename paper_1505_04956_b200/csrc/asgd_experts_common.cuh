@@ -19,6 +19,7 @@ inline bool float_type(int t) { return t == ASGD_F32 || t == ASGD_BF16 || t == A
 inline bool eight_bit_type(int t) { return t == ASGD_E4M3 || t == ASGD_E5M2; }
 inline size_t type_bytes(int t) { return t == ASGD_F32 ? 4 : (t == ASGD_BF16 || t == ASGD_F16) ? 2 : 1; }
 inline bool aligned(const void* p, size_t n) { return ((uintptr_t)p & (n - 1)) == 0; }
+template <typename... P> inline bool aligned_words(const P*... p) { return (aligned(p, 4) && ...); }       // 32-bit arrays (null is fine)
 inline long long ceil_div(long long a, long long b) { return (a + b - 1) / b; }
 
 template <typename T> struct Elem;

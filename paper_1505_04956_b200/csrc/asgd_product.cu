@@ -185,8 +185,8 @@ extern "C" int asgd_product(const asgd_product_args* args, void* stream) {
   // row, column and inner numbers of whole tiles (256 at most) stay inside 32 bits
   if (std::max({a.M, a.N, a.K}) > ASGD_PRODUCT_MAX || a.groups > ASGD_MAX_EXPERTS) return ASGD_EUNSUPPORTED;
   if (a.M == 0 || a.N == 0) return ASGD_OK;
-  if (!a.c || !aligned(a.c, type_bytes(a.c_type))) return ASGD_EINVAL;
-  if (a.K > 0 && (!a.a || !a.b || !a.a_scale || !a.b_scale || !aligned(a.a, 16) || !aligned(a.b, 16) || !aligned(a.a_scale, 4) || !aligned(a.b_scale, 4))) return ASGD_EINVAL;
+  if (!a.c || !aligned(a.c, type_bytes(a.c_type)) || !aligned_words(a.offsets)) return ASGD_EINVAL;
+  if (a.K > 0 && (!a.a || !a.b || !a.a_scale || !a.b_scale || !aligned(a.a, 16) || !aligned(a.b, 16) || !aligned_words(a.a_scale, a.b_scale))) return ASGD_EINVAL;
   if (a.groups > 1 && !a.inner && (a.b_group % 16 || a.b_group < 0)) return ASGD_EINVAL;
   Params p;
   p.M = (int)a.M; p.N = (int)a.N; p.K = (int)a.K; p.groups = a.groups; p.inner = a.inner;

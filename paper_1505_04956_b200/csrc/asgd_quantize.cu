@@ -459,6 +459,7 @@ extern "C" int asgd_quantize(const asgd_quantize_args* args, void* stream) {
   if (a.M > 0x7fffffffll || a.K > ASGD_QUANTIZE_MAX) return ASGD_EUNSUPPORTED;   // column numbers stay inside 32 bits
   if (a.M == 0 || a.K == 0) return ASGD_OK;
   if ((!a.q && !a.qt) || (a.rows_x > 0 && !a.x) || !aligned(a.x, type_bytes(a.x_type))) return ASGD_EINVAL;
+  if (!aligned_words(a.source, a.weights, a.scale, a.scale_t)) return ASGD_EINVAL;
   if (((a.q || a.square) && !a.scale) || (a.qt && !a.square && !a.scale_t)) return ASGD_EINVAL;
   Args p;
   p.a = a;

@@ -587,6 +587,7 @@ extern "C" int asgd_route(const asgd_route_config* cfg, int64_t T, const void* l
   if (!config_ok(cfg) || T < 0 || !float_type(type) || ld < cfg->experts) return ASGD_EINVAL;
   if (!config_supported(cfg)) return ASGD_EUNSUPPORTED;
   if (T > 0 && (!logits || !ids || !weights || !aligned(logits, type_bytes(type)))) return ASGD_EINVAL;
+  if (!aligned_words(bias, ids, weights, offsets, rows, source)) return ASGD_EINVAL;
   const bool plan = offsets || rows || source;
   const long long need = (long long)T * cfg->top_k + (long long)cfg->experts * (cfg->align - 1);
   if (plan) {
@@ -637,7 +638,7 @@ extern "C" int asgd_route_grad(const asgd_route_config* cfg, int64_t T, const vo
   if (!config_ok(cfg) || T < 0 || !float_type(type) || ld < cfg->experts || ld_out < cfg->experts) return ASGD_EINVAL;
   if (!config_supported(cfg) || T > 0x7fffffffll) return ASGD_EUNSUPPORTED;
   if (T == 0) return ASGD_OK;
-  if (!logits || !ids || !dweights || !dlogits || !aligned(logits, type_bytes(type)) || !aligned(dlogits, type_bytes(type))) return ASGD_EINVAL;
+  if (!logits || !ids || !dweights || !dlogits || !aligned(logits, type_bytes(type)) || !aligned(dlogits, type_bytes(type)) || !aligned_words(ids, dweights)) return ASGD_EINVAL;
   GradArgs a{*cfg, T, ld, ld_out, logits, ids, dweights, dlogits};
   asgd_route_config shape = *cfg;
   shape.groups = shape.groups_kept = 1;                                // groups have no part in the gradient

@@ -6,7 +6,7 @@ import torch
 
 from paper_1505_04956_b200 import binding, experts
 
-from .test_experts_host import _p, _q
+from .test_experts_host import _cfg, _p, _q
 
 EINVAL, EUNSUPPORTED, ECUDA, OK = binding.ASGD_EINVAL, binding.ASGD_EUNSUPPORTED, binding.ASGD_ECUDA, binding.ASGD_OK
 
@@ -94,3 +94,44 @@ def test_tensors_of_another_device_are_refused(name, args, kw, monkeypatch):
     for t in tensors:                                    # one of them elsewhere
         with pytest.raises(ValueError):
             call({t: 1})
+
+
+# ---------------------------------------------------------------------------------------------------------------
+# alignment of 32-bit arrays
+# ---------------------------------------------------------------------------------------------------------------
+
+P, ODD = C.c_void_p(1 << 20), C.c_void_p((1 << 20) + 2)
+
+
+@pytest.mark.parametrize("at", [5, 6, 7, 8, 9, 10])
+def test_route_refuses_arrays_that_are_not_aligned(at):
+    args = [C.byref(_cfg()), 10, P, 0, 64, P, P, P, P, P, P, 40, None, 0, None]
+    args[at] = ODD                                       # bias, ids, weights, offsets, rows, source
+    assert experts._load().asgd_route(*args) == EINVAL
+
+
+@pytest.mark.parametrize("at", [5, 6])
+def test_route_grad_refuses_arrays_that_are_not_aligned(at):
+    args = [C.byref(_cfg()), 10, P, 0, 64, P, P, P, 64, None]
+    args[at] = ODD
+    assert experts._load().asgd_route_grad(*args) == EINVAL
+
+
+@pytest.mark.parametrize("bad", [dict(source=ODD.value), dict(source=P.value, weights=ODD.value), dict(scale=ODD.value),
+                                 dict(qt=P.value, ldqt=256, scale_t=ODD.value)])
+def test_quantize_refuses_arrays_that_are_not_aligned(bad):
+    assert experts._load().asgd_quantize(C.byref(_q(**bad)), None) == EINVAL
+
+
+@pytest.mark.parametrize("bad", [dict(offsets=ODD.value, groups=2), dict(a_scale=ODD.value), dict(b_scale=ODD.value)])
+def test_product_refuses_arrays_that_are_not_aligned(bad):
+    assert experts._load().asgd_product(C.byref(_p(**bad)), None) == EINVAL
+
+
+def test_combine_refuses_arrays_that_are_not_aligned():
+    L = experts._load()
+    for rows, weights in ((ODD, P), (P, ODD)):
+        assert L.asgd_combine(4, 64, 2, P, 1, 8, 64, rows, weights, P, 64, None) == EINVAL
+    for i in range(4):
+        rows, weights, source, dweights = (ODD if i == j else P for j in range(4))
+        assert L.asgd_combine_grad(4, 64, 2, P, 1, 64, P, 8, 64, rows, weights, source, P, 64, dweights, None) == EINVAL
