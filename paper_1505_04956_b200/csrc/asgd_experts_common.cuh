@@ -51,6 +51,12 @@ template <typename T> __device__ __forceinline__ uint4 pack16(const float (&v)[k
   return u;
 }
 
+// Whether a CUDA call went well; the error of one that did not is this call's, and left to no later one.
+inline bool good(cudaError_t e) {
+  if (e != cudaSuccess) cudaGetLastError();
+  return e == cudaSuccess;
+}
+
 // A launch that may begin while the kernel before it in the stream ends: blocks come up as SMs fall free, and wait (first
 // thing, wait_for_stream) until all that was before is complete and visible.
 template <typename... P, typename... A> inline bool launch_after(void (*kernel)(P...), dim3 grid, unsigned threads, size_t smem, cudaStream_t st, A&&... args) {
@@ -64,7 +70,7 @@ template <typename... P, typename... A> inline bool launch_after(void (*kernel)(
   cfg.stream = st;
   cfg.attrs = &early;
   cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, kernel, P(args)...) == cudaSuccess;
+  return good(cudaLaunchKernelEx(&cfg, kernel, P(args)...));
 }
 // (in a kernel that another one of the same call follows) the next kernel's blocks may come up as soon as there is room
 __device__ __forceinline__ void let_next_come() { asm volatile("griddepcontrol.launch_dependents;"); }

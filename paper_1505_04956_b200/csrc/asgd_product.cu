@@ -34,7 +34,7 @@ PFN_cuTensorMapEncodeTiled encoder() {
   if (!f) {
     void* fn = nullptr;
     cudaDriverEntryPointQueryResult q;
-    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &q) != cudaSuccess || !fn) return nullptr;
+    if (!good(cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &q)) || !fn) return nullptr;
     f = (PFN_cuTensorMapEncodeTiled)fn;
     known.store(f);
   }
@@ -67,10 +67,10 @@ long long most_tiles(const Params& p, int bm, int bn) {
 // Raises a kernel's shared-memory limit, once per device (`done`: a bit per device, of this kernel).
 template <typename K> bool allow_smem(K kernel, size_t bytes, std::atomic<unsigned long long>& done) {
   int dev = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess) return false;
+  if (!good(cudaGetDevice(&dev))) return false;
   const unsigned long long bit = 1ull << (dev & 63);
   if (dev < 64 && (done.load() & bit)) return true;
-  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) != cudaSuccess) return false;
+  if (!good(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes))) return false;
   done.fetch_or(bit);
   return true;
 }
@@ -105,7 +105,7 @@ template <int BN, bool kSplit> int launch_few(const asgd_product_args& a, Params
   cfg.stream = st;
   cfg.attrs = attrs;
   cfg.numAttrs = kSplit ? 2 : 1;
-  return cudaLaunchKernelEx(&cfg, product_few_kernel<BN, kSplit>, p, map_u, map_v) == cudaSuccess ? ASGD_OK : ASGD_ECUDA;
+  return good(cudaLaunchKernelEx(&cfg, product_few_kernel<BN, kSplit>, p, map_u, map_v)) ? ASGD_OK : ASGD_ECUDA;
 }
 
 // Blocks per tile of the few-rows kernel: a power of two, with two K blocks each at least, whose clusters are on the SMs
@@ -212,13 +212,13 @@ extern "C" int asgd_product(const asgd_product_args* args, void* stream) {
 
 extern "C" int asgd_experts_sync(void* stream) {
   const cudaStream_t st = (cudaStream_t)stream;
-  if (cudaStreamSynchronize(st) != cudaSuccess) return ASGD_ECUDA;
+  if (!good(cudaStreamSynchronize(st))) return ASGD_ECUDA;
   static std::mutex turn;                              // g_taken holds one answer at a time
   const std::lock_guard<std::mutex> mine(turn);
   int status = 0;
   if (!launch_after(take_status_kernel, dim3(1), 1, 0, st)) return ASGD_ECUDA;
-  if (cudaMemcpyFromSymbolAsync(&status, g_taken, sizeof(int), 0, cudaMemcpyDeviceToHost, st) != cudaSuccess) return ASGD_ECUDA;
-  return cudaStreamSynchronize(st) == cudaSuccess ? status : ASGD_ECUDA;
+  if (!good(cudaMemcpyFromSymbolAsync(&status, g_taken, sizeof(int), 0, cudaMemcpyDeviceToHost, st))) return ASGD_ECUDA;
+  return good(cudaStreamSynchronize(st)) ? status : ASGD_ECUDA;
 }
 
 extern "C" int asgd_product_set_wait_drill(uint32_t wait_limit, int32_t withhold) {

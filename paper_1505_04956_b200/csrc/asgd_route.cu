@@ -464,6 +464,7 @@ __global__ void __launch_bounds__(kThreads) place_kernel(const RouteArgs a) {
 
 // nothing to route: an empty plan
 __global__ void empty_plan_kernel(const RouteArgs a) {
+  wait_for_stream();
   for (int e = threadIdx.x; e <= a.c.experts; e += blockDim.x) a.offsets[e] = 0;
   for (long long r = threadIdx.x; r < a.source_len; r += blockDim.x) a.source[r] = -1;
 }
@@ -613,10 +614,7 @@ extern "C" int asgd_route(const asgd_route_config* cfg, int64_t T, const void* l
   a.hist = (int*)workspace;
   a.stride = (int)ceil_div(a.chunks, 4) * 4;
   a.totals = a.hist + (want ? (size_t)a.stride * cfg->experts : 0);
-  if (T == 0) {
-    if (plan) empty_plan_kernel<<<1, kThreads, 0, st>>>(a);
-    return cudaGetLastError() == cudaSuccess ? ASGD_OK : ASGD_ECUDA;
-  }
+  if (T == 0) return !plan || launch_after(empty_plan_kernel, dim3(1), kThreads, 0, st, a) ? ASGD_OK : ASGD_ECUDA;
   const bool one = one_block(cfg, T);
   bool ok = false;
   with_shape(*cfg, [&](auto s, auto l) {

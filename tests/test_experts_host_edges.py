@@ -135,3 +135,12 @@ def test_combine_refuses_arrays_that_are_not_aligned():
     for i in range(4):
         rows, weights, source, dweights = (ODD if i == j else P for j in range(4))
         assert L.asgd_combine_grad(4, 64, 2, P, 1, 64, P, 8, 64, rows, weights, source, P, 64, dweights, None) == EINVAL
+
+
+def test_an_error_is_not_reported_again_by_a_later_call():
+    # without a GPU the first call fails with a CUDA error; a call that launches nothing has none of its own
+    if torch.cuda.is_available():
+        pytest.skip("needs a machine without a GPU")
+    L = experts._load()
+    assert L.asgd_experts_sync(None) == ECUDA
+    assert L.asgd_route(C.byref(_cfg()), 0, None, 0, 64, None, None, None, None, None, None, 0, None, 0, None) == OK
