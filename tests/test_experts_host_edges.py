@@ -1,5 +1,8 @@
 """Refusals of the operators of a layer of experts at the edges of what they take, without a GPU."""
 import ctypes as C
+import os
+import subprocess
+import sys
 
 import pytest
 import torch
@@ -8,6 +11,7 @@ from paper_1505_04956_b200 import binding, experts
 
 from .test_experts_host import _cfg, _p, _q
 
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 EINVAL, EUNSUPPORTED, ECUDA, OK = binding.ASGD_EINVAL, binding.ASGD_EUNSUPPORTED, binding.ASGD_ECUDA, binding.ASGD_OK
 
 
@@ -144,3 +148,17 @@ def test_an_error_is_not_reported_again_by_a_later_call():
     L = experts._load()
     assert L.asgd_experts_sync(None) == ECUDA
     assert L.asgd_route(C.byref(_cfg()), 0, None, 0, 64, None, None, None, None, None, None, 0, None, 0, None) == OK
+
+
+# ---------------------------------------------------------------------------------------------------------------
+# the package
+# ---------------------------------------------------------------------------------------------------------------
+
+def test_the_package_comes_up_without_torch():
+    # what needs torch is loaded when it is asked for: building and the K-Means binding are not to wait for it
+    code = ("import sys; import paper_1505_04956_b200 as pkg; from paper_1505_04956_b200 import build, binding; pkg.load(); "
+            "assert 'torch' not in sys.modules; assert pkg.experts.BLOCK == 128; from paper_1505_04956_b200 import asgd_route; assert pkg.asgd_route is asgd_route; "
+            "assert 'torch' in sys.modules; ns = {}; exec('from paper_1505_04956_b200 import *', ns); "
+            "assert all(n in ns for n in pkg.__all__) and 'asgd_product' in pkg.__all__; "
+            "assert not hasattr(pkg, 'asgd_nothing')")
+    subprocess.run([sys.executable, "-c", code], check=True, cwd=ROOT)
