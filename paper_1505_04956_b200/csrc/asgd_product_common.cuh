@@ -137,7 +137,8 @@ struct Tile {
 };
 
 // What the blocks know of the groups, in shared memory: prefix[g], the tiles (of bm rows) of the groups before g, and
-// start[g], the first row (or K number) of group g.  All threads of the block; ends with a barrier.
+// start[g], the first row (or K number) of group g.  All threads of the block; ends with a barrier.  (Offsets by plain loads:
+// the kernel that writes them may still run when this one comes up, so they are not constant for its life.)
 struct Groups {
   int prefix[ASGD_MAX_EXPERTS + 1], start[ASGD_MAX_EXPERTS + 1], warp_part[32];
 };
@@ -145,7 +146,7 @@ __device__ inline void count_tiles(const Params& p, int bm, Groups& gs) {
   const int G = max(p.groups, 1), tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
   const int limit = p.inner ? p.K : p.M;
   if (p.groups)
-    for (int g = tid; g <= G; g += blockDim.x) gs.start[g] = min(max(__ldg(p.offsets + g), 0), limit);
+    for (int g = tid; g <= G; g += blockDim.x) gs.start[g] = min(max(p.offsets[g], 0), limit);
   else if (tid <= 1) gs.start[tid] = tid ? limit : 0;
   __syncthreads();
   const int per = (G + blockDim.x - 1) / blockDim.x;

@@ -162,3 +162,15 @@ def test_the_package_comes_up_without_torch():
             "assert all(n in ns for n in pkg.__all__) and 'asgd_product' in pkg.__all__; "
             "assert not hasattr(pkg, 'asgd_nothing')")
     subprocess.run([sys.executable, "-c", code], check=True, cwd=ROOT)
+
+
+def test_kernels_that_come_up_early_take_nothing_for_constant():
+    # read-only loads (and const __restrict__, which allows them) promise that nothing writes the memory while the kernel
+    # runs; a kernel that waits for the one before it inside the stream cannot promise that
+    csrc = os.path.join(ROOT, "paper_1505_04956_b200", "csrc")
+    files = [f for f in os.listdir(csrc) if f.startswith(("asgd_route", "asgd_quantize", "asgd_product", "asgd_combine", "asgd_experts"))]
+    assert len(files) >= 8
+    for f in files:
+        text = open(os.path.join(csrc, f)).read()
+        for word in ("__ldg", "__restrict__", "ld.global.nc"):
+            assert word not in text, (f, word)
