@@ -13,7 +13,7 @@
 //
 // Warp roles: 0 issues the TMA loads (128-byte K blocks of both operands, swizzled, through a ring of slots); 1 and 3
 // issue the products, K blocks in turn (a commit holds its thread for several hundred cycles), one commit per K block,
-// which says "the slot is free" and "the accumulator is full"; 2 brings the scales (asynchronous 4-byte copies; a load
+// which says "the slot is free" and "the accumulator is full"; 2 brings the scales (asynchronous copies of 16 or 4 bytes; a load
 // into registers would hold the reading warps); the warps from 4 on read the accumulators (tcgen05.ld: one column of C per thread; with 64 or
 // more tokens two warps share a column's rows) and keep the sums.  Blocks are persistent and take tiles in turn.  Every
 // wait is bounded.

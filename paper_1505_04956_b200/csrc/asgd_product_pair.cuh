@@ -7,19 +7,21 @@
 //
 // Warp roles in each block: 0 issues the TMA loads of the block's halves, which all report to the first block's barrier;
 // 1 and 3, in the first block, issue the products and commit each K block to a barrier in both blocks, which says "the slot
-// is free" to the copies and "the accumulator is full" to the readers; 2 brings the scales (asynchronous 4-byte copies; a
+// is free" to the copies and "the accumulator is full" to the readers; 2 brings the scales (asynchronous copies of 16 or 4 bytes; a
 // load into registers would hold the reading warps); 4 to 11 read the accumulators, a row of C per thread and 128 columns
 // per warp, and add them, scaled, to sums in registers.  Warps 0 to 3 hand most of their registers to these (56 and 224 a
 // thread; with 40 and 232 8192^3 takes 538 us instead of 515, with 72 and 216 a sixth more).  A row's scale and, with
 // 128 x 128 blocks of B, the columns' scale are one number per thread, so that a product of the K block costs one multiply-add.
 //
-// What bounds it: a K block's way round, not a pipe.  Its products take the tensor cores 512 cycles, and about 1000 from
-// their issue until the readers see them; reading them out takes 300 to 380, and the word back to the issuing thread 300.
-// Tensor memory holds two stages of 256 columns, so a K block takes half of that, some 950 cycles, where 512 would be the
-// tensor cores' own rate (products alone, without readers: 570; four stages of 128 columns: 1250, since halves of the columns
-// read the rows of A twice and shared memory is then the bound).  8192 x 8192 x 8192: 515 us (2.13 PFLOP/s; 615 us where the
-// power limit holds the clock near 1.4 GHz), 32 groups of 16384 rows by 2744 x 2064: 142 us (184), of which a fifth is rows of
-// tiles that no group fills and a sixth the way of C through shared memory.  With a scale per column the readers' arithmetic
+// What bounds it: a K block's way round, and the readers' multiply-adds in it.  Its products take the tensor cores 512
+// cycles, and about 1000 from their issue until the readers see them; reading them out, with half of the adds, takes 300 to
+// 380, and the word back to the issuing thread 300.  Tensor memory holds two stages of 256 columns, so a K block takes half of
+// that, some 950 cycles, where 512 would be the tensor cores' own rate (readers that only hand the accumulator back: 564;
+// that load it and do not add: 619; that add without a load: 940; four stages of 128 columns: 1250, since halves of the columns
+// read the rows of A twice and shared memory is then the bound).  On the device: 8192 x 8192 x 8192 510 us (2.16 PFLOP/s; in a
+// user's loop of calls, where the power limit holds the clock near 1.4 GHz, 590 to 609), 32 groups of 16384 rows by 2744 x 2064
+// 145 to 155 us (174 to 186), of which a fifth is rows of tiles that no group fills and a sixth the way of C through shared
+// memory.  With a scale per column the readers' arithmetic
 // is the pace, some 1500 cycles a K block (870 without it): weight gradients of 16 groups, 16384 rows, 2048 x 2048, 131 us.
 // C straight from registers, 32 bytes a thread, took 541 us where the way through shared memory took 525 (8192^3), and
 // 166 where that took 149 (weight gradient).

@@ -3,6 +3,8 @@
 The functions carry the C names and marshal arguments: they check shapes and types, take outputs from torch's
 allocator and pass strides on.  Every number is computed in the library's kernels, on the current CUDA stream or the
 one given; a call's tensors are on the current device (that of the stream, where one is given).
+These are calls of a library: outputs carry no gradient, whatever the inputs ask for, and no autograd function joins a
+forward call with its gradient's.  A caller keeps what the gradient needs and calls it (expert_layer.Layer.gradients).
 
     ids, weights, offsets, rows, source = asgd_route(logits, 8, score="sigmoid", bias=balance, align=128)
     xq, xs = asgd_quantize(x, source=source, per_token=8)                 # tokens in the experts' order, 8 bits
