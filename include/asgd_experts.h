@@ -190,7 +190,7 @@ int asgd_combine_grad(int64_t T, int64_t D, int32_t top_k, const void *dy, int32
  * meanwhile is lost).  With several streams in use, wait for all of them, then call this once for all. */
 int asgd_experts_sync(void *stream);
 /* Failure drill of asgd_product's bounded waits, as asgd_set_wait_drill: later launches of this process give a wait up
- * after wait_limit polls, and with withhold = 1 the first copy of every block is announced but never issued.
+ * after wait_limit polls (copies and products in flight end all the same before a kernel leaves), and with withhold = 1 the first copy of every block is announced but never issued.
  * Defaults 2^22 and 0.  ASGD_EINVAL for wait_limit = 0. */
 int asgd_product_set_wait_drill(uint32_t wait_limit, int32_t withhold);
 

@@ -54,6 +54,11 @@ __device__ inline void commit(unsigned long long* bar) {
 __device__ inline void arrive(unsigned long long* bar) {
   asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_u32(bar)) : "memory");
 }
+__device__ inline unsigned in_block(const void* smem, unsigned rank) {         // the same place in another block of the cluster
+  unsigned a;
+  asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(smem_u32(smem)), "r"(rank));
+  return a;
+}
 __device__ inline void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ inline void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 __device__ inline void copy4(float* dst, const float* src, bool there) {       // asynchronous; zero where not there
@@ -82,6 +87,14 @@ __device__ inline bool wait(unsigned long long* bar, unsigned parity, unsigned l
   }
   *reinterpret_cast<volatile int*>(abort) = 1;
   return false;
+}
+
+// A block in which a wait ran out leaves when its copies and products in flight have ended, whichever thread issued them and
+// whether or not that thread knew.  This wait is bounded as well, by the limit given and by 2^14 polls at
+// least (1.3 ms; a copy or a product takes microseconds).
+__device__ inline void wait_in_flight(unsigned long long* bar, unsigned parity, unsigned limit) {
+  limit = max(limit, 1u << 14);
+  for (unsigned n = 0; n < limit && !mbar_try_wait(bar, parity); ++n) {}
 }
 
 __device__ inline void store_c(void* c, int type, long long at, float v) {

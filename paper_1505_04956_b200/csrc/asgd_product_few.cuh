@@ -55,11 +55,6 @@ __device__ inline unsigned cluster_size() {
 __device__ inline void cluster_sync() {
   asm volatile("barrier.cluster.arrive.release;\nbarrier.cluster.wait.acquire;" ::: "memory");
 }
-__device__ inline unsigned in_block(const void* smem, unsigned rank) {         // the same place in another block of the cluster
-  unsigned a;
-  asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(smem_u32(smem)), "r"(rank));
-  return a;
-}
 __device__ inline float4 load_cluster4(unsigned addr) {
   float4 v;
   asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
@@ -76,7 +71,7 @@ product_few_kernel(const Params p, const __grid_constant__ CUtensorMap map_u, co
   float* scales = reinterpret_cast<float*>(ring + (size_t)S * F::kSlotBytes);          // [slot][kScales]
   unsigned long long* bars = reinterpret_cast<unsigned long long*>(scales + S * F::kScales);
   Groups& gs = *reinterpret_cast<Groups*>(bars + F::COUNT);
-  int* misc = reinterpret_cast<int*>(&gs + 1);                                          // [0] tensor memory, [1] abort
+  int* misc = reinterpret_cast<int*>(&gs + 1);                                          // [0] tensor memory, [1] abort, [2] copies issued
   int* abort = misc + 1;
   const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
   const int rank = kSplit ? (int)cluster_rank() : 0, share = kSplit ? (int)cluster_size() : 1;
@@ -133,11 +128,7 @@ product_few_kernel(const Params p, const __grid_constant__ CUtensorMap map_u, co
           }
         }
       }
-      if (!ok)                                       // copies in flight land before the block leaves
-        for (unsigned q = 0; q < S && q < it; ++q) {
-          const unsigned last = (it - 1 - q) / S;    // the slot's last use
-          for (unsigned n = 0; n < p.wait_limit && !mbar_try_wait(bars + F::FULL + q, last & 1); ++n) {}
-        }
+      misc[2] = (int)it;                             // K blocks whose copies were issued
     }
   } else if (wid == 1 || wid == 3) {
     if (lane == 0) {
@@ -158,10 +149,6 @@ product_few_kernel(const Params p, const __grid_constant__ CUtensorMap map_u, co
           for (int k4 = 0; k4 < 4; ++k4) if (k4 < steps) mma_f8(tmem + stage * BN, du + 2 * k4, dv + 2 * k4, p.idesc, k4 != 0);
           commit(bars + F::DONE + q);
         }
-      }
-      if (!ok && it) {                               // products in flight end before the tensor memory is freed
-        commit(bars + F::DRAIN + me);
-        for (unsigned n = 0; n < p.wait_limit && !mbar_try_wait(bars + F::DRAIN + me, 0); ++n) {}
       }
     }
   } else if (wid == 2) {
@@ -274,6 +261,17 @@ product_few_kernel(const Params p, const __grid_constant__ CUtensorMap map_u, co
     __syncthreads();
   }
   fence_after();
+  if (*reinterpret_cast<volatile int*>(abort)) {     // a wait ran out: what is in flight ends first
+    if (wid == 0 && lane == 0) {
+      const unsigned issued = (unsigned)misc[2];
+      for (unsigned q = 0; q < S && q < issued; ++q) wait_in_flight(bars + F::FULL + q, ((issued - 1 - q) / S) & 1, p.wait_limit);      // a slot's last use
+    } else if ((wid == 1 || wid == 3) && lane == 0) {
+      commit(bars + F::DRAIN + (wid >> 1));
+      wait_in_flight(bars + F::DRAIN + (wid >> 1), 0, p.wait_limit);
+    }
+    __syncthreads();
+    fence_after();
+  }
   if (wid == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(F::kCols));
   if (tid == 0 && *reinterpret_cast<volatile int*>(abort)) atomicMin(&g_status, ASGD_ETIMEOUT);
 }

@@ -52,11 +52,6 @@ __device__ inline unsigned full_of(unsigned it) { return P_FULL + (it & 1) * kPa
 __device__ inline unsigned full_phase(unsigned it) { return it / (2 * kPairSlots) & 1; }
 static_assert(kPairSlots % 2 == 1, "a slot meets the issuing threads in turn");
 
-__device__ inline unsigned in_first_block(const void* smem) {                  // the same place in the pair's first block
-  unsigned r;
-  asm("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(r) : "r"(smem_u32(smem)));
-  return r;
-}
 __device__ inline unsigned rank_in_pair() {
   unsigned r;
   asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
@@ -218,7 +213,7 @@ product_pair_kernel(const Params p, const __grid_constant__ CUtensorMap map_a, c
   float* scales = reinterpret_cast<float*>(stages + 8 * kStageBytes);                   // [slot][kScales]
   unsigned long long* bars = reinterpret_cast<unsigned long long*>(scales + S * kScales);
   Groups& gs = *reinterpret_cast<Groups*>(bars + P_COUNT);
-  int* misc = reinterpret_cast<int*>(&gs + 1);        // [0] tensor memory, [1] abort, [2, 3] K blocks whose copies each block has issued, [4] the other block gave up
+  int* misc = reinterpret_cast<int*>(&gs + 1);        // [0] tensor memory, [1] abort, [2, 3] K blocks whose copies each block has issued, [4] one of the blocks gave up
   int* abort = misc + 1;
   const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
   const unsigned rank = rank_in_pair();
@@ -250,7 +245,7 @@ product_pair_kernel(const Params p, const __grid_constant__ CUtensorMap map_a, c
   if (wid < 4) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
     if (wid == 0 && lane == 0) {
-      const unsigned bars0 = in_first_block(bars);
+      const unsigned bars0 = in_block(bars, 0);
       unsigned it = 0;
       bool ok = true;
       for (int tile = pair; tile < tiles && ok; tile += pairs) {
@@ -268,7 +263,7 @@ product_pair_kernel(const Params p, const __grid_constant__ CUtensorMap map_a, c
           }
         }
       }
-      store_cluster(in_first_block(misc + 2 + rank), it);
+      store_cluster(in_block(misc + 2 + rank, 0), it);
     } else if ((wid == 1 || wid == 3) && lane == 0 && rank == 0) {
       // Two issuing threads, one per accumulator stage, K blocks in turn: a commit holds the thread that issues it for
       // several hundred cycles, and the other thread's products fill the gap.
@@ -292,10 +287,6 @@ product_pair_kernel(const Params p, const __grid_constant__ CUtensorMap map_a, c
           for (int k4 = 0; k4 < 4; ++k4) if (k4 < steps) mma_f8_pair(tmem + stage * kPairCols, da + 2 * k4, db + 2 * k4, p.idesc, k4 != 0);
           commit_pair(bars + P_DONE + q);
         }
-      }
-      if (!ok && it) {                               // products in flight end before the tensor memory is freed
-        commit_pair(bars + P_DRAIN + me);
-        for (unsigned n = 0; n < p.wait_limit && !mbar_try_wait(bars + P_DRAIN + me, 0); ++n) {}
       }
     } else if (wid == 2) {
       const LaneGroups lg(p, gs, lane);
@@ -331,7 +322,7 @@ product_pair_kernel(const Params p, const __grid_constant__ CUtensorMap map_a, c
   } else {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 224;");
     const int quarter = wid & 3, half = (wid - 4) >> 2;
-    const unsigned free0 = in_first_block(bars + P_ACCEMPTY);
+    const unsigned free0 = in_block(bars + P_ACCEMPTY, 0);
     const unsigned at_tmem = tmem + ((unsigned)(quarter * 32) << 16) + half * 128;
     unsigned char* stage_smem = stages + (wid - 4) * kStageBytes;
     const LaneGroups lg(p, gs, lane);
@@ -430,8 +421,12 @@ product_pair_kernel(const Params p, const __grid_constant__ CUtensorMap map_a, c
     __syncwarp();
   }
   // Both blocks are through.  Where one gave up, the first block settles its barriers: bytes announced that nobody will
-  // send, copies issued that nobody announced; then every copy in flight has landed when the last phases are complete.
-  if (*reinterpret_cast<volatile int*>(abort) && lane == 0) store_cluster(in_first_block(misc + 4), 1);
+  // send, copies issued that nobody announced; then every copy in flight has landed when the last phases are complete.  The
+  // products, and the word of them in both blocks, end as well.
+  if (*reinterpret_cast<volatile int*>(abort) && lane == 0) {
+    store_cluster(in_block(misc + 4, 0), 1);
+    store_cluster(in_block(misc + 4, 1), 1);
+  }
   fence_before();
   pair_sync();
   fence_after();
@@ -443,9 +438,13 @@ product_pair_kernel(const Params p, const __grid_constant__ CUtensorMap map_a, c
     }
     if (p.withhold && last) complete_tx(bars + full_of(0), ((mine > 0) + (other > 0)) * kPairBytes);
     for (unsigned i = last > 2 * S ? last - 2 * S : 0; i < last; ++i)          // every barrier's last use
-      for (unsigned n = 0; n < p.wait_limit && !mbar_try_wait(bars + full_of(i), full_phase(i)); ++n) {}
+      wait_in_flight(bars + full_of(i), full_phase(i), p.wait_limit);
     atomicMin(&g_status, ASGD_ETIMEOUT);
+  } else if ((wid == 1 || wid == 3) && lane == 0 && *reinterpret_cast<volatile int*>(misc + 4)) {
+    if (rank == 0) commit_pair(bars + P_DRAIN + (wid >> 1));
+    wait_in_flight(bars + P_DRAIN + (wid >> 1), 0, p.wait_limit);
   }
+  __syncwarp();
   pair_sync();
   if (wid == 1) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u));
 }

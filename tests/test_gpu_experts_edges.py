@@ -360,3 +360,35 @@ def test_a_padded_plan_is_fed_on(T, E, top_k, D, N, popular):
         s = slice(at[e], at[e + 1])
         _check_product(dwt[e], a64[:, s], b64[:, s], at[e + 1] - at[e], F32)
     pkg.asgd_experts_sync()
+
+
+@pytest.mark.parametrize("withhold", [False, True])
+@pytest.mark.parametrize("M, N, K, inner", [(8, 512, 1024, 0), (5, 256, 512, 0), (60, 4096, 4096, 0), (600, 1024, 1024, 0), (2500, 2048, 2048, 0), (600, 520, 40 * 128, 40)])
+def test_waits_given_up_at_any_time_leave_nothing_in_flight(M, N, K, inner, withhold):
+    # a wait given up after a few polls runs out anywhere in the kernel, with copies and products on their way
+    a, sa = _operand(M, K, E4, 1)
+    b, sb = _operand(N, K, E4, 2, not inner)
+    offsets = (torch.arange(inner + 1) * (K // max(inner, 1))).to(torch.int32).cuda()
+
+    def call():
+        if inner:
+            return pkg.asgd_product_inner(a, sa, b, sb, offsets)
+        return pkg.asgd_product(a, sa, b, sb, out_dtype=F32)
+    want = call()
+    pkg.asgd_experts_sync()
+    ran_out = 0
+    for limit in (1, 2, 3, 5, 9, 17, 40, 100, 300):
+        try:
+            pkg.asgd_product_set_wait_drill(limit, withhold)
+            got = call()
+            try:
+                pkg.asgd_experts_sync()
+                assert not withhold and torch.equal(got, want)
+            except binding.AsgdError as err:
+                assert err.status == binding.ASGD_ETIMEOUT
+                ran_out += 1
+        finally:
+            pkg.asgd_product_set_wait_drill()
+        assert torch.equal(call(), want)
+        pkg.asgd_experts_sync()
+    assert ran_out == 9 if withhold else ran_out <= 9
