@@ -16,6 +16,7 @@ from . import inputs
 from .binding import Asgd, make_config
 from .experts import (asgd_combine, asgd_combine_grad, asgd_experts_sync, asgd_product, asgd_product_inner, asgd_quantize, asgd_route,
                       asgd_route_grad)
+from .gradients import asgd_clip_grads
 
 ALIGN = 128                     # grouped rows per block of the weight gradients' sums
 E5M2 = torch.float8_e5m2        # gradients have the wider range
@@ -84,11 +85,14 @@ class Layer:
         dx = asgd_combine(dxg, c["rows"]) + self.temperature * dlogits @ self.router
         return self.temperature * dlogits.t() @ x, dw1, dw2, dx
 
-    def step(self, x, target, rate, balance=0.002):
-        """One step of gradient descent on the mean squared error; returns it (a tensor) and the experts' loads."""
+    def step(self, x, target, rate, balance=0.002, max_norm=None):
+        """One step of gradient descent on the mean squared error, its gradients clipped to `max_norm` together where that is given;
+        returns the error (a tensor) and the experts' loads."""
         y, c = self.forward(x)
         diff = y - target
         drouter, dw1, dw2, _ = self.gradients(x, diff * (2.0 / diff.numel()), c)
+        if max_norm is not None:
+            asgd_clip_grads((drouter, dw1, dw2), max_norm)
         self.router -= 0.05 * rate * drouter                    # the centres are learnt already
         self.w1 -= rate * dw1
         self.w2 -= rate * dw2
@@ -119,12 +123,12 @@ def make_task(tokens, d, clusters, seed=0):
     return X, target
 
 
-def main(tokens=8192, d=256, experts=8, hidden=512, steps=60, rate=1.0):
+def main(tokens=8192, d=256, experts=8, hidden=512, steps=60, rate=1.0, max_norm=None):
     X, target = make_task(tokens, d, experts)
     layer = make_layer(X, experts, hidden)
     first = last = None
     for i in range(steps):
-        loss, loads = layer.step(X, target, rate)
+        loss, loads = layer.step(X, target, rate, max_norm=max_norm)
         if i % 10 == 0 or i == steps - 1:
             last = float(loss)
             first = last if first is None else first
