@@ -4,13 +4,12 @@
 // A scale belongs to 128 neighbours along K, so the products of one K block go into a fresh accumulator in tensor
 // memory (four tcgen05.mma of K = 32), and threads add them, scaled, to sums they keep in registers while the tensor
 // cores fill the other accumulator stage.
-#include <cudaTypedefs.h>
-
 #include <algorithm>
 #include <atomic>
 #include <cmath>
 #include <mutex>
 
+#include "asgd_maps.cuh"
 #include "asgd_product_few.cuh"
 #include "asgd_product_pair.cuh"
 
@@ -28,51 +27,12 @@ __global__ void take_status_kernel() {
 
 // ---- host ----
 
-PFN_cuTensorMapEncodeTiled encoder() {
-  static std::atomic<PFN_cuTensorMapEncodeTiled> known{nullptr};
-  PFN_cuTensorMapEncodeTiled f = known.load();
-  if (!f) {
-    void* fn = nullptr;
-    cudaDriverEntryPointQueryResult q;
-    if (!good(cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &q)) || !fn) return nullptr;
-    f = (PFN_cuTensorMapEncodeTiled)fn;
-    known.store(f);
-  }
-  return f;
-}
-// a matrix [outer][rows][cols]; strides in bytes; what lies beyond is read as zeros and not written
-bool encode(CUtensorMap* map, CUtensorMapDataType type, CUtensorMapSwizzle swizzle, const void* base, long long cols, long long rows, long long outer,
-            long long row_bytes, long long outer_bytes, unsigned box_cols, unsigned box_rows) {
-  const PFN_cuTensorMapEncodeTiled f = encoder();
-  if (!f) return false;
-  cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)outer};
-  cuuint64_t strides[2] = {(cuuint64_t)row_bytes, (cuuint64_t)(outer > 1 ? outer_bytes : row_bytes)};
-  cuuint32_t box[3] = {box_cols, box_rows, 1};
-  cuuint32_t estr[3] = {1, 1, 1};
-  return f(map, type, 3, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
-           CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
-// 128-byte K blocks of an 8-bit operand
-bool encode(CUtensorMap* map, const void* base, long long cols, long long rows, long long outer, long long ld, long long outer_stride, unsigned box_rows) {
-  return encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, CU_TENSOR_MAP_SWIZZLE_128B, base, cols, rows, outer, ld, outer_stride, kKB, box_rows);
-}
-
 constexpr long long kMostTiles = 0x7fffffffll - 2 * kSMs;    // a block's next tile number stays inside 32 bits
 
 // the most tiles of bm x bn there can be: what the offsets say is known on the device alone
 long long most_tiles(const Params& p, int bm, int bn) {
   const long long rows = p.inner ? ceil_div(p.M, bm) * p.groups : ceil_div(p.M, bm) + p.groups;
   return rows * ceil_div(p.N, bn);
-}
-// Raises a kernel's shared-memory limit, once per device (`done`: a bit per device, of this kernel).
-template <typename K> bool allow_smem(K kernel, size_t bytes, std::atomic<unsigned long long>& done) {
-  int dev = 0;
-  if (!good(cudaGetDevice(&dev))) return false;
-  const unsigned long long bit = 1ull << (dev & 63);
-  if (dev < 64 && (done.load() & bit)) return true;
-  if (!good(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes))) return false;
-  done.fetch_or(bit);
-  return true;
 }
 // fp32 accumulators; formats of the MMA's first and second operand (0 = E4M3, 1 = E5M2); its columns and rows
 unsigned instruction(int type0, int type1, int cols, int rows) {
@@ -174,6 +134,23 @@ Kernel choose(const Params& p) {
 }
 
 }  // namespace
+
+// For the kernels of other sources that report to the same word and take the same drill (asgd_maps.cuh).
+namespace asgd {
+namespace experts {
+WaitDrill wait_drill() { return {g_wait_limit.load(), g_withhold.load()}; }
+int* status_word() {
+  static std::atomic<int*> known[64];
+  int dev = 0;
+  if (!good(cudaGetDevice(&dev))) return nullptr;
+  if (dev < 64 && known[dev].load()) return known[dev].load();
+  void* at = nullptr;
+  if (!good(cudaGetSymbolAddress(&at, g_status))) return nullptr;
+  if (dev < 64) known[dev].store(reinterpret_cast<int*>(at));
+  return reinterpret_cast<int*>(at);
+}
+}  // namespace experts
+}  // namespace asgd
 
 extern "C" int asgd_product(const asgd_product_args* args, void* stream) {
   if (!args) return ASGD_EINVAL;
