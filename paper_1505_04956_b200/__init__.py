@@ -2,9 +2,8 @@
 
 `binding` wraps the C ABI of libasgd.so one to one; `inputs` draws seeded synthetic workloads;
 `build` compiles the library in-tree.  `experts` holds the operators of a layer of experts behind learnt
-centres: routing, 8-bit operands and products, combination; `fp4` has 4-bit
-operands and products, `gradients` the norm of many gradients and clipping.
-Nothing here computes on the CPU.
+centres: routing, 8-bit operands and products, combination; `serving` is the whole layer for a few tokens, `fp4` has 4-bit
+operands and products, `gradients` the norm of many gradients and clipping.  Nothing here computes on the CPU.
 """
 import importlib
 
@@ -17,7 +16,8 @@ _EXPERTS = ("EXPERT_EXPORTS", "asgd_combine", "asgd_combine_grad", "asgd_experts
             "asgd_product_set_wait_drill", "asgd_quantize", "asgd_route", "asgd_route_grad")
 _GRADIENTS = ("GRADIENT_EXPORTS", "asgd_clip_grads", "asgd_grad_norm")
 _FP4 = ("FP4_EXPORTS", "asgd_dequantize4", "asgd_product4", "asgd_quantize4")
-_MODULE_OF = {name: module for module, names in (("experts", _EXPERTS), ("fp4", _FP4), ("gradients", _GRADIENTS)) for name in names}
+_SERVING = ("LAYER_EXPORTS", "asgd_expert_layer")
+_MODULE_OF = {name: module for module, names in (("experts", _EXPERTS), ("fp4", _FP4), ("gradients", _GRADIENTS), ("serving", _SERVING)) for name in names}
 
 __all__ = ["Asgd", "AsgdConfig", "AsgdError", "make_config", "asgd_workspace_bytes", "asgd_fit_host",
            "asgd_fit_host_bytes", "asgd_eval_noalloc", "load", "LIB_PATH", "EXPORTS", "PATH_AUTO", "PATH_FP32", "PATH_TC_FP16",

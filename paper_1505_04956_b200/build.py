@@ -9,7 +9,7 @@ PKG = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libasgd.so")
 SOURCES = ["asgd_api.cu", "asgd_noalloc.cu", "asgd_route.cu", "asgd_quantize.cu", "asgd_product.cu", "asgd_combine.cu",
-           "asgd_gradients.cu", "asgd_fp4.cu", "asgd_product4.cu"]
+           "asgd_gradients.cu", "asgd_fp4.cu", "asgd_product4.cu", "asgd_expert_layer.cu"]
 OBJ = os.path.join(PKG, "_build")
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",

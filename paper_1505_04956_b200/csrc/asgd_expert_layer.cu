@@ -1,0 +1,765 @@
+// A whole layer of experts for a few tokens in one kernel.  The contract is in include/asgd_expert_layer.h.
+//
+// The bytes of the weights of the experts in use are the bound, so the design keeps them coming.  One block per SM, all at
+// once.  The K blocks (128 columns of W by 128 rows) of all tiles of W1 that any token needs count as one run, and each block
+// takes an equal stretch of it, wherever tiles begin and end; the same again with W2.  A block's copies of weights run ahead through
+// a ring of slots, W2's behind W1's, whatever the tokens' side is waiting for: while blocks meet between the two
+// products, some 150 KB of weights per SM are in flight or there already.
+//
+// The steps:
+//   0  logits (with a router) and the tokens in 8 bits, by all warps of all blocks.   -- blocks meet
+//   1  every block chooses the experts of all tokens for itself, and lists the rows by expert (integers and a few numbers
+//      per token; cheaper than to hand them round).  Then its stretch of W1: sums of partial tiles go to the workspace.  -- blocks meet
+//   2  sums of a tile's stretches in the blocks' order, activation, 8 bits.   -- blocks meet (the copies of W2 went on)
+//   3  its stretch of W2, sums to the workspace.   -- blocks meet
+//   4  sums of the stretches and of a token's experts in their order, y.
+// No sum depends on timing: every order is fixed by the sizes and the loads.
+//
+// A tile is 128 rows of W (the MMA's M) by BN tokens of one expert (its N; an expert with more has several chunks); a
+// K block's products leave tensor memory and are added, scaled, in registers, as in asgd_product_few.cuh.
+//
+// Warp roles after step 0: 0 issues the copies of weights; 1 and 3 issue the products, K blocks in turn; 2 brings the tokens'
+// rows (gathered, 16-byte asynchronous copies into the swizzled layout that a tensor map would write) and the scales; 4 to 11
+// read the accumulators, and do steps 2 and 4.  Every wait is bounded, those of blocks for one another too.
+#include <algorithm>
+
+#include "../../include/asgd_expert_layer.h"
+#include "asgd_choose.cuh"
+#include "asgd_maps.cuh"
+#include "asgd_product_few.cuh"
+
+namespace {
+
+constexpr int kThreads = 384, kWarps = kThreads / 32, kReaders = 8;
+constexpr int kAhead = 4;                            // K blocks of tokens' rows in flight
+constexpr int kMostRows = ASGD_LAYER_MAX_ASSIGNMENTS;
+constexpr int kTokenWords = ASGD_LAYER_MAX_TOKENS / 32;
+enum { MEET_TOKENS, MEET_SUMS, MEET_HIDDEN, MEET_OUT, MEETINGS };
+
+// What the blocks of a launch share, at the workspace's start; zeros before it.
+struct Shared {
+  struct { unsigned count, pad[31]; } meeting[MEETINGS];
+  unsigned gave_up, pad[31];
+};
+
+struct Matrix {                                      // W1 or W2
+  int tiles, kblocks;                                // of 128 rows, of 128 columns
+  const float* scale;
+  long long row, block, group;
+  unsigned idesc;
+};
+
+struct LayerArgs : Choice {
+  int T, d, h, rows1, gated, silu;
+  const void* x;
+  long long ldx;
+  int type, x_wide;                                  // rows of x start at four numbers' alignment
+  void* y;
+  long long ldy;
+  const void* logits;
+  long long ld_logits;
+  int logits_type;
+  const void* router;
+  long long ld_router;
+  int router_type, router_wide;
+  const float* shift;
+  float temperature;
+  Matrix w[2];
+  int* ids;
+  float* weights;
+  // workspace
+  Shared* shared;
+  float* made_logits;                                // [T][E]
+  unsigned char* xq;                                 // [T][w[0].kblocks * 128]
+  float* xs;                                         // [T][w[0].kblocks]
+  unsigned char* hq;                                 // [rows][w[1].kblocks * 128]
+  float* hs;
+  float* sums;                                       // [rows of all tiles + BN per block][128]
+  unsigned wait_limit;
+  int withhold;
+  int* status;
+};
+
+template <int BN> struct Layer {
+  static constexpr int kSlots = BN == 64 ? 8 : 10;   // even: a slot always meets the same issuing thread
+  static constexpr unsigned kWeights = kU * kKB, kTokens = BN * kKB, kSlotBytes = kWeights + kTokens;
+  static constexpr int kScales = BN + 4;             // of a slot: the tokens', then the weights' one
+  static constexpr int kRows = BN / 2;               // tokens of a tile that a reading thread has
+  static constexpr unsigned kCols = kAccStages * BN;
+  enum { FULL = 0, READY = kSlots, DONE = 2 * kSlots, SEMPTY = 3 * kSlots, ACCEMPTY = 4 * kSlots, DRAIN = ACCEMPTY + kAccStages, COUNT = DRAIN + 2 };
+  static constexpr size_t kRing = (size_t)kSlots * kSlotBytes;
+  static constexpr size_t kSmem = 1024 + kRing + (size_t)kSlots * kScales * 4 + COUNT * 8;
+  static_assert(kSlots > kAhead, "copies of tokens' rows are handed over before their slots come round");
+  static_assert(kSlots % 2 == 0 && kCols >= 32, "slots, tensor memory");
+};
+
+// The rows (assignments) in the experts' order.
+struct Plan {
+  short ids[kMostRows];                              // of an assignment
+  float weights[kMostRows];
+  short order[kMostRows];                            // the assignment of a row
+  short row_of[kMostRows];                           // the row of an assignment, -1: none
+  short chunk_of[kMostRows];                         // of a row
+  short expert[kMostRows], first[kMostRows], rows[kMostRows];      // of a chunk
+  int part[2][kWarps];
+  int chunks, total_rows;
+};
+// While the plan is made, where the ring will be.
+struct Making {
+  unsigned scratch[kWarps][kScratch];
+  unsigned mask[ASGD_MAX_EXPERTS][kTokenWords];      // the tokens of an expert
+  int start[ASGD_MAX_EXPERTS], chunk[ASGD_MAX_EXPERTS];
+};
+constexpr size_t kMost = 227 * 1024 - sizeof(Plan) - 64;
+static_assert(Layer<16>::kSmem <= kMost && Layer<32>::kSmem <= kMost && Layer<64>::kSmem <= kMost, "shared memory");
+static_assert(sizeof(Making) <= Layer<16>::kRing, "the plan is made where the ring will be");
+
+// ---- blocks that wait for one another ----
+
+__device__ __forceinline__ void come(unsigned* count) { asm volatile("red.release.gpu.global.add.u32 [%0], 1;" ::"l"(count) : "memory"); }
+__device__ __forceinline__ unsigned look(const unsigned* p) {
+  unsigned v;
+  asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(v) : "l"(p) : "memory");
+  return v;
+}
+// by one thread: all blocks have come
+__device__ inline bool meet(Shared* sh, int which, unsigned limit, int* abort) {
+  limit = max(limit, 1u << 10);                      // a drill that gives copies up after a few polls still lets blocks meet
+  for (unsigned it = 0; it < limit; ++it) {
+    if (look(&sh->meeting[which].count) >= gridDim.x) return true;
+    if ((it & 15u) == 15u && (*reinterpret_cast<volatile int*>(abort) || look(&sh->gave_up))) break;
+    __nanosleep(20);
+  }
+  *reinterpret_cast<volatile int*>(abort) = 1;
+  return false;
+}
+
+// ---- tokens ----
+
+// four numbers from number `at` of a row on, zeros from `end` on
+template <typename T> __device__ __forceinline__ float4 four(const T* row, int at, int end, bool wide) {
+  float v[4];
+  if (wide && at + 4 <= end) {
+    if constexpr (sizeof(T) == 4) return *reinterpret_cast<const float4*>(row + at);
+    else {
+      const uint2 u = *reinterpret_cast<const uint2*>(row + at);
+      const T* e = reinterpret_cast<const T*>(&u);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[i] = Elem<T>::to_f(e[i]);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = at + i < end ? Elem<T>::to_f(row[at + i]) : 0.f;
+  }
+  return make_float4(v[0], v[1], v[2], v[3]);
+}
+__device__ __forceinline__ float4 four(const void* base, int type, long long row, int at, int end, bool wide) {
+  if (type == ASGD_F32) return four(reinterpret_cast<const float*>(base) + row, at, end, wide);
+  if (type == ASGD_BF16) return four(reinterpret_cast<const __nv_bfloat16*>(base) + row, at, end, wide);
+  return four(reinterpret_cast<const __half*>(base) + row, at, end, wide);
+}
+__device__ __forceinline__ float one(const void* base, int type, long long at) {
+  if (type == ASGD_F32) return reinterpret_cast<const float*>(base)[at];
+  if (type == ASGD_BF16) return __bfloat162float(reinterpret_cast<const __nv_bfloat16*>(base)[at]);
+  return __half2float(reinterpret_cast<const __half*>(base)[at]);
+}
+
+// A warp rounds a block of 128 numbers, four per lane, as asgd_quantize does (E4M3).
+__device__ __forceinline__ void round_block(const float4& v, unsigned char* q, float* scale, int lane) {
+  float m = fmaxf(fmaxf(fabsf(v.x), fabsf(v.y)), fmaxf(fabsf(v.z), fabsf(v.w)));
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(kAll, m, o));
+  m = fmaxf(m, 7.888609052210118e-31f);              // 2^-100
+  const float inv = __fdiv_rn(448.f, m);
+  const unsigned lo = __nv_cvt_float2_to_fp8x2(make_float2(v.x * inv, v.y * inv), __NV_SATFINITE, __NV_E4M3);
+  const unsigned hi = __nv_cvt_float2_to_fp8x2(make_float2(v.z * inv, v.w * inv), __NV_SATFINITE, __NV_E4M3);
+  reinterpret_cast<unsigned*>(q)[lane] = lo | hi << 16;
+  if (lane == 0) *scale = __fmul_rn(m, 1.f / 448.f);
+}
+
+// Logits of a router: four warps share a row of it and up to eight tokens; a block has three such groups of warps.
+constexpr int kLogitTokens = 8, kLogitWarps = 4, kLogitGroups = kWarps / kLogitWarps;
+__device__ inline void make_logits(const LayerArgs& a, float (*part)[kLogitWarps][kLogitTokens], int lane, int wid) {
+  const int E = a.c.experts, sets = (a.T + kLogitTokens - 1) / kLogitTokens, units = E * sets, group = wid / kLogitWarps, sub = wid % kLogitWarps;
+  const int per = kLogitGroups * (int)gridDim.x;
+  for (int u0 = (int)blockIdx.x * kLogitGroups; u0 < units; u0 += per) {
+    const int u = u0 + group, e = u / sets, t0 = u % sets * kLogitTokens, n = u < units ? min(kLogitTokens, a.T - t0) : 0;
+    float acc[kLogitTokens];
+#pragma unroll
+    for (int t = 0; t < kLogitTokens; ++t) acc[t] = 0.f;
+    if (n > 0) {
+#pragma unroll 4
+      for (int k = (sub * 32 + lane) * 4; k < a.d; k += kLogitWarps * 128) {
+        const float4 r = four(a.router, a.router_type, e * a.ld_router, k, a.d, a.router_wide);
+#pragma unroll
+        for (int t = 0; t < kLogitTokens; ++t)
+          if (t < n) {
+            const float4 v = four(a.x, a.type, (t0 + t) * a.ldx, k, a.d, a.x_wide);
+            acc[t] = fmaf(v.x, r.x, fmaf(v.y, r.y, fmaf(v.z, r.z, fmaf(v.w, r.w, acc[t]))));
+          }
+      }
+    }
+#pragma unroll
+    for (int t = 0; t < kLogitTokens; ++t) {
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) acc[t] += __shfl_xor_sync(kAll, acc[t], o);
+      if (lane == 0) part[group][sub][t] = acc[t];
+    }
+    __syncthreads();
+    if (sub == 0 && lane < n) {
+      float s = part[group][0][lane];
+#pragma unroll
+      for (int w = 1; w < kLogitWarps; ++w) s += part[group][w][lane];
+      a.made_logits[(long long)(t0 + lane) * E + e] = (s - (a.shift ? a.shift[e] : 0.f)) * a.temperature;
+    }
+    __syncthreads();
+  }
+}
+
+// ---- the choice and the plan, by the whole block ----
+
+template <int S> __device__ __forceinline__ void choose_all(const LayerArgs& a, Plan& plan, Making& m, int lane, int wid) {
+  const int E = a.c.experts, K = a.c.top_k;
+  for (int t = wid; t < a.T; t += kWarps) {
+    float x[S];
+#pragma unroll
+    for (int j = 0; j < S; ++j) {
+      const int e = j * 32 + lane;
+      x[j] = e >= E ? -INFINITY : a.made_logits ? __ldcg(a.made_logits + (long long)t * E + e) : one(a.logits, a.logits_type, t * a.ld_logits + e);
+    }
+    int place, id;
+    float w;
+    choose<S, 32>(a, x, lane, m.scratch[wid], place, id, w);
+    if (place >= 0) {
+      plan.ids[t * K + place] = (short)id;
+      plan.weights[t * K + place] = w;
+      if (id >= 0) atomicOr(&m.mask[id][t >> 5], 1u << (t & 31));
+      if (blockIdx.x == 0 && a.ids) a.ids[t * K + place] = id;
+      if (blockIdx.x == 0 && a.weights) a.weights[t * K + place] = w;
+    }
+  }
+}
+template <int BN> __device__ inline void make_plan(const LayerArgs& a, Plan& plan, Making& m, int tid, int lane, int wid) {
+  const int E = a.c.experts, K = a.c.top_k, n = a.T * K;
+  for (int i = tid; i < E * kTokenWords; i += kThreads) (&m.mask[0][0])[i] = 0;
+  __syncthreads();
+  if (E <= 128) choose_all<4>(a, plan, m, lane, wid);
+  else if (E <= 256) choose_all<8>(a, plan, m, lane, wid);
+  else choose_all<32>(a, plan, m, lane, wid);
+  __syncthreads();
+  // rows and chunks before each expert
+  constexpr int kPer = (ASGD_MAX_EXPERTS + kThreads - 1) / kThreads;
+  int mine = 0, mine_chunks = 0, count[kPer];
+#pragma unroll
+  for (int q = 0; q < kPer; ++q) {
+    const int e = tid * kPer + q;
+    count[q] = 0;
+    if (e < E)
+#pragma unroll
+      for (int w = 0; w < kTokenWords; ++w) count[q] += __popc(m.mask[e][w]);
+    mine += count[q];
+    mine_chunks += (count[q] + BN - 1) / BN;
+  }
+  int inc = mine, inc_chunks = mine_chunks;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int v = __shfl_up_sync(kAll, inc, o), w = __shfl_up_sync(kAll, inc_chunks, o);
+    if (lane >= o) { inc += v; inc_chunks += w; }
+  }
+  if (lane == 31) { plan.part[0][wid] = inc; plan.part[1][wid] = inc_chunks; }
+  __syncthreads();
+  int run = inc - mine, chunk = inc_chunks - mine_chunks;
+  for (int w = 0; w < wid; ++w) { run += plan.part[0][w]; chunk += plan.part[1][w]; }
+#pragma unroll
+  for (int q = 0; q < kPer; ++q) {
+    const int e = tid * kPer + q;
+    if (e < E) m.start[e] = run;
+    for (int r = 0; r < count[q]; r += BN, ++chunk) {
+      const int rows = min(BN, count[q] - r);
+      plan.expert[chunk] = (short)e;
+      plan.first[chunk] = (short)(run + r);
+      plan.rows[chunk] = (short)rows;
+      for (int i = 0; i < rows; ++i) plan.chunk_of[run + r + i] = (short)chunk;
+    }
+    run += count[q];
+  }
+  if (tid == kThreads - 1) { plan.total_rows = run; plan.chunks = chunk; }
+  __syncthreads();
+  for (int i = tid; i < n; i += kThreads) {
+    const int e = plan.ids[i], t = i / K;
+    int r = -1;
+    if (e >= 0) {
+      r = m.start[e];
+#pragma unroll
+      for (int w = 0; w < kTokenWords; ++w) {
+        const int b = t - 32 * w;
+        r += __popc(m.mask[e][w] & (b >= 32 ? kAll : b > 0 ? (1u << b) - 1u : 0u));
+      }
+      plan.order[r] = (short)i;
+    }
+    plan.row_of[i] = (short)r;
+  }
+  __syncthreads();
+}
+
+// ---- stretches ----
+
+// Blocks that a matrix's K blocks are dealt out to: with one at least, so that no block between two others has nothing.
+__device__ __forceinline__ unsigned dealt(unsigned all) { return min(all, gridDim.x); }
+// A block's K blocks of all tiles of a matrix.
+struct Stretch {
+  unsigned from, to;
+  int chunk, tile, kb;                               // where it is
+  __device__ __forceinline__ Stretch(const Matrix& w, int chunks) {
+    const unsigned all = (unsigned)chunks * w.tiles * w.kblocks;
+    const unsigned n = dealt(all), b = min(blockIdx.x, n);
+    from = all * b / n;
+    to = b < n ? all * (b + 1) / n : from;
+    const unsigned t = from / w.kblocks;
+    kb = (int)(from - t * w.kblocks);
+    chunk = (int)(t / w.tiles);
+    tile = (int)(t - chunk * w.tiles);
+  }
+  __device__ __forceinline__ bool there() const { return from < to; }
+  __device__ __forceinline__ void next(const Matrix& w) {
+    ++from;
+    if (++kb == w.kblocks) {
+      kb = 0;
+      if (++tile == w.tiles) { tile = 0; ++chunk; }
+    }
+  }
+};
+// Sums of a tile's rows: in front of them those of all tiles before it, and BN for every block that ended a stretch before.
+template <int BN> __device__ __forceinline__ long long sums_at(const Plan& plan, const Matrix& w, int chunk, int tile, int block) {
+  return (long long)plan.first[chunk] * w.tiles + tile * plan.rows[chunk] + block * BN;
+}
+// What a number of a tile's result is: four neighbouring ones of a row, over the blocks that have a part in the tile.
+template <int BN> struct Sum {
+  const float* at;
+  int blocks;
+  __device__ __forceinline__ Sum(const LayerArgs& a, const Plan& plan, const Matrix& w, int row, int tile) {
+    const int chunk = plan.chunk_of[row];
+    const unsigned all = (unsigned)plan.chunks * w.tiles * w.kblocks, t = (unsigned)chunk * w.tiles + tile;
+    const unsigned n = dealt(all), lo = ((t * w.kblocks + 1) * n - 1) / all, hi = ((t + 1) * w.kblocks * n - 1) / all;
+    blocks = (int)(hi - lo) + 1;
+    at = a.sums + (sums_at<BN>(plan, w, chunk, tile, (int)lo) + row - plan.first[chunk]) * 128;
+  }
+  __device__ __forceinline__ float4 four(int col) const {
+    float4 s = __ldcg(reinterpret_cast<const float4*>(at + col));
+    for (int b = 1; b < blocks; ++b) {
+      const float4 v = __ldcg(reinterpret_cast<const float4*>(at + (long long)b * BN * 128 + col));
+      s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
+    }
+    return s;
+  }
+  __device__ __forceinline__ float get(int col) const {
+    float s = __ldcg(at + col);
+    for (int b = 1; b < blocks; ++b) s += __ldcg(at + (long long)b * BN * 128 + col);
+    return s;
+  }
+};
+// four numbers of u from number j on of row `row`
+template <int BN> __device__ __forceinline__ float4 hidden(const LayerArgs& a, const Plan& plan, int row, int j, int end) {
+  const Matrix& w = a.w[0];
+  if (j % 4 == 0 && j + 4 <= end) return Sum<BN>(a, plan, w, row, j / 128).four(j % 128);
+  float v[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v[i] = j + i < end ? Sum<BN>(a, plan, w, row, (j + i) / 128).get((j + i) % 128) : 0.f;
+  return make_float4(v[0], v[1], v[2], v[3]);
+}
+__device__ __forceinline__ float activated(float u, bool silu) {
+  if (silu) return u / (1.f + expf(-u));
+  const float r = fmaxf(u, 0.f);
+  return u != u ? u : r * r;                         // (the larger of a NaN and 0 would be 0)
+}
+
+__device__ __forceinline__ void readers_sync() { asm volatile("bar.sync 1, %0;" ::"n"(kReaders * 32) : "memory"); }
+
+__device__ __forceinline__ void tmem_load8(unsigned taddr, float* v) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+               : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]) : "r"(taddr) : "memory");
+}
+
+template <int BN> __global__ void __launch_bounds__(kThreads, 1)
+expert_layer_kernel(const __grid_constant__ LayerArgs a, const __grid_constant__ CUtensorMap map_1, const __grid_constant__ CUtensorMap map_2) {
+  using L = Layer<BN>;
+  constexpr int S = L::kSlots;
+  extern __shared__ __align__(1024) unsigned char smem_dyn[];
+  __shared__ Plan plan;
+  __shared__ int misc[4];                            // [0] tensor memory, [1] abort, [2] K blocks whose copies were issued, [3] whether the readers go on
+  unsigned char* ring = smem_dyn + ((1024u - (smem_u32(smem_dyn) & 1023u)) & 1023u);
+  float* scales = reinterpret_cast<float*>(ring + L::kRing);
+  unsigned long long* bars = reinterpret_cast<unsigned long long*>(scales + S * L::kScales);
+  int* abort = misc + 1;
+  const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
+
+  if (tid == 0) {
+    prefetch_map(&map_1);
+    prefetch_map(&map_2);
+    for (int q = 0; q < S; ++q) {
+      mbar_init(bars + L::FULL + q, 1); mbar_init(bars + L::READY + q, 1); mbar_init(bars + L::DONE + q, 1); mbar_init(bars + L::SEMPTY + q, kReaders);
+    }
+    for (int q = 0; q < kAccStages; ++q) mbar_init(bars + L::ACCEMPTY + q, kReaders);
+    for (int q = 0; q < 2; ++q) mbar_init(bars + L::DRAIN + q, 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    misc[1] = misc[2] = 0;
+  }
+  if (wid == 1) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(misc)), "r"(L::kCols) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  // step 0
+  for (int u = (int)blockIdx.x * kWarps + wid; u < a.T * a.w[0].kblocks; u += (int)gridDim.x * kWarps) {
+    const int t = u / a.w[0].kblocks, b = u % a.w[0].kblocks;
+    round_block(four(a.x, a.type, t * a.ldx, b * 128 + lane * 4, a.d, a.x_wide), a.xq + (long long)u * 128, a.xs + u, lane);
+  }
+  Making& making = *reinterpret_cast<Making*>(ring);
+  if (a.router) make_logits(a, reinterpret_cast<float (*)[kLogitWarps][kLogitTokens]>(ring), lane, wid);
+  __threadfence();
+  __syncthreads();
+  if (tid == 0) {
+    come(&a.shared->meeting[MEET_TOKENS].count);
+    if (a.router) meet(a.shared, MEET_TOKENS, a.wait_limit, abort);
+  }
+  __syncthreads();
+  make_plan<BN>(a, plan, making, tid, lane, wid);
+  asm volatile("fence.proxy.async.shared::cta;" ::: "memory");             // the ring was the plan's scratch until here
+  fence_before();
+  __syncthreads();
+  fence_after();
+  const unsigned tmem = (unsigned)misc[0];
+  const int chunks = plan.chunks, rows = plan.total_rows;
+
+  if (wid == 0) {
+    if (lane == 0) {
+      unsigned it = 0;
+      bool ok = !*reinterpret_cast<volatile int*>(abort);
+      for (int f = 0; f < 2 && ok && chunks; ++f) {
+        const Matrix& w = a.w[f];
+        for (Stretch s(w, chunks); s.there(); s.next(w), ++it) {
+          const unsigned q = it % S;
+          if (it >= S && !(ok = wait(bars + L::DONE + q, (it / S - 1) & 1, a.wait_limit, abort))) break;
+          mbar_expect_tx(bars + L::FULL + q, L::kWeights);
+          if (!(a.withhold && it == 0)) tma_load_3d(ring + (size_t)q * L::kSlotBytes, f ? &map_2 : &map_1, s.kb * kKB, s.tile * kU, plan.expert[s.chunk], bars + L::FULL + q);
+        }
+      }
+      misc[2] = (int)it;
+    }
+  } else if (wid == 1 || wid == 3) {
+    if (lane == 0) {
+      const unsigned me = (unsigned)wid >> 1;
+      unsigned it = 0;
+      bool ok = true;
+      for (int f = 0; f < 2 && ok && chunks; ++f) {
+        const unsigned idesc = a.w[f].idesc;
+        for (Stretch s(a.w[f], chunks); s.there(); ++s.from, ++it) {
+          if ((it & 1) != me) continue;
+          const unsigned q = it % S, stage = it % kAccStages;
+          if (!(ok = wait(bars + L::FULL + q, (it / S) & 1, a.wait_limit, abort) && wait(bars + L::READY + q, (it / S) & 1, a.wait_limit, abort))) break;
+          const unsigned long long du = operand_desc(ring + (size_t)q * L::kSlotBytes), dv = operand_desc(ring + (size_t)q * L::kSlotBytes + L::kWeights);
+          if (it >= kAccStages && !(ok = wait(bars + L::ACCEMPTY + stage, (it / kAccStages - 1) & 1, a.wait_limit, abort))) break;
+          fence_after();
+#pragma unroll
+          for (int k4 = 0; k4 < 4; ++k4) mma_f8(tmem + stage * BN, du + 2 * k4, dv + 2 * k4, idesc, k4 != 0);
+          commit(bars + L::DONE + q);
+        }
+      }
+    }
+  } else if (wid == 2) {
+    unsigned it = 0, given = 0;                      // K blocks asked for, and handed over
+    bool ok = true;
+    auto hand_over = [&]() {                         // the oldest one, which has arrived
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      __syncwarp();
+      if (lane == 0) arrive(bars + L::READY + given % S);
+      ++given;
+    };
+    for (int f = 0; f < 2 && ok && chunks; ++f) {
+      bool met = true;
+      if (lane == 0) met = meet(a.shared, f ? MEET_HIDDEN : MEET_TOKENS, a.wait_limit, abort);
+      if (!(ok = __all_sync(kAll, met))) break;
+      const Matrix& w = a.w[f];
+      const unsigned char* from = f ? a.hq : a.xq;
+      const float* from_scales = f ? a.hs : a.xs;
+      constexpr int kCopies = BN * 8 / 32;           // 16-byte pieces of a lane
+      long long at[kCopies];                         // its rows' first numbers, -1: none
+      const float* of_token[BN > 32 ? 2 : 1];
+      const float* of_weights = nullptr;
+      bool fresh = true;
+      for (Stretch s(w, chunks); s.there(); s.next(w), ++it) {
+        if (fresh || s.kb == 0) {
+          fresh = false;
+          const int first = plan.first[s.chunk], n = plan.rows[s.chunk];
+          auto row_at = [&](int r) { return f ? first + r : plan.order[first + r] / a.c.top_k; };
+#pragma unroll
+          for (int i = 0; i < kCopies; ++i) {
+            const int r = i * 4 + (lane >> 3);
+            at[i] = r < n ? (long long)row_at(r) * (w.kblocks * 128) + (lane & 7) * 16 : -1;
+          }
+#pragma unroll
+          for (int i = 0; i < (BN > 32 ? 2 : 1); ++i) of_token[i] = i * 32 + lane < n ? from_scales + (long long)row_at(i * 32 + lane) * w.kblocks : nullptr;
+          of_weights = w.scale + plan.expert[s.chunk] * w.group + s.tile * w.row;
+        }
+        const unsigned q = it % S;
+        if (it >= S && !(ok = __all_sync(kAll, wait(bars + L::SEMPTY + q, (it / S - 1) & 1, a.wait_limit, abort)))) break;
+        unsigned char* to = ring + (size_t)q * L::kSlotBytes + L::kWeights;
+#pragma unroll
+        for (int i = 0; i < kCopies; ++i) {
+          const int r = i * 4 + (lane >> 3);
+          copy16(reinterpret_cast<float*>(to + r * kKB + (((lane & 7) ^ (r & 7)) << 4)),
+                 reinterpret_cast<const float*>(at[i] >= 0 ? from + at[i] + s.kb * 128 : from), at[i] >= 0 ? 16 : 0);
+        }
+        float* sc = scales + q * L::kScales;
+#pragma unroll
+        for (int i = 0; i < (BN > 32 ? 2 : 1); ++i)
+          if (i * 32 + lane < BN) copy4(sc + i * 32 + lane, of_token[i] ? of_token[i] + s.kb : from_scales, of_token[i] != nullptr);
+        if (lane == 0) copy4(sc + BN, of_weights + s.kb * w.block, true);
+        asm volatile("cp.async.commit_group;" ::: "memory");
+        if (it - given >= kAhead) {
+          asm volatile("cp.async.wait_group %0;" ::"n"(kAhead) : "memory");
+          hand_over();
+        }
+      }
+      asm volatile("cp.async.wait_all;" ::: "memory");
+      while (ok && given < it) hand_over();
+    }
+    asm volatile("cp.async.wait_all;" ::: "memory");
+  } else if (wid >= 4) {
+    const int quarter = wid & 3, c_first = ((wid - 4) >> 2) * L::kRows;                 // the warp's rows of W and tokens
+    const unsigned at_tmem = tmem + ((unsigned)(quarter * 32) << 16) + c_first;
+    const int reader = (int)blockIdx.x * kReaders + wid - 4, readers = (int)gridDim.x * kReaders;
+    unsigned it = 0;
+    bool ok = true;                                  // (all readers go the same way, see below)
+    for (int f = 0; f < 2 && ok; ++f) {
+      const Matrix& w = a.w[f];
+      if (chunks) {
+        float acc[L::kRows];
+        for (Stretch s(w, chunks); s.there();) {
+#pragma unroll
+          for (int c = 0; c < L::kRows; ++c) acc[c] = 0.f;
+          const int chunk = s.chunk, tile = s.tile;
+          const unsigned n = min((unsigned)(w.kblocks - s.kb), s.to - s.from);             // of this tile
+          for (unsigned i = 0; i < n; ++i, ++it) {
+            const unsigned q = it % S, stage = it % kAccStages;
+            ok = wait(bars + L::READY + q, (it / S) & 1, a.wait_limit, abort) && wait(bars + L::DONE + q, (it / S) & 1, a.wait_limit, abort);
+            if (!(ok = __all_sync(kAll, ok))) break;
+            fence_after();
+            const float* sc = scales + q * L::kScales;
+            float v[L::kRows];
+#pragma unroll
+            for (int c = 0; c < L::kRows; c += 8) tmem_load8(at_tmem + stage * BN + c, v + c);
+            const float of_weights = sc[BN];
+            tmem_wait();
+            fence_before();
+            __syncwarp();
+            if (lane == 0) arrive(bars + L::ACCEMPTY + stage);
+#pragma unroll
+            for (int c = 0; c < L::kRows; c += 4) {
+              const float4 t = *reinterpret_cast<const float4*>(sc + c_first + c);
+              acc[c] = fmaf(v[c] * of_weights, t.x, acc[c]);
+              acc[c + 1] = fmaf(v[c + 1] * of_weights, t.y, acc[c + 1]);
+              acc[c + 2] = fmaf(v[c + 2] * of_weights, t.z, acc[c + 2]);
+              acc[c + 3] = fmaf(v[c + 3] * of_weights, t.w, acc[c + 3]);
+            }
+            __syncwarp();
+            if (lane == 0) arrive(bars + L::SEMPTY + q);
+          }
+          if (!ok) break;
+          float* to = a.sums + (sums_at<BN>(plan, w, chunk, tile, (int)blockIdx.x) + c_first) * 128 + quarter * 32 + lane;
+          const int left = plan.rows[chunk] - c_first;
+#pragma unroll
+          for (int c = 0; c < L::kRows; ++c) if (c < left) to[c * 128] = acc[c];
+          // the next tile
+          s.from += n;
+          s.kb = 0;
+          if (++s.tile == w.tiles) { s.tile = 0; ++s.chunk; }
+        }
+      }
+      __threadfence();
+      readers_sync();
+      // (one thread decides for all readers: where a warp gave up, the block does not come, and the meeting fails)
+      if (tid == 128) {
+        const int which = f ? MEET_OUT : MEET_SUMS;
+        if (!*reinterpret_cast<volatile int*>(abort)) come(&a.shared->meeting[which].count);
+        misc[3] = meet(a.shared, which, a.wait_limit, abort);
+      }
+      readers_sync();
+      ok = *reinterpret_cast<volatile int*>(misc + 3) != 0;
+      if (!ok) break;
+      if (f == 0) {
+        const int hb = a.w[1].kblocks;
+        for (int u = reader; u < rows * hb; u += readers) {
+          const int row = u / hb, j = u % hb * 128 + lane * 4;
+          float4 v = hidden<BN>(a, plan, row, min(j, a.h), a.h);
+          v = make_float4(activated(v.x, a.silu), activated(v.y, a.silu), activated(v.z, a.silu), activated(v.w, a.silu));
+          if (a.gated) {
+            const float4 up = hidden<BN>(a, plan, row, a.h + min(j, a.h), 2 * a.h);
+            v.x *= up.x; v.y *= up.y; v.z *= up.z; v.w *= up.w;
+          }
+          round_block(v, a.hq + (long long)u * 128, a.hs + u, lane);
+        }
+        __threadfence();
+        readers_sync();
+        if (tid == 128) come(&a.shared->meeting[MEET_HIDDEN].count);
+      } else {
+        for (int u = reader; u < a.T * w.tiles; u += readers) {
+          const int t = u / w.tiles, tile = u % w.tiles, c = tile * 128 + lane * 4;
+          float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+          for (int j = 0; j < a.c.top_k; ++j) {
+            const int row = plan.row_of[t * a.c.top_k + j];
+            if (row < 0) continue;
+            const float wt = plan.weights[t * a.c.top_k + j];
+            const float4 z = Sum<BN>(a, plan, w, row, tile).four(lane * 4);
+            y.x = fmaf(wt, z.x, y.x); y.y = fmaf(wt, z.y, y.y); y.z = fmaf(wt, z.z, y.z); y.w = fmaf(wt, z.w, y.w);
+          }
+          const float v[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+          for (int i = 0; i < 4; ++i) if (c + i < a.d) store_c(a.y, a.type, t * a.ldy + c + i, v[i]);
+        }
+      }
+    }
+  }
+  __syncwarp();
+  fence_before();
+  __syncthreads();
+  fence_after();
+  if (*reinterpret_cast<volatile int*>(abort)) {     // a wait ran out: what is in flight ends first
+    if (tid == 0) atomicExch(&a.shared->gave_up, 1u);
+    if (wid == 0 && lane == 0) {
+      const unsigned issued = (unsigned)misc[2];
+      for (unsigned q = 0; q < S && q < issued; ++q) wait_in_flight(bars + L::FULL + q, ((issued - 1 - q) / S) & 1, a.wait_limit);      // a slot's last use
+    } else if ((wid == 1 || wid == 3) && lane == 0) {
+      commit(bars + L::DRAIN + (wid >> 1));
+      wait_in_flight(bars + L::DRAIN + (wid >> 1), 0, a.wait_limit);
+    }
+    __syncthreads();
+    fence_after();
+  }
+  if (wid == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(L::kCols));
+  if (tid == 0 && *reinterpret_cast<volatile int*>(abort)) atomicMin(a.status, ASGD_ETIMEOUT);
+}
+
+// ---- host ----
+
+constexpr size_t up256(size_t n) { return (n + 255) / 256 * 256; }
+
+// Tokens of a tile: an expert's as a rule fit into one chunk (its weights then are read once).
+int tokens_of(long long assignments, int experts) {
+  const double mean = (double)assignments / experts;
+  return mean <= 8 ? 16 : mean <= 18 ? 32 : 64;
+}
+struct Places {
+  size_t logits, xq, xs, hq, hs, sums, bytes;
+};
+Places places(const asgd_route_config& c, const asgd_expert_layer_args& a) {
+  const size_t T = (size_t)a.T, rows = T * c.top_k, rows1 = (size_t)a.h * (a.gated ? 2 : 1);
+  const size_t kb1 = (size_t)ceil_div(a.d, 128), kb2 = (size_t)ceil_div(a.h, 128), tiles = std::max((size_t)ceil_div((long long)rows1, 128), kb1);
+  Places p;
+  size_t at = up256(sizeof(Shared));
+  auto take = [&](size_t n) { const size_t here = at; at += up256(n); return here; };
+  p.logits = take(a.router ? T * c.experts * 4 : 0);
+  p.xq = take(T * kb1 * 128);
+  p.xs = take(T * kb1 * 4);
+  p.hq = take(rows * kb2 * 128);
+  p.hs = take(rows * kb2 * 4);
+  p.sums = take((rows * tiles + (size_t)kSMs * tokens_of((long long)rows, c.experts)) * 512);
+  p.bytes = at;
+  return p;
+}
+// Sizes alone: ASGD_OK, or why not.
+int sizes_ok(const asgd_route_config* c, const asgd_expert_layer_args* a) {
+  if (!config_ok(c) || !a || a->T < 0 || a->d < 1 || a->h < 1 || (a->gated != 0 && a->gated != 1)) return ASGD_EINVAL;
+  if (!config_supported(c) || a->T > ASGD_LAYER_MAX_TOKENS || a->T * c->top_k > ASGD_LAYER_MAX_ASSIGNMENTS) return ASGD_EUNSUPPORTED;
+  if (a->d > ASGD_LAYER_MAX_WIDTH || a->h > ASGD_LAYER_MAX_WIDTH || a->h * (a->gated ? 2 : 1) > ASGD_LAYER_MAX_WIDTH) return ASGD_EUNSUPPORTED;
+  // K blocks of all chunks (a row each at worst), times the blocks, in 32 bits
+  const long long rows1 = a->h * (a->gated ? 2 : 1), most = std::max(ceil_div(rows1, 128) * ceil_div(a->d, 128), ceil_div(a->d, 128) * ceil_div(a->h, 128));
+  if (most * (a->T * c->top_k) * (kSMs + 1) > 0x7fffffffll) return ASGD_EUNSUPPORTED;
+  return ASGD_OK;
+}
+
+template <int BN> int launch(const asgd_route_config& c, const asgd_expert_layer_args& a, const LayerArgs& p, cudaStream_t st) {
+  CUtensorMap map_1{}, map_2{};
+  if (!encode(&map_1, a.w1, a.d, p.rows1, c.experts, a.ldw1, a.w1_group, kU)) return ASGD_EINVAL;
+  if (!encode(&map_2, a.w2, a.h, a.d, c.experts, a.ldw2, a.w2_group, kU)) return ASGD_EINVAL;
+  static std::atomic<unsigned long long> done{0};
+  if (!allow_smem(expert_layer_kernel<BN>, Layer<BN>::kSmem, done)) return ASGD_ECUDA;
+  if (!good(cudaMemsetAsync(p.shared, 0, sizeof(Shared), st))) return ASGD_ECUDA;
+  cudaLaunchAttribute all;
+  all.id = cudaLaunchAttributeCooperative;
+  all.val.cooperative = 1;
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3(kSMs);
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = Layer<BN>::kSmem;
+  cfg.stream = st;
+  cfg.attrs = &all;
+  cfg.numAttrs = 1;
+  return good(cudaLaunchKernelEx(&cfg, expert_layer_kernel<BN>, p, map_1, map_2)) ? ASGD_OK : ASGD_ECUDA;
+}
+
+unsigned instruction(int weights_type, int cols) {   // fp32 accumulators; weights by tokens (E4M3)
+  return 1u << 4 | (weights_type == ASGD_E5M2 ? 1u : 0u) << 7 | (unsigned)(cols >> 3) << 17 | (unsigned)(kU >> 4) << 24;
+}
+
+}  // namespace
+
+extern "C" int asgd_expert_layer_workspace_bytes(const asgd_route_config* cfg, const asgd_expert_layer_args* args, size_t* bytes) {
+  if (!bytes) return ASGD_EINVAL;
+  const int bad = sizes_ok(cfg, args);
+  if (bad) return bad;
+  *bytes = places(*cfg, *args).bytes;
+  return ASGD_OK;
+}
+
+extern "C" int asgd_expert_layer(const asgd_route_config* cfg, const asgd_expert_layer_args* args, void* workspace, size_t workspace_bytes, void* stream) {
+  const int bad = sizes_ok(cfg, args);
+  if (bad) return bad;
+  const asgd_expert_layer_args& a = *args;
+  const asgd_route_config& c = *cfg;
+  const long long rows1 = a.h * (a.gated ? 2 : 1), E = c.experts;
+  if (!float_type(a.type) || !eight_bit_type(a.w1_type) || !eight_bit_type(a.w2_type)) return ASGD_EINVAL;
+  if (a.activation != ASGD_ACT_RELU2 && a.activation != ASGD_ACT_SILU) return ASGD_EINVAL;
+  if ((a.logits && a.router) || (a.shift && !a.router)) return ASGD_EINVAL;
+  if (a.logits && (!float_type(a.logits_type) || a.ld_logits < E || !aligned(a.logits, type_bytes(a.logits_type)))) return ASGD_EINVAL;
+  if (a.router && (!float_type(a.router_type) || a.ld_router < a.d || !aligned(a.router, type_bytes(a.router_type)))) return ASGD_EINVAL;
+  if (a.ldx < a.d || a.ldy < a.d || a.ldw1 < a.d || a.ldw2 < a.h || a.ldw1 % 16 || a.ldw2 % 16) return ASGD_EINVAL;
+  if (E > 1 && (a.w1_group < 0 || a.w2_group < 0 || a.w1_group % 16 || a.w2_group % 16)) return ASGD_EINVAL;
+  if (!aligned_words(a.shift, a.bias, a.w1_scale, a.w2_scale, a.ids, a.weights)) return ASGD_EINVAL;
+  if (a.T == 0) return ASGD_OK;
+  if (!a.x || !a.y || (!a.logits && !a.router) || !aligned(a.x, type_bytes(a.type)) || !aligned(a.y, type_bytes(a.type))) return ASGD_EINVAL;
+  if (!a.w1 || !a.w2 || !a.w1_scale || !a.w2_scale || !aligned(a.w1, 16) || !aligned(a.w2, 16)) return ASGD_EINVAL;
+  const Places at = places(c, a);
+  if (!workspace || workspace_bytes < at.bytes) return ASGD_ENOMEM;
+  if (!aligned(workspace, 256)) return ASGD_EINVAL;
+
+  const WaitDrill drill = wait_drill();
+  const int bn = tokens_of(a.T * c.top_k, c.experts);
+  unsigned char* base = reinterpret_cast<unsigned char*>(workspace);
+  LayerArgs p{};
+  static_cast<Choice&>(p) = choice_of(c, a.bias);
+  p.T = (int)a.T; p.d = (int)a.d; p.h = (int)a.h; p.rows1 = (int)rows1; p.gated = a.gated; p.silu = a.activation == ASGD_ACT_SILU;
+  p.x = a.x; p.ldx = a.ldx; p.type = a.type;
+  p.x_wide = aligned(a.x, 4 * type_bytes(a.type)) && a.ldx % 4 == 0;
+  p.y = a.y; p.ldy = a.ldy;
+  p.logits = a.logits; p.ld_logits = a.ld_logits; p.logits_type = a.logits_type;
+  p.router = a.router; p.ld_router = a.ld_router; p.router_type = a.router_type;
+  p.router_wide = a.router && aligned(a.router, 4 * type_bytes(a.router_type)) && a.ld_router % 4 == 0;
+  p.shift = a.shift; p.temperature = a.temperature;
+  p.w[0] = {(int)ceil_div(rows1, 128), (int)ceil_div(a.d, 128), a.w1_scale, a.w1_scale_row, a.w1_scale_block, a.w1_scale_group, instruction(a.w1_type, bn)};
+  p.w[1] = {(int)ceil_div(a.d, 128), (int)ceil_div(a.h, 128), a.w2_scale, a.w2_scale_row, a.w2_scale_block, a.w2_scale_group, instruction(a.w2_type, bn)};
+  p.ids = a.ids; p.weights = a.weights;
+  p.shared = reinterpret_cast<Shared*>(base);
+  p.made_logits = a.router ? reinterpret_cast<float*>(base + at.logits) : nullptr;
+  p.xq = base + at.xq;
+  p.xs = reinterpret_cast<float*>(base + at.xs);
+  p.hq = base + at.hq;
+  p.hs = reinterpret_cast<float*>(base + at.hs);
+  p.sums = reinterpret_cast<float*>(base + at.sums);
+  p.wait_limit = drill.limit;
+  p.withhold = drill.withhold;
+  p.status = status_word();
+  if (!p.status) return ASGD_ECUDA;
+  const cudaStream_t st = (cudaStream_t)stream;
+  return bn == 16 ? launch<16>(c, a, p, st) : bn == 32 ? launch<32>(c, a, p, st) : launch<64>(c, a, p, st);
+}

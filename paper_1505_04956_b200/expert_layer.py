@@ -17,6 +17,7 @@ from .binding import Asgd, make_config
 from .experts import (asgd_combine, asgd_combine_grad, asgd_experts_sync, asgd_product, asgd_product_inner, asgd_quantize, asgd_route,
                       asgd_route_grad)
 from .gradients import asgd_clip_grads
+from .serving import asgd_expert_layer
 
 ALIGN = 128                     # grouped rows per block of the weight gradients' sums
 E5M2 = torch.float8_e5m2        # gradients have the wider range
@@ -71,6 +72,16 @@ class Layer:
         y = asgd_combine(z, rows, weights)
         return y, dict(logits=logits, ids=ids, weights=weights, offsets=offsets, rows=rows, source=source, r=r, z=z,
                        xt=(xqt, xst), ht=(hqt, hst), w1t=w1t, w2t=w2t)
+
+    def eight_bits(self):
+        """The experts' matrices as serve() takes them: for steps that change nothing they are made once."""
+        return tuple(eight_bits(w)[0] for w in (self.w1, self.w2))
+
+    def serve(self, x, weights=None):
+        """y of the few tokens of a serving step (128 at most), of x's type, in one call; `weights` as eight_bits() gives them."""
+        (w1, s1), (w2, s2) = self.eight_bits() if weights is None else weights
+        return asgd_expert_layer(x, w1, s1, w2, s2, self.top_k, router=self.router, shift=self.shift, temperature=self.temperature,
+                                 activation="relu2", score="sigmoid", bias=self.bias)
 
     def gradients(self, x, dy, c):
         """Gradients of router, w1 and w2 and of the layer's input, from dy [T, d] fp32."""
