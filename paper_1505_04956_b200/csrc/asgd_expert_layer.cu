@@ -8,8 +8,8 @@
 //
 // The steps:
 //   0  logits (with a router) and the tokens in 8 bits, by all warps of all blocks.   -- blocks meet
-//   1  every block chooses the experts of all tokens for itself, and lists the rows by expert (integers and a few numbers
-//      per token; cheaper than to hand them round).  Then its stretch of W1: sums of partial tiles go to the workspace.  -- blocks meet
+//   1  every block chooses the experts of all tokens for itself (more than 24 tokens are shared out, and the blocks meet once more), and lists
+//      the rows by expert.  Then its stretch of W1: sums of partial tiles go to the workspace.  -- blocks meet
 //   2  sums of a tile's stretches in the blocks' order, activation, 8 bits.   -- blocks meet (the copies of W2 went on)
 //   3  its stretch of W2, sums to the workspace.   -- blocks meet
 //   4  sums of the stretches and of a token's experts in their order, y.
@@ -31,10 +31,10 @@
 namespace {
 
 constexpr int kThreads = 384, kWarps = kThreads / 32, kReaders = 8;
-constexpr int kAhead = 4;                            // K blocks of tokens' rows in flight
 constexpr int kMostRows = ASGD_LAYER_MAX_ASSIGNMENTS;
+constexpr int kChoices = 2 * kWarps;                 // tokens that every block chooses for itself; with more the blocks share them out and meet
 constexpr int kTokenWords = ASGD_LAYER_MAX_TOKENS / 32;
-enum { MEET_TOKENS, MEET_SUMS, MEET_HIDDEN, MEET_OUT, MEETINGS };
+enum { MEET_TOKENS, MEET_CHOICE, MEET_SUMS, MEET_HIDDEN, MEET_OUT, MEETINGS };
 
 // What the blocks of a launch share, at the workspace's start; zeros before it.
 struct Shared {
@@ -70,6 +70,8 @@ struct LayerArgs : Choice {
   // workspace
   Shared* shared;
   float* made_logits;                                // [T][E]
+  int* made_ids;                                     // [T][top_k], where the blocks share the choices of many tokens
+  float* made_weights;
   unsigned char* xq;                                 // [T][w[0].kblocks * 128]
   float* xs;                                         // [T][w[0].kblocks]
   unsigned char* hq;                                 // [rows][w[1].kblocks * 128]
@@ -83,6 +85,7 @@ struct LayerArgs : Choice {
 template <int BN> struct Layer {
   static constexpr int kSlots = BN == 64 ? 8 : 10;   // even: a slot always meets the same issuing thread
   static constexpr unsigned kWeights = kU * kKB, kTokens = BN * kKB, kSlotBytes = kWeights + kTokens;
+  static constexpr int kAhead = kSlots - 2;          // K blocks of tokens' rows in flight
   static constexpr int kScales = BN + 4;             // of a slot: the tokens', then the weights' one
   static constexpr int kRows = BN / 2;               // tokens of a tile that a reading thread has
   static constexpr unsigned kCols = kAccStages * BN;
@@ -103,10 +106,12 @@ struct Plan {
   short expert[kMostRows], first[kMostRows], rows[kMostRows];      // of a chunk
   int part[2][kWarps];
   int chunks, total_rows;
+  unsigned per[2];                                   // K blocks of a block, of W1 and W2
 };
 // While the plan is made, where the ring will be.
 struct Making {
-  unsigned scratch[kWarps][kScratch];
+  unsigned key[kWarps][ASGD_MAX_EXPERTS];            // of the choices
+  float x[kWarps][ASGD_MAX_EXPERTS];
   unsigned mask[ASGD_MAX_EXPERTS][kTokenWords];      // the tokens of an expert
   int start[ASGD_MAX_EXPERTS], chunk[ASGD_MAX_EXPERTS];
 };
@@ -128,7 +133,6 @@ __device__ inline bool meet(Shared* sh, int which, unsigned limit, int* abort) {
   for (unsigned it = 0; it < limit; ++it) {
     if (look(&sh->meeting[which].count) >= gridDim.x) return true;
     if ((it & 15u) == 15u && (*reinterpret_cast<volatile int*>(abort) || look(&sh->gave_up))) break;
-    __nanosleep(20);
   }
   *reinterpret_cast<volatile int*>(abort) = 1;
   return false;
@@ -136,32 +140,26 @@ __device__ inline bool meet(Shared* sh, int which, unsigned limit, int* abort) {
 
 // ---- tokens ----
 
+template <typename T> __device__ __forceinline__ float4 four(const T* at) {             // aligned
+  if constexpr (sizeof(T) == 4) return *reinterpret_cast<const float4*>(at);
+  else {
+    const uint2 u = *reinterpret_cast<const uint2*>(at);
+    const T* e = reinterpret_cast<const T*>(&u);
+    return make_float4(Elem<T>::to_f(e[0]), Elem<T>::to_f(e[1]), Elem<T>::to_f(e[2]), Elem<T>::to_f(e[3]));
+  }
+}
 // four numbers from number `at` of a row on, zeros from `end` on
 template <typename T> __device__ __forceinline__ float4 four(const T* row, int at, int end, bool wide) {
+  if (wide && at + 4 <= end) return four(row + at);
   float v[4];
-  if (wide && at + 4 <= end) {
-    if constexpr (sizeof(T) == 4) return *reinterpret_cast<const float4*>(row + at);
-    else {
-      const uint2 u = *reinterpret_cast<const uint2*>(row + at);
-      const T* e = reinterpret_cast<const T*>(&u);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) v[i] = Elem<T>::to_f(e[i]);
-    }
-  } else {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] = at + i < end ? Elem<T>::to_f(row[at + i]) : 0.f;
-  }
+  for (int i = 0; i < 4; ++i) v[i] = at + i < end ? Elem<T>::to_f(row[at + i]) : 0.f;
   return make_float4(v[0], v[1], v[2], v[3]);
 }
 __device__ __forceinline__ float4 four(const void* base, int type, long long row, int at, int end, bool wide) {
   if (type == ASGD_F32) return four(reinterpret_cast<const float*>(base) + row, at, end, wide);
   if (type == ASGD_BF16) return four(reinterpret_cast<const __nv_bfloat16*>(base) + row, at, end, wide);
   return four(reinterpret_cast<const __half*>(base) + row, at, end, wide);
-}
-__device__ __forceinline__ float one(const void* base, int type, long long at) {
-  if (type == ASGD_F32) return reinterpret_cast<const float*>(base)[at];
-  if (type == ASGD_BF16) return __bfloat162float(reinterpret_cast<const __nv_bfloat16*>(base)[at]);
-  return __half2float(reinterpret_cast<const __half*>(base)[at]);
 }
 
 // A warp rounds a block of 128 numbers, four per lane, as asgd_quantize does (E4M3).
@@ -177,30 +175,52 @@ __device__ __forceinline__ void round_block(const float4& v, unsigned char* q, f
   if (lane == 0) *scale = __fmul_rn(m, 1.f / 448.f);
 }
 
-// Logits of a router: four warps share a row of it and up to eight tokens; a block has three such groups of warps.
+// Logits of a router: four warps share a row of it and kTok tokens; a block has three such groups of warps.  (The types are the
+// template's, so that a step's loads are all in flight at once: with a switch around each, 60 tokens took 16 us.)
 constexpr int kLogitTokens = 8, kLogitWarps = 4, kLogitGroups = kWarps / kLogitWarps;
-__device__ inline void make_logits(const LayerArgs& a, float (*part)[kLogitWarps][kLogitTokens], int lane, int wid) {
-  const int E = a.c.experts, sets = (a.T + kLogitTokens - 1) / kLogitTokens, units = E * sets, group = wid / kLogitWarps, sub = wid % kLogitWarps;
-  const int per = kLogitGroups * (int)gridDim.x;
+template <typename X, typename R, int kTok> __device__ __forceinline__ void logit_sums(const LayerArgs& a, int e, int t0, int n, int first, float (&acc)[kLogitTokens]) {
+  const R* r = reinterpret_cast<const R*>(a.router) + e * a.ld_router;
+  const X* x[kTok];
+#pragma unroll
+  for (int t = 0; t < kTok; ++t) x[t] = reinterpret_cast<const X*>(a.x) + (t0 + min(t, n - 1)) * a.ldx;      // (places behind the last token repeat it)
+  const bool wide = a.router_wide && a.x_wide;
+  const int whole = wide ? a.d / 4 * 4 : 0;          // numbers read four at a time
+  for (int k = first; k < whole; k += kLogitWarps * 128) {
+    const float4 m = four(r + k);
+    float4 v[kTok];
+#pragma unroll
+    for (int t = 0; t < kTok; ++t) v[t] = four(x[t] + k);
+#pragma unroll
+    for (int t = 0; t < kTok; ++t) acc[t] = fmaf(v[t].x, m.x, fmaf(v[t].y, m.y, fmaf(v[t].z, m.z, fmaf(v[t].w, m.w, acc[t]))));
+  }
+#pragma unroll 1
+  for (int k = whole + first / 4; k < a.d; k += kLogitWarps * 32) {
+    const float m = Elem<R>::to_f(r[k]);
+#pragma unroll
+    for (int t = 0; t < kTok; ++t) acc[t] = fmaf(Elem<X>::to_f(x[t][k]), m, acc[t]);
+  }
+}
+template <int kTok> __device__ inline void make_logits(const LayerArgs& a, float (*part)[kLogitWarps][kLogitTokens], int lane, int wid) {
+  const int E = a.c.experts, sets = (a.T + kTok - 1) / kTok, units = E * sets, group = wid / kLogitWarps, sub = wid % kLogitWarps;
+  const int per = kLogitGroups * (int)gridDim.x, first = (sub * 32 + lane) * 4;
   for (int u0 = (int)blockIdx.x * kLogitGroups; u0 < units; u0 += per) {
-    const int u = u0 + group, e = u / sets, t0 = u % sets * kLogitTokens, n = u < units ? min(kLogitTokens, a.T - t0) : 0;
+    const int u = u0 + group, e = u / sets, t0 = u % sets * kTok, n = u < units ? min(kTok, a.T - t0) : 0;
     float acc[kLogitTokens];
 #pragma unroll
     for (int t = 0; t < kLogitTokens; ++t) acc[t] = 0.f;
     if (n > 0) {
-#pragma unroll 4
-      for (int k = (sub * 32 + lane) * 4; k < a.d; k += kLogitWarps * 128) {
-        const float4 r = four(a.router, a.router_type, e * a.ld_router, k, a.d, a.router_wide);
-#pragma unroll
-        for (int t = 0; t < kLogitTokens; ++t)
-          if (t < n) {
-            const float4 v = four(a.x, a.type, (t0 + t) * a.ldx, k, a.d, a.x_wide);
-            acc[t] = fmaf(v.x, r.x, fmaf(v.y, r.y, fmaf(v.z, r.z, fmaf(v.w, r.w, acc[t]))));
-          }
-      }
+      auto of = [&](auto x) {
+        using X = decltype(x);
+        if (a.router_type == ASGD_F32) logit_sums<X, float, kTok>(a, e, t0, n, first, acc);
+        else if (a.router_type == ASGD_BF16) logit_sums<X, __nv_bfloat16, kTok>(a, e, t0, n, first, acc);
+        else logit_sums<X, __half, kTok>(a, e, t0, n, first, acc);
+      };
+      if (a.type == ASGD_F32) of(float());
+      else if (a.type == ASGD_BF16) of(__nv_bfloat16());
+      else of(__half());
     }
 #pragma unroll
-    for (int t = 0; t < kLogitTokens; ++t) {
+    for (int t = 0; t < kTok; ++t) {
 #pragma unroll
       for (int o = 16; o > 0; o >>= 1) acc[t] += __shfl_xor_sync(kAll, acc[t], o);
       if (lane == 0) part[group][sub][t] = acc[t];
@@ -218,34 +238,129 @@ __device__ inline void make_logits(const LayerArgs& a, float (*part)[kLogitWarps
 
 // ---- the choice and the plan, by the whole block ----
 
-template <int S> __device__ __forceinline__ void choose_all(const LayerArgs& a, Plan& plan, Making& m, int lane, int wid) {
-  const int E = a.c.experts, K = a.c.top_k;
-  for (int t = wid; t < a.T; t += kWarps) {
-    float x[S];
-#pragma unroll
-    for (int j = 0; j < S; ++j) {
-      const int e = j * 32 + lane;
-      x[j] = e >= E ? -INFINITY : a.made_logits ? __ldcg(a.made_logits + (long long)t * E + e) : one(a.logits, a.logits_type, t * a.ld_logits + e);
+// A warp chooses for one token, as asgd_route does, from logits and keys in shared memory: lane l has the experts l, l + 32, ...  A kernel
+// that runs once for a few tokens meets its instructions cold, so this code is short: loops over what a lane has, where asgd_route's is unrolled
+// over registers (which took 10 us for a first token among 256 experts in groups, and 2 for every further one).
+template <typename T> __device__ __forceinline__ void read_logits(const T* row, int E, int lane, float* x) {
+#pragma unroll 4
+  for (int e = lane; e < E; e += 32) x[e] = Elem<T>::to_f(__ldcg(row + e));
+}
+__device__ inline void choose_one(const LayerArgs& a, int t, float* x, unsigned* key, int lane, int& id, float& weight) {
+  const asgd_route_config& c = a.c;
+  const int E = c.experts, K = c.top_k;
+  const bool by_logit = a.bias == nullptr && c.group_top == 1, sigmoid_scores = c.score == ASGD_SCORE_SIGMOID;
+  __syncwarp();
+  if (a.made_logits) read_logits(a.made_logits + (long long)t * E, E, lane, x);
+  else if (a.logits_type == ASGD_F32) read_logits(reinterpret_cast<const float*>(a.logits) + t * a.ld_logits, E, lane, x);
+  else if (a.logits_type == ASGD_BF16) read_logits(reinterpret_cast<const __nv_bfloat16*>(a.logits) + t * a.ld_logits, E, lane, x);
+  else read_logits(reinterpret_cast<const __half*>(a.logits) + t * a.ld_logits, E, lane, x);
+  Softmax f{0.f, 1.f};
+  if (!sigmoid_scores) {
+    float m = -INFINITY, sum = 0.f;
+    for (int e = lane; e < E; e += 32) m = e == lane ? x[e] : fmaxf(m, x[e]);
+    f.m = lanes_max<32>(m);
+#pragma unroll 4
+    for (int e = lane; e < E; e += 32) sum += f.part(x[e]);
+    f.sum = lanes_sum<32>(sum);
+  }
+  unsigned best = 0;                                 // the lane's largest key, and whose it is
+  int whose = -1;
+#pragma unroll 4
+  for (int e = lane; e < E; e += 32) {
+    float v = x[e];
+    const bool there = v > -INFINITY;
+    if (!by_logit) {
+      v = sigmoid_scores ? sigmoid(v) : f.score(v);
+      if (a.bias) v = __fadd_rn(v, a.bias[e]);
     }
-    int place, id;
+    const unsigned k = there && v > -INFINITY ? ordered(v) : 0u;
+    key[e] = k;
+    if (k > best) { best = k; whose = e; }
+  }
+  __syncwarp();
+  auto look_again = [&]() {
+    best = 0;
+    whose = -1;
+#pragma unroll 4
+    for (int e = lane; e < E; e += 32) {
+      const unsigned k = key[e];
+      if (k > best) { best = k; whose = e; }
+    }
+  };
+  if (c.groups_kept < c.groups) {                    // see keep_groups
+    const int per = E / c.groups, shift = a.group_lanes, g = lane >> shift, sub = lane & ((1 << shift) - 1);
+    unsigned m1 = 0, m2 = 0;
+    if (g < c.groups)
+#pragma unroll 4
+      for (int i = sub; i < per; i += 1 << shift) {
+        const unsigned k = key[g * per + i];
+        m2 = max(m2, min(m1, k));
+        m1 = max(m1, k);
+      }
+    for (int o = 1; o < 1 << shift; o <<= 1) {       // the two largest of two lanes' two largest
+      const unsigned o1 = __shfl_xor_sync(kAll, m1, o), o2 = __shfl_xor_sync(kAll, m2, o);
+      m2 = max(min(m1, o1), max(m2, o2));
+      m1 = max(m1, o1);
+    }
+    if (c.group_top == 2 && m2) m1 = ordered(__fadd_rn(from_ordered(m1), from_ordered(m2)));
+    const unsigned got = __shfl_sync(kAll, m1, (lane << shift) & 31);
+    unsigned mine = lane < c.groups ? got : 0u, kept = 0;
+    for (int i = 0; i < c.groups_kept; ++i) {
+      const unsigned top = __reduce_max_sync(kAll, mine);
+      const unsigned holders = __ballot_sync(kAll, top && mine == top), first = holders & (0u - holders);      // the lowest of them, if any
+      kept |= first;
+      if ((first >> lane) & 1u) mine = 0;
+    }
+    for (int e = lane; e < E; e += 32) {
+      const int of = a.group_magic ? (int)__umulhi((unsigned)e, a.group_magic) : e;
+      if (!((kept >> of) & 1u)) key[e] = 0u;
+    }
+    look_again();
+  }
+  id = -1;
+  for (int i = 0; i < K; ++i) {
+    const unsigned top = __reduce_max_sync(kAll, best);
+    if (!top) break;                                 // nothing is left
+    const int first = (int)__reduce_min_sync(kAll, best == top ? (unsigned)whose : 0x7fffffffu);      // of equal keys the lowest expert's
+    if (lane == i) id = first;
+    if (whose == first) {
+      key[first] = 0u;
+      look_again();
+    }
+  }
+  const float chosen = id >= 0 ? x[id] : 0.f, s = id < 0 ? 0.f : sigmoid_scores ? sigmoid(chosen) : f.score(chosen);
+  weight = 0.f;
+  if (c.renormalise) {
+    const float sum = lanes_sum<32>(s);
+    if (id >= 0) weight = c.scale * s / (sum + 1e-20f);
+  } else if (id >= 0) {
+    weight = c.scale * s;
+  }
+}
+// The choices of tokens first, first + step, ..., of a warp, to arrays of all tokens' choices.
+template <typename Id> __device__ __forceinline__ void choose_some(const LayerArgs& a, int first, int step, float* x, unsigned* key, int lane, Id* ids, float* weights) {
+  const int K = a.c.top_k;
+  for (int t = first; t < a.T; t += step) {
+    int id;
     float w;
-    choose<S, 32>(a, x, lane, m.scratch[wid], place, id, w);
-    if (place >= 0) {
-      plan.ids[t * K + place] = (short)id;
-      plan.weights[t * K + place] = w;
-      if (id >= 0) atomicOr(&m.mask[id][t >> 5], 1u << (t & 31));
-      if (blockIdx.x == 0 && a.ids) a.ids[t * K + place] = id;
-      if (blockIdx.x == 0 && a.weights) a.weights[t * K + place] = w;
+    choose_one(a, t, x, key, lane, id, w);
+    if (lane < K) {
+      ids[t * K + lane] = (Id)id;
+      weights[t * K + lane] = w;
     }
   }
 }
+// Rows by expert from the choices in plan.ids.  The whole block.
 template <int BN> __device__ inline void make_plan(const LayerArgs& a, Plan& plan, Making& m, int tid, int lane, int wid) {
   const int E = a.c.experts, K = a.c.top_k, n = a.T * K;
   for (int i = tid; i < E * kTokenWords; i += kThreads) (&m.mask[0][0])[i] = 0;
   __syncthreads();
-  if (E <= 128) choose_all<4>(a, plan, m, lane, wid);
-  else if (E <= 256) choose_all<8>(a, plan, m, lane, wid);
-  else choose_all<32>(a, plan, m, lane, wid);
+  for (int i = tid; i < n; i += kThreads) {
+    const int e = plan.ids[i], t = i / K;
+    if (e >= 0) atomicOr(&m.mask[e][t >> 5], 1u << (t & 31));
+    if (blockIdx.x == 0 && a.ids) a.ids[i] = e;
+    if (blockIdx.x == 0 && a.weights) a.weights[i] = plan.weights[i];
+  }
   __syncthreads();
   // rows and chunks before each expert
   constexpr int kPer = (ASGD_MAX_EXPERTS + kThreads - 1) / kThreads;
@@ -273,29 +388,34 @@ template <int BN> __device__ inline void make_plan(const LayerArgs& a, Plan& pla
 #pragma unroll
   for (int q = 0; q < kPer; ++q) {
     const int e = tid * kPer + q;
-    if (e < E) m.start[e] = run;
+    if (e < E) { m.start[e] = run; m.chunk[e] = chunk; }
     for (int r = 0; r < count[q]; r += BN, ++chunk) {
-      const int rows = min(BN, count[q] - r);
       plan.expert[chunk] = (short)e;
       plan.first[chunk] = (short)(run + r);
-      plan.rows[chunk] = (short)rows;
-      for (int i = 0; i < rows; ++i) plan.chunk_of[run + r + i] = (short)chunk;
+      plan.rows[chunk] = (short)min(BN, count[q] - r);
     }
     run += count[q];
   }
-  if (tid == kThreads - 1) { plan.total_rows = run; plan.chunks = chunk; }
+  if (tid == kThreads - 1) {
+    plan.total_rows = run;
+    plan.chunks = chunk;
+#pragma unroll
+    for (int f = 0; f < 2; ++f) plan.per[f] = ((unsigned)chunk * a.w[f].tiles * a.w[f].kblocks + gridDim.x - 1) / gridDim.x;
+  }
   __syncthreads();
   for (int i = tid; i < n; i += kThreads) {
     const int e = plan.ids[i], t = i / K;
     int r = -1;
     if (e >= 0) {
-      r = m.start[e];
+      int rank = 0;
 #pragma unroll
       for (int w = 0; w < kTokenWords; ++w) {
         const int b = t - 32 * w;
-        r += __popc(m.mask[e][w] & (b >= 32 ? kAll : b > 0 ? (1u << b) - 1u : 0u));
+        rank += __popc(m.mask[e][w] & (b >= 32 ? kAll : b > 0 ? (1u << b) - 1u : 0u));
       }
+      r = m.start[e] + rank;
       plan.order[r] = (short)i;
+      plan.chunk_of[r] = (short)(m.chunk[e] + rank / BN);
     }
     plan.row_of[i] = (short)r;
   }
@@ -304,17 +424,14 @@ template <int BN> __device__ inline void make_plan(const LayerArgs& a, Plan& pla
 
 // ---- stretches ----
 
-// Blocks that a matrix's K blocks are dealt out to: with one at least, so that no block between two others has nothing.
-__device__ __forceinline__ unsigned dealt(unsigned all) { return min(all, gridDim.x); }
-// A block's K blocks of all tiles of a matrix.
+// A block's K blocks of all tiles of a matrix: `per` of them, the last blocks fewer or none.
 struct Stretch {
   unsigned from, to;
   int chunk, tile, kb;                               // where it is
-  __device__ __forceinline__ Stretch(const Matrix& w, int chunks) {
+  __device__ __forceinline__ Stretch(const Matrix& w, int chunks, unsigned per) {
     const unsigned all = (unsigned)chunks * w.tiles * w.kblocks;
-    const unsigned n = dealt(all), b = min(blockIdx.x, n);
-    from = all * b / n;
-    to = b < n ? all * (b + 1) / n : from;
+    from = min(all, blockIdx.x * per);
+    to = min(all, from + per);
     const unsigned t = from / w.kblocks;
     kb = (int)(from - t * w.kblocks);
     chunk = (int)(t / w.tiles);
@@ -333,38 +450,37 @@ struct Stretch {
 template <int BN> __device__ __forceinline__ long long sums_at(const Plan& plan, const Matrix& w, int chunk, int tile, int block) {
   return (long long)plan.first[chunk] * w.tiles + tile * plan.rows[chunk] + block * BN;
 }
-// What a number of a tile's result is: four neighbouring ones of a row, over the blocks that have a part in the tile.
-template <int BN> struct Sum {
+// Where the numbers of a row are, of one tile: the sums of every block that has a part in it, in order.
+template <int BN> struct Parts {
   const float* at;
   int blocks;
-  __device__ __forceinline__ Sum(const LayerArgs& a, const Plan& plan, const Matrix& w, int row, int tile) {
+  __device__ __forceinline__ Parts(const LayerArgs& a, const Plan& plan, int f, int row, int tile) {
+    const Matrix& w = a.w[f];
     const int chunk = plan.chunk_of[row];
-    const unsigned all = (unsigned)plan.chunks * w.tiles * w.kblocks, t = (unsigned)chunk * w.tiles + tile;
-    const unsigned n = dealt(all), lo = ((t * w.kblocks + 1) * n - 1) / all, hi = ((t + 1) * w.kblocks * n - 1) / all;
-    blocks = (int)(hi - lo) + 1;
+    const unsigned x = ((unsigned)chunk * w.tiles + tile) * w.kblocks, per = plan.per[f], lo = x / per;
+    blocks = (int)((x + w.kblocks - 1) / per - lo) + 1;
     at = a.sums + (sums_at<BN>(plan, w, chunk, tile, (int)lo) + row - plan.first[chunk]) * 128;
   }
-  __device__ __forceinline__ float4 four(int col) const {
-    float4 s = __ldcg(reinterpret_cast<const float4*>(at + col));
-    for (int b = 1; b < blocks; ++b) {
-      const float4 v = __ldcg(reinterpret_cast<const float4*>(at + (long long)b * BN * 128 + col));
-      s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
-    }
-    return s;
-  }
-  __device__ __forceinline__ float get(int col) const {
-    float s = __ldcg(at + col);
-    for (int b = 1; b < blocks; ++b) s += __ldcg(at + (long long)b * BN * 128 + col);
-    return s;
-  }
 };
-// four numbers of u from number j on of row `row`
-template <int BN> __device__ __forceinline__ float4 hidden(const LayerArgs& a, const Plan& plan, int row, int j, int end) {
-  const Matrix& w = a.w[0];
-  if (j % 4 == 0 && j + 4 <= end) return Sum<BN>(a, plan, w, row, j / 128).four(j % 128);
+template <int BN> __device__ __forceinline__ float4 add_parts(float4 s, const float* at, int blocks) {       // those behind the first
+  for (int b = 1; b < blocks; ++b) {
+    const float4 v = __ldcg(reinterpret_cast<const float4*>(at + b * (BN * 128)));
+    s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
+  }
+  return s;
+}
+// four numbers of u from number j on of row `row`, one by one (h not a multiple of four)
+template <int BN> __device__ inline float4 hidden_one_by_one(const LayerArgs& a, const Plan& plan, int row, int j, int end) {
   float v[4];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) v[i] = j + i < end ? Sum<BN>(a, plan, w, row, (j + i) / 128).get((j + i) % 128) : 0.f;
+  for (int i = 0; i < 4; ++i) {
+    v[i] = 0.f;
+    if (j + i < end) {
+      const Parts<BN> p(a, plan, 0, row, (j + i) / 128);
+      v[i] = __ldcg(p.at + (j + i) % 128);
+      for (int b = 1; b < p.blocks; ++b) v[i] += __ldcg(p.at + b * (BN * 128) + (j + i) % 128);
+    }
+  }
   return make_float4(v[0], v[1], v[2], v[3]);
 }
 __device__ __forceinline__ float activated(float u, bool silu) {
@@ -414,13 +530,38 @@ expert_layer_kernel(const __grid_constant__ LayerArgs a, const __grid_constant__
     round_block(four(a.x, a.type, t * a.ldx, b * 128 + lane * 4, a.d, a.x_wide), a.xq + (long long)u * 128, a.xs + u, lane);
   }
   Making& making = *reinterpret_cast<Making*>(ring);
-  if (a.router) make_logits(a, reinterpret_cast<float (*)[kLogitWarps][kLogitTokens]>(ring), lane, wid);
-  __threadfence();
+  if (a.router) {
+    auto part = reinterpret_cast<float (*)[kLogitWarps][kLogitTokens]>(ring);
+    if (a.T == 1) make_logits<1>(a, part, lane, wid);
+    else make_logits<kLogitTokens>(a, part, lane, wid);
+  }
+  const bool share = a.T > kChoices;
+  float* x = making.x[wid];
+  unsigned* key = making.key[wid];
+  if (share && !a.router) choose_some(a, (int)blockIdx.x + wid * (int)gridDim.x, (int)gridDim.x * kWarps, x, key, lane, a.made_ids, a.made_weights);
   __syncthreads();
   if (tid == 0) {
     come(&a.shared->meeting[MEET_TOKENS].count);
-    if (a.router) meet(a.shared, MEET_TOKENS, a.wait_limit, abort);
+    if (a.router || share) meet(a.shared, MEET_TOKENS, a.wait_limit, abort);
   }
+  __syncthreads();
+  if (share && a.router) {
+    choose_some(a, (int)blockIdx.x + wid * (int)gridDim.x, (int)gridDim.x * kWarps, x, key, lane, a.made_ids, a.made_weights);
+    __syncthreads();
+    if (tid == 0) {
+      come(&a.shared->meeting[MEET_CHOICE].count);
+      meet(a.shared, MEET_CHOICE, a.wait_limit, abort);
+    }
+    __syncthreads();
+  }
+  if (!share) choose_some(a, wid, kWarps, x, key, lane, plan.ids, plan.weights);
+  else
+    for (int i = tid; i < a.T * a.c.top_k; i += kThreads) {
+      // (what a block that gave up did not write could be anything)
+      const int id = __ldcg(a.made_ids + i);
+      plan.ids[i] = (short)(id >= 0 && id < a.c.experts ? id : -1);
+      plan.weights[i] = __ldcg(a.made_weights + i);
+    }
   __syncthreads();
   make_plan<BN>(a, plan, making, tid, lane, wid);
   asm volatile("fence.proxy.async.shared::cta;" ::: "memory");             // the ring was the plan's scratch until here
@@ -436,7 +577,7 @@ expert_layer_kernel(const __grid_constant__ LayerArgs a, const __grid_constant__
       bool ok = !*reinterpret_cast<volatile int*>(abort);
       for (int f = 0; f < 2 && ok && chunks; ++f) {
         const Matrix& w = a.w[f];
-        for (Stretch s(w, chunks); s.there(); s.next(w), ++it) {
+        for (Stretch s(w, chunks, plan.per[f]); s.there(); s.next(w), ++it) {
           const unsigned q = it % S;
           if (it >= S && !(ok = wait(bars + L::DONE + q, (it / S - 1) & 1, a.wait_limit, abort))) break;
           mbar_expect_tx(bars + L::FULL + q, L::kWeights);
@@ -452,7 +593,7 @@ expert_layer_kernel(const __grid_constant__ LayerArgs a, const __grid_constant__
       bool ok = true;
       for (int f = 0; f < 2 && ok && chunks; ++f) {
         const unsigned idesc = a.w[f].idesc;
-        for (Stretch s(a.w[f], chunks); s.there(); ++s.from, ++it) {
+        for (Stretch s(a.w[f], chunks, plan.per[f]); s.there(); ++s.from, ++it) {
           if ((it & 1) != me) continue;
           const unsigned q = it % S, stage = it % kAccStages;
           if (!(ok = wait(bars + L::FULL + q, (it / S) & 1, a.wait_limit, abort) && wait(bars + L::READY + q, (it / S) & 1, a.wait_limit, abort))) break;
@@ -486,7 +627,7 @@ expert_layer_kernel(const __grid_constant__ LayerArgs a, const __grid_constant__
       const float* of_token[BN > 32 ? 2 : 1];
       const float* of_weights = nullptr;
       bool fresh = true;
-      for (Stretch s(w, chunks); s.there(); s.next(w), ++it) {
+      for (Stretch s(w, chunks, plan.per[f]); s.there(); s.next(w), ++it) {
         if (fresh || s.kb == 0) {
           fresh = false;
           const int first = plan.first[s.chunk], n = plan.rows[s.chunk];
@@ -515,8 +656,8 @@ expert_layer_kernel(const __grid_constant__ LayerArgs a, const __grid_constant__
           if (i * 32 + lane < BN) copy4(sc + i * 32 + lane, of_token[i] ? of_token[i] + s.kb : from_scales, of_token[i] != nullptr);
         if (lane == 0) copy4(sc + BN, of_weights + s.kb * w.block, true);
         asm volatile("cp.async.commit_group;" ::: "memory");
-        if (it - given >= kAhead) {
-          asm volatile("cp.async.wait_group %0;" ::"n"(kAhead) : "memory");
+        if (it - given >= L::kAhead) {
+          asm volatile("cp.async.wait_group %0;" ::"n"(L::kAhead) : "memory");
           hand_over();
         }
       }
@@ -534,7 +675,7 @@ expert_layer_kernel(const __grid_constant__ LayerArgs a, const __grid_constant__
       const Matrix& w = a.w[f];
       if (chunks) {
         float acc[L::kRows];
-        for (Stretch s(w, chunks); s.there();) {
+        for (Stretch s(w, chunks, plan.per[f]); s.there();) {
 #pragma unroll
           for (int c = 0; c < L::kRows; ++c) acc[c] = 0.f;
           const int chunk = s.chunk, tile = s.tile;
@@ -575,7 +716,6 @@ expert_layer_kernel(const __grid_constant__ LayerArgs a, const __grid_constant__
           if (++s.tile == w.tiles) { s.tile = 0; ++s.chunk; }
         }
       }
-      __threadfence();
       readers_sync();
       // (one thread decides for all readers: where a warp gave up, the block does not come, and the meeting fails)
       if (tid == 128) {
@@ -590,28 +730,65 @@ expert_layer_kernel(const __grid_constant__ LayerArgs a, const __grid_constant__
         const int hb = a.w[1].kblocks;
         for (int u = reader; u < rows * hb; u += readers) {
           const int row = u / hb, j = u % hb * 128 + lane * 4;
-          float4 v = hidden<BN>(a, plan, row, min(j, a.h), a.h);
-          v = make_float4(activated(v.x, a.silu), activated(v.y, a.silu), activated(v.z, a.silu), activated(v.w, a.silu));
-          if (a.gated) {
-            const float4 up = hidden<BN>(a, plan, row, a.h + min(j, a.h), 2 * a.h);
-            v.x *= up.x; v.y *= up.y; v.z *= up.z; v.w *= up.w;
+          float4 v = make_float4(0.f, 0.f, 0.f, 0.f), up = v;
+          if (a.h % 4 == 0) {
+            if (j < a.h) {
+              const int j2 = a.gated ? a.h + j : j;
+              const Parts<BN> p(a, plan, 0, row, j / 128), p2(a, plan, 0, row, j2 / 128);
+              const float *at = p.at + j % 128, *at2 = p2.at + j2 % 128;
+              v = __ldcg(reinterpret_cast<const float4*>(at));
+              up = __ldcg(reinterpret_cast<const float4*>(at2));
+              v = add_parts<BN>(v, at, p.blocks);
+              if (a.gated) up = add_parts<BN>(up, at2, p2.blocks);
+            }
+          } else {
+            v = hidden_one_by_one<BN>(a, plan, row, j, a.h);
+            if (a.gated) up = hidden_one_by_one<BN>(a, plan, row, a.h + min(j, a.h), 2 * a.h);
           }
+          v = make_float4(activated(v.x, a.silu), activated(v.y, a.silu), activated(v.z, a.silu), activated(v.w, a.silu));
+          if (a.gated) { v.x *= up.x; v.y *= up.y; v.z *= up.z; v.w *= up.w; }
           round_block(v, a.hq + (long long)u * 128, a.hs + u, lane);
         }
-        __threadfence();
         readers_sync();
         if (tid == 128) come(&a.shared->meeting[MEET_HIDDEN].count);
       } else {
+        const int K = a.c.top_k;
         for (int u = reader; u < a.T * w.tiles; u += readers) {
           const int t = u / w.tiles, tile = u % w.tiles, c = tile * 128 + lane * 4;
+          // lane j: where the j-th choice's numbers are
+          unsigned long long at = 0;
+          int blocks = 0;
+          float wt = 0.f;
+          if (lane < K) {
+            const int row = plan.row_of[t * K + lane];
+            if (row >= 0) {
+              const Parts<BN> p(a, plan, 1, row, tile);
+              at = reinterpret_cast<unsigned long long>(p.at);
+              blocks = p.blocks;
+              wt = plan.weights[t * K + lane];
+            }
+          }
           float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-          for (int j = 0; j < a.c.top_k; ++j) {
-            const int row = plan.row_of[t * a.c.top_k + j];
-            if (row < 0) continue;
-            const float wt = plan.weights[t * a.c.top_k + j];
-            const float4 z = Sum<BN>(a, plan, w, row, tile).four(lane * 4);
-            y.x = fmaf(wt, z.x, y.x); y.y = fmaf(wt, z.y, y.y); y.z = fmaf(wt, z.z, y.z); y.w = fmaf(wt, z.w, y.w);
+          for (int j0 = 0; j0 < K; j0 += 8) {
+            float4 z[8];
+            const float* from[8];
+            int n[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              const int j = min(j0 + i, 31);
+              from[i] = reinterpret_cast<const float*>(__shfl_sync(kAll, at, j)) + lane * 4;
+              n[i] = __shfl_sync(kAll, blocks, j);
+              z[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+              if (j0 + i < K && n[i]) z[i] = __ldcg(reinterpret_cast<const float4*>(from[i]));
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              const float q = __shfl_sync(kAll, wt, min(j0 + i, 31));
+              if (j0 + i < K && n[i]) {
+                z[i] = add_parts<BN>(z[i], from[i], n[i]);
+                y.x = fmaf(q, z[i].x, y.x); y.y = fmaf(q, z[i].y, y.y); y.z = fmaf(q, z[i].z, y.z); y.w = fmaf(q, z[i].w, y.w);
+              }
+            }
           }
           const float v[4] = {y.x, y.y, y.z, y.w};
 #pragma unroll
@@ -650,7 +827,7 @@ int tokens_of(long long assignments, int experts) {
   return mean <= 8 ? 16 : mean <= 18 ? 32 : 64;
 }
 struct Places {
-  size_t logits, xq, xs, hq, hs, sums, bytes;
+  size_t logits, ids, weights, xq, xs, hq, hs, sums, bytes;
 };
 Places places(const asgd_route_config& c, const asgd_expert_layer_args& a) {
   const size_t T = (size_t)a.T, rows = T * c.top_k, rows1 = (size_t)a.h * (a.gated ? 2 : 1);
@@ -659,6 +836,8 @@ Places places(const asgd_route_config& c, const asgd_expert_layer_args& a) {
   size_t at = up256(sizeof(Shared));
   auto take = [&](size_t n) { const size_t here = at; at += up256(n); return here; };
   p.logits = take(a.router ? T * c.experts * 4 : 0);
+  p.ids = take(rows * 4);
+  p.weights = take(rows * 4);
   p.xq = take(T * kb1 * 128);
   p.xs = take(T * kb1 * 4);
   p.hq = take(rows * kb2 * 128);
@@ -751,6 +930,8 @@ extern "C" int asgd_expert_layer(const asgd_route_config* cfg, const asgd_expert
   p.ids = a.ids; p.weights = a.weights;
   p.shared = reinterpret_cast<Shared*>(base);
   p.made_logits = a.router ? reinterpret_cast<float*>(base + at.logits) : nullptr;
+  p.made_ids = reinterpret_cast<int*>(base + at.ids);
+  p.made_weights = reinterpret_cast<float*>(base + at.weights);
   p.xq = base + at.xq;
   p.xs = reinterpret_cast<float*>(base + at.xs);
   p.hq = base + at.hq;
