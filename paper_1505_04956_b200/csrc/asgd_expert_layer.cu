@@ -114,6 +114,7 @@ struct Making {
   float x[kWarps][ASGD_MAX_EXPERTS];
   unsigned mask[ASGD_MAX_EXPERTS][kTokenWords];      // the tokens of an expert
   int start[ASGD_MAX_EXPERTS], chunk[ASGD_MAX_EXPERTS];
+  float bias[ASGD_MAX_EXPERTS];
 };
 constexpr size_t kMost = 227 * 1024 - sizeof(Plan) - 64;
 static_assert(Layer<16>::kSmem <= kMost && Layer<32>::kSmem <= kMost && Layer<64>::kSmem <= kMost, "shared memory");
@@ -136,6 +137,18 @@ __device__ inline bool meet(Shared* sh, int which, unsigned limit, int* abort) {
   }
   *reinterpret_cast<volatile int*>(abort) = 1;
   return false;
+}
+
+// A copy of weights, which are read once a step: the first to leave L2, so that they do not drive out what every step reads again
+// (router, scales, and the kernel's own instructions, each of whose lines is otherwise fetched anew from HBM).
+__device__ inline unsigned long long leaves_first() {
+  unsigned long long p;
+  asm("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(p));
+  return p;
+}
+__device__ inline void load_weights(void* dst, const CUtensorMap* map, int x, int y, int z, unsigned long long* bar, unsigned long long policy) {
+  asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1, {%2, %3, %4}], [%5], %6;"
+               ::"r"(smem_u32(dst)), "l"(map), "r"(x), "r"(y), "r"(z), "r"(smem_u32(bar)), "l"(policy) : "memory");
 }
 
 // ---- tokens ----
@@ -245,7 +258,7 @@ template <typename T> __device__ __forceinline__ void read_logits(const T* row, 
 #pragma unroll 4
   for (int e = lane; e < E; e += 32) x[e] = Elem<T>::to_f(__ldcg(row + e));
 }
-__device__ inline void choose_one(const LayerArgs& a, int t, float* x, unsigned* key, int lane, int& id, float& weight) {
+__device__ inline void choose_one(const LayerArgs& a, int t, const float* bias, float* x, unsigned* key, int lane, int& id, float& weight) {
   const asgd_route_config& c = a.c;
   const int E = c.experts, K = c.top_k;
   const bool by_logit = a.bias == nullptr && c.group_top == 1, sigmoid_scores = c.score == ASGD_SCORE_SIGMOID;
@@ -271,7 +284,7 @@ __device__ inline void choose_one(const LayerArgs& a, int t, float* x, unsigned*
     const bool there = v > -INFINITY;
     if (!by_logit) {
       v = sigmoid_scores ? sigmoid(v) : f.score(v);
-      if (a.bias) v = __fadd_rn(v, a.bias[e]);
+      if (a.bias) v = __fadd_rn(v, bias[e]);
     }
     const unsigned k = there && v > -INFINITY ? ordered(v) : 0u;
     key[e] = k;
@@ -337,31 +350,52 @@ __device__ inline void choose_one(const LayerArgs& a, int t, float* x, unsigned*
     weight = c.scale * s;
   }
 }
-// The choices of tokens first, first + step, ..., of a warp, to arrays of all tokens' choices.
-template <typename Id> __device__ __forceinline__ void choose_some(const LayerArgs& a, int first, int step, float* x, unsigned* key, int lane, Id* ids, float* weights) {
+// The choices of tokens first, first + step, ..., of a warp, to arrays of all tokens' choices; mask: where the tokens of each expert
+// are marked, too.
+template <typename Id> __device__ __forceinline__ void choose_some(const LayerArgs& a, int first, int step, Making& m, int lane, int wid, Id* ids, float* weights, bool mark) {
   const int K = a.c.top_k;
   for (int t = first; t < a.T; t += step) {
     int id;
     float w;
-    choose_one(a, t, x, key, lane, id, w);
+    choose_one(a, t, m.bias, m.x[wid], m.key[wid], lane, id, w);
     if (lane < K) {
       ids[t * K + lane] = (Id)id;
       weights[t * K + lane] = w;
+      if (mark && id >= 0) atomicOr(&m.mask[id][t >> 5], 1u << (t & 31));
     }
   }
 }
-// Rows by expert from the choices in plan.ids.  The whole block.
+// Rows by expert of 32 assignments at most, by a warp: lane i has assignment i; a row is the number of lanes before it by expert and place.
+template <int BN> __device__ inline void make_small_plan(const LayerArgs& a, Plan& plan, int lane) {
+  const int n = a.T * a.c.top_k, e = lane < n ? plan.ids[lane] : -1;
+  int row = 0, rank = 0;
+  for (int i = 0; i < n; ++i) {
+    const int o = __shfl_sync(kAll, e, i);
+    const bool same = o == e && i < lane;
+    row += (o >= 0 && o < e) || same;
+    rank += same;
+  }
+  const unsigned there = __ballot_sync(kAll, e >= 0);
+  // chunks begin where a rank is a multiple of BN; in the rows' order
+  unsigned begins = e >= 0 && rank % BN == 0 ? 1u << row : 0u;
+  begins = __reduce_or_sync(kAll, begins);
+  if (lane < n) plan.row_of[lane] = (short)(e >= 0 ? row : -1);
+  if (e >= 0) {
+    const int chunk = __popc(begins & (2u << row) - 1u) - 1;
+    plan.order[row] = (short)lane;
+    plan.chunk_of[row] = (short)chunk;
+    if ((begins >> row) & 1u) {
+      const unsigned later = begins & ~((2u << row) - 1u);
+      plan.expert[chunk] = (short)e;
+      plan.first[chunk] = (short)row;
+      plan.rows[chunk] = (short)((later ? __ffs(later) - 1 : __popc(there)) - row);
+    }
+  }
+  if (lane == 0) { plan.total_rows = __popc(there); plan.chunks = __popc(begins); }
+}
+// Rows by expert from the choices in plan.ids and the marked tokens.  The whole block.
 template <int BN> __device__ inline void make_plan(const LayerArgs& a, Plan& plan, Making& m, int tid, int lane, int wid) {
   const int E = a.c.experts, K = a.c.top_k, n = a.T * K;
-  for (int i = tid; i < E * kTokenWords; i += kThreads) (&m.mask[0][0])[i] = 0;
-  __syncthreads();
-  for (int i = tid; i < n; i += kThreads) {
-    const int e = plan.ids[i], t = i / K;
-    if (e >= 0) atomicOr(&m.mask[e][t >> 5], 1u << (t & 31));
-    if (blockIdx.x == 0 && a.ids) a.ids[i] = e;
-    if (blockIdx.x == 0 && a.weights) a.weights[i] = plan.weights[i];
-  }
-  __syncthreads();
   // rows and chunks before each expert
   constexpr int kPer = (ASGD_MAX_EXPERTS + kThreads - 1) / kThreads;
   int mine = 0, mine_chunks = 0, count[kPer];
@@ -396,12 +430,7 @@ template <int BN> __device__ inline void make_plan(const LayerArgs& a, Plan& pla
     }
     run += count[q];
   }
-  if (tid == kThreads - 1) {
-    plan.total_rows = run;
-    plan.chunks = chunk;
-#pragma unroll
-    for (int f = 0; f < 2; ++f) plan.per[f] = ((unsigned)chunk * a.w[f].tiles * a.w[f].kblocks + gridDim.x - 1) / gridDim.x;
-  }
+  if (tid == kThreads - 1) { plan.total_rows = run; plan.chunks = chunk; }
   __syncthreads();
   for (int i = tid; i < n; i += kThreads) {
     const int e = plan.ids[i], t = i / K;
@@ -419,7 +448,6 @@ template <int BN> __device__ inline void make_plan(const LayerArgs& a, Plan& pla
     }
     plan.row_of[i] = (short)r;
   }
-  __syncthreads();
 }
 
 // ---- stretches ----
@@ -462,13 +490,60 @@ template <int BN> struct Parts {
     at = a.sums + (sums_at<BN>(plan, w, chunk, tile, (int)lo) + row - plan.first[chunk]) * 128;
   }
 };
-template <int BN> __device__ __forceinline__ float4 add_parts(float4 s, const float* at, int blocks) {       // those behind the first
-  for (int b = 1; b < blocks; ++b) {
-    const float4 v = __ldcg(reinterpret_cast<const float4*>(at + b * (BN * 128)));
-    s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
+// Four neighbouring numbers of several results at once, each the sum of its parts in order; the loads of the results are in flight
+// together.  (One after another each took L2's latency for every part: 6 us for a token's eight choices.)
+template <int BN, int N> __device__ __forceinline__ void add_up(const float* const (&at)[N], const int (&blocks)[N], float4 (&sum)[N]) {
+  int most = 0;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    sum[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (blocks[i]) sum[i] = __ldcg(reinterpret_cast<const float4*>(at[i]));
+    most = max(most, blocks[i]);
   }
-  return s;
+#pragma unroll 1
+  for (int b = 1; b < most; ++b) {
+    float4 v[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      v[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (b < blocks[i]) v[i] = __ldcg(reinterpret_cast<const float4*>(at[i] + b * (BN * 128)));
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      if (b < blocks[i]) { sum[i].x += v[i].x; sum[i].y += v[i].y; sum[i].z += v[i].z; sum[i].w += v[i].w; }
+  }
 }
+// Where the four numbers of a row's u from number j on are, and those that gate them (h is a multiple of four).
+template <int BN> struct HiddenAt {
+  const float* at[2] = {nullptr, nullptr};
+  int blocks[2] = {0, 0};
+  __device__ __forceinline__ HiddenAt() {}
+  __device__ __forceinline__ HiddenAt(const LayerArgs& a, const Plan& plan, int row, int j) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      if (j >= a.h || (i && !a.gated)) continue;
+      const Parts<BN> p(a, plan, 0, row, (i * a.h + j) / 128);
+      at[i] = p.at + (i * a.h + j) % 128;
+      blocks[i] = p.blocks;
+    }
+  }
+};
+// Lane j: where a token's j-th choice's four numbers of a tile are (for lane 0), and its weight.
+template <int BN> struct ChoiceAt {
+  unsigned long long at = 0;
+  int blocks = 0;
+  float weight = 0.f;
+  __device__ __forceinline__ ChoiceAt() {}
+  __device__ __forceinline__ ChoiceAt(const LayerArgs& a, const Plan& plan, int t, int tile, int lane) {
+    if (lane >= a.c.top_k) return;
+    const int i = t * a.c.top_k + lane, row = plan.row_of[i];
+    if (row < 0) return;
+    const Parts<BN> p(a, plan, 1, row, tile);
+    at = reinterpret_cast<unsigned long long>(p.at);
+    blocks = p.blocks;
+    weight = plan.weights[i];
+  }
+};
 // four numbers of u from number j on of row `row`, one by one (h not a multiple of four)
 template <int BN> __device__ inline float4 hidden_one_by_one(const LayerArgs& a, const Plan& plan, int row, int j, int end) {
   float v[4];
@@ -524,29 +599,41 @@ expert_layer_kernel(const __grid_constant__ LayerArgs a, const __grid_constant__
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(misc)), "r"(L::kCols) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
+  // What is read soon comes now: from cold memory a first read takes 2 to 3 us.
+  Making& making = *reinterpret_cast<Making*>(ring);
+  const bool share = a.T > kChoices;
+  if (a.bias)
+    for (int e = tid; e < a.c.experts; e += kThreads) copy4(making.bias + e, a.bias + e, true);
+  if (a.logits) {
+    const int t = share ? (int)blockIdx.x + wid * (int)gridDim.x : wid, size = a.logits_type == ASGD_F32 ? 4 : 2;
+    const char* row = reinterpret_cast<const char*>(a.logits) + t * a.ld_logits * size;
+    if (t < a.T)
+      for (int at = lane * 128; at < a.c.experts * size; at += 32 * 128) asm volatile("prefetch.global.L2 [%0];" ::"l"(row + at));
+  }
+  for (int i = tid; i < a.c.experts * kTokenWords; i += kThreads) (&making.mask[0][0])[i] = 0;
   // step 0
   for (int u = (int)blockIdx.x * kWarps + wid; u < a.T * a.w[0].kblocks; u += (int)gridDim.x * kWarps) {
     const int t = u / a.w[0].kblocks, b = u % a.w[0].kblocks;
     round_block(four(a.x, a.type, t * a.ldx, b * 128 + lane * 4, a.d, a.x_wide), a.xq + (long long)u * 128, a.xs + u, lane);
   }
-  Making& making = *reinterpret_cast<Making*>(ring);
   if (a.router) {
-    auto part = reinterpret_cast<float (*)[kLogitWarps][kLogitTokens]>(ring);
+    auto part = reinterpret_cast<float (*)[kLogitWarps][kLogitTokens]>(making.x);
     if (a.T == 1) make_logits<1>(a, part, lane, wid);
     else make_logits<kLogitTokens>(a, part, lane, wid);
   }
-  const bool share = a.T > kChoices;
-  float* x = making.x[wid];
-  unsigned* key = making.key[wid];
-  if (share && !a.router) choose_some(a, (int)blockIdx.x + wid * (int)gridDim.x, (int)gridDim.x * kWarps, x, key, lane, a.made_ids, a.made_weights);
+  asm volatile("cp.async.wait_all;" ::: "memory");
   __syncthreads();
+  if (share && !a.router) {
+    choose_some(a, (int)blockIdx.x + wid * (int)gridDim.x, (int)gridDim.x * kWarps, making, lane, wid, a.made_ids, a.made_weights, false);
+    __syncthreads();
+  }
   if (tid == 0) {
     come(&a.shared->meeting[MEET_TOKENS].count);
     if (a.router || share) meet(a.shared, MEET_TOKENS, a.wait_limit, abort);
   }
-  __syncthreads();
+  if (a.router || share) __syncthreads();
   if (share && a.router) {
-    choose_some(a, (int)blockIdx.x + wid * (int)gridDim.x, (int)gridDim.x * kWarps, x, key, lane, a.made_ids, a.made_weights);
+    choose_some(a, (int)blockIdx.x + wid * (int)gridDim.x, (int)gridDim.x * kWarps, making, lane, wid, a.made_ids, a.made_weights, false);
     __syncthreads();
     if (tid == 0) {
       come(&a.shared->meeting[MEET_CHOICE].count);
@@ -554,16 +641,30 @@ expert_layer_kernel(const __grid_constant__ LayerArgs a, const __grid_constant__
     }
     __syncthreads();
   }
-  if (!share) choose_some(a, wid, kWarps, x, key, lane, plan.ids, plan.weights);
+  const int assignments = a.T * a.c.top_k;
+  if (!share) choose_some(a, wid, kWarps, making, lane, wid, plan.ids, plan.weights, true);
   else
-    for (int i = tid; i < a.T * a.c.top_k; i += kThreads) {
+    for (int i = tid; i < assignments; i += kThreads) {
       // (what a block that gave up did not write could be anything)
-      const int id = __ldcg(a.made_ids + i);
-      plan.ids[i] = (short)(id >= 0 && id < a.c.experts ? id : -1);
+      const int id = __ldcg(a.made_ids + i), t = i / a.c.top_k;
+      const bool ok = id >= 0 && id < a.c.experts;
+      plan.ids[i] = (short)(ok ? id : -1);
       plan.weights[i] = __ldcg(a.made_weights + i);
+      if (ok) atomicOr(&making.mask[id][t >> 5], 1u << (t & 31));
     }
   __syncthreads();
-  make_plan<BN>(a, plan, making, tid, lane, wid);
+  if (blockIdx.x == 0)
+    for (int i = tid; i < assignments; i += kThreads) {
+      if (a.ids) a.ids[i] = plan.ids[i];
+      if (a.weights) a.weights[i] = plan.weights[i];
+    }
+  if (assignments <= 32) {
+    if (wid == 0) make_small_plan<BN>(a, plan, lane);
+  } else {
+    make_plan<BN>(a, plan, making, tid, lane, wid);
+  }
+  __syncthreads();
+  if (tid < 2) plan.per[tid] = ((unsigned)plan.chunks * a.w[tid].tiles * a.w[tid].kblocks + gridDim.x - 1) / gridDim.x;
   asm volatile("fence.proxy.async.shared::cta;" ::: "memory");             // the ring was the plan's scratch until here
   fence_before();
   __syncthreads();
@@ -573,6 +674,7 @@ expert_layer_kernel(const __grid_constant__ LayerArgs a, const __grid_constant__
 
   if (wid == 0) {
     if (lane == 0) {
+      const unsigned long long policy = leaves_first();
       unsigned it = 0;
       bool ok = !*reinterpret_cast<volatile int*>(abort);
       for (int f = 0; f < 2 && ok && chunks; ++f) {
@@ -581,7 +683,7 @@ expert_layer_kernel(const __grid_constant__ LayerArgs a, const __grid_constant__
           const unsigned q = it % S;
           if (it >= S && !(ok = wait(bars + L::DONE + q, (it / S - 1) & 1, a.wait_limit, abort))) break;
           mbar_expect_tx(bars + L::FULL + q, L::kWeights);
-          if (!(a.withhold && it == 0)) tma_load_3d(ring + (size_t)q * L::kSlotBytes, f ? &map_2 : &map_1, s.kb * kKB, s.tile * kU, plan.expert[s.chunk], bars + L::FULL + q);
+          if (!(a.withhold && it == 0)) load_weights(ring + (size_t)q * L::kSlotBytes, f ? &map_2 : &map_1, s.kb * kKB, s.tile * kU, plan.expert[s.chunk], bars + L::FULL + q, policy);
         }
       }
       misc[2] = (int)it;
@@ -615,6 +717,14 @@ expert_layer_kernel(const __grid_constant__ LayerArgs a, const __grid_constant__
       if (lane == 0) arrive(bars + L::READY + given % S);
       ++given;
     };
+    if (chunks) {                                    // the scales of W2, so that they are not waited for later on
+      const Matrix& w = a.w[1];
+      const Stretch s(w, chunks, plan.per[1]);
+      for (unsigned x = s.from + lane; x < s.to; x += 32) {
+        const int tile = (int)(x / w.kblocks);
+        asm volatile("prefetch.global.L2 [%0];" ::"l"(w.scale + plan.expert[tile / w.tiles] * w.group + tile % w.tiles * w.row + (x - tile * w.kblocks) * w.block));
+      }
+    }
     for (int f = 0; f < 2 && ok && chunks; ++f) {
       bool met = true;
       if (lane == 0) met = meet(a.shared, f ? MEET_HIDDEN : MEET_TOKENS, a.wait_limit, abort);
@@ -716,6 +826,12 @@ expert_layer_kernel(const __grid_constant__ LayerArgs a, const __grid_constant__
           if (++s.tile == w.tiles) { s.tile = 0; ++s.chunk; }
         }
       }
+      // what comes after the meeting, as far as it can be known before
+      const int hb = a.w[1].kblocks;
+      HiddenAt<BN> hidden;
+      ChoiceAt<BN> choice;
+      if (f == 0 && reader < rows * hb && a.h % 4 == 0) hidden = HiddenAt<BN>(a, plan, reader / hb, reader % hb * 128 + lane * 4);
+      if (f == 1 && reader < a.T * w.tiles) choice = ChoiceAt<BN>(a, plan, reader / w.tiles, reader % w.tiles, lane);
       readers_sync();
       // (one thread decides for all readers: where a warp gave up, the block does not come, and the meeting fails)
       if (tid == 128) {
@@ -727,20 +843,15 @@ expert_layer_kernel(const __grid_constant__ LayerArgs a, const __grid_constant__
       ok = *reinterpret_cast<volatile int*>(misc + 3) != 0;
       if (!ok) break;
       if (f == 0) {
-        const int hb = a.w[1].kblocks;
         for (int u = reader; u < rows * hb; u += readers) {
           const int row = u / hb, j = u % hb * 128 + lane * 4;
           float4 v = make_float4(0.f, 0.f, 0.f, 0.f), up = v;
           if (a.h % 4 == 0) {
-            if (j < a.h) {
-              const int j2 = a.gated ? a.h + j : j;
-              const Parts<BN> p(a, plan, 0, row, j / 128), p2(a, plan, 0, row, j2 / 128);
-              const float *at = p.at + j % 128, *at2 = p2.at + j2 % 128;
-              v = __ldcg(reinterpret_cast<const float4*>(at));
-              up = __ldcg(reinterpret_cast<const float4*>(at2));
-              v = add_parts<BN>(v, at, p.blocks);
-              if (a.gated) up = add_parts<BN>(up, at2, p2.blocks);
-            }
+            if (u != reader) hidden = HiddenAt<BN>(a, plan, row, j);
+            float4 both[2];
+            add_up<BN>(hidden.at, hidden.blocks, both);
+            v = both[0];
+            up = both[1];
           } else {
             v = hidden_one_by_one<BN>(a, plan, row, j, a.h);
             if (a.gated) up = hidden_one_by_one<BN>(a, plan, row, a.h + min(j, a.h), 2 * a.h);
@@ -755,19 +866,7 @@ expert_layer_kernel(const __grid_constant__ LayerArgs a, const __grid_constant__
         const int K = a.c.top_k;
         for (int u = reader; u < a.T * w.tiles; u += readers) {
           const int t = u / w.tiles, tile = u % w.tiles, c = tile * 128 + lane * 4;
-          // lane j: where the j-th choice's numbers are
-          unsigned long long at = 0;
-          int blocks = 0;
-          float wt = 0.f;
-          if (lane < K) {
-            const int row = plan.row_of[t * K + lane];
-            if (row >= 0) {
-              const Parts<BN> p(a, plan, 1, row, tile);
-              at = reinterpret_cast<unsigned long long>(p.at);
-              blocks = p.blocks;
-              wt = plan.weights[t * K + lane];
-            }
-          }
+          if (u != reader) choice = ChoiceAt<BN>(a, plan, t, tile, lane);
           float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
           for (int j0 = 0; j0 < K; j0 += 8) {
             float4 z[8];
@@ -776,18 +875,14 @@ expert_layer_kernel(const __grid_constant__ LayerArgs a, const __grid_constant__
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
               const int j = min(j0 + i, 31);
-              from[i] = reinterpret_cast<const float*>(__shfl_sync(kAll, at, j)) + lane * 4;
-              n[i] = __shfl_sync(kAll, blocks, j);
-              z[i] = make_float4(0.f, 0.f, 0.f, 0.f);
-              if (j0 + i < K && n[i]) z[i] = __ldcg(reinterpret_cast<const float4*>(from[i]));
+              from[i] = reinterpret_cast<const float*>(__shfl_sync(kAll, choice.at, j)) + lane * 4;
+              n[i] = __shfl_sync(kAll, choice.blocks, j);            // (lanes from top_k on have none)
             }
+            add_up<BN>(from, n, z);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-              const float q = __shfl_sync(kAll, wt, min(j0 + i, 31));
-              if (j0 + i < K && n[i]) {
-                z[i] = add_parts<BN>(z[i], from[i], n[i]);
-                y.x = fmaf(q, z[i].x, y.x); y.y = fmaf(q, z[i].y, y.y); y.z = fmaf(q, z[i].z, y.z); y.w = fmaf(q, z[i].w, y.w);
-              }
+              const float q = __shfl_sync(kAll, choice.weight, min(j0 + i, 31));
+              if (j0 + i < K && n[i]) { y.x = fmaf(q, z[i].x, y.x); y.y = fmaf(q, z[i].y, y.y); y.z = fmaf(q, z[i].z, y.z); y.w = fmaf(q, z[i].w, y.w); }
             }
           }
           const float v[4] = {y.x, y.y, y.z, y.w};
