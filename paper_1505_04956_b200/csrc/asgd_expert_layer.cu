@@ -85,14 +85,12 @@ struct LayerArgs : Choice {
 template <int BN> struct Layer {
   static constexpr int kSlots = BN == 64 ? 8 : 10;   // even: a slot always meets the same issuing thread
   static constexpr unsigned kWeights = kU * kKB, kTokens = BN * kKB, kSlotBytes = kWeights + kTokens;
-  static constexpr int kAhead = kSlots - 2;          // K blocks of tokens' rows in flight
   static constexpr int kScales = BN + 4;             // of a slot: the tokens', then the weights' one
   static constexpr int kRows = BN / 2;               // tokens of a tile that a reading thread has
   static constexpr unsigned kCols = kAccStages * BN;
   enum { FULL = 0, READY = kSlots, DONE = 2 * kSlots, SEMPTY = 3 * kSlots, ACCEMPTY = 4 * kSlots, DRAIN = ACCEMPTY + kAccStages, COUNT = DRAIN + 2 };
   static constexpr size_t kRing = (size_t)kSlots * kSlotBytes;
   static constexpr size_t kSmem = 1024 + kRing + (size_t)kSlots * kScales * 4 + COUNT * 8;
-  static_assert(kSlots > kAhead, "copies of tokens' rows are handed over before their slots come round");
   static_assert(kSlots % 2 == 0 && kCols >= 32, "slots, tensor memory");
 };
 
@@ -588,7 +586,7 @@ expert_layer_kernel(const __grid_constant__ LayerArgs a, const __grid_constant__
     prefetch_map(&map_1);
     prefetch_map(&map_2);
     for (int q = 0; q < S; ++q) {
-      mbar_init(bars + L::FULL + q, 1); mbar_init(bars + L::READY + q, 1); mbar_init(bars + L::DONE + q, 1); mbar_init(bars + L::SEMPTY + q, kReaders);
+      mbar_init(bars + L::FULL + q, 1); mbar_init(bars + L::READY + q, 32); mbar_init(bars + L::DONE + q, 1); mbar_init(bars + L::SEMPTY + q, kReaders);
     }
     for (int q = 0; q < kAccStages; ++q) mbar_init(bars + L::ACCEMPTY + q, kReaders);
     for (int q = 0; q < 2; ++q) mbar_init(bars + L::DRAIN + q, 1);
@@ -702,6 +700,7 @@ expert_layer_kernel(const __grid_constant__ LayerArgs a, const __grid_constant__
           const unsigned long long du = operand_desc(ring + (size_t)q * L::kSlotBytes), dv = operand_desc(ring + (size_t)q * L::kSlotBytes + L::kWeights);
           if (it >= kAccStages && !(ok = wait(bars + L::ACCEMPTY + stage, (it / kAccStages - 1) & 1, a.wait_limit, abort))) break;
           fence_after();
+          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");      // the tokens' rows were written by ordinary copies
 #pragma unroll
           for (int k4 = 0; k4 < 4; ++k4) mma_f8(tmem + stage * BN, du + 2 * k4, dv + 2 * k4, idesc, k4 != 0);
           commit(bars + L::DONE + q);
@@ -709,14 +708,8 @@ expert_layer_kernel(const __grid_constant__ LayerArgs a, const __grid_constant__
       }
     }
   } else if (wid == 2) {
-    unsigned it = 0, given = 0;                      // K blocks asked for, and handed over
+    unsigned it = 0;
     bool ok = true;
-    auto hand_over = [&]() {                         // the oldest one, which has arrived
-      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-      __syncwarp();
-      if (lane == 0) arrive(bars + L::READY + given % S);
-      ++given;
-    };
     if (chunks) {                                    // the scales of W2, so that they are not waited for later on
       const Matrix& w = a.w[1];
       const Stretch s(w, chunks, plan.per[1]);
@@ -765,14 +758,8 @@ expert_layer_kernel(const __grid_constant__ LayerArgs a, const __grid_constant__
         for (int i = 0; i < (BN > 32 ? 2 : 1); ++i)
           if (i * 32 + lane < BN) copy4(sc + i * 32 + lane, of_token[i] ? of_token[i] + s.kb : from_scales, of_token[i] != nullptr);
         if (lane == 0) copy4(sc + BN, of_weights + s.kb * w.block, true);
-        asm volatile("cp.async.commit_group;" ::: "memory");
-        if (it - given >= L::kAhead) {
-          asm volatile("cp.async.wait_group %0;" ::"n"(L::kAhead) : "memory");
-          hand_over();
-        }
+        arrive_after_copies(bars + L::READY + q);
       }
-      asm volatile("cp.async.wait_all;" ::: "memory");
-      while (ok && given < it) hand_over();
     }
     asm volatile("cp.async.wait_all;" ::: "memory");
   } else if (wid >= 4) {
