@@ -597,6 +597,7 @@ expert_layer_kernel(const __grid_constant__ LayerArgs a, const __grid_constant__
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(misc)), "r"(L::kCols) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
+  wait_for_stream();                                 // what comes before reads nothing of the call's but its arguments
   // What is read soon comes now: from cold memory a first read takes 2 to 3 us.
   Making& making = *reinterpret_cast<Making*>(ring);
   const bool share = a.T > kChoices;
@@ -899,6 +900,13 @@ expert_layer_kernel(const __grid_constant__ LayerArgs a, const __grid_constant__
   if (tid == 0 && *reinterpret_cast<volatile int*>(abort)) atomicMin(a.status, ASGD_ETIMEOUT);
 }
 
+// The meetings' counts begin at zero.  (A kernel, so that the next one can come up beside it.)
+__global__ void begin_kernel(Shared* sh) {
+  wait_for_stream();
+  let_next_come();
+  for (unsigned i = threadIdx.x; i < sizeof(Shared) / 4; i += blockDim.x) reinterpret_cast<unsigned*>(sh)[i] = 0;
+}
+
 // ---- host ----
 
 constexpr size_t up256(size_t n) { return (n + 255) / 256 * 256; }
@@ -945,17 +953,19 @@ template <int BN> int launch(const asgd_route_config& c, const asgd_expert_layer
   if (!encode(&map_2, a.w2, a.h, a.d, c.experts, a.ldw2, a.w2_group, kU)) return ASGD_EINVAL;
   static std::atomic<unsigned long long> done{0};
   if (!allow_smem(expert_layer_kernel<BN>, Layer<BN>::kSmem, done)) return ASGD_ECUDA;
-  if (!good(cudaMemsetAsync(p.shared, 0, sizeof(Shared), st))) return ASGD_ECUDA;
-  cudaLaunchAttribute all;
-  all.id = cudaLaunchAttributeCooperative;
-  all.val.cooperative = 1;
+  if (!launch_after(begin_kernel, dim3(1), 64, 0, st, p.shared)) return ASGD_ECUDA;
+  cudaLaunchAttribute all[2];
+  all[0].id = cudaLaunchAttributeCooperative;
+  all[0].val.cooperative = 1;
+  all[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;      // see launch_after
+  all[1].val.programmaticStreamSerializationAllowed = 1;
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3(kSMs);
   cfg.blockDim = dim3(kThreads);
   cfg.dynamicSmemBytes = Layer<BN>::kSmem;
   cfg.stream = st;
-  cfg.attrs = &all;
-  cfg.numAttrs = 1;
+  cfg.attrs = all;
+  cfg.numAttrs = 2;
   return good(cudaLaunchKernelEx(&cfg, expert_layer_kernel<BN>, p, map_1, map_2)) ? ASGD_OK : ASGD_ECUDA;
 }
 
