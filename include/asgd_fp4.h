@@ -31,8 +31,8 @@ extern "C" {
  * NaN has the scale NaN and zeros.  The rows may be gathered and weighted on the way, as asgd_quantize does it.
  */
 typedef struct asgd_quantize4_args {
-  int64_t M, K;            /* rows and columns of the result; M <= 2^31 - 1, K <= ASGD_QUANTIZE_MAX; above 2^25 - 512
-                              K is ASGD_EUNSUPPORTED                                                        */
+  int64_t M, K;            /* rows and columns of the result; M <= 2^31 - 1, above K = 2^25 - 519
+                              ASGD_EUNSUPPORTED (so for asgd_dequantize4)                                   */
   const void *x;           /* [rows_x][ldx] of x_type, or of M rows without `source`                        */
   int64_t ldx;
   int64_t rows_x;          /* rows of x (equal to M without source)                                         */

@@ -2,12 +2,16 @@
 // include/asgd_fp4.h.
 //
 // A number is read once and stays in registers from the search for its block's largest magnitude to the rounding; the bytes
-// are the bound.  A lane takes 16-byte pieces of a row, so that a warp's loads are neighbours; 4 lanes (16-bit numbers) or 8
-// (fp32) have a block together and find its maximum by exchanges.  Magnitudes are compared as integers: floats of one sign
+// are the bound.  A lane takes pieces of a row of 32 bytes (16 where rows do not start at 32), two or four of them in flight,
+// so that a warp's loads are neighbours; 2 lanes (16-bit numbers) or 4 (fp32) have a block together and find its maximum by
+// exchanges.  8192 x 4096 bf16 numbers 14.2 us (5.9 TB/s; with 16-byte pieces 19), back 12.6; gathered four times 47, where the
+// instructions are the bound (some four a number), back 57 (6.0 TB/s).  Magnitudes are compared as integers: floats of one sign
 // are ordered like their bits, and infinities and NaNs come out on top.  The power of two comes from the largest one's
 // exponent and one comparison of its mantissa (a <= 6 s with a = m 2^k: s = 2^(k - 2) up to m = 1.5, else 2^(k - 1)), and
 // scaling by it is exact, so the one rounding is that of the conversion.
 #include <cuda_fp4.h>
+
+#include <type_traits>
 
 #include "../../include/asgd_fp4.h"
 #include "asgd_rows.cuh"
@@ -28,21 +32,49 @@ struct Args {
   int q_wide;                                        // rows of q start at whole pieces
 };
 
+// What a lane takes of a row at a time: 16 bytes, or 32 where rows start at multiples of that.
+template <int kBytes> struct __align__(kBytes) Piece { unsigned w[kBytes / 4]; };
+__device__ __forceinline__ Piece<32> read_piece(const void* at, Piece<32>*) {
+  Piece<32> p;
+  asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+               : "=r"(p.w[0]), "=r"(p.w[1]), "=r"(p.w[2]), "=r"(p.w[3]), "=r"(p.w[4]), "=r"(p.w[5]), "=r"(p.w[6]), "=r"(p.w[7]) : "l"(at) : "memory");
+  return p;
+}
+__device__ __forceinline__ Piece<16> read_piece(const void* at, Piece<16>*) { return *reinterpret_cast<const Piece<16>*>(at); }
+__device__ __forceinline__ void write_piece(void* at, const Piece<32>& p) {
+  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+               ::"l"(at), "r"(p.w[0]), "r"(p.w[1]), "r"(p.w[2]), "r"(p.w[3]), "r"(p.w[4]), "r"(p.w[5]), "r"(p.w[6]), "r"(p.w[7]) : "memory");
+}
+__device__ __forceinline__ void write_piece(void* at, const Piece<16>& p) { *reinterpret_cast<Piece<16>*>(at) = p; }
+
 // bits of the largest magnitude among a piece's numbers, as fp32
-template <typename T> __device__ __forceinline__ unsigned largest(const uint4& w) {
+template <typename T, int kBytes> __device__ __forceinline__ unsigned largest(const Piece<kBytes>& p) {
+  constexpr unsigned kMask = sizeof(T) == 4 ? 0x7fffffffu : 0x7fff7fffu;
+  unsigned m = p.w[0] & kMask;
   if constexpr (sizeof(T) == 4) {
-    return max(max(w.x & 0x7fffffffu, w.y & 0x7fffffffu), max(w.z & 0x7fffffffu, w.w & 0x7fffffffu));
+#pragma unroll
+    for (int i = 1; i < kBytes / 4; ++i) m = max(m, p.w[i] & kMask);
+    return m;
   } else {                                           // two at a time
-    const unsigned m = __vmaxu2(__vmaxu2(w.x & 0x7fff7fffu, w.y & 0x7fff7fffu), __vmaxu2(w.z & 0x7fff7fffu, w.w & 0x7fff7fffu));
+#pragma unroll
+    for (int i = 1; i < kBytes / 4; ++i) m = __vmaxu2(m, p.w[i] & kMask);
     const unsigned short h = (unsigned short)max(m & 0xffffu, m >> 16);
     return __float_as_uint(Elem<T>::to_f(*reinterpret_cast<const T*>(&h))) & 0x7fffffffu;
   }
 }
+// V 4-bit numbers (V / 2 bytes) as one store
+template <int V> __device__ __forceinline__ void store_codes(unsigned char* to, const unsigned (&w)[V > 8 ? 2 : 1]) {
+  if constexpr (V == 16) *reinterpret_cast<uint2*>(to) = make_uint2(w[0], w[1]);
+  else if constexpr (V == 8) *reinterpret_cast<unsigned*>(to) = w[0];
+  else *reinterpret_cast<unsigned short*>(to) = (unsigned short)w[0];
+}
 
 // A warp takes a stretch of a row: U pieces per lane, all loaded before the first is used.
-template <typename T, bool kVec, bool kWeights, int U> __global__ void __launch_bounds__(kThreads) rows4_kernel(const Args p) {
+// kAlign: bytes that rows of x start at multiples of, 32 or 16; 0: anywhere.
+template <typename T, int kAlign, bool kWeights, int U> __global__ void __launch_bounds__(kThreads) rows4_kernel(const Args p) {
   wait_for_stream();
-  constexpr int V = kPer16<T>, LB = ASGD_BLOCK4 / V;                     // numbers per piece, lanes per block
+  constexpr int kBytes = kAlign == 32 ? 32 : 16, V = kBytes / (int)sizeof(T), LB = ASGD_BLOCK4 / V;     // numbers per piece, lanes per block
+  using P = Piece<kBytes>;
   const asgd_quantize4_args& a = p.a;
   const int lane = threadIdx.x & 31, K = (int)a.K;
   const long long r = (long long)blockIdx.x * kWarps + (threadIdx.x >> 5);
@@ -51,30 +83,42 @@ template <typename T, bool kVec, bool kWeights, int U> __global__ void __launch_
   float factor;
   const long long from = input_row(p, r, factor);
   const T* row = reinterpret_cast<const T*>(a.x) + from * a.ldx;
-  uint4 raw[U];
-  if constexpr (kVec || sizeof(T) == 4) {
+  P raw[U];
+  if constexpr (kAlign || sizeof(T) == 4) {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int c = c0 + u * 32 * V;
-      raw[u] = make_uint4(0, 0, 0, 0);
-      if (from >= 0 && c < K) raw[u] = load<T, uint4, kVec>(row, c, K);
+#pragma unroll
+      for (int i = 0; i < kBytes / 4; ++i) raw[u].w[i] = 0;
+      if (from < 0 || c >= K) continue;
+      if (kAlign && c + V <= K) raw[u] = read_piece(row + c, (P*)nullptr);
+      else {
+        T* e = reinterpret_cast<T*>(raw[u].w);
+#pragma unroll
+        for (int i = 0; i < V; ++i) if (c + i < K) e[i] = row[c + i];
+      }
     }
   } else {
     Unaligned<T, uint4> two[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) two[u].start(p, row, c0 + u * 32 * V, from >= 0 && c0 + u * 32 * V < K);
 #pragma unroll
-    for (int u = 0; u < U; ++u) raw[u] = two[u].get(row, c0 + u * 32 * V, K, from >= 0 && c0 + u * 32 * V < K);
+    for (int u = 0; u < U; ++u) {
+      const uint4 w = two[u].get(row, c0 + u * 32 * V, K, from >= 0 && c0 + u * 32 * V < K);
+      raw[u].w[0] = w.x; raw[u].w[1] = w.y; raw[u].w[2] = w.z; raw[u].w[3] = w.w;
+    }
   }
   unsigned char* q = reinterpret_cast<unsigned char*>(a.q) + r * a.ldq;
   unsigned char* scale = reinterpret_cast<unsigned char*>(a.scale) + r * a.scale_row;
 #pragma unroll
   for (int u = 0; u < U; ++u) {
     const int c = c0 + u * 32 * V;
+    T* e = reinterpret_cast<T*>(raw[u].w);
     float v[V];
-    unpack16<T>(raw[u], v);
     unsigned m = 0;
     if (kWeights) {
+#pragma unroll
+      for (int i = 0; i < V; ++i) v[i] = Elem<T>::to_f(e[i]);
 #pragma unroll
       for (int i = 0; i < V; ++i) { v[i] = __fmul_rn(v[i], factor); m = max(m, __float_as_uint(v[i]) & 0x7fffffffu); }
     } else {
@@ -87,91 +131,141 @@ template <typename T, bool kVec, bool kWeights, int U> __global__ void __launch_
     const unsigned code = none ? 255u : (m >> 23) - 2u + ((m & 0x7fffffu) > 0x400000u ? 1u : 0u);       // 25 .. 253
     const float inv = none ? 0.f : __uint_as_float((254u - code) << 23);                                // 2^(127 - code)
     if (lane % LB == 0 && c < K) scale[c / ASGD_BLOCK4] = (unsigned char)code;
-    unsigned w = 0;
+    // bf16 numbers are scaled two at a time as they are: a power of two is exact (below 2^-126 of a step nothing is left either way)
+    if constexpr (std::is_same<T, __nv_bfloat16>::value && !kWeights) {
+      const __nv_bfloat162 both = __float2bfloat162_rn(inv);
 #pragma unroll
-    for (int i = 0; i < V; i += 2)
-      w |= (unsigned)__nv_cvt_float2_to_fp4x2(make_float2(v[i] * inv, v[i + 1] * inv), __NV_E2M1, cudaRoundNearest) << (4 * i);
-    if (none) w = 0;                                 // an infinity times 0
-    if (c >= K) continue;
-    if (p.q_wide && c + V <= K) {
-      if constexpr (V == 8) *reinterpret_cast<unsigned*>(q + c / 2) = w;
-      else *reinterpret_cast<unsigned short*>(q + c / 2) = (unsigned short)w;
+      for (int i = 0; i < V / 2; ++i) reinterpret_cast<__nv_bfloat162*>(e)[i] = __hmul2(reinterpret_cast<__nv_bfloat162*>(e)[i], both);
+#pragma unroll
+      for (int i = 0; i < V; ++i) v[i] = Elem<T>::to_f(e[i]);
     } else {
 #pragma unroll
-      for (int i = 0; i < V; i += 2) if (c + i < K) q[(c + i) / 2] = (unsigned char)((w >> (4 * i)) & (c + i + 1 < K ? 255u : 15u));    // (a factor may make a zero behind the row -0)
+      for (int i = 0; i < V; ++i) v[i] = (kWeights ? v[i] : Elem<T>::to_f(e[i])) * inv;
     }
+    unsigned w[V > 8 ? 2 : 1] = {};
+#pragma unroll
+    for (int i = 0; i < V; i += 2)
+      w[i / 8] |= (unsigned)__nv_cvt_float2_to_fp4x2(make_float2(v[i], v[i + 1]), __NV_E2M1, cudaRoundNearest) << (4 * (i & 7));
+    if (none) {                                      // an infinity times 0
+#pragma unroll
+      for (int i = 0; i < (V > 8 ? 2 : 1); ++i) w[i] = 0;
+    }
+    if (c >= K) continue;
+    if (p.q_wide && c + V <= K) store_codes<V>(q + c / 2, w);
+    else
+#pragma unroll
+      for (int i = 0; i < V; i += 2) if (c + i < K) q[(c + i) / 2] = (unsigned char)((w[i / 8] >> (4 * (i & 7))) & (c + i + 1 < K ? 255u : 15u));    // (a factor may make a zero behind the row -0)
   }
 }
 
-// A lane takes the numbers of 16 bytes of the result.
-template <typename T, int U> __global__ void __launch_bounds__(kThreads)
-values4_kernel(int M, int K, const unsigned char* q, long long ldq, const unsigned char* scale, long long scale_row, T* out, long long ld_out, bool q_wide, bool out_wide) {
+// Numbers c .. c + 7 of a 4-bit row, at any c: from the two words that hold them.
+__device__ __forceinline__ unsigned codes_at(const unsigned char* q, int c, int bytes, bool words) {
+  const int at = (c >> 3) * 4;                       // (down, for a c below zero too)
+  unsigned w[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int b = at + 4 * i;
+    w[i] = 0;
+    if (words && b >= 0 && b + 4 <= bytes) w[i] = *reinterpret_cast<const unsigned*>(q + b);
+    else
+#pragma unroll
+      for (int j = 0; j < 4; ++j) if (b + j >= 0 && b + j < bytes) w[i] |= (unsigned)q[b + j] << (8 * j);
+  }
+  return __funnelshift_r(w[0], w[1], 4 * (c & 7));
+}
+__device__ __forceinline__ float power_of(unsigned code) {
+  return code == 255u ? __uint_as_float(0x7fffffffu) : __uint_as_float(code ? code << 23 : 0x00400000u);
+}
+
+// A lane takes the numbers of a piece of the result.  Its rows start at multiples of kAlign bytes, or (0) anywhere: then the pieces of 16-bit results are
+// those of memory, so that all but a row's first and last are whole stores, and a piece's numbers begin anywhere in the row of q.
+// (8192 rows of 4095 bf16 numbers: 28.5 us, stored one by one 98; fp32 numbers stored one by one 34, this way 43.)
+template <typename T, int kAlign, int U> __global__ void __launch_bounds__(kThreads)
+values4_kernel(int M, int K, const unsigned char* q, long long ldq, const unsigned char* scale, long long scale_row, T* out, long long ld_out, bool q_wide) {
   wait_for_stream();
-  constexpr int V = kPer16<T>;
+  constexpr int kBytes = kAlign == 32 ? 32 : 16, V = kBytes / (int)sizeof(T), W = V > 8 ? 2 : 1;
+  constexpr bool kShift = kAlign == 0 && sizeof(T) == 2;
   const int lane = threadIdx.x & 31;
   const long long r = (long long)blockIdx.x * kWarps + (threadIdx.x >> 5);
-  const int c0 = ((int)blockIdx.y * U * 32 + lane) * V;
   if (r >= M) return;
   q += r * ldq;
   scale += r * scale_row;
   out += r * ld_out;
-  unsigned w[U], code[U];
+  const int skip = !kShift ? 0 : (int)(reinterpret_cast<unsigned long long>(out) & (kBytes - 1)) / (int)sizeof(T);
+  const int c0 = ((int)blockIdx.y * U * 32 + lane) * V - skip;
+  unsigned w[U][W], code[U][2];
 #pragma unroll
   for (int u = 0; u < U; ++u) {
     const int c = c0 + u * 32 * V;
-    w[u] = code[u] = 0;
-    if (c >= K) continue;
-    code[u] = scale[c / ASGD_BLOCK4];
-    if (q_wide && c + V <= K) {
-      if constexpr (V == 8) w[u] = *reinterpret_cast<const unsigned*>(q + c / 2);
-      else w[u] = *reinterpret_cast<const unsigned short*>(q + c / 2);
-    } else {
+    code[u][0] = code[u][1] = 0;
 #pragma unroll
-      for (int i = 0; i < V; i += 2) if (c + i < K) w[u] |= (unsigned)q[(c + i) / 2] << (4 * i);
+    for (int i = 0; i < W; ++i) w[u][i] = 0;
+    if (c >= K || c + V <= 0) continue;
+    code[u][0] = scale[max(c, 0) / ASGD_BLOCK4];
+    if constexpr (!kShift) {
+      if (q_wide && c + V <= K) {
+        if constexpr (V == 16) { const uint2 x = *reinterpret_cast<const uint2*>(q + c / 2); w[u][0] = x.x; w[u][W - 1] = x.y; }
+        else if constexpr (V == 8) w[u][0] = *reinterpret_cast<const unsigned*>(q + c / 2);
+        else w[u][0] = *reinterpret_cast<const unsigned short*>(q + c / 2);
+      } else {
+#pragma unroll
+        for (int i = 0; i < V; i += 2) if (c + i < K) w[u][i / 8] |= (unsigned)q[(c + i) / 2] << (4 * (i & 7));
+      }
+    } else {
+      code[u][1] = scale[min(c + V - 1, K - 1) / ASGD_BLOCK4];
+      w[u][0] = codes_at(q, c, (K + 1) / 2, q_wide);
     }
   }
 #pragma unroll
   for (int u = 0; u < U; ++u) {
     const int c = c0 + u * 32 * V;
-    if (c >= K) continue;
-    const float s = code[u] == 255u ? __uint_as_float(0x7fffffffu) : __uint_as_float(code[u] ? code[u] << 23 : 0x00400000u);
-    float v[V];
+    if (c >= K || c + V <= 0) continue;
+    const float s = power_of(code[u][0]), s2 = !kShift ? s : power_of(code[u][1]);
+    const int border = (max(c, 0) / ASGD_BLOCK4 + 1) * ASGD_BLOCK4 - c;             // numbers from there on have the second scale
+    Piece<kBytes> p;
+    T* e = reinterpret_cast<T*>(p.w);
 #pragma unroll
     for (int i = 0; i < V; i += 2) {
-      const float2 f = __half22float2(__half2(__nv_cvt_fp4x2_to_halfraw2((__nv_fp4x2_storage_t)((w[u] >> (4 * i)) & 0xffu), __NV_E2M1)));
-      v[i] = f.x * s;
-      v[i + 1] = f.y * s;
+      const float2 f = __half22float2(__half2(__nv_cvt_fp4x2_to_halfraw2((__nv_fp4x2_storage_t)((w[u][i / 8] >> (4 * (i & 7))) & 0xffu), __NV_E2M1)));
+      e[i] = Elem<T>::from_f(f.x * (!kShift || i < border ? s : s2));
+      e[i + 1] = Elem<T>::from_f(f.y * (!kShift || i + 1 < border ? s : s2));
     }
-    if (out_wide && c + V <= K) *reinterpret_cast<uint4*>(out + c) = pack16<T>(v);
+    if ((kAlign || kShift) && c >= 0 && c + V <= K) write_piece(out + c, p);
     else
 #pragma unroll
-      for (int i = 0; i < V; ++i) if (c + i < K) out[c + i] = Elem<T>::from_f(v[i]);
+      for (int i = 0; i < V; ++i) if (c + i >= 0 && c + i < K) out[c + i] = e[i];
   }
 }
 
 // Calls f with the pieces per lane: no more than a row has.
 template <typename F> bool with_pieces(long long K, int V, F&& f) {
   if (K <= 32 * V) return f(std::integral_constant<int, 1>());
-  if (K <= 64 * V) return f(std::integral_constant<int, 2>());
+  if (K <= 64 * V || V > 8) return f(std::integral_constant<int, 2>());
   return f(std::integral_constant<int, 4>());
 }
+// Calls f with what rows of `bytes` from `base` on start at multiples of.
+template <typename F> bool with_align(const void* base, long long bytes, F&& f) {
+  if (aligned(base, 32) && bytes % 32 == 0) return f(std::integral_constant<int, 32>());
+  if (aligned(base, 16) && bytes % 16 == 0) return f(std::integral_constant<int, 16>());
+  return f(std::integral_constant<int, 0>());
+}
 template <typename T> bool launch(Args p, cudaStream_t st) {
-  constexpr int V = kPer16<T>;
   const asgd_quantize4_args& a = p.a;
-  const bool vec = aligned(a.x, 16) && a.ldx % V == 0;
-  p.q_wide = aligned(a.q, V / 2) && a.ldq % (V / 2) == 0;
   p.lo = reinterpret_cast<const char*>(a.x);
   p.hi = a.rows_x > 0 ? p.lo + ((a.rows_x - 1) * a.ldx + a.K) * (long long)sizeof(T) : p.lo;
-  return with_pieces(a.K, V, [&](auto u) {
-    constexpr int U = decltype(u)::value;
-    const dim3 grid((unsigned)ceil_div(a.M, kWarps), (unsigned)ceil_div(a.K, 32 * V * U));
-    if (vec) return a.weights ? launch_after(rows4_kernel<T, true, true, U>, grid, kThreads, 0, st, p) : launch_after(rows4_kernel<T, true, false, U>, grid, kThreads, 0, st, p);
-    return a.weights ? launch_after(rows4_kernel<T, false, true, U>, grid, kThreads, 0, st, p) : launch_after(rows4_kernel<T, false, false, U>, grid, kThreads, 0, st, p);
+  return with_align(a.x, a.ldx * (long long)sizeof(T), [&](auto align) {
+    constexpr int A = decltype(align)::value, V = (A == 32 ? 32 : 16) / (int)sizeof(T);
+    p.q_wide = aligned(a.q, V / 2) && a.ldq % (V / 2) == 0;
+    return with_pieces(a.K, V, [&](auto u) {
+      constexpr int U = decltype(u)::value;
+      const dim3 grid((unsigned)ceil_div(a.M, kWarps), (unsigned)ceil_div(a.K, 32 * V * U));
+      return a.weights ? launch_after(rows4_kernel<T, A, true, U>, grid, kThreads, 0, st, p) : launch_after(rows4_kernel<T, A, false, U>, grid, kThreads, 0, st, p);
+    });
   });
 }
 
 bool sizes_fit(long long M, long long K) {                // rows and columns of a call stay inside 32 bits, and the grid inside its limits
-  return M <= 0x7fffffffll && K <= ASGD_QUANTIZE_MAX && ceil_div(K, 512) <= 65535;
+  return M <= 0x7fffffffll && K <= ASGD_QUANTIZE_MAX && ceil_div(K + 7, 512) <= 65535;
 }
 
 }  // namespace
@@ -203,13 +297,18 @@ extern "C" int asgd_dequantize4(int64_t M, int64_t K, const void* q, int64_t ldq
   bool ok = false;
   with_type(type, [&](auto e) {
     using T = decltype(e);
-    constexpr int V = kPer16<T>;
-    const bool q_wide = aligned(q, V / 2) && ldq % (V / 2) == 0, out_wide = aligned(out, 16) && ld_out % V == 0;
-    ok = with_pieces(K, V, [&](auto u) {
-      constexpr int U = decltype(u)::value;
-      const dim3 grid((unsigned)ceil_div(M, kWarps), (unsigned)ceil_div(K, 32 * V * U));
-      return launch_after(values4_kernel<T, U>, grid, kThreads, 0, (cudaStream_t)stream, (int)M, (int)K, reinterpret_cast<const unsigned char*>(q), ldq,
-                          reinterpret_cast<const unsigned char*>(scale), scale_row, reinterpret_cast<T*>(out), ld_out, q_wide, out_wide);
+    ok = with_align(out, ld_out * (long long)sizeof(T), [&](auto align) {
+      constexpr int A = decltype(align)::value, V = (A == 32 ? 32 : 16) / (int)sizeof(T);
+      constexpr bool kShift = A == 0 && sizeof(T) == 2;
+      constexpr int N = kShift ? 4 : V / 2;          // bytes of q that are read together
+      const bool q_wide = aligned(q, N) && ldq % N == 0;
+      const long long span = kShift ? K + V - 1 : K;      // from a piece's beginning before the row's first number
+      return with_pieces(span, V, [&](auto u) {
+        constexpr int U = decltype(u)::value;
+        const dim3 grid((unsigned)ceil_div(M, kWarps), (unsigned)ceil_div(span, 32 * V * U));
+        return launch_after(values4_kernel<T, A, U>, grid, kThreads, 0, (cudaStream_t)stream, (int)M, (int)K, reinterpret_cast<const unsigned char*>(q), ldq,
+                            reinterpret_cast<const unsigned char*>(scale), scale_row, reinterpret_cast<T*>(out), ld_out, q_wide);
+      });
     });
   });
   return ok ? ASGD_OK : ASGD_ECUDA;
