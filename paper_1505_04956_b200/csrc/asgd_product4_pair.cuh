@@ -59,6 +59,13 @@ __device__ inline bool wait_cluster(unsigned long long* bar, unsigned parity, un
   return false;
 }
 
+// one lane of a whole warp, known as such to the compiler: what it issues takes its operands from uniform registers
+__device__ inline bool elect_one() {
+  unsigned me;
+  asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.u32 %0, 1, 0, p;\n}" : "=r"(me));
+  return me != 0;
+}
+
 template <int NT> __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
 product4_pair_kernel(const Params4 p, const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
                      const __grid_constant__ CUtensorMap map_sa, const __grid_constant__ CUtensorMap map_sb, const __grid_constant__ CUtensorMap map_c) {
@@ -139,42 +146,50 @@ product4_pair_kernel(const Params4 p, const __grid_constant__ CUtensorMap map_a,
       }
       misc[5] = (int)asked;
       store_cluster(in_block(misc + 2 + rank, 0), it);
-    } else if (wid == 1 && lane == 0 && rank == 0) {
+    } else if (wid == 1 && rank == 0) {
+      const unsigned at = __shfl_sync(kAll, tmem, 0);
       unsigned it = 0, su = 0, n = 0;                // K blocks, units, tiles
       bool ok = true;
       for (int tile = pair; tile < tiles && ok && blocks > 0; tile += pairs, ++n) {
-        const unsigned stage = n % P4::kStages, d = tmem + stage * NT;
-        for (int u = 0; u < p.kblocks && ok; ++u, ++su) {
+        const unsigned stage = n % P4::kStages, d = at + stage * NT;
+        for (int u = 0; u < p.kblocks; ++u, ++su) {
           const unsigned sq = su % kScaleSlots;
-          if (!(ok = wait_cluster(bars + Q_TURNED + sq, (su / kScaleSlots) & 1, p.wait_limit, abort))) break;
-          const unsigned char* sf = scales + sq * kScaleSlotBytes;
-          for (int b = 0; b < 2 && 2 * u + b < blocks; ++b, ++it) {
-            const unsigned q = it % S;
-            if (!(ok = wait(bars + Q_FULL + q, (it / S) & 1, p.wait_limit, abort))) break;
-            if (u == 0 && b == 0 && n >= P4::kStages && !(ok = wait(bars + Q_ACCEMPTY + stage, (n / P4::kStages - 1) & 1, p.wait_limit, abort))) break;
-            fence_after();
-            const unsigned cols = tmem + P4::kScaleCols + (it & 1) * 24;                // A's: 2 x 4 columns, B's: 2 x 8
-            const int steps = steps4(p.K - (2 * u + b) * kKB, 4);
+          ok = wait_cluster(bars + Q_TURNED + sq, (su / kScaleSlots) & 1, p.wait_limit, abort);
+          if (u == 0 && n >= P4::kStages) ok = ok && wait(bars + Q_ACCEMPTY + stage, (n / P4::kStages - 1) & 1, p.wait_limit, abort);
+          if (!(ok = __all_sync(kAll, ok))) break;
+          fence_after();
+          const bool last = u + 1 == p.kblocks;
+          const int here = last && (blocks & 1) ? 1 : 2;
+          if (elect_one()) {
 #pragma unroll
-            for (int a = 0; a < 2; ++a)
-              if (2 * a < steps) {
-                const unsigned char* atom = sf + (2 * b + a) * kAtom;
-                copy_scales_pair(cols + 4 * a, scale_desc(atom));
-                copy_scales_pair(cols + 8 + 8 * a, scale_desc(atom + kTurned));
-                copy_scales_pair(cols + 12 + 8 * a, scale_desc(atom + 2 * kTurned));
-              }
-            const unsigned long long da = operand_desc(ring + (size_t)q * P4::kSlotBytes), db = operand_desc(ring + (size_t)q * P4::kSlotBytes + kHalfBytes);
+            for (int b = 0; b < 2; ++b) {
+              if (b >= here) break;
+              const unsigned q = (it + b) % S;
+              const unsigned cols = at + P4::kScaleCols + b * 24;                       // A's: 2 x 4 columns, B's: 2 x 8
+              const unsigned char* atom = scales + sq * kScaleSlotBytes + 2 * b * kAtom;
+              const int steps = steps4(p.K - (2 * u + b) * kKB, 4);
 #pragma unroll
-            for (int k = 0; k < 4; ++k)
-              if (k < steps)
-                mma_f4_pair(d, da + 2 * k, db + 2 * k, with_scales(p.idesc, k), cols + 4 * (k >> 1), cols + 8 + 8 * (k >> 1), k != 0 || b != 0 || u != 0);
-            commit_pair(bars + Q_DONE + q);
+              for (int a = 0; a < 2; ++a)
+                if (2 * a < steps) {
+                  copy_scales_pair(cols + 4 * a, scale_desc(atom + a * kAtom));
+                  copy_scales_pair(cols + 8 + 8 * a, scale_desc(atom + a * kAtom + kTurned));
+                  copy_scales_pair(cols + 12 + 8 * a, scale_desc(atom + a * kAtom + 2 * kTurned));
+                }
+              const unsigned long long da = operand_desc(ring + (size_t)q * P4::kSlotBytes), db = operand_desc(ring + (size_t)q * P4::kSlotBytes + kHalfBytes);
+#pragma unroll
+              for (int k = 0; k < 4; ++k)
+                if (k < steps)
+                  mma_f4_pair(d, da + 2 * k, db + 2 * k, with_scales(p.idesc, k), cols + 4 * (k >> 1), cols + 8 + 8 * (k >> 1), k != 0 || b != 0 || u != 0);
+              commit_pair(bars + Q_DONE + q);
+            }
+            if (last) commit_pair(bars + Q_ACCFULL + stage);
           }
+          __syncwarp();
+          it += here;
         }
-        if (ok) commit_pair(bars + Q_ACCFULL + stage);
       }
     } else if (wid >= 2) {
-      unsigned su = 0;
+      unsigned su = 0, it = 0;
       bool ok = true;
       for (int tile = pair; tile < tiles && ok; tile += pairs)
         for (int u = 0; u < p.kblocks; ++u, ++su) {
@@ -186,6 +201,13 @@ product4_pair_kernel(const Params4 p, const __grid_constant__ CUtensorMap map_a,
             turn_scales(at + kTurned, 128, lane);
           } else {
             turn_scales(at + 2 * kTurned, NT - 128, lane);
+            // the unit's operands too, so that the issuing warp has one barrier to wait for
+            const int here = min(2, blocks - 2 * u);
+            if (rank == 0) {
+              for (int b = 0; b < here && ok; ++b) ok = wait(bars + Q_FULL + (it + b) % S, ((it + b) / S) & 1, p.wait_limit, abort);
+              if (!(ok = __all_sync(kAll, ok))) break;
+            }
+            it += here;
           }
           if (lane == 0) arrive_release_cluster(in_block(bars + Q_TURNED + sq, 0));
         }
