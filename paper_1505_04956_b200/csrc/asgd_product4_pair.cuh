@@ -156,15 +156,16 @@ product4_pair_kernel(const Params4 p, const __grid_constant__ CUtensorMap map_a,
           const unsigned sq = su % kScaleSlots;
           ok = wait_cluster(bars + Q_TURNED + sq, (su / kScaleSlots) & 1, p.wait_limit, abort);
           if (u == 0 && n >= P4::kStages) ok = ok && wait(bars + Q_ACCEMPTY + stage, (n / P4::kStages - 1) & 1, p.wait_limit, abort);
-          if (!(ok = __all_sync(kAll, ok))) break;
-          fence_after();
           const bool last = u + 1 == p.kblocks;
           const int here = last && (blocks & 1) ? 1 : 2;
-          if (elect_one()) {
 #pragma unroll
-            for (int b = 0; b < 2; ++b) {
-              if (b >= here) break;
-              const unsigned q = (it + b) % S;
+          for (int b = 0; b < 2; ++b) {
+            if (b >= here) break;
+            const unsigned q = it % S;
+            ok = ok && wait(bars + Q_FULL + q, (it / S) & 1, p.wait_limit, abort);
+            if (!(ok = __all_sync(kAll, ok))) break;
+            fence_after();
+            if (elect_one()) {
               const unsigned cols = at + P4::kScaleCols + b * 24;                       // A's: 2 x 4 columns, B's: 2 x 8
               const unsigned char* atom = scales + sq * kScaleSlotBytes + 2 * b * kAtom;
               const int steps = steps4(p.K - (2 * u + b) * kKB, 4);
@@ -181,15 +182,16 @@ product4_pair_kernel(const Params4 p, const __grid_constant__ CUtensorMap map_a,
                 if (k < steps)
                   mma_f4_pair(d, da + 2 * k, db + 2 * k, with_scales(p.idesc, k), cols + 4 * (k >> 1), cols + 8 + 8 * (k >> 1), k != 0 || b != 0 || u != 0);
               commit_pair(bars + Q_DONE + q);
+              if (last && b + 1 == here) commit_pair(bars + Q_ACCFULL + stage);
             }
-            if (last) commit_pair(bars + Q_ACCFULL + stage);
+            __syncwarp();
+            ++it;
           }
-          __syncwarp();
-          it += here;
+          if (!ok) break;
         }
       }
     } else if (wid >= 2) {
-      unsigned su = 0, it = 0;
+      unsigned su = 0;
       bool ok = true;
       for (int tile = pair; tile < tiles && ok; tile += pairs)
         for (int u = 0; u < p.kblocks; ++u, ++su) {
@@ -201,13 +203,6 @@ product4_pair_kernel(const Params4 p, const __grid_constant__ CUtensorMap map_a,
             turn_scales(at + kTurned, 128, lane);
           } else {
             turn_scales(at + 2 * kTurned, NT - 128, lane);
-            // the unit's operands too, so that the issuing warp has one barrier to wait for
-            const int here = min(2, blocks - 2 * u);
-            if (rank == 0) {
-              for (int b = 0; b < here && ok; ++b) ok = wait(bars + Q_FULL + (it + b) % S, ((it + b) / S) & 1, p.wait_limit, abort);
-              if (!(ok = __all_sync(kAll, ok))) break;
-            }
-            it += here;
           }
           if (lane == 0) arrive_release_cluster(in_block(bars + Q_TURNED + sq, 0));
         }
