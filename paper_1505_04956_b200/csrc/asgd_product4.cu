@@ -102,7 +102,7 @@ Kernel choose(const Params& p) {
     const int bm = rows_of[k];
     // tile rows: a group's last one is half full on average, and a group with rows has one at least
     const double tile_rows = groups > 1 ? std::max(std::min((double)p.M, (double)groups), (double)p.M / bm + 0.5 * groups) : (double)ceil_div(p.M, bm);
-    const double tiles = std::ceil(tile_rows) * (double)ceil_div(p.N, k == PAIR ? 224 : kU);
+    const double tiles = std::ceil(tile_rows) * (double)ceil_div(p.N, k == PAIR ? 256 : kU);
     const int split = k == PAIR ? 1 : split_of(p, bm);
     const double turns = std::ceil(tiles * split / (k == PAIR ? kSMs / 2 : kSMs));
     const double us = turns * (std::ceil((double)p.kblocks / split) * unit_us[k] + 0.5) + (split > 1 ? 1.0 : 0.0) + (k == PAIR ? 1.0 : 0.0);
@@ -145,6 +145,6 @@ extern "C" int asgd_product4(const asgd_product4_args* args, void* stream) {
     case FEW32: return launch_few<32>(a, p, st);
     case FEW64: return launch_few<64>(a, p, st);
     case FEW128: return launch_few<128>(a, p, st);
-    default: return launch_pair<224>(a, p, st);
+    default: return launch_pair<256>(a, p, st);
   }
 }

@@ -43,20 +43,26 @@ __device__ inline unsigned with_scales(unsigned idesc, int k) { return idesc | (
 // instructions of 64 numbers (32 bytes) that `bytes` of a row take, n at most
 __device__ inline int steps4(int bytes, int n) { return min(n, (bytes + 31) >> 5); }
 
-// A warp turns the scales of `rows` rows (16 bytes each) into four atoms, in place; rows from there to 128 have zeros.
-__device__ inline void turn_scales(unsigned char* at, int rows, int lane) {
+// A warp turns the scales of `rows` rows (16 bytes each, `pitch` bytes apart) into four atoms, in place or elsewhere; rows from there to
+// 128 have zeros.  What it has read, and (whole warp between) what it writes; a fence for the tensor pipe's reads afterwards.
+struct ScaleRows4 {
   uint4 r[4];
+  __device__ __forceinline__ void read(const unsigned char* from, int pitch, int rows, int lane) {
 #pragma unroll
-  for (int c = 0; c < 4; ++c) {
-    r[c] = make_uint4(0, 0, 0, 0);
-    if (32 * c + lane < rows) r[c] = *reinterpret_cast<const uint4*>(at + (32 * c + lane) * 16);
+    for (int c = 0; c < 4; ++c) {
+      r[c] = make_uint4(0, 0, 0, 0);
+      if (32 * c + lane < rows) r[c] = *reinterpret_cast<const uint4*>(from + (32 * c + lane) * pitch);
+    }
   }
-  __syncwarp();
-  uint4* to = reinterpret_cast<uint4*>(at) + lane;
-  to[0] = make_uint4(r[0].x, r[1].x, r[2].x, r[3].x);
-  to[kAtom / 16] = make_uint4(r[0].y, r[1].y, r[2].y, r[3].y);
-  to[2 * kAtom / 16] = make_uint4(r[0].z, r[1].z, r[2].z, r[3].z);
-  to[3 * kAtom / 16] = make_uint4(r[0].w, r[1].w, r[2].w, r[3].w);
+  __device__ __forceinline__ void write(unsigned char* at, int lane) const {
+    uint4* to = reinterpret_cast<uint4*>(at) + lane;
+    to[0] = make_uint4(r[0].x, r[1].x, r[2].x, r[3].x);
+    to[kAtom / 16] = make_uint4(r[0].y, r[1].y, r[2].y, r[3].y);
+    to[2 * kAtom / 16] = make_uint4(r[0].z, r[1].z, r[2].z, r[3].z);
+    to[3 * kAtom / 16] = make_uint4(r[0].w, r[1].w, r[2].w, r[3].w);
+  }
+};
+__device__ inline void turned() {
   asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   __syncwarp();
 }
@@ -194,7 +200,12 @@ product4_few_kernel(const Params4 p, const __grid_constant__ CUtensorMap map_u, 
       for (int kb = t.kb0; kb < t.kb1; ++kb, ++it) {
         const unsigned q = it % S;
         if (!(ok = __all_sync(kAll, wait(bars + F::FULL + q, (it / S) & 1, p.wait_limit, abort)))) break;
-        turn_scales(ring + (size_t)q * F::kSlotBytes + F::kScalesAt + (wid - 2) * kTurned, wid == 2 ? kU : BN, lane);
+        unsigned char* at = ring + (size_t)q * F::kSlotBytes + F::kScalesAt + (wid - 2) * kTurned;
+        ScaleRows4 rows;
+        rows.read(at, 16, wid == 2 ? kU : BN, lane);
+        __syncwarp();
+        rows.write(at, lane);
+        turned();
         if (lane == 0) arrive(bars + F::TURNED + q);
       }
     }

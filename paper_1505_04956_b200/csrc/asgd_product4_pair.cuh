@@ -17,9 +17,10 @@
 
 namespace {
 
-constexpr int kPair4Slots = 5, kScaleSlots = 3;
+constexpr int kPair4Slots = 5, kScaleSlots = 4;      // K blocks of operands, units of scales
+constexpr int kPair4Pieces = 1;                      // of a warp's stage on the way to C
 constexpr unsigned kScaleSlotBytes = 3 * kTurned;    // the block's rows of A, the first 128 rows of B, the others
-enum { Q_FULL = 0, Q_DONE = kPair4Slots, Q_SFULL = 2 * kPair4Slots, Q_TURNED = Q_SFULL + kScaleSlots, Q_ACCFULL = Q_TURNED + kScaleSlots,
+enum { Q_FULL = 0, Q_DONE = kPair4Slots, Q_SFULL = 2 * kPair4Slots, Q_TURNED = Q_SFULL + kScaleSlots, Q_SDONE = Q_TURNED + kScaleSlots, Q_ACCFULL = Q_SDONE + kScaleSlots,
        Q_ACCEMPTY = Q_ACCFULL + 2, Q_DRAIN = Q_ACCEMPTY + 2, Q_COUNT = Q_DRAIN + 1 };
 
 template <int NT> struct Pair4 {
@@ -28,7 +29,7 @@ template <int NT> struct Pair4 {
   static constexpr unsigned kScalesCopied = (kHalf + NT) * 16;
   static constexpr int kStages = 2 * NT + 48 <= 512 ? 2 : 1;
   static constexpr unsigned kScaleCols = kStages * NT;
-  static constexpr size_t kSmem = 1024 + (size_t)kPair4Slots * kSlotBytes + kScaleSlots * kScaleSlotBytes + 8 * kStageBytes + Q_COUNT * 8 + sizeof(Groups) + 64;
+  static constexpr size_t kSmem = 1024 + (size_t)kPair4Slots * kSlotBytes + kScaleSlots * kScaleSlotBytes + 8 * kPair4Pieces * kPieceBytes + Q_COUNT * 8 + sizeof(Groups) + 64;
   static_assert(kScaleCols + 48 <= 512 && NT % 32 == 0 && NT > 128 && NT <= 256 && kHalfCols % 8 == 0, "tile");
   static_assert(kSmem <= kSmemLimit, "shared memory");
 };
@@ -75,7 +76,7 @@ product4_pair_kernel(const Params4 p, const __grid_constant__ CUtensorMap map_a,
   unsigned char* ring = smem_dyn + ((1024u - (smem_u32(smem_dyn) & 1023u)) & 1023u);
   unsigned char* scales = ring + (size_t)S * P4::kSlotBytes;
   unsigned char* stages = scales + kScaleSlots * kScaleSlotBytes;
-  unsigned long long* bars = reinterpret_cast<unsigned long long*>(stages + 8 * kStageBytes);
+  unsigned long long* bars = reinterpret_cast<unsigned long long*>(stages + 8 * kPair4Pieces * kPieceBytes);
   Groups& gs = *reinterpret_cast<Groups*>(bars + Q_COUNT);
   int* misc = reinterpret_cast<int*>(&gs + 1);       // [0] tensor memory, [1] abort, [2, 3] K blocks whose copies each block has issued, [4] one of the blocks gave up, [5] units of scales this one has asked for
   int* abort = misc + 1;
@@ -91,7 +92,7 @@ product4_pair_kernel(const Params4 p, const __grid_constant__ CUtensorMap map_a,
     prefetch_map(&map_sb);
     if (p.c_by_map) prefetch_map(&map_c);
     for (int q = 0; q < S; ++q) { mbar_init(bars + Q_FULL + q, 1); mbar_init(bars + Q_DONE + q, 1); }
-    for (int q = 0; q < kScaleSlots; ++q) { mbar_init(bars + Q_SFULL + q, 1); mbar_init(bars + Q_TURNED + q, 4); }
+    for (int q = 0; q < kScaleSlots; ++q) { mbar_init(bars + Q_SFULL + q, 1); mbar_init(bars + Q_TURNED + q, rank ? 2 : 3); mbar_init(bars + Q_SDONE + q, 1); }
     for (int q = 0; q < 2; ++q) { mbar_init(bars + Q_ACCFULL + q, 1); mbar_init(bars + Q_ACCEMPTY + q, 16); }
     mbar_init(bars + Q_DRAIN, 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -114,16 +115,14 @@ product4_pair_kernel(const Params4 p, const __grid_constant__ CUtensorMap map_a,
     asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
     if (wid == 0 && lane == 0) {
       const unsigned bars0 = in_block(bars, 0);
-      unsigned it = 0, su = 0, asked = 0, last[kScaleSlots] = {};    // K blocks, units; the K block that a slot of scales was last used with
+      unsigned it = 0, su = 0, asked = 0;            // K blocks, units; units whose scales were asked for
       bool ok = true;
       for (int tile = pair; tile < tiles && ok; tile += pairs) {
         const Tile t = find_tile(p, kPairRows, NT, kPairBand, gs, tile);
         for (int u = 0; u < p.kblocks && ok; ++u, ++su) {
           const unsigned sq = su % kScaleSlots;
-          unsigned since = 0;                        // (a register array has no running index)
-#pragma unroll
-          for (int i = 0; i < kScaleSlots; ++i) if (i == (int)sq) since = last[i];
-          if (su >= kScaleSlots && !(ok = wait(bars + Q_DONE + since % S, (since / S) & 1, p.wait_limit, abort))) break;
+          // (a barrier of its own: the K block that a slot of scales was last used with may be two rounds of its slot ago)
+          if (su >= kScaleSlots && !(ok = wait(bars + Q_SDONE + sq, (su / kScaleSlots - 1) & 1, p.wait_limit, abort))) break;
           unsigned char* to = scales + sq * kScaleSlotBytes;
           mbar_expect_tx(bars + Q_SFULL + sq, P4::kScalesCopied);
           tma_load_3d(to, &map_sa, u * 16, t.m0 + (int)rank * kHalf, 0, bars + Q_SFULL + sq);
@@ -140,8 +139,6 @@ product4_pair_kernel(const Params4 p, const __grid_constant__ CUtensorMap map_a,
               tma_load_pair(data + kHalfBytes, &map_b, kb * kKB, t.n0 + (int)rank * P4::kHalfCols, t.g, full);
             }
           }
-#pragma unroll
-          for (int i = 0; i < kScaleSlots; ++i) if (i == (int)sq) last[i] = it - 1;
         }
       }
       misc[5] = (int)asked;
@@ -182,6 +179,7 @@ product4_pair_kernel(const Params4 p, const __grid_constant__ CUtensorMap map_a,
                 if (k < steps)
                   mma_f4_pair(d, da + 2 * k, db + 2 * k, with_scales(p.idesc, k), cols + 4 * (k >> 1), cols + 8 + 8 * (k >> 1), k != 0 || b != 0 || u != 0);
               commit_pair(bars + Q_DONE + q);
+              if (b + 1 == here) commit_pair(bars + Q_SDONE + sq);
               if (last && b + 1 == here) commit_pair(bars + Q_ACCFULL + stage);
             }
             __syncwarp();
@@ -190,6 +188,17 @@ product4_pair_kernel(const Params4 p, const __grid_constant__ CUtensorMap map_a,
           if (!ok) break;
         }
       }
+    } else if (wid == 1 && lane == 0) {
+      // The second block's word that its scales are turned.  (A release for the whole cluster waits for what its thread has in
+      // flight, 1400 cycles in the warps that turn them: 8192^3 285 us.)
+      unsigned su = 0;
+      bool ok = true;
+      for (int tile = pair; tile < tiles && ok; tile += pairs)
+        for (int u = 0; u < p.kblocks && ok; ++u, ++su) {
+          const unsigned sq = su % kScaleSlots;
+          ok = wait(bars + Q_TURNED + sq, (su / kScaleSlots) & 1, p.wait_limit, abort);
+          if (ok) arrive_release_cluster(in_block(bars + Q_TURNED + sq, 0));
+        }
     } else if (wid >= 2) {
       unsigned su = 0;
       bool ok = true;
@@ -197,14 +206,15 @@ product4_pair_kernel(const Params4 p, const __grid_constant__ CUtensorMap map_a,
         for (int u = 0; u < p.kblocks; ++u, ++su) {
           const unsigned sq = su % kScaleSlots;
           if (!(ok = __all_sync(kAll, wait(bars + Q_SFULL + sq, (su / kScaleSlots) & 1, p.wait_limit, abort)))) break;
-          unsigned char* at = scales + sq * kScaleSlotBytes;
-          if (wid == 2) {
-            turn_scales(at, kHalf, lane);
-            turn_scales(at + kTurned, 128, lane);
-          } else {
-            turn_scales(at + 2 * kTurned, NT - 128, lane);
-          }
-          if (lane == 0) arrive_release_cluster(in_block(bars + Q_TURNED + sq, 0));
+          unsigned char* at = scales + sq * kScaleSlotBytes + (wid - 2) * (2 * kTurned);
+          ScaleRows4 one, two;
+          one.read(at, 16, wid == 2 ? kHalf : NT - 128, lane);
+          if (wid == 2) two.read(at + kTurned, 16, 128, lane);
+          __syncwarp();
+          one.write(at, lane);
+          if (wid == 2) two.write(at + kTurned, lane);
+          turned();
+          if (lane == 0) arrive(bars + Q_TURNED + sq);
         }
     }
     __syncwarp();
@@ -213,7 +223,7 @@ product4_pair_kernel(const Params4 p, const __grid_constant__ CUtensorMap map_a,
     const int quarter = wid & 3, half = (wid - 4) >> 2;
     const unsigned free0 = in_block(bars + Q_ACCEMPTY, 0);
     const unsigned at_tmem = tmem + ((unsigned)(quarter * 32) << 16) + half * 128;
-    unsigned char* stage_smem = stages + (wid - 4) * kStageBytes;
+    unsigned char* stage_smem = stages + (wid - 4) * (kPair4Pieces * kPieceBytes);
     const LaneGroups lg(p, gs, lane);
     unsigned n_tile = 0;
     for (int tile = pair; tile < tiles; tile += pairs, ++n_tile) {
@@ -242,9 +252,9 @@ product4_pair_kernel(const Params4 p, const __grid_constant__ CUtensorMap map_a,
       o.at = m * p.ldc + n;
       o.by_map = p.c_by_map && o.rows == 32;
       if (o.rows > 0 && o.cols > 0) {
-        if (p.c_type == ASGD_F32) store_rows<float, false>(acc, stage_smem, reinterpret_cast<float*>(p.c), o, lane);
-        else if (p.c_type == ASGD_BF16) store_rows<__nv_bfloat16, false>(acc, stage_smem, reinterpret_cast<__nv_bfloat16*>(p.c), o, lane);
-        else store_rows<__half, false>(acc, stage_smem, reinterpret_cast<__half*>(p.c), o, lane);
+        if (p.c_type == ASGD_F32) store_rows<float, false, kPair4Pieces>(acc, stage_smem, reinterpret_cast<float*>(p.c), o, lane);
+        else if (p.c_type == ASGD_BF16) store_rows<__nv_bfloat16, false, kPair4Pieces>(acc, stage_smem, reinterpret_cast<__nv_bfloat16*>(p.c), o, lane);
+        else store_rows<__half, false, kPair4Pieces>(acc, stage_smem, reinterpret_cast<__half*>(p.c), o, lane);
       }
     }
     if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");

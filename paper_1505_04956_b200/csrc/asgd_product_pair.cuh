@@ -141,7 +141,7 @@ struct Out {
 
 // 64 bytes of every row make a piece of the warp's stage, with parts of 16 bytes exchanged by row (the 64-byte swizzle),
 // so that no access meets a bank more than twice.
-template <typename T, bool kFragments> __device__ __forceinline__ void store_rows(const float (&acc)[128], unsigned char* stage, T* c, const Out& o, int lane) {
+template <typename T, bool kFragments, int kPieces = kStagePieces> __device__ __forceinline__ void store_rows(const float (&acc)[128], unsigned char* stage, T* c, const Out& o, int lane) {
   constexpr int per = 64 / (int)sizeof(T), part = 16 / (int)sizeof(T);         // numbers of a row in a piece, in a part
   T* corner = c + o.at;
   const bool whole = ((reinterpret_cast<unsigned long long>(corner) | ((unsigned long long)o.ldc * sizeof(T))) & 15) == 0;
@@ -153,9 +153,9 @@ template <typename T, bool kFragments> __device__ __forceinline__ void store_row
   }
 #pragma unroll
   for (int first = 0; first < 128; first += per) {
-    unsigned char* piece = stage + first / per % kStagePieces * kPieceBytes;
+    unsigned char* piece = stage + first / per % kPieces * kPieceBytes;
     // the copy before last, out of the same place, has read it (a piece that is copied is a group of its own)
-    if (lane == 0) asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(kStagePieces - 1) : "memory");
+    if (lane == 0) asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(kPieces - 1) : "memory");
     __syncwarp();
     if constexpr (!kFragments) {
 #pragma unroll

@@ -288,6 +288,25 @@ def test_product4_of_groups(loads, N, K, out, first):
             _check_product(c[r], _values64(a[r], sa[r]), _values64(b[g], sb[g]), out)
 
 
+@pytest.mark.parametrize("N, K", [(2744, 2080), (1300, 600), (1024, 200), (2300, 5130), (700, 130)])
+def test_products_of_many_tiles_and_any_number_of_blocks(N, K):
+    # tile after tile through every block, with odd and even numbers of K blocks and units, loads that differ
+    loads = [700, 3, 0, 1200, 256, 511, 90, 2000, 1, 1300, 800, 640]
+    offsets = torch.tensor([0] + loads).cumsum(0).to(torch.int32).cuda()
+    a, sa = _operand(sum(loads), K, 3)
+    b, sb = _operand(N, K, 4, (len(loads),))
+    c = pkg.asgd_product4(a, sa, b, sb, offsets=offsets, out_dtype=F32)
+    pkg.asgd_experts_sync()
+    at = offsets.tolist()
+    for g in range(len(loads)):
+        r = slice(at[g], at[g + 1])
+        if loads[g]:
+            _check_product(c[r], _values64(a[r], sa[r]), _values64(b[g], sb[g]), F32)
+    for _ in range(5):
+        assert torch.equal(c, pkg.asgd_product4(a, sa, b, sb, offsets=offsets, out_dtype=F32))
+    pkg.asgd_experts_sync()
+
+
 def test_a_nan_scale_stays_in_its_row():
     for M, N in ((6, 300), (600, 2300)):
         a, sa = _operand(M, 640, 5)
