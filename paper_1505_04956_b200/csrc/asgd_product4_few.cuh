@@ -27,6 +27,13 @@ struct Params4 : Params {                            // K and the leading dimens
   int* status;
 };
 
+// one lane of a whole warp, known as such to the compiler: what it issues takes its operands from uniform registers
+__device__ inline bool elect_one() {
+  unsigned me;
+  asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.u32 %0, 1, 0, p;\n}" : "=r"(me));
+  return me != 0;
+}
+
 // scales of 128 rows by 128 numbers of K, 32 lanes of 16 bytes, into four columns of tensor memory (and the same in each quarter of its lanes)
 __device__ inline unsigned long long scale_desc(const void* smem) {
   return (unsigned long long)((smem_u32(smem) & 0x3FFFFu) >> 4) | (unsigned long long)(128 >> 4) << 32 | 1ull << 46;
@@ -158,21 +165,23 @@ product4_few_kernel(const Params4 p, const __grid_constant__ CUtensorMap map_u, 
       misc[2] = (int)it;
     }
   } else if (wid == 1) {
-    if (lane == 0) {
-      unsigned it = 0, n = 0;                        // units, tiles with units
-      bool ok = true;
-      for (int tile = first; tile < tiles && ok; tile += step) {
-        const Tile t = tile_at(tile);
-        if (t.kb0 >= t.kb1) continue;
-        const unsigned stage = n & 1, d = tmem + stage * BN;
-        for (int kb = t.kb0; kb < t.kb1; ++kb, ++it) {
-          const unsigned q = it % S;
-          if (!(ok = wait(bars + F::FULL + q, (it / S) & 1, p.wait_limit, abort) && wait(bars + F::TURNED + q, (it / S) & 1, p.wait_limit, abort))) break;
-          if (kb == t.kb0 && n >= 2 && !(ok = wait(bars + F::ACCEMPTY + stage, (n / 2 - 1) & 1, p.wait_limit, abort))) break;
-          fence_after();
-          unsigned char* slot = ring + (size_t)q * F::kSlotBytes;
-          const unsigned scales = tmem + F::kScaleCols + (it & 1) * 32;
-          const int steps = steps4(p.K - kb * kUnit, 8);
+    const unsigned at = __shfl_sync(kAll, tmem, 0);
+    // a tile's units are the same for every tile
+    const int units = kSplit ? p.kblocks * (rank + 1) / share - p.kblocks * rank / share : p.kblocks, from = kSplit ? p.kblocks * rank / share : 0;
+    unsigned it = 0, n = 0;                          // units, tiles
+    bool ok = true;
+    for (int tile = first; tile < tiles && units && ok; tile += step, ++n) {
+      const unsigned stage = n & 1, d = at + stage * BN;
+      for (int u = 0; u < units; ++u, ++it) {
+        const unsigned q = it % S;
+        ok = wait(bars + F::FULL + q, (it / S) & 1, p.wait_limit, abort) && wait(bars + F::TURNED + q, (it / S) & 1, p.wait_limit, abort);
+        if (u == 0 && n >= 2) ok = ok && wait(bars + F::ACCEMPTY + stage, (n / 2 - 1) & 1, p.wait_limit, abort);
+        if (!(ok = __all_sync(kAll, ok))) break;
+        fence_after();
+        if (elect_one()) {
+          const unsigned char* slot = ring + (size_t)q * F::kSlotBytes;
+          const unsigned scales = at + F::kScaleCols + (it & 1) * 32;
+          const int steps = steps4(p.K - (from + u) * kUnit, 8);
 #pragma unroll
           for (int a = 0; a < 4; ++a)
             if (2 * a < steps) {
@@ -184,12 +193,11 @@ product4_few_kernel(const Params4 p, const __grid_constant__ CUtensorMap map_u, 
           for (int k = 0; k < 8; ++k)
             if (k < steps)
               mma_f4(d, du + (k >> 2) * (kU * kKB >> 4) + 2 * (k & 3), dv + (k >> 2) * (F::kPiece >> 4) + 2 * (k & 3), with_scales(p.idesc, k),
-                     scales + 4 * (k >> 1), scales + 16 + 4 * (k >> 1), k != 0 || kb != t.kb0);
+                     scales + 4 * (k >> 1), scales + 16 + 4 * (k >> 1), k != 0 || u != 0);
           commit(bars + F::DONE + q);
+          if (u + 1 == units) commit(bars + F::ACCFULL + stage);
         }
-        if (!ok) break;
-        commit(bars + F::ACCFULL + stage);
-        ++n;
+        __syncwarp();
       }
     }
   } else if (wid < 4) {

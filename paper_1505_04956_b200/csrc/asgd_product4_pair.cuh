@@ -60,13 +60,6 @@ __device__ inline bool wait_cluster(unsigned long long* bar, unsigned parity, un
   return false;
 }
 
-// one lane of a whole warp, known as such to the compiler: what it issues takes its operands from uniform registers
-__device__ inline bool elect_one() {
-  unsigned me;
-  asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.u32 %0, 1, 0, p;\n}" : "=r"(me));
-  return me != 0;
-}
-
 template <int NT> __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
 product4_pair_kernel(const Params4 p, const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
                      const __grid_constant__ CUtensorMap map_sa, const __grid_constant__ CUtensorMap map_sb, const __grid_constant__ CUtensorMap map_c) {
