@@ -688,24 +688,26 @@ expert_layer_kernel(const __grid_constant__ LayerArgs a, const __grid_constant__
       misc[2] = (int)it;
     }
   } else if (wid == 1 || wid == 3) {
-    if (lane == 0) {
-      const unsigned me = (unsigned)wid >> 1;
-      unsigned it = 0;
-      bool ok = true;
-      for (int f = 0; f < 2 && ok && chunks; ++f) {
-        const unsigned idesc = a.w[f].idesc;
-        for (Stretch s(a.w[f], chunks, plan.per[f]); s.there(); ++s.from, ++it) {
-          if ((it & 1) != me) continue;
-          const unsigned q = it % S, stage = it % kAccStages;
-          if (!(ok = wait(bars + L::FULL + q, (it / S) & 1, a.wait_limit, abort) && wait(bars + L::READY + q, (it / S) & 1, a.wait_limit, abort))) break;
-          const unsigned long long du = operand_desc(ring + (size_t)q * L::kSlotBytes), dv = operand_desc(ring + (size_t)q * L::kSlotBytes + L::kWeights);
-          if (it >= kAccStages && !(ok = wait(bars + L::ACCEMPTY + stage, (it / kAccStages - 1) & 1, a.wait_limit, abort))) break;
-          fence_after();
+    const unsigned me = (unsigned)wid >> 1, at = __shfl_sync(kAll, tmem, 0);
+    unsigned it = 0;
+    bool ok = true;
+    for (int f = 0; f < 2 && ok && chunks; ++f) {
+      const unsigned idesc = a.w[f].idesc;
+      for (Stretch s(a.w[f], chunks, plan.per[f]); s.there(); ++s.from, ++it) {
+        if ((it & 1) != me) continue;
+        const unsigned q = it % S, stage = it % kAccStages;
+        ok = wait(bars + L::FULL + q, (it / S) & 1, a.wait_limit, abort) && wait(bars + L::READY + q, (it / S) & 1, a.wait_limit, abort);
+        if (it >= kAccStages) ok = ok && wait(bars + L::ACCEMPTY + stage, (it / kAccStages - 1) & 1, a.wait_limit, abort);
+        if (!(ok = __all_sync(kAll, ok))) break;
+        fence_after();
+        if (elect_one()) {
           asm volatile("fence.proxy.async.shared::cta;" ::: "memory");      // the tokens' rows were written by ordinary copies
+          const unsigned long long du = operand_desc(ring + (size_t)q * L::kSlotBytes), dv = operand_desc(ring + (size_t)q * L::kSlotBytes + L::kWeights);
 #pragma unroll
-          for (int k4 = 0; k4 < 4; ++k4) mma_f8(tmem + stage * BN, du + 2 * k4, dv + 2 * k4, idesc, k4 != 0);
+          for (int k4 = 0; k4 < 4; ++k4) mma_f8(at + stage * BN, du + 2 * k4, dv + 2 * k4, idesc, k4 != 0);
           commit(bars + L::DONE + q);
         }
+        __syncwarp();
       }
     }
   } else if (wid == 2) {

@@ -27,13 +27,6 @@ struct Params4 : Params {                            // K and the leading dimens
   int* status;
 };
 
-// one lane of a whole warp, known as such to the compiler: what it issues takes its operands from uniform registers
-__device__ inline bool elect_one() {
-  unsigned me;
-  asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.u32 %0, 1, 0, p;\n}" : "=r"(me));
-  return me != 0;
-}
-
 // scales of 128 rows by 128 numbers of K, 32 lanes of 16 bytes, into four columns of tensor memory (and the same in each quarter of its lanes)
 __device__ inline unsigned long long scale_desc(const void* smem) {
   return (unsigned long long)((smem_u32(smem) & 0x3FFFFu) >> 4) | (unsigned long long)(128 >> 4) << 32 | 1ull << 46;
