@@ -113,6 +113,8 @@ struct Making {
   unsigned mask[ASGD_MAX_EXPERTS][kTokenWords];      // the tokens of an expert
   int start[ASGD_MAX_EXPERTS], chunk[ASGD_MAX_EXPERTS];
   float bias[ASGD_MAX_EXPERTS];
+  uint2 found[kWarps][32];                           // keys that reach a bound, and whose they are
+  int place[kWarps][32];
 };
 constexpr size_t kMost = 227 * 1024 - sizeof(Plan) - 64;
 static_assert(Layer<16>::kSmem <= kMost && Layer<32>::kSmem <= kMost && Layer<64>::kSmem <= kMost, "shared memory");
@@ -256,7 +258,7 @@ template <typename T> __device__ __forceinline__ void read_logits(const T* row, 
 #pragma unroll 4
   for (int e = lane; e < E; e += 32) x[e] = Elem<T>::to_f(__ldcg(row + e));
 }
-__device__ inline void choose_one(const LayerArgs& a, int t, const float* bias, float* x, unsigned* key, int lane, int& id, float& weight) {
+__device__ inline void choose_one(const LayerArgs& a, int t, const float* bias, float* x, unsigned* key, uint2* found, int* place, int lane, int& id, float& weight) {
   const asgd_route_config& c = a.c;
   const int E = c.experts, K = c.top_k;
   const bool by_logit = a.bias == nullptr && c.group_top == 1, sigmoid_scores = c.score == ASGD_SCORE_SIGMOID;
@@ -289,15 +291,6 @@ __device__ inline void choose_one(const LayerArgs& a, int t, const float* bias, 
     if (k > best) { best = k; whose = e; }
   }
   __syncwarp();
-  auto look_again = [&]() {
-    best = 0;
-    whose = -1;
-#pragma unroll 4
-    for (int e = lane; e < E; e += 32) {
-      const unsigned k = key[e];
-      if (k > best) { best = k; whose = e; }
-    }
-  };
   if (c.groups_kept < c.groups) {                    // see keep_groups
     const int per = E / c.groups, shift = a.group_lanes, g = lane >> shift, sub = lane & ((1 << shift) - 1);
     unsigned m1 = 0, m2 = 0;
@@ -322,21 +315,61 @@ __device__ inline void choose_one(const LayerArgs& a, int t, const float* bias, 
       kept |= first;
       if ((first >> lane) & 1u) mine = 0;
     }
+    best = 0;
+    whose = -1;
+#pragma unroll 4
     for (int e = lane; e < E; e += 32) {
       const int of = a.group_magic ? (int)__umulhi((unsigned)e, a.group_magic) : e;
-      if (!((kept >> of) & 1u)) key[e] = 0u;
+      const unsigned k = (kept >> of) & 1u ? key[e] : 0u;
+      key[e] = k;
+      if (k > best) { best = k; whose = e; }
     }
-    look_again();
   }
+  // What reaches the top_k-th largest of the lanes' largest keys (top_k keys at least) is gathered and ranked by counting.
   id = -1;
+  unsigned top = best, bound = 1u;
   for (int i = 0; i < K; ++i) {
-    const unsigned top = __reduce_max_sync(kAll, best);
-    if (!top) break;                                 // nothing is left
-    const int first = (int)__reduce_min_sync(kAll, best == top ? (unsigned)whose : 0x7fffffffu);      // of equal keys the lowest expert's
-    if (lane == i) id = first;
-    if (whose == first) {
-      key[first] = 0u;
-      look_again();
+    const unsigned b = __reduce_max_sync(kAll, top);
+    bound = max(b, 1u);
+    if (!b) break;                                   // fewer lanes than that have a key: all of them
+    top = top == b ? 0u : top;
+  }
+  int n = 0;
+  for (int e0 = 0; e0 < E; e0 += 32) {
+    const unsigned k = e0 + lane < E ? key[e0 + lane] : 0u;
+    const bool there = k >= bound;
+    const unsigned votes = __ballot_sync(kAll, there);
+    const int at = n + __popc(votes & ((1u << lane) - 1u));
+    if (there && at < 32) found[at] = make_uint2(k, (unsigned)(e0 + lane));
+    n += __popc(votes);
+  }
+  if (n <= 32) {
+    __syncwarp();
+    const uint2 mine = lane < n ? found[lane] : make_uint2(0u, 0u);
+    int rank = 0;
+#pragma unroll 4
+    for (int i = 0; i < n; ++i) {                    // keys above, and equal ones of lower experts
+      const unsigned k = __shfl_sync(kAll, mine.x, i);
+      rank += i < lane ? k >= mine.x : k > mine.x;
+    }
+    if (lane < n && rank < K) place[rank] = (int)mine.y;
+    __syncwarp();
+    if (lane < min(n, K)) id = place[lane];
+  } else {                                           // one by one
+    for (int i = 0; i < K; ++i) {
+      const unsigned most = __reduce_max_sync(kAll, best);
+      if (!most) break;                              // nothing is left
+      const int first = (int)__reduce_min_sync(kAll, best == most ? (unsigned)whose : 0x7fffffffu);      // of equal keys the lowest expert's
+      if (lane == i) id = first;
+      if (whose == first) {
+        key[first] = 0u;
+        best = 0;
+        whose = -1;
+        for (int e = lane; e < E; e += 32) {
+          const unsigned k = key[e];
+          if (k > best) { best = k; whose = e; }
+        }
+      }
     }
   }
   const float chosen = id >= 0 ? x[id] : 0.f, s = id < 0 ? 0.f : sigmoid_scores ? sigmoid(chosen) : f.score(chosen);
@@ -355,7 +388,7 @@ template <typename Id> __device__ __forceinline__ void choose_some(const LayerAr
   for (int t = first; t < a.T; t += step) {
     int id;
     float w;
-    choose_one(a, t, m.bias, m.x[wid], m.key[wid], lane, id, w);
+    choose_one(a, t, m.bias, m.x[wid], m.key[wid], m.found[wid], m.place[wid], lane, id, w);
     if (lane < K) {
       ids[t * K + lane] = (Id)id;
       weights[t * K + lane] = w;
@@ -364,6 +397,7 @@ template <typename Id> __device__ __forceinline__ void choose_some(const LayerAr
   }
 }
 // Rows by expert of 32 assignments at most, by a warp: lane i has assignment i; a row is the number of lanes before it by expert and place.
+// (Two assignments a lane took longer than the whole block's way: 64 of them 3.5 us instead of 2.4.)
 template <int BN> __device__ inline void make_small_plan(const LayerArgs& a, Plan& plan, int lane) {
   const int n = a.T * a.c.top_k, e = lane < n ? plan.ids[lane] : -1;
   int row = 0, rank = 0;

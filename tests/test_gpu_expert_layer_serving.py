@@ -184,6 +184,33 @@ def test_the_layer_is_what_the_separate_operators_give():
     assert float((y - want).norm() / want.norm()) < 2.0 ** -8
 
 
+@pytest.mark.parametrize("T, E, top_k, groups, kept", [(5, 300, 8, 1, 1), (7, 1000, 32, 1, 1), (16, 64, 4, 1, 1), (8, 96, 7, 6, 3), (40, 512, 16, 8, 8), (100, 33, 3, 11, 5), (2, 32, 32, 1, 1)])
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("kind", ["ties", "gone", "all equal"])
+def test_choices_with_ties_and_unavailable_experts_are_those_of_the_routing(T, E, top_k, groups, kept, score, kind):
+    g = _gen(T + E)
+    logits = torch.randn(T, E, generator=g, device="cuda")
+    if kind == "ties":
+        logits = torch.round(logits * 2) / 2
+    elif kind == "all equal":
+        logits = torch.zeros(T, E, device="cuda")
+    else:
+        logits[torch.rand(T, E, generator=g, device="cuda") < 0.97] = -math.inf
+    d, h = 16, 16
+    w1, s1 = _matrices(g, 1, h, d)
+    w2, s2 = _matrices(g, 1, d, h)
+    many = lambda t: t.expand(E, *t.shape[1:]).contiguous() if t.dtype == F32 else t.view(torch.uint8).expand(E, *t.shape[1:]).contiguous().view(t.dtype)      # noqa: E731
+    x = torch.randn(T, d, generator=g, device="cuda")
+    kw = dict(score=score, groups=groups, groups_kept=kept, group_top=1, scale=1.5)
+    want_ids, want_weights = pkg.asgd_route(logits, top_k, plan=False, **kw)
+    y, ids, weights = pkg.asgd_expert_layer(x, many(w1), many(s1), many(w2), many(s2), top_k, logits=logits, choice=True, **kw)
+    pkg.asgd_experts_sync()
+    assert torch.equal(ids, want_ids)
+    if score == "sigmoid":                                                         # (a softmax without any logit above -inf is NaN)
+        assert float((weights - want_weights).abs().max()) <= 64 * U * 1.5
+        _check(x, many(w1), many(s1), many(w2), many(s2), (y, ids, weights), "relu2", min_tight=False)
+
+
 def test_layer_of_nothing_and_unavailable_experts():
     args, kw = _case(4, 8, 3, 256, 128, True, "silu", F32, "softmax", 1, None, (E4, E4))
     x, w1, s1, w2, s2, top_k = args
