@@ -56,20 +56,24 @@ template <typename T> __device__ __forceinline__ void unpack(const Piece& p, flo
 #pragma unroll
   for (int i = 0; i < kPer<T>; ++i) v[i] = Elem<T>::to_f(e[i]);
 }
-// Piece u of a tensor of n numbers; zeros behind its end.  wide: pieces start at their boundaries.
-template <typename T> __device__ __forceinline__ Piece load_piece(const T* x, long long n, long long u, bool wide) {
+// Pieces are those of memory, 32 bytes from a multiple of 32 on, so that a view that begins anywhere is read whole piece by whole piece;
+// its first and last ones may have numbers that are not its own.
+template <typename T> __device__ __forceinline__ int skipped(const T* x) { return (int)(reinterpret_cast<unsigned long long>(x) & (kPiece - 1)) / (int)sizeof(T); }
+// Piece u of a tensor of n numbers behind `skip`; zeros for numbers that are not its own.
+template <typename T> __device__ __forceinline__ Piece load_piece(const T* x, long long n, long long u, int skip) {
   constexpr int V = kPer<T>;
+  const long long at = u * V - skip;
   Piece p;
-  if (wide && (u + 1) * V <= n) {
+  if (at >= 0 && at + V <= n) {
     asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
-                 : "=r"(p.w[0]), "=r"(p.w[1]), "=r"(p.w[2]), "=r"(p.w[3]), "=r"(p.w[4]), "=r"(p.w[5]), "=r"(p.w[6]), "=r"(p.w[7]) : "l"(x + u * V) : "memory");
+                 : "=r"(p.w[0]), "=r"(p.w[1]), "=r"(p.w[2]), "=r"(p.w[3]), "=r"(p.w[4]), "=r"(p.w[5]), "=r"(p.w[6]), "=r"(p.w[7]) : "l"(x + at) : "memory");
     return p;
   }
 #pragma unroll
   for (int i = 0; i < 8; ++i) p.w[i] = 0;
   T* e = reinterpret_cast<T*>(p.w);
 #pragma unroll
-  for (int i = 0; i < V; ++i) if (u * V + i < n) e[i] = x[u * V + i];
+  for (int i = 0; i < V; ++i) if (at + i >= 0 && at + i < n) e[i] = x[at + i];
   return p;
 }
 __device__ __forceinline__ void store_piece(void* to, const Piece& p) {              // read again by nobody here
@@ -78,7 +82,7 @@ __device__ __forceinline__ void store_piece(void* to, const Piece& p) {         
 }
 template <typename T> __device__ __forceinline__ double squares(const T* x, long long n, long long from, long long to) {
   constexpr int V = kPer<T>;
-  const bool wide = (reinterpret_cast<unsigned long long>(x) & (kPiece - 1)) == 0;
+  const int skip = skipped(x);
   double sum[2] = {0.0, 0.0};
   auto add = [&](const Piece& w) {
     float v[V];
@@ -90,40 +94,42 @@ template <typename T> __device__ __forceinline__ double squares(const T* x, long
   for (; u + (kFlight - 1) * kThreads < to; u += kFlight * kThreads) {
     Piece w[kFlight];
 #pragma unroll
-    for (int k = 0; k < kFlight; ++k) w[k] = load_piece<T>(x, n, u + k * kThreads, wide);
+    for (int k = 0; k < kFlight; ++k) w[k] = load_piece<T>(x, n, u + k * kThreads, skip);
 #pragma unroll
     for (int k = 0; k < kFlight; ++k) add(w[k]);
   }
-  for (; u < to; u += kThreads) add(load_piece<T>(x, n, u, wide));
+  for (; u < to; u += kThreads) add(load_piece<T>(x, n, u, skip));
   return sum[0] + sum[1];
 }
 template <typename T> __device__ __forceinline__ void scale_pieces(const T* x, T* out, long long n, long long from, long long to, float f) {
   constexpr int V = kPer<T>;
-  const bool wide = ((reinterpret_cast<unsigned long long>(x) | reinterpret_cast<unsigned long long>(out)) & (kPiece - 1)) == 0;
+  const int skip = skipped(x);
+  const bool alike = skipped(out) == skip;           // else the results are written one by one
   auto put = [&](long long u, const Piece& w) {
     float v[V];
     unpack<T>(w, v);
 #pragma unroll
     for (int i = 0; i < V; ++i) v[i] *= f;
-    if (wide && (u + 1) * V <= n) {
+    const long long at = u * V - skip;
+    if (alike && at >= 0 && at + V <= n) {
       Piece to;
       T* e = reinterpret_cast<T*>(to.w);
 #pragma unroll
       for (int i = 0; i < V; ++i) e[i] = Elem<T>::from_f(v[i]);
-      store_piece(out + u * V, to);
+      store_piece(out + at, to);
     } else
 #pragma unroll
-      for (int i = 0; i < V; ++i) if (u * V + i < n) out[u * V + i] = Elem<T>::from_f(v[i]);
+      for (int i = 0; i < V; ++i) if (at + i >= 0 && at + i < n) out[at + i] = Elem<T>::from_f(v[i]);
   };
   long long u = to - 1 - threadIdx.x;
   for (; u - (kFlight - 1) * kThreads >= from; u -= kFlight * kThreads) {
     Piece w[kFlight];
 #pragma unroll
-    for (int k = 0; k < kFlight; ++k) w[k] = load_piece<T>(x, n, u - k * kThreads, wide);
+    for (int k = 0; k < kFlight; ++k) w[k] = load_piece<T>(x, n, u - k * kThreads, skip);
 #pragma unroll
     for (int k = 0; k < kFlight; ++k) put(u - k * kThreads, w[k]);
   }
-  for (; u >= from; u -= kThreads) put(u, load_piece<T>(x, n, u, wide));
+  for (; u >= from; u -= kThreads) put(u, load_piece<T>(x, n, u, skip));
 }
 
 // the tensor that holds piece u
@@ -198,7 +204,8 @@ template <int N> void fill(List<N>& l, const asgd_gradient* list, long long coun
     if (g.n == 0) continue;
     const int i = l.count++;
     l.x[i] = g.x; l.out[i] = g.out; l.n[i] = g.n; l.type[i] = (unsigned char)g.type;
-    l.first[i + 1] = l.first[i] + ceil_div(g.n, kPiece / (long long)type_bytes(g.type));
+    const long long size = (long long)type_bytes(g.type), skip = (long long)((uintptr_t)g.x & (kPiece - 1)) / size;
+    l.first[i + 1] = l.first[i] + ceil_div(g.n + skip, kPiece / size);
   }
 }
 // Blocks: two pieces a thread at least, so that few numbers take few blocks (and few partial sums).

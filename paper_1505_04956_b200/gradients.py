@@ -7,8 +7,10 @@ current CUDA stream or the one given, and nothing is known to autograd.
 """
 from __future__ import annotations
 
-import array
 import ctypes as C
+import functools
+import operator
+import struct
 
 import torch
 
@@ -37,27 +39,38 @@ def _load():
     return _lib
 
 
-# Attribute by attribute over the whole list: a call of hundreds of tensors takes as long on the host as on the device.
+# Attribute by attribute over the whole list, without a Python step per tensor where nothing is wrong: a call of hundreds of tensors
+# takes longer on the host than on the device.
+_dtype = operator.attrgetter("dtype")
+_tensor_types = {torch.Tensor, torch.nn.Parameter}
+
+
 def _checked(tensors, on, what):
     """The types' numbers of contiguous tensors on device `on`."""
-    _need(all(type(t) is torch.Tensor or isinstance(t, torch.Tensor) for t in tensors), "%s must be tensors", what)
-    _need(all(t.is_cuda for t in tensors), "%s must be CUDA tensors: the library has no host path", what)
-    _need(set(map(torch.Tensor.get_device, tensors)) <= {on}, "%s must be on cuda:%d, the current device", what, on)
+    _need(set(map(type, tensors)) <= _tensor_types or all(isinstance(t, torch.Tensor) for t in tensors), "%s must be tensors", what)
+    devices = set(map(torch.Tensor.get_device, tensors))
+    _need(min(devices, default=0) >= 0, "%s must be CUDA tensors: the library has no host path", what)
+    _need(devices <= {on}, "%s must be on cuda:%d, the current device", what, on)
     _need(all(map(torch.Tensor.is_contiguous, tensors)), "%s must be contiguous", what)
-    types = [_FLOAT.get(t.dtype) for t in tensors]
+    types = list(map(_FLOAT.get, map(_dtype, tensors)))
     _need(None not in types, "%s must be of fp32, bf16 or fp16", what)
     return types
 
 
+@functools.lru_cache(maxsize=256)
+def _workspace(n):
+    need = C.c_size_t(0)
+    _chk(_load().asgd_gradients_workspace_bytes(n, C.byref(need)), "asgd_gradients_workspace_bytes")
+    return need.value
+
+
 def _call(tensors, out, max_norm):
-    tensors = list(tensors)
+    if type(tensors) is not list:
+        tensors = list(tensors)
     on = _current_device() if _current_device is not None else -1
     _need(on >= 0, "there is no CUDA device: the library has no host path")
     types, n = _checked(tensors, on, "the tensors"), len(tensors)
-    at = sizes = []
-    if n:
-        at = list(map(torch.Tensor.data_ptr, tensors))
-        sizes = list(map(torch.Tensor.numel, tensors))
+    at, sizes = list(map(torch.Tensor.data_ptr, tensors)), list(map(torch.Tensor.numel, tensors))
     to = at
     if max_norm is not None:
         if out is not None:
@@ -69,16 +82,13 @@ def _call(tensors, out, max_norm):
         _need(len(set(there)) == len(there), "the same memory is given twice")
     flat = [0] * (4 * n)                                  # asgd_gradient by words; a type's upper half is `reserved`
     flat[0::4], flat[1::4], flat[2::4], flat[3::4] = at, to, sizes, types
-    table = array.array("q", flat)
-    need, dev = C.c_size_t(0), torch.device("cuda", on)
-    _chk(_load().asgd_gradients_workspace_bytes(n, C.byref(need)), "asgd_gradients_workspace_bytes")
-    work = _new((need.value,), (1,), dtype=torch.uint8, device=dev)
+    table, need, dev = struct.pack("%dq" % (4 * n), *flat), _workspace(n), torch.device("cuda", on)
+    work = _new((need,), (1,), dtype=torch.uint8, device=dev)
     norm = _new((), (), dtype=torch.float32, device=dev)
-    list_ptr = table.buffer_info()[0] if n else None
     if max_norm is None:
-        _chk(_load().asgd_grad_norm(list_ptr, n, norm.data_ptr(), work.data_ptr(), need.value, _handle(on)), "asgd_grad_norm")
+        _chk(_load().asgd_grad_norm(table or None, n, norm.data_ptr(), work.data_ptr(), need, _handle(on)), "asgd_grad_norm")
     else:
-        _chk(_load().asgd_clip_grads(list_ptr, n, max_norm, norm.data_ptr(), work.data_ptr(), need.value, _handle(on)), "asgd_clip_grads")
+        _chk(_load().asgd_clip_grads(table or None, n, max_norm, norm.data_ptr(), work.data_ptr(), need, _handle(on)), "asgd_clip_grads")
     return norm
 
 

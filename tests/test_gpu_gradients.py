@@ -51,7 +51,7 @@ CASES = [
 
 
 @pytest.mark.parametrize("sizes, types", CASES)
-@pytest.mark.parametrize("offset", [0, 1])
+@pytest.mark.parametrize("offset", [0, 1, 4, 13])
 def test_norm_and_clipping(sizes, types, offset):
     ts = _tensors(len(sizes), sizes, types, 0.1, offset)
     for max_norm in (0.25, 1e9):
@@ -73,6 +73,26 @@ def test_numbers_around_a_tensor_stay():
     t = base[1001:2002]
     pkg.asgd_clip_grads([t], 0.5)
     assert bool((base[:1001] == 1).all()) and bool((base[2002:] == 1).all()) and bool((t < 1).all())
+
+
+@pytest.mark.parametrize("dtype", [F32, BF, F16])
+def test_views_of_one_buffer(dtype):
+    # neighbours in memory that begin anywhere, in place and into a buffer that begins elsewhere
+    sizes = [1, 2, 3, 5, 8, 13, 40, 1000, 100_001, 7, 4096]
+    flat = torch.randn(sum(sizes) + 9, generator=torch.Generator(device="cuda").manual_seed(2), device="cuda").to(dtype)
+    for first in (0, 1, 5):
+        at = [first + sum(sizes[:i]) for i in range(len(sizes))]
+        ts = [flat[a:a + n] for a, n in zip(at, sizes)]
+        keep = flat.clone()
+        room = torch.full((sum(sizes) + 9,), 7.0, device="cuda", dtype=dtype)
+        out = [room[a + 2:a + 2 + n] for a, n in zip(at, sizes)]
+        norm = pkg.asgd_clip_grads(ts, 0.5, out=out)
+        _check(ts, 0.5, norm, out)
+        assert bool((room[:first + 2] == 7).all()) and bool((room[first + 2 + sum(sizes):] == 7).all()) and torch.equal(flat, keep)
+        pkg.asgd_clip_grads(ts, 0.5)
+        assert all(torch.equal(a, b) for a, b in zip(ts, out))
+        assert torch.equal(flat[:first], keep[:first]) and torch.equal(flat[first + sum(sizes):], keep[first + sum(sizes):])
+        flat.copy_(keep)
 
 
 def test_no_numbers():
