@@ -73,9 +73,9 @@ struct LayerArgs : Choice {
   int* made_ids;                                     // [T][top_k], where the blocks share the choices of many tokens
   float* made_weights;
   unsigned char* xq;                                 // [T][w[0].kblocks * 128]
-  float* xs;                                         // [T][w[0].kblocks]
+  float* xs;                                         // [w[0].kblocks][T]: a K block's are neighbours
   unsigned char* hq;                                 // [rows][w[1].kblocks * 128]
-  float* hs;
+  float* hs;                                         // [w[1].kblocks][T * top_k]
   float* sums;                                       // [rows of all tiles + BN per block][128]
   unsigned wait_limit;
   int withhold;
@@ -198,6 +198,7 @@ template <typename X, typename R, int kTok> __device__ __forceinline__ void logi
   for (int t = 0; t < kTok; ++t) x[t] = reinterpret_cast<const X*>(a.x) + (t0 + min(t, n - 1)) * a.ldx;      // (places behind the last token repeat it)
   const bool wide = a.router_wide && a.x_wide;
   const int whole = wide ? a.d / 4 * 4 : 0;          // numbers read four at a time
+#pragma unroll(kTok == 1 ? 4 : 2)
   for (int k = first; k < whole; k += kLogitWarps * 128) {
     const float4 m = four(r + k);
     float4 v[kTok];
@@ -647,7 +648,7 @@ expert_layer_kernel(const __grid_constant__ LayerArgs a, const __grid_constant__
   // step 0
   for (int u = (int)blockIdx.x * kWarps + wid; u < a.T * a.w[0].kblocks; u += (int)gridDim.x * kWarps) {
     const int t = u / a.w[0].kblocks, b = u % a.w[0].kblocks;
-    round_block(four(a.x, a.type, t * a.ldx, b * 128 + lane * 4, a.d, a.x_wide), a.xq + (long long)u * 128, a.xs + u, lane);
+    round_block(four(a.x, a.type, t * a.ldx, b * 128 + lane * 4, a.d, a.x_wide), a.xq + (long long)u * 128, a.xs + b * a.T + t, lane);
   }
   if (a.router) {
     auto part = reinterpret_cast<float (*)[kLogitWarps][kLogitTokens]>(making.x);
@@ -762,6 +763,7 @@ expert_layer_kernel(const __grid_constant__ LayerArgs a, const __grid_constant__
       const Matrix& w = a.w[f];
       const unsigned char* from = f ? a.hq : a.xq;
       const float* from_scales = f ? a.hs : a.xs;
+      const int per_block = f ? a.T * a.c.top_k : a.T;
       constexpr int kCopies = BN * 8 / 32;           // 16-byte pieces of a lane
       long long at[kCopies];                         // its rows' first numbers, -1: none
       const float* of_token[BN > 32 ? 2 : 1];
@@ -778,7 +780,7 @@ expert_layer_kernel(const __grid_constant__ LayerArgs a, const __grid_constant__
             at[i] = r < n ? (long long)row_at(r) * (w.kblocks * 128) + (lane & 7) * 16 : -1;
           }
 #pragma unroll
-          for (int i = 0; i < (BN > 32 ? 2 : 1); ++i) of_token[i] = i * 32 + lane < n ? from_scales + (long long)row_at(i * 32 + lane) * w.kblocks : nullptr;
+          for (int i = 0; i < (BN > 32 ? 2 : 1); ++i) of_token[i] = i * 32 + lane < n ? from_scales + row_at(i * 32 + lane) : nullptr;
           of_weights = w.scale + plan.expert[s.chunk] * w.group + s.tile * w.row;
         }
         const unsigned q = it % S;
@@ -793,7 +795,7 @@ expert_layer_kernel(const __grid_constant__ LayerArgs a, const __grid_constant__
         float* sc = scales + q * L::kScales;
 #pragma unroll
         for (int i = 0; i < (BN > 32 ? 2 : 1); ++i)
-          if (i * 32 + lane < BN) copy4(sc + i * 32 + lane, of_token[i] ? of_token[i] + s.kb : from_scales, of_token[i] != nullptr);
+          if (i * 32 + lane < BN) copy4(sc + i * 32 + lane, of_token[i] ? of_token[i] + s.kb * per_block : from_scales, of_token[i] != nullptr);
         if (lane == 0) copy4(sc + BN, of_weights + s.kb * w.block, true);
         arrive_after_copies(bars + L::READY + q);
       }
@@ -867,22 +869,34 @@ expert_layer_kernel(const __grid_constant__ LayerArgs a, const __grid_constant__
       ok = *reinterpret_cast<volatile int*>(misc + 3) != 0;
       if (!ok) break;
       if (f == 0) {
-        for (int u = reader; u < rows * hb; u += readers) {
-          const int row = u / hb, j = u % hb * 128 + lane * 4;
-          float4 v = make_float4(0.f, 0.f, 0.f, 0.f), up = v;
-          if (a.h % 4 == 0) {
-            if (u != reader) hidden = HiddenAt<BN>(a, plan, row, j);
-            float4 both[2];
-            add_up<BN>(hidden.at, hidden.blocks, both);
-            v = both[0];
-            up = both[1];
-          } else {
-            v = hidden_one_by_one<BN>(a, plan, row, j, a.h);
-            if (a.gated) up = hidden_one_by_one<BN>(a, plan, row, a.h + min(j, a.h), 2 * a.h);
-          }
+        auto finish = [&](int u, float4 v, const float4& up) {
           v = make_float4(activated(v.x, a.silu), activated(v.y, a.silu), activated(v.z, a.silu), activated(v.w, a.silu));
           if (a.gated) { v.x *= up.x; v.y *= up.y; v.z *= up.z; v.w *= up.w; }
-          round_block(v, a.hq + (long long)u * 128, a.hs + u, lane);
+          round_block(v, a.hq + (long long)u * 128, a.hs + u % hb * (a.T * a.c.top_k) + u / hb, lane);
+        };
+        const int units = rows * hb;
+        if (a.h % 4 == 0) {
+          for (int u = reader; u < units; u += 2 * readers) {               // two at a time: their loads are in flight together
+            const int u2 = u + readers;
+            if (u != reader) hidden = HiddenAt<BN>(a, plan, u / hb, u % hb * 128 + lane * 4);
+            HiddenAt<BN> other;
+            if (u2 < units) other = HiddenAt<BN>(a, plan, u2 / hb, u2 % hb * 128 + lane * 4);
+            const float* const at[4] = {hidden.at[0], hidden.at[1], other.at[0], other.at[1]};
+            const int blocks[4] = {hidden.blocks[0], hidden.blocks[1], other.blocks[0], other.blocks[1]};
+            float4 v[4];
+            add_up<BN>(at, blocks, v);
+            finish(u, v[0], v[1]);
+            if (u2 < units) finish(u2, v[2], v[3]);
+          }
+        } else {
+#pragma unroll 1
+          for (int u = reader; u < units; u += readers) {
+            const int row = u / hb, j = u % hb * 128 + lane * 4;
+            const float4 v = hidden_one_by_one<BN>(a, plan, row, j, a.h);
+            float4 up = v;
+            if (a.gated) up = hidden_one_by_one<BN>(a, plan, row, a.h + min(j, a.h), 2 * a.h);
+            finish(u, v, up);
+          }
         }
         readers_sync();
         if (tid == 128) come(&a.shared->meeting[MEET_HIDDEN].count);
