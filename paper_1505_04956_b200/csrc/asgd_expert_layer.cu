@@ -748,17 +748,17 @@ expert_layer_kernel(const __grid_constant__ LayerArgs a, const __grid_constant__
   } else if (wid == 2) {
     unsigned it = 0;
     bool ok = true;
-    if (chunks) {                                    // the scales of W2, so that they are not waited for later on
-      const Matrix& w = a.w[1];
-      const Stretch s(w, chunks, plan.per[1]);
-      for (unsigned x = s.from + lane; x < s.to; x += 32) {
-        const int tile = (int)(x / w.kblocks);
-        asm volatile("prefetch.global.L2 [%0];" ::"l"(w.scale + plan.expert[tile / w.tiles] * w.group + tile % w.tiles * w.row + (x - tile * w.kblocks) * w.block));
-      }
-    }
     for (int f = 0; f < 2 && ok && chunks; ++f) {
       bool met = true;
-      if (lane == 0) met = meet(a.shared, f ? MEET_HIDDEN : MEET_TOKENS, a.wait_limit, abort);
+      if (f) {                                       // the scales of W2, so that they are not waited for later on
+        const Matrix& w = a.w[1];
+        const Stretch s(w, chunks, plan.per[1]);
+        for (unsigned x = s.from + lane; x < s.to; x += 32) {
+          const int tile = (int)(x / w.kblocks);
+          asm volatile("prefetch.global.L2 [%0];" ::"l"(w.scale + plan.expert[tile / w.tiles] * w.group + tile % w.tiles * w.row + (x - tile * w.kblocks) * w.block));
+        }
+      }
+      if (lane == 0 && (f || !(a.router || share))) met = meet(a.shared, f ? MEET_HIDDEN : MEET_TOKENS, a.wait_limit, abort);      // (the block has met for the tokens already, or not)
       if (!(ok = __all_sync(kAll, met))) break;
       const Matrix& w = a.w[f];
       const unsigned char* from = f ? a.hq : a.xq;

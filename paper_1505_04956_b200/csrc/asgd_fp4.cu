@@ -62,6 +62,14 @@ template <typename T, int kBytes> __device__ __forceinline__ unsigned largest(co
     return __float_as_uint(Elem<T>::to_f(*reinterpret_cast<const T*>(&h))) & 0x7fffffffu;
   }
 }
+// eight numbers as 4-bit ones, the first in the lowest bits
+__device__ __forceinline__ unsigned eight_codes(const float* v) {
+  unsigned w;
+  asm("{\n .reg .b8 a, b, c, d;\n cvt.rn.satfinite.e2m1x2.f32 a, %2, %1;\n cvt.rn.satfinite.e2m1x2.f32 b, %4, %3;\n cvt.rn.satfinite.e2m1x2.f32 c, %6, %5;\n"
+      " cvt.rn.satfinite.e2m1x2.f32 d, %8, %7;\n mov.b32 %0, {a, b, c, d};\n}"
+      : "=r"(w) : "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]));
+  return w;
+}
 // V 4-bit numbers (V / 2 bytes) as one store
 template <int V> __device__ __forceinline__ void store_codes(unsigned char* to, const unsigned (&w)[V > 8 ? 2 : 1]) {
   if constexpr (V == 16) *reinterpret_cast<uint2*>(to) = make_uint2(w[0], w[1]);
@@ -143,9 +151,14 @@ template <typename T, int kAlign, bool kWeights, int U> __global__ void __launch
       for (int i = 0; i < V; ++i) v[i] = (kWeights ? v[i] : Elem<T>::to_f(e[i])) * inv;
     }
     unsigned w[V > 8 ? 2 : 1] = {};
+    if constexpr (V >= 8) {
 #pragma unroll
-    for (int i = 0; i < V; i += 2)
-      w[i / 8] |= (unsigned)__nv_cvt_float2_to_fp4x2(make_float2(v[i], v[i + 1]), __NV_E2M1, cudaRoundNearest) << (4 * (i & 7));
+      for (int i = 0; i < V; i += 8) w[i / 8] = eight_codes(v + i);
+    } else {
+#pragma unroll
+      for (int i = 0; i < V; i += 2)
+        w[0] |= (unsigned)__nv_cvt_float2_to_fp4x2(make_float2(v[i], v[i + 1]), __NV_E2M1, cudaRoundNearest) << (4 * i);
+    }
     if (none) {                                      // an infinity times 0
 #pragma unroll
       for (int i = 0; i < (V > 8 ? 2 : 1); ++i) w[i] = 0;
