@@ -18,9 +18,9 @@
 // A tile is 128 rows of W (the MMA's M) by BN tokens of one expert (its N; an expert with more has several chunks); a
 // K block's products leave tensor memory and are added, scaled, in registers, as in asgd_product_few.cuh.
 //
-// Warp roles after step 0: 0 issues the copies of weights; 1 and 3 issue the products, K blocks in turn; 2 brings the tokens'
-// rows (gathered, 16-byte asynchronous copies into the swizzled layout that a tensor map would write) and the scales; 4 to 11
-// read the accumulators, and do steps 2 and 4.  Every wait is bounded, those of blocks for one another too.
+// Warp roles after step 0: 0 issues the copies of weights; 1 and 3 issue the products, K blocks in turn; 2 and 12 to 14 bring the
+// tokens' rows (gathered, 16-byte asynchronous copies into the swizzled layout that a tensor map would write) and the scales, K blocks in
+// turn; 4 to 11 read the accumulators, and do steps 2 and 4.  Every wait is bounded, those of blocks for one another too.
 #include <algorithm>
 
 #include "../../include/asgd_expert_layer.h"
@@ -30,7 +30,7 @@
 
 namespace {
 
-constexpr int kThreads = 384, kWarps = kThreads / 32, kReaders = 8;
+constexpr int kThreads = 512, kWarps = kThreads / 32, kReaders = 8, kLoaders = 4;
 constexpr int kMostRows = ASGD_LAYER_MAX_ASSIGNMENTS;
 constexpr int kChoices = 2 * kWarps;                 // tokens that every block chooses for itself; with more the blocks share them out and meet
 constexpr int kTokenWords = ASGD_LAYER_MAX_TOKENS / 32;
@@ -91,6 +91,7 @@ template <int BN> struct Layer {
   enum { FULL = 0, READY = kSlots, DONE = 2 * kSlots, SEMPTY = 3 * kSlots, ACCEMPTY = 4 * kSlots, DRAIN = ACCEMPTY + kAccStages, COUNT = DRAIN + 2 };
   static constexpr size_t kRing = (size_t)kSlots * kSlotBytes;
   static constexpr size_t kSmem = 1024 + kRing + (size_t)kSlots * kScales * 4 + COUNT * 8;
+  static_assert(kSlots > kLoaders, "a loading warp meets every phase of what it waits for");
   static_assert(kSlots % 2 == 0 && kCols >= 32, "slots, tensor memory");
 };
 
@@ -499,12 +500,12 @@ struct Stretch {
     tile = (int)(t - chunk * w.tiles);
   }
   __device__ __forceinline__ bool there() const { return from < to; }
-  __device__ __forceinline__ void next(const Matrix& w) {
-    ++from;
-    if (++kb == w.kblocks) {
-      kb = 0;
-      if (++tile == w.tiles) { tile = 0; ++chunk; }
-    }
+  // K blocks of the tile it is in, and the next tile
+  __device__ __forceinline__ int here(const Matrix& w) const { return (int)min((unsigned)(w.kblocks - kb), to - from); }
+  __device__ __forceinline__ void next_tile(const Matrix& w) {
+    from += here(w);
+    kb = 0;
+    if (++tile == w.tiles) { tile = 0; ++chunk; }
   }
 };
 // Sums of a tile's rows: in front of them those of all tiles before it, and BN for every block that ended a stretch before.
@@ -711,13 +712,17 @@ expert_layer_kernel(const __grid_constant__ LayerArgs a, const __grid_constant__
       const unsigned long long policy = leaves_first();
       unsigned it = 0;
       bool ok = !*reinterpret_cast<volatile int*>(abort);
+#pragma unroll
       for (int f = 0; f < 2 && ok && chunks; ++f) {
         const Matrix& w = a.w[f];
-        for (Stretch s(w, chunks, plan.per[f]); s.there(); s.next(w), ++it) {
-          const unsigned q = it % S;
-          if (it >= S && !(ok = wait(bars + L::DONE + q, (it / S - 1) & 1, a.wait_limit, abort))) break;
-          mbar_expect_tx(bars + L::FULL + q, L::kWeights);
-          if (!(a.withhold && it == 0)) load_weights(ring + (size_t)q * L::kSlotBytes, f ? &map_2 : &map_1, s.kb * kKB, s.tile * kU, plan.expert[s.chunk], bars + L::FULL + q, policy);
+        for (Stretch s(w, chunks, plan.per[f]); s.there() && ok; s.next_tile(w)) {
+          const int expert = plan.expert[s.chunk], end = s.kb + s.here(w);
+          for (int kb = s.kb; kb < end; ++kb, ++it) {
+            const unsigned q = it % S;
+            if (it >= S && !(ok = wait(bars + L::DONE + q, (it / S - 1) & 1, a.wait_limit, abort))) break;
+            mbar_expect_tx(bars + L::FULL + q, L::kWeights);
+            if (!(a.withhold && it == 0)) load_weights(ring + (size_t)q * L::kSlotBytes, f ? &map_2 : &map_1, kb * kKB, s.tile * kU, expert, bars + L::FULL + q, policy);
+          }
         }
       }
       misc[2] = (int)it;
@@ -726,6 +731,7 @@ expert_layer_kernel(const __grid_constant__ LayerArgs a, const __grid_constant__
     const unsigned me = (unsigned)wid >> 1, at = __shfl_sync(kAll, tmem, 0);
     unsigned it = 0;
     bool ok = true;
+#pragma unroll
     for (int f = 0; f < 2 && ok && chunks; ++f) {
       const unsigned idesc = a.w[f].idesc;
       for (Stretch s(a.w[f], chunks, plan.per[f]); s.there(); ++s.from, ++it) {
@@ -745,68 +751,63 @@ expert_layer_kernel(const __grid_constant__ LayerArgs a, const __grid_constant__
         __syncwarp();
       }
     }
-  } else if (wid == 2) {
-    unsigned it = 0;
+  } else if (wid == 2 || (wid >= 4 + kReaders && wid < 3 + kReaders + kLoaders)) {
+    // Four warps, K blocks in turn: one took 700 cycles for a K block of 16 tokens, 1500 for 64, and set the pace.
+    const int me = wid == 2 ? 0 : wid - (3 + kReaders);
+    unsigned it = 0;                                 // K blocks before the tile
     bool ok = true;
+#pragma unroll
     for (int f = 0; f < 2 && ok && chunks; ++f) {
+      const Matrix& w = a.w[f];
       bool met = true;
-      if (f) {                                       // the scales of W2, so that they are not waited for later on
-        const Matrix& w = a.w[1];
-        const Stretch s(w, chunks, plan.per[1]);
-        for (unsigned x = s.from + lane; x < s.to; x += 32) {
-          const int tile = (int)(x / w.kblocks);
-          asm volatile("prefetch.global.L2 [%0];" ::"l"(w.scale + plan.expert[tile / w.tiles] * w.group + tile % w.tiles * w.row + (x - tile * w.kblocks) * w.block));
-        }
-      }
       if (lane == 0 && (f || !(a.router || share))) met = meet(a.shared, f ? MEET_HIDDEN : MEET_TOKENS, a.wait_limit, abort);      // (the block has met for the tokens already, or not)
       if (!(ok = __all_sync(kAll, met))) break;
-      const Matrix& w = a.w[f];
       const unsigned char* from = f ? a.hq : a.xq;
       const float* from_scales = f ? a.hs : a.xs;
       const int per_block = f ? a.T * a.c.top_k : a.T;
       constexpr int kCopies = BN * 8 / 32;           // 16-byte pieces of a lane
-      long long at[kCopies];                         // its rows' first numbers, -1: none
-      const float* of_token[BN > 32 ? 2 : 1];
-      const float* of_weights = nullptr;
-      bool fresh = true;
-      for (Stretch s(w, chunks, plan.per[f]); s.there(); s.next(w), ++it) {
-        if (fresh || s.kb == 0) {
-          fresh = false;
-          const int first = plan.first[s.chunk], n = plan.rows[s.chunk];
-          auto row_at = [&](int r) { return f ? first + r : plan.order[first + r] / a.c.top_k; };
-#pragma unroll
-          for (int i = 0; i < kCopies; ++i) {
-            const int r = i * 4 + (lane >> 3);
-            at[i] = r < n ? (long long)row_at(r) * (w.kblocks * 128) + (lane & 7) * 16 : -1;
-          }
-#pragma unroll
-          for (int i = 0; i < (BN > 32 ? 2 : 1); ++i) of_token[i] = i * 32 + lane < n ? from_scales + row_at(i * 32 + lane) : nullptr;
-          of_weights = w.scale + plan.expert[s.chunk] * w.group + s.tile * w.row;
-        }
-        const unsigned q = it % S;
-        if (it >= S && !(ok = __all_sync(kAll, wait(bars + L::SEMPTY + q, (it / S - 1) & 1, a.wait_limit, abort)))) break;
-        unsigned char* to = ring + (size_t)q * L::kSlotBytes + L::kWeights;
+      for (Stretch s(w, chunks, plan.per[f]); s.there() && ok; s.next_tile(w)) {
+        const int first = plan.first[s.chunk], n = plan.rows[s.chunk], here = s.here(w);
+        auto row_at = [&](int r) { return f ? first + r : plan.order[first + r] / a.c.top_k; };
+        const unsigned char* at[kCopies];            // its rows' first numbers, null: none
 #pragma unroll
         for (int i = 0; i < kCopies; ++i) {
           const int r = i * 4 + (lane >> 3);
-          copy16(reinterpret_cast<float*>(to + r * kKB + (((lane & 7) ^ (r & 7)) << 4)),
-                 reinterpret_cast<const float*>(at[i] >= 0 ? from + at[i] + s.kb * 128 : from), at[i] >= 0 ? 16 : 0);
+          at[i] = r < n ? from + (long long)row_at(r) * (w.kblocks * 128) + (lane & 7) * 16 : nullptr;
         }
-        float* sc = scales + q * L::kScales;
+        const float* of_token[BN > 32 ? 2 : 1];
 #pragma unroll
-        for (int i = 0; i < (BN > 32 ? 2 : 1); ++i)
-          if (i * 32 + lane < BN) copy4(sc + i * 32 + lane, of_token[i] ? of_token[i] + s.kb * per_block : from_scales, of_token[i] != nullptr);
-        if (lane == 0) copy4(sc + BN, of_weights + s.kb * w.block, true);
-        arrive_after_copies(bars + L::READY + q);
+        for (int i = 0; i < (BN > 32 ? 2 : 1); ++i) of_token[i] = i * 32 + lane < n ? from_scales + row_at(i * 32 + lane) : nullptr;
+        const float* of_weights = w.scale + plan.expert[s.chunk] * w.group + s.tile * w.row;
+        for (int i0 = (me - it) & (kLoaders - 1); i0 < here; i0 += kLoaders) {
+          const unsigned k = it + i0, q = k % S;
+          const int kb = s.kb + i0;
+          // (a slot's K block two rounds ago has been read: this warp has waited for a later one, kLoaders < S)
+          if (k >= S && !(ok = __all_sync(kAll, wait(bars + L::SEMPTY + q, (k / S - 1) & 1, a.wait_limit, abort)))) break;
+          unsigned char* to = ring + (size_t)q * L::kSlotBytes + L::kWeights;
+#pragma unroll
+          for (int i = 0; i < kCopies; ++i) {
+            const int r = i * 4 + (lane >> 3);
+            copy16(reinterpret_cast<float*>(to + r * kKB + (((lane & 7) ^ (r & 7)) << 4)), reinterpret_cast<const float*>(at[i] ? at[i] + kb * 128 : from), at[i] ? 16 : 0);
+          }
+          float* sc = scales + q * L::kScales;
+#pragma unroll
+          for (int i = 0; i < (BN > 32 ? 2 : 1); ++i)
+            if (i * 32 + lane < BN) copy4(sc + i * 32 + lane, of_token[i] ? of_token[i] + kb * per_block : from_scales, of_token[i] != nullptr);
+          if (lane == 0) copy4(sc + BN, of_weights + kb * w.block, true);
+          arrive_after_copies(bars + L::READY + q);
+        }
+        it += here;
       }
     }
     asm volatile("cp.async.wait_all;" ::: "memory");
-  } else if (wid >= 4) {
+  } else if (wid >= 4 && wid < 4 + kReaders) {
     const int quarter = wid & 3, c_first = ((wid - 4) >> 2) * L::kRows;                 // the warp's rows of W and tokens
     const unsigned at_tmem = tmem + ((unsigned)(quarter * 32) << 16) + c_first;
     const int reader = (int)blockIdx.x * kReaders + wid - 4, readers = (int)gridDim.x * kReaders;
     unsigned it = 0;
     bool ok = true;                                  // (all readers go the same way, see below)
+#pragma unroll
     for (int f = 0; f < 2 && ok; ++f) {
       const Matrix& w = a.w[f];
       if (chunks) {
@@ -815,8 +816,8 @@ expert_layer_kernel(const __grid_constant__ LayerArgs a, const __grid_constant__
 #pragma unroll
           for (int c = 0; c < L::kRows; ++c) acc[c] = 0.f;
           const int chunk = s.chunk, tile = s.tile;
-          const unsigned n = min((unsigned)(w.kblocks - s.kb), s.to - s.from);             // of this tile
-          for (unsigned i = 0; i < n; ++i, ++it) {
+          const int n = s.here(w);
+          for (int i = 0; i < n; ++i, ++it) {
             const unsigned q = it % S, stage = it % kAccStages;
             ok = wait(bars + L::READY + q, (it / S) & 1, a.wait_limit, abort) && wait(bars + L::DONE + q, (it / S) & 1, a.wait_limit, abort);
             if (!(ok = __all_sync(kAll, ok))) break;
@@ -846,10 +847,7 @@ expert_layer_kernel(const __grid_constant__ LayerArgs a, const __grid_constant__
           const int left = plan.rows[chunk] - c_first;
 #pragma unroll
           for (int c = 0; c < L::kRows; ++c) if (c < left) to[c * 128] = acc[c];
-          // the next tile
-          s.from += n;
-          s.kb = 0;
-          if (++s.tile == w.tiles) { s.tile = 0; ++s.chunk; }
+          s.next_tile(w);
         }
       }
       // what comes after the meeting, as far as it can be known before
