@@ -20,8 +20,8 @@ extern "C" {
 
 typedef struct asgd_gradient {
   const void *x; /* n numbers of `type`, one after another, aligned to their type (NULL where n = 0)       */
-  void *out;     /* the clipped ones, of the same type: x itself or memory that no x and no other out is in;
-                    not used by asgd_grad_norm                                                             */
+  void *out;     /* the clipped ones, of the same type: x itself or memory that no x and no other out is in
+                    (ASGD_EINVAL where they meet); not used by asgd_grad_norm                              */
   int64_t n;     /* 0 .. ASGD_GRADIENT_MAX                                                                 */
   int32_t type;  /* ASGD_F32 / BF16 / F16                                                                  */
   int32_t reserved; /* 0 */

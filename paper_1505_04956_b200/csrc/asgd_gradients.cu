@@ -4,13 +4,15 @@
 // adding up the same partial sums in the same order) the factor and the scaling.  The bytes are the bound: the list of
 // tensors counts as one run of 32-byte pieces, and every block takes an equal stretch of it, whatever tensors it meets there.
 // The second pass walks each stretch from its end, where the first one's last bytes are still in L2.
-// Loads and stores of 32 bytes a thread, two of them in flight, with 1024 threads an SM: 344 M bf16 numbers of 56 tensors 345 us
+// Loads and stores of 32 bytes a thread, two of them in flight, with 1024 threads an SM: 344 M bf16 numbers of 56 tensors 355 us
 // (three passes at HBM's rate would be 316); 16 bytes, four in flight, 465; eight 434; two with 2048 threads 413.  The norm alone of 87 M numbers of
 // 512 tensors 42.5 us (5.5 TB/s) where 16 bytes took 65.
 // Squares are added in fp64: a number of fp32 squared passes fp32's range from 2^64 on, and long sums in fp32 lose digits;
 // the conversions and multiply-adds (two instructions a number) hide behind the loads (sums by eight in fp32 gained nothing).
 #include <algorithm>
 #include <cmath>
+#include <new>
+#include <vector>
 
 #include "../../include/asgd_gradients.h"
 #include "asgd_experts_common.cuh"
@@ -235,6 +237,28 @@ template <int N> int scale_launches(const asgd_gradient* list, long long count, 
 
 constexpr long long kMostTensors = 1ll << 20;
 
+// Whether what a clipping call writes meets anything else of the call's: ranges by where they begin, against the furthest end so far.
+bool overlaps(const asgd_gradient* list, int64_t count) {
+  struct Range { uintptr_t from, to; bool written; };
+  std::vector<Range> all;
+  all.reserve((size_t)count * 2);
+  for (int64_t i = 0; i < count; ++i) {
+    const asgd_gradient& g = list[i];
+    const size_t bytes = (size_t)g.n * type_bytes(g.type);
+    if (!bytes) continue;
+    all.push_back({(uintptr_t)g.out, (uintptr_t)g.out + bytes, true});
+    if (g.x != g.out) all.push_back({(uintptr_t)g.x, (uintptr_t)g.x + bytes, false});
+  }
+  std::sort(all.begin(), all.end(), [](const Range& a, const Range& b) { return a.from < b.from; });
+  uintptr_t read = 0, written = 0;                   // ends
+  for (const Range& r : all) {
+    if (r.from < written || (r.written && r.from < read)) return true;
+    uintptr_t& end = r.written ? written : read;
+    end = std::max(end, r.to);
+  }
+  return false;
+}
+
 size_t bytes_of(long long count) { return (size_t)(ceil_div(std::max(count, 1ll), kMany) * kBlocks) * sizeof(double); }
 
 int check(const asgd_gradient* list, int64_t count, bool scaled, const float* norm, const void* workspace, size_t bytes) {
@@ -248,7 +272,13 @@ int check(const asgd_gradient* list, int64_t count, bool scaled, const float* no
     if (scaled && g.n > 0 && (!g.out || !aligned(g.out, type_bytes(g.type)))) return ASGD_EINVAL;
   }
   if (!workspace || bytes < bytes_of(count)) return ASGD_ENOMEM;
-  return aligned(workspace, 16) ? ASGD_OK : ASGD_EINVAL;
+  if (!aligned(workspace, 16)) return ASGD_EINVAL;
+  if (scaled && count > 0) try {
+    if (overlaps(list, count)) return ASGD_EINVAL;
+  } catch (const std::bad_alloc&) {                  // of the host's memory
+    return ASGD_ENOMEM;
+  }
+  return ASGD_OK;
 }
 
 }  // namespace

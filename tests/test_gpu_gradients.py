@@ -151,6 +151,21 @@ def test_results_do_not_depend_on_timing_and_a_graph_replays():
     _check(ts, 0.1, norm, again)
 
 
+def test_neighbours_and_inputs_that_share_memory():
+    buffer = torch.randn(1000, generator=torch.Generator("cuda").manual_seed(3), device="cuda")
+    before = buffer.clone()
+    out = torch.empty(2, 600, device="cuda")
+    norm = pkg.asgd_clip_grads([buffer[:600], buffer[400:]], 1.0, out=[out[0], out[1]])
+    factor = 1.0 / (math.sqrt((before[:600].double() ** 2).sum() + (before[400:].double() ** 2).sum()) + 1e-6)
+    for got, x in ((out[0], before[:600]), (out[1], before[400:])):
+        assert ((got.double() - x.double() * factor).abs() <= 6 * U * (x.double() * factor).abs() + SMALLEST[F32]).all()
+    assert torch.equal(buffer, before)
+    assert torch.equal(pkg.asgd_clip_grads([buffer[600:], buffer[:600]], 1e9), pkg.asgd_grad_norm([before[600:], before[:600]]))
+    with pytest.raises(pkg.AsgdError):
+        pkg.asgd_clip_grads([buffer[:600], buffer[599:]], 1.0)
+    assert torch.equal(buffer, before) and float(norm) > 1
+
+
 def test_refusals():
     x = torch.ones(10, device="cuda")
     for bad in ([x, x], [x[::2]], [x.double()], [x.cpu()], [x.int()]):

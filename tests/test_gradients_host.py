@@ -60,6 +60,17 @@ def test_refuses_outputs_that_are_not_there():
     assert [L.asgd_clip_grads(C.addressof(b), 1, 1.0, P, P, 1 << 20, None) for b in bad] == [EINVAL] * 3
 
 
+@pytest.mark.parametrize("items", [
+    (dict(), dict()), (dict(), dict(x=P + 36, out=P + 36)), (dict(), dict(x=P + 4096, out=P + 16, n=1)), (dict(n=1000), dict(x=P + 80, out=P + 8192), dict(x=P + 400, out=P + 400)),
+    (dict(out=P + 4),), (dict(out=P - 4, type=1),), (dict(x=P + 4096, out=P + 8192), dict(x=P + 8200, out=P + 12288)),
+    (dict(out=P + 4096), dict(out=P + 4132)), (dict(n=0), dict(n=4, type=1), dict(x=P + 6, out=P + 6, n=1, type=1))])
+def test_refuses_to_clip_what_meets(items):
+    """Numbers that are written twice, or written while they are another tensor's input."""
+    for order in (items, items[::-1]):
+        list_ = _list(*order)
+        assert gradients._load().asgd_clip_grads(C.addressof(list_), len(items), 1.0, P, P, 1 << 20, None) == EINVAL
+
+
 def test_refuses_arguments():
     assert _both(None, 1) == (EINVAL, EINVAL)
     assert _both(_list({}), -1) == (EINVAL, EINVAL)
