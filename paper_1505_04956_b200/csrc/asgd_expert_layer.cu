@@ -8,7 +8,7 @@
 //
 // The steps:
 //   0  logits (with a router) and the tokens in 8 bits, by all warps of all blocks.   -- blocks meet
-//   1  every block chooses the experts of all tokens for itself (more than 24 tokens are shared out, and the blocks meet once more), and lists
+//   1  every block chooses the experts of all tokens for itself (more than 30 tokens are shared out, and the blocks meet once more), and lists
 //      the rows by expert.  Then its stretch of W1: sums of partial tiles go to the workspace.  -- blocks meet
 //   2  sums of a tile's stretches in the blocks' order, activation, 8 bits.   -- blocks meet (the copies of W2 went on)
 //   3  its stretch of W2, sums to the workspace.   -- blocks meet
@@ -32,7 +32,8 @@ namespace {
 
 constexpr int kThreads = 512, kWarps = kThreads / 32, kReaders = 8, kLoaders = 4;
 constexpr int kMostRows = ASGD_LAYER_MAX_ASSIGNMENTS;
-constexpr int kChoices = 2 * kWarps;                 // tokens that every block chooses for itself; with more the blocks share them out and meet
+constexpr int kDry = kWarps - 1;                     // the warp that goes ahead, see the kernel
+constexpr int kChoices = 2 * kDry;                   // tokens that every block chooses for itself; with more the blocks share them out and meet
 constexpr int kTokenWords = ASGD_LAYER_MAX_TOKENS / 32;
 enum { MEET_TOKENS, MEET_CHOICE, MEET_SUMS, MEET_HIDDEN, MEET_OUT, MEETINGS };
 
@@ -189,9 +190,9 @@ __device__ __forceinline__ void round_block(const float4& v, unsigned char* q, f
   if (lane == 0) *scale = __fmul_rn(m, 1.f / 448.f);
 }
 
-// Logits of a router: four warps share a row of it and kTok tokens; a block has three such groups of warps.  (The types are the
+// Logits of a router: four warps share a row of it and kTok tokens; a block has three such groups.  (The types are the
 // template's, so that a step's loads are all in flight at once: with a switch around each, 60 tokens took 16 us.)
-constexpr int kLogitTokens = 8, kLogitWarps = 4, kLogitGroups = kWarps / kLogitWarps;
+constexpr int kLogitTokens = 8, kLogitWarps = 4, kLogitGroups = kDry / kLogitWarps;
 template <typename X, typename R, int kTok> __device__ __forceinline__ void logit_sums(const LayerArgs& a, int e, int t0, int n, int first, float (&acc)[kLogitTokens]) {
   const R* r = reinterpret_cast<const R*>(a.router) + e * a.ld_router;
   const X* x[kTok];
@@ -215,11 +216,12 @@ template <typename X, typename R, int kTok> __device__ __forceinline__ void logi
     for (int t = 0; t < kTok; ++t) acc[t] = fmaf(Elem<X>::to_f(x[t][k]), m, acc[t]);
   }
 }
+__device__ __forceinline__ void others_sync() { asm volatile("bar.sync 2, %0;" ::"n"(kDry * 32) : "memory"); }      // all warps but the one that goes ahead
 template <int kTok> __device__ inline void make_logits(const LayerArgs& a, float (*part)[kLogitWarps][kLogitTokens], int lane, int wid) {
   const int E = a.c.experts, sets = (a.T + kTok - 1) / kTok, units = E * sets, group = wid / kLogitWarps, sub = wid % kLogitWarps;
   const int per = kLogitGroups * (int)gridDim.x, first = (sub * 32 + lane) * 4;
   for (int u0 = (int)blockIdx.x * kLogitGroups; u0 < units; u0 += per) {
-    const int u = u0 + group, e = u / sets, t0 = u % sets * kTok, n = u < units ? min(kTok, a.T - t0) : 0;
+    const int u = u0 + group, e = u / sets, t0 = u % sets * kTok, n = u < units && group < kLogitGroups ? min(kTok, a.T - t0) : 0;
     float acc[kLogitTokens];
 #pragma unroll
     for (int t = 0; t < kLogitTokens; ++t) acc[t] = 0.f;
@@ -238,16 +240,16 @@ template <int kTok> __device__ inline void make_logits(const LayerArgs& a, float
     for (int t = 0; t < kTok; ++t) {
 #pragma unroll
       for (int o = 16; o > 0; o >>= 1) acc[t] += __shfl_xor_sync(kAll, acc[t], o);
-      if (lane == 0) part[group][sub][t] = acc[t];
+      if (lane == 0 && group < kLogitGroups) part[group][sub][t] = acc[t];
     }
-    __syncthreads();
+    others_sync();
     if (sub == 0 && lane < n) {
       float s = part[group][0][lane];
 #pragma unroll
       for (int w = 1; w < kLogitWarps; ++w) s += part[group][w][lane];
       a.made_logits[(long long)(t0 + lane) * E + e] = (s - (a.shift ? a.shift[e] : 0.f)) * a.temperature;
     }
-    __syncthreads();
+    others_sync();
   }
 }
 
@@ -260,12 +262,14 @@ template <typename T> __device__ __forceinline__ void read_logits(const T* row, 
 #pragma unroll 4
   for (int e = lane; e < E; e += 32) x[e] = Elem<T>::to_f(__ldcg(row + e));
 }
-__device__ inline void choose_one(const LayerArgs& a, int t, const float* bias, float* x, unsigned* key, uint2* found, int* place, int lane, int& id, float& weight) {
+__device__ inline void choose_one(const LayerArgs& a, int t, const float* bias, float* x, unsigned* key, uint2* found, int* place, int lane, bool dry, int& id, float& weight) {
   const asgd_route_config& c = a.c;
   const int E = c.experts, K = c.top_k;
   const bool by_logit = a.bias == nullptr && c.group_top == 1, sigmoid_scores = c.score == ASGD_SCORE_SIGMOID;
   __syncwarp();
-  if (a.made_logits) read_logits(a.made_logits + (long long)t * E, E, lane, x);
+  if (dry)
+    for (int e = lane; e < E; e += 32) x[e] = (float)e;
+  else if (a.made_logits) read_logits(a.made_logits + (long long)t * E, E, lane, x);
   else if (a.logits_type == ASGD_F32) read_logits(reinterpret_cast<const float*>(a.logits) + t * a.ld_logits, E, lane, x);
   else if (a.logits_type == ASGD_BF16) read_logits(reinterpret_cast<const __nv_bfloat16*>(a.logits) + t * a.ld_logits, E, lane, x);
   else read_logits(reinterpret_cast<const __half*>(a.logits) + t * a.ld_logits, E, lane, x);
@@ -383,25 +387,30 @@ __device__ inline void choose_one(const LayerArgs& a, int t, const float* bias, 
     weight = c.scale * s;
   }
 }
-// The choices of tokens first, first + step, ..., of a warp, to arrays of all tokens' choices; mask: where the tokens of each expert
-// are marked, too.
-template <typename Id> __device__ __forceinline__ void choose_some(const LayerArgs& a, int first, int step, Making& m, int lane, int wid, Id* ids, float* weights, bool mark) {
-  const int K = a.c.top_k;
-  for (int t = first; t < a.T; t += step) {
+// The choices of tokens first, first + step, ..., of a warp: to the workspace where the blocks share them out, or to the plan, with the
+// tokens of each expert marked.  dry: as if for a token, without a result.
+__device__ __forceinline__ void choose_some(const LayerArgs& a, int first, int step, Plan& plan, Making& m, int lane, int wid, bool share, bool dry) {
+  const int K = a.c.top_k, end = dry ? 1 : a.T;
+#pragma unroll 1
+  for (int t = first; t < end; t += step) {
     int id;
     float w;
-    choose_one(a, t, m.bias, m.x[wid], m.key[wid], m.found[wid], m.place[wid], lane, id, w);
-    if (lane < K) {
-      ids[t * K + lane] = (Id)id;
-      weights[t * K + lane] = w;
-      if (mark && id >= 0) atomicOr(&m.mask[id][t >> 5], 1u << (t & 31));
+    choose_one(a, t, m.bias, m.x[wid], m.key[wid], m.found[wid], m.place[wid], lane, dry, id, w);
+    if (lane >= K || dry) continue;
+    if (share) {
+      a.made_ids[t * K + lane] = id;
+      a.made_weights[t * K + lane] = w;
+    } else {
+      plan.ids[t * K + lane] = (short)id;
+      plan.weights[t * K + lane] = w;
+      if (id >= 0) atomicOr(&m.mask[id][t >> 5], 1u << (t & 31));
     }
   }
 }
 // Rows by expert of 32 assignments at most, by a warp: lane i has assignment i; a row is the number of lanes before it by expert and place.
 // (Two assignments a lane took longer than the whole block's way: 64 of them 3.5 us instead of 2.4.)
-template <int BN> __device__ inline void make_small_plan(const LayerArgs& a, Plan& plan, int lane) {
-  const int n = a.T * a.c.top_k, e = lane < n ? plan.ids[lane] : -1;
+template <int BN> __device__ inline void make_small_plan(Plan& plan, int n, int lane) {
+  const int e = lane < n ? plan.ids[lane] : -1;
   int row = 0, rank = 0;
   for (int i = 0; i < n; ++i) {
     const int o = __shfl_sync(kAll, e, i);
@@ -427,9 +436,9 @@ template <int BN> __device__ inline void make_small_plan(const LayerArgs& a, Pla
   }
   if (lane == 0) { plan.total_rows = __popc(there); plan.chunks = __popc(begins); }
 }
-// Rows by expert from the choices in plan.ids and the marked tokens.  The whole block.
-template <int BN> __device__ inline void make_plan(const LayerArgs& a, Plan& plan, Making& m, int tid, int lane, int wid) {
-  const int E = a.c.experts, K = a.c.top_k, n = a.T * K;
+// Rows by expert from the choices in plan.ids and the marked tokens.  The whole block; dry: a warp, of no tokens.
+template <int BN> __device__ inline void make_plan(const LayerArgs& a, Plan& plan, Making& m, int tid, int lane, int wid, bool dry) {
+  const int E = a.c.experts, K = a.c.top_k, n = dry ? 0 : a.T * K;
   // rows and chunks before each expert
   constexpr int kPer = (ASGD_MAX_EXPERTS + kThreads - 1) / kThreads;
   int mine = 0, mine_chunks = 0, count[kPer];
@@ -439,7 +448,7 @@ template <int BN> __device__ inline void make_plan(const LayerArgs& a, Plan& pla
     count[q] = 0;
     if (e < E)
 #pragma unroll
-      for (int w = 0; w < kTokenWords; ++w) count[q] += __popc(m.mask[e][w]);
+      for (int w = 0; w < kTokenWords; ++w) count[q] += dry ? 0 : __popc(m.mask[e][w]);
     mine += count[q];
     mine_chunks += (count[q] + BN - 1) / BN;
   }
@@ -450,7 +459,7 @@ template <int BN> __device__ inline void make_plan(const LayerArgs& a, Plan& pla
     if (lane >= o) { inc += v; inc_chunks += w; }
   }
   if (lane == 31) { plan.part[0][wid] = inc; plan.part[1][wid] = inc_chunks; }
-  __syncthreads();
+  if (!dry) __syncthreads();
   int run = inc - mine, chunk = inc_chunks - mine_chunks;
   for (int w = 0; w < wid; ++w) { run += plan.part[0][w]; chunk += plan.part[1][w]; }
 #pragma unroll
@@ -465,7 +474,7 @@ template <int BN> __device__ inline void make_plan(const LayerArgs& a, Plan& pla
     run += count[q];
   }
   if (tid == kThreads - 1) { plan.total_rows = run; plan.chunks = chunk; }
-  __syncthreads();
+  if (!dry) __syncthreads();
   for (int i = tid; i < n; i += kThreads) {
     const int e = plan.ids[i], t = i / K;
     int r = -1;
@@ -633,70 +642,79 @@ expert_layer_kernel(const __grid_constant__ LayerArgs a, const __grid_constant__
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(misc)), "r"(L::kCols) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
-  wait_for_stream();                                 // what comes before reads nothing of the call's but its arguments
-  // What is read soon comes now: from cold memory a first read takes 2 to 3 us.
   Making& making = *reinterpret_cast<Making*>(ring);
   const bool share = a.T > kChoices;
-  if (a.bias)
-    for (int e = tid; e < a.c.experts; e += kThreads) copy4(making.bias + e, a.bias + e, true);
-  if (a.logits) {
-    const int t = share ? (int)blockIdx.x + wid * (int)gridDim.x : wid, size = a.logits_type == ASGD_F32 ? 4 : 2;
-    const char* row = reinterpret_cast<const char*>(a.logits) + t * a.ld_logits * size;
-    if (t < a.T)
-      for (int at = lane * 128; at < a.c.experts * size; at += 32 * 128) asm volatile("prefetch.global.L2 [%0];" ::"l"(row + at));
-  }
-  for (int i = tid; i < a.c.experts * kTokenWords; i += kThreads) (&making.mask[0][0])[i] = 0;
-  // step 0
-  for (int u = (int)blockIdx.x * kWarps + wid; u < a.T * a.w[0].kblocks; u += (int)gridDim.x * kWarps) {
-    const int t = u / a.w[0].kblocks, b = u % a.w[0].kblocks;
-    round_block(four(a.x, a.type, t * a.ldx, b * 128 + lane * 4, a.d, a.x_wide), a.xq + (long long)u * 128, a.xs + b * a.T + t, lane);
-  }
-  if (a.router) {
-    auto part = reinterpret_cast<float (*)[kLogitWarps][kLogitTokens]>(making.x);
-    if (a.T == 1) make_logits<1>(a, part, lane, wid);
-    else make_logits<kLogitTokens>(a, part, lane, wid);
-  }
-  asm volatile("cp.async.wait_all;" ::: "memory");
-  __syncthreads();
-  if (share && !a.router) {
-    choose_some(a, (int)blockIdx.x + wid * (int)gridDim.x, (int)gridDim.x * kWarps, making, lane, wid, a.made_ids, a.made_weights, false);
-    __syncthreads();
-  }
-  if (tid == 0) {
-    come(&a.shared->meeting[MEET_TOKENS].count);
-    if (a.router || share) meet(a.shared, MEET_TOKENS, a.wait_limit, abort);
-  }
-  if (a.router || share) __syncthreads();
-  if (share && a.router) {
-    choose_some(a, (int)blockIdx.x + wid * (int)gridDim.x, (int)gridDim.x * kWarps, making, lane, wid, a.made_ids, a.made_weights, false);
-    __syncthreads();
-    if (tid == 0) {
-      come(&a.shared->meeting[MEET_CHOICE].count);
-      meet(a.shared, MEET_CHOICE, a.wait_limit, abort);
-    }
-    __syncthreads();
-  }
   const int assignments = a.T * a.c.top_k;
-  if (!share) choose_some(a, wid, kWarps, making, lane, wid, plan.ids, plan.weights, true);
-  else
-    for (int i = tid; i < assignments; i += kThreads) {
-      // (what a block that gave up did not write could be anything)
-      const int id = __ldcg(a.made_ids + i), t = i / a.c.top_k;
-      const bool ok = id >= 0 && id < a.c.experts;
-      plan.ids[i] = (short)(ok ? id : -1);
-      plan.weights[i] = __ldcg(a.made_weights + i);
-      if (ok) atomicOr(&making.mask[id][t >> 5], 1u << (t & 31));
+  // The last warp goes ahead: it walks through the choice and the plan once for nothing, while the others wait for the stream and do step 0, so
+  // that their instructions are there when the others come (a line of them that no cache of the SM has costs some 500 cycles; without it
+  // the two took 7 us for one token of 128 experts).  It takes part in nothing else until the choices are made.
+#pragma unroll 1
+  for (int dry = wid == kDry; dry >= 0; --dry) {
+    const bool ahead = wid == kDry;                  // (its second time round it only meets the others)
+    if (!ahead) {
+      wait_for_stream();                             // what comes before reads nothing of the call's but its arguments
+      // What is read soon comes now: from cold memory a first read takes 2 to 3 us.
+      if (a.bias)
+        for (int e = tid; e < a.c.experts; e += kDry * 32) copy4(making.bias + e, a.bias + e, true);
+      if (a.logits) {
+        const int t = share ? (int)blockIdx.x + wid * (int)gridDim.x : wid, size = a.logits_type == ASGD_F32 ? 4 : 2;
+        const char* row = reinterpret_cast<const char*>(a.logits) + t * a.ld_logits * size;
+        if (t < a.T)
+          for (int at = lane * 128; at < a.c.experts * size; at += 32 * 128) asm volatile("prefetch.global.L2 [%0];" ::"l"(row + at));
+      }
+      for (int i = tid; i < a.c.experts * kTokenWords; i += kDry * 32) (&making.mask[0][0])[i] = 0;
+      // step 0
+      for (int u = (int)blockIdx.x * kDry + wid; u < a.T * a.w[0].kblocks; u += (int)gridDim.x * kDry) {
+        const int t = u / a.w[0].kblocks, b = u % a.w[0].kblocks;
+        round_block(four(a.x, a.type, t * a.ldx, b * 128 + lane * 4, a.d, a.x_wide), a.xq + (long long)u * 128, a.xs + b * a.T + t, lane);
+      }
+      if (a.router) {
+        auto part = reinterpret_cast<float (*)[kLogitWarps][kLogitTokens]>(making.x);
+        if (a.T == 1) make_logits<1>(a, part, lane, wid);
+        else make_logits<kLogitTokens>(a, part, lane, wid);
+      }
+      asm volatile("cp.async.wait_all;" ::: "memory");
+      others_sync();
+      if (a.router) {
+        if (tid == 0) {
+          come(&a.shared->meeting[MEET_TOKENS].count);
+          meet(a.shared, MEET_TOKENS, a.wait_limit, abort);
+        }
+        others_sync();
+      } else if (!share && tid == 0) {
+        come(&a.shared->meeting[MEET_TOKENS].count);
+      }
+    } else if (!dry) {
+      wait_for_stream();
     }
-  __syncthreads();
-  if (blockIdx.x == 0)
-    for (int i = tid; i < assignments; i += kThreads) {
-      if (a.ids) a.ids[i] = plan.ids[i];
-      if (a.weights) a.weights[i] = plan.weights[i];
+    if (!ahead || dry) choose_some(a, dry ? 0 : share ? (int)blockIdx.x + wid * (int)gridDim.x : wid, share ? (int)gridDim.x * kDry : kDry, plan, making, lane, wid, share, dry);
+    if (!dry) {
+      __syncthreads();
+      if (share) {
+        const int which = a.router ? MEET_CHOICE : MEET_TOKENS;
+        if (tid == 0) {
+          come(&a.shared->meeting[which].count);
+          meet(a.shared, which, a.wait_limit, abort);
+        }
+        __syncthreads();
+        for (int i = tid; i < assignments; i += kThreads) {
+          // (what a block that gave up did not write could be anything)
+          const int id = __ldcg(a.made_ids + i), t = i / a.c.top_k;
+          const bool ok = id >= 0 && id < a.c.experts;
+          plan.ids[i] = (short)(ok ? id : -1);
+          plan.weights[i] = __ldcg(a.made_weights + i);
+          if (ok) atomicOr(&making.mask[id][t >> 5], 1u << (t & 31));
+        }
+        __syncthreads();
+      }
+      if (blockIdx.x == 0)
+        for (int i = tid; i < assignments; i += kThreads) {
+          if (a.ids) a.ids[i] = plan.ids[i];
+          if (a.weights) a.weights[i] = plan.weights[i];
+        }
     }
-  if (assignments <= 32) {
-    if (wid == 0) make_small_plan<BN>(a, plan, lane);
-  } else {
-    make_plan<BN>(a, plan, making, tid, lane, wid);
+    if (assignments > 32) make_plan<BN>(a, plan, making, tid, lane, wid, dry);
+    else if (wid == (dry ? kDry : 0)) make_small_plan<BN>(plan, dry ? 0 : assignments, lane);
   }
   __syncthreads();
   if (tid < 2) plan.per[tid] = ((unsigned)plan.chunks * a.w[tid].tiles * a.w[tid].kblocks + gridDim.x - 1) / gridDim.x;
