@@ -289,6 +289,29 @@ def test_layer_in_a_graph_and_on_several_streams():
     pkg.asgd_experts_sync()
 
 
+def test_graphs_replayed_at_once_on_several_streams_beside_products():
+    """Layers of several streams, each of which wants all SMs, and products that hold some of them."""
+    cases = [_case(8, 32, 4, 512, 256, True, "silu", BF, "softmax", 1, F32, (E4, E4)), _case(40, 16, 4, 384, 200, False, "relu2", F16, "sigmoid", 1, None, (E4, E4))]
+    a = torch.randn(700, 1024, generator=_gen(5), device="cuda", dtype=BF)
+    w = pkg.asgd_quantize4(torch.randn(2048, 1024, generator=_gen(6), device="cuda", dtype=BF))
+    calls = [lambda args=args, kw=kw: pkg.asgd_expert_layer(*args, **kw) for args, kw in cases] + [lambda: pkg.asgd_product4(*pkg.asgd_quantize4(a), *w)]
+    want = [call() for call in calls]
+    graphs, got = [], []
+    for call in calls:
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            got.append([call() for _ in range(8)])
+    streams = [torch.cuda.Stream() for _ in calls]
+    torch.cuda.synchronize()
+    for _ in range(10):
+        for graph, stream in zip(graphs, streams):
+            with torch.cuda.stream(stream):
+                graph.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(g, v) for v, gs in zip(want, got) for g in gs)
+    pkg.asgd_experts_sync()
+
+
 @pytest.mark.parametrize("T, router", [(1, None), (30, F32)])
 @pytest.mark.parametrize("limit, withhold", [(2000, True), (1, False), (40, False)])
 def test_waits_given_up_leave_the_device_usable(T, router, limit, withhold):
