@@ -183,13 +183,13 @@ int asgd_combine_grad(int64_t T, int64_t D, int32_t top_k, const void *dy, int32
                       int64_t R, int64_t ldz, const int32_t *rows, const float *weights, const int32_t *source, void *dz,
                       int64_t ld_dz, float *dweights, void *stream);
 
-/* Wait for the stream and return what asgd_product calls on this device have reported since the last asgd_experts_sync:
- * ASGD_OK, ASGD_EINVAL (offsets, see above) or ASGD_ETIMEOUT (a bounded wait on the kernel's own copies or products ran
+/* Wait for the stream and return what asgd_product calls on this device (and those of asgd_product4, asgd_fp4.h, and
+ * asgd_expert_layer, asgd_expert_layer.h) have reported since the last asgd_experts_sync: ASGD_OK, ASGD_EINVAL (offsets, see above) or ASGD_ETIMEOUT (a bounded wait on the kernel's own copies or products ran
  * out; the outputs of that call are not to be used); of several the last named.  This is the one state between calls:
  * there is one report per device, shared by all of its streams, and the call that takes it clears it (no report that comes
  * meanwhile is lost).  With several streams in use, wait for all of them, then call this once for all. */
 int asgd_experts_sync(void *stream);
-/* Failure drill of asgd_product's bounded waits, as asgd_set_wait_drill: later launches of this process give a wait up
+/* Failure drill of these functions' bounded waits, as asgd_set_wait_drill: later launches of this process give a wait up
  * after wait_limit polls (copies and products in flight end all the same before a kernel leaves), and with withhold = 1 the first copy of every block is announced but never issued.
  * Defaults 2^22 and 0.  ASGD_EINVAL for wait_limit = 0. */
 int asgd_product_set_wait_drill(uint32_t wait_limit, int32_t withhold);

@@ -4,7 +4,9 @@
 // (rows of A, the tokens: the MMA's N), and with fewer tiles than SMs a cluster of blocks shares a tile's K units and adds up
 // through distributed shared memory, in the blocks' order.  What differs: the tensor cores apply the powers of two themselves
 // (kind::mxf4, block scales), so that the sums of a whole row stay in tensor memory until the tile is through, and nothing is
-// read out on the way.  The weights' bytes are the bound.
+// read out on the way.  The weights' bytes are the bound.  256 rows over 64 matrices of 2048 x 2048: 26 us (4.3 TB/s; the last turn of tiles is a
+// third of them), 5 rows by 4096 x 4096: 6.2 us, the chain of launch, maps, first copies and the cluster's sum.  Every instruction of the tensor pipe
+// is issued by an elected thread: behind `lane == 0` the compiler walks the warp's lanes one by one, some 80 cycles each (8.7 and 36 us).
 //
 // A unit is 512 numbers of K: two 128-byte swizzled pieces of either operand, and 16 bytes of scales a row, which is what a
 // tensor map can copy.  The tensor cores want scales in tensor memory, where one 32-bit column of a lane holds four scales of one row,

@@ -3,9 +3,13 @@
 //
 // tcgen05.mma of a pair (cta_group::2, kind::mxf4) multiplies 256 rows of A by NT rows of B; each SM holds half of either
 // operand and the scales of its rows of A and of all of the tile's rows of B.  The sums of a tile stay in tensor memory until
-// its last K block; with NT = 224 two tiles' sums (448 columns) and two K blocks' scales (24 columns each) fit its 512
-// columns, so that a tile's way out runs beside the next one's products.  Scales come and are turned as in
-// asgd_product4_few.cuh, 512 numbers of K at a time.
+// its last K block.  Scales come and are turned as in asgd_product4_few.cuh, 512 numbers of K at a time, through slots of their own.
+//
+// What bounds it: a K block of 256 numbers is 35 KB per SM out of L2 for 2 x 256 x 128 x 256 operations, and L2 gives some 9 TB/s in all: 8192^3 takes
+// 250 us (4.4 PFLOP/s), without its copies 162, without its stores 217.  So a tile is as wide as it can be: NT = 256 leaves no room for a second tile's
+// sums, and the readers take a tile's sums into registers at once so that the next tile's products begin; NT = 224 with two tiles' sums, whose
+// way out is hidden whole, takes 278 (16384 rows over 32 of 2744 x 2080: 94 us, this way 87).  Five slots of operands and one piece of a warp's stage (four
+// slots and two pieces: 251 and 89); other orders of the tiles (bands of 4 to 16 rows of them) are within 2 %.
 //
 // Warp roles in each block: 0 issues the copies (the halves of the operands report to the first block's barrier, the scales to
 // the block's own); 1, in the first block, issues the products and the scales' copies into both SMs' tensor memory; 2 and 3 turn the
