@@ -91,8 +91,8 @@ template <int NT> int launch_pair(const asgd_product4_args& a, Params4 p, cudaSt
 }
 
 // Which kernel: the one whose blocks are through first, by the units and the tiles that the busiest of them meets.  The microseconds of
-// each are a fit to a sweep of 70 shapes in which each kernel was forced (dense and grouped, 5 to 16384 rows); there the rule's kernel is the
-// best one or within 5 % of it but for one shape, 11 % off.
+// each are a fit to a sweep of 64 shapes in which each kernel was forced (dense and grouped, 5 to 16384 rows); there the rule's kernel is the
+// best one or within 5 % of it but for two, 6 and 11 % off.
 enum Kernel { FEW16, FEW32, FEW64, FEW128, PAIR };
 Kernel choose(const Params& p) {
   static const int rows_of[5] = {16, 32, 64, 128, kPairRows};
