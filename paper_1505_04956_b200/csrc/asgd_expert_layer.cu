@@ -562,18 +562,20 @@ template <int BN, int N> __device__ __forceinline__ void add_up(const float* con
       if (b < blocks[i]) { sum[i].x += v[i].x; sum[i].y += v[i].y; sum[i].z += v[i].z; sum[i].w += v[i].w; }
   }
 }
-// Where the four numbers of a row's u from number j on are, and those that gate them (h is a multiple of four).
+// Where a lane's four numbers of u are, for four results at once: the blocks of 128 of units u, u + step, ..., or (gated) two units' and what gates
+// them (h is a multiple of four).
 template <int BN> struct HiddenAt {
-  const float* at[2] = {nullptr, nullptr};
-  int blocks[2] = {0, 0};
+  const float* at[4] = {};
+  int blocks[4] = {};
   __device__ __forceinline__ HiddenAt() {}
-  __device__ __forceinline__ HiddenAt(const LayerArgs& a, const Plan& plan, int row, int j) {
+  __device__ __forceinline__ HiddenAt(const LayerArgs& a, const Plan& plan, int u, int step, int units, int hb, int lane) {
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      if (j >= a.h || (i && !a.gated)) continue;
-      const Parts<BN> p(a, plan, 0, row, (i * a.h + j) / 128);
-      at[i] = p.at + (i * a.h + j) % 128;
-      blocks[i] = p.blocks;
+    for (int r = 0; r < 4; ++r) {
+      const int unit = u + (a.gated ? r >> 1 : r) * step, j = unit % hb * 128 + lane * 4, first = a.gated && (r & 1) ? a.h : 0;
+      if (unit >= units || j >= a.h) continue;
+      const Parts<BN> p(a, plan, 0, unit / hb, (first + j) / 128);
+      at[r] = p.at + (first + j) % 128;
+      blocks[r] = p.blocks;
     }
   }
 };
@@ -878,7 +880,7 @@ expert_layer_kernel(const __grid_constant__ LayerArgs a, const __grid_constant__
       const int hb = a.w[1].kblocks;
       HiddenAt<BN> hidden;
       ChoiceAt<BN> choice;
-      if (f == 0 && reader < rows * hb && a.h % 4 == 0) hidden = HiddenAt<BN>(a, plan, reader / hb, reader % hb * 128 + lane * 4);
+      if (f == 0 && reader < rows * hb && a.h % 4 == 0) hidden = HiddenAt<BN>(a, plan, reader, readers, rows * hb, hb, lane);
       if (f == 1 && reader < a.T * w.tiles) choice = ChoiceAt<BN>(a, plan, reader / w.tiles, reader % w.tiles, lane);
       readers_sync();
       // (one thread decides for all readers: where a warp gave up, the block does not come, and the meeting fails)
@@ -898,17 +900,19 @@ expert_layer_kernel(const __grid_constant__ LayerArgs a, const __grid_constant__
         };
         const int units = rows * hb;
         if (a.h % 4 == 0) {
-          for (int u = reader; u < units; u += 2 * readers) {               // two at a time: their loads are in flight together
-            const int u2 = u + readers;
-            if (u != reader) hidden = HiddenAt<BN>(a, plan, u / hb, u % hb * 128 + lane * 4);
-            HiddenAt<BN> other;
-            if (u2 < units) other = HiddenAt<BN>(a, plan, u2 / hb, u2 % hb * 128 + lane * 4);
-            const float* const at[4] = {hidden.at[0], hidden.at[1], other.at[0], other.at[1]};
-            const int blocks[4] = {hidden.blocks[0], hidden.blocks[1], other.blocks[0], other.blocks[1]};
+          const int many = a.gated ? 2 : 4;
+#pragma unroll 1
+          for (int u = reader; u < units; u += many * readers) {            // several at a time: their loads are in flight together
+            if (u != reader) hidden = HiddenAt<BN>(a, plan, u, readers, units, hb, lane);
             float4 v[4];
-            add_up<BN>(at, blocks, v);
-            finish(u, v[0], v[1]);
-            if (u2 < units) finish(u2, v[2], v[3]);
+            add_up<BN>(hidden.at, hidden.blocks, v);
+            if (a.gated) {
+              finish(u, v[0], v[1]);
+              if (u + readers < units) finish(u + readers, v[2], v[3]);
+            } else {
+#pragma unroll
+              for (int r = 0; r < 4; ++r) if (u + r * readers < units) finish(u + r * readers, v[r], v[r]);
+            }
           }
         } else {
 #pragma unroll 1
