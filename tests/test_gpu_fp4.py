@@ -135,6 +135,21 @@ def test_quantize4_strides_and_rows_that_start_anywhere(dtype):
         pkg.asgd_quantize4(big.t())
 
 
+@pytest.mark.parametrize("K", [2, 6, 30, 130, 514, 1030, 4094])
+def test_rows_of_32_bits_that_start_at_8_bytes(K):
+    x = _numbers(37, K, F32, K)
+    assert x.stride(0) % 4 == 2
+    q, s = pkg.asgd_quantize4(x)
+    wide_q, wide_s = pkg.asgd_quantize4(torch.nn.functional.pad(x, (0, 2)))
+    assert torch.equal(q.view(torch.uint8), wide_q.view(torch.uint8)[:, :K // 2]) and torch.equal(s.view(torch.uint8), wide_s.view(torch.uint8)[:, :s.shape[1]])
+    back = pkg.asgd_dequantize4(q, s, K, dtype=F32)
+    assert torch.equal(back, pkg.asgd_dequantize4(wide_q, wide_s, K + 2, dtype=F32)[:, :K])
+    shifted = torch.zeros(37 * K + 2, device="cuda")
+    shifted[2:] = x.flatten()
+    got = pkg.asgd_quantize4(shifted[2:].view(37, K))
+    assert torch.equal(got[0].view(torch.uint8), q.view(torch.uint8)) and torch.equal(got[1].view(torch.uint8), s.view(torch.uint8))
+
+
 @pytest.mark.parametrize("dtype", [F32, BF, F16])
 def test_quantize4_infinity_nan_and_extremes(dtype):
     x = torch.ones(6, 96, device="cuda", dtype=dtype)
