@@ -18,11 +18,11 @@
 // A tile is 128 rows of W (the MMA's M) by BN tokens of one expert (its N; an expert with more has several chunks); a
 // K block's products leave tensor memory and are added, scaled, in registers, as in asgd_product_few.cuh.
 //
-// What bounds it: one token of 128 experts (d 2048, h 768 gated, top 8) takes 28.7 us, of which its 39 MB need 6; the rest is a chain of
+// What bounds it: one token of 128 experts (d 2048, h 768 gated, top 8) takes 28.4 us, of which its 39 MB need 6; the rest is a chain of
 // steps that wait for one another (choice and plan 6, the meetings 5, activation 2, first bytes and last sums of either product 5, the launch 3).
 // Eight tokens of 256 experts take 44 us (181 MB, 28 of them), 60 tokens 55 (186 MB): the weights come at 5 to 7 TB/s once they are on their
 // way.  On the way there, 8 tokens: one warp that brings the tokens' rows 48, four 44.5; scales asked for before W1's copies are on their way
-// 53; a grid of partial tiles' sums added part by part, 6 us for a token's eight choices, all choices together 2.
+// 53; the sums of a token's eight choices one after another 6 of them, together 2.
 //
 // Warp roles after step 0: 0 issues the copies of weights; 1 and 3 issue the products, K blocks in turn; 2 and 12 to 14 bring the
 // tokens' rows (gathered, 16-byte asynchronous copies into the swizzled layout that a tensor map would write) and the scales, K blocks in
@@ -401,7 +401,7 @@ __device__ __forceinline__ void choose_some(const LayerArgs& a, int first, int s
   for (int t = first; t < end; t += step) {
     int id;
     float w;
-    choose_one(a, t, m.bias, m.x[wid], m.key[wid], m.found[wid], m.place[wid], lane, dry, id, w);
+    choose_one(a, t, dry ? m.x[wid] : m.bias, m.x[wid], m.key[wid], m.found[wid], m.place[wid], lane, dry, id, w);
     if (lane >= K || dry) continue;
     if (share) {
       a.made_ids[t * K + lane] = id;

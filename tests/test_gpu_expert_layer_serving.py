@@ -124,6 +124,12 @@ SHAPES = [
     (33, 4, 3, 2304, 65, True, "relu2", BF, "softmax", 1, F32, (E4, E4)),
     (17, 64, 32, 300, 300, True, "silu", F32, "sigmoid", 1, None, (E4, E4)),
     (2, 3, 2, 4000, 2000, True, "silu", F32, "softmax", 1, F32, (E4, E4)),
+    # where the blocks begin to share the choices out, and around 32 assignments
+    (30, 12, 3, 384, 256, True, "silu", BF, "sigmoid", 3, F32, (E4, E4)),
+    (31, 12, 3, 384, 256, False, "relu2", BF, "softmax", 1, None, (E4, E4)),
+    (31, 40, 1, 256, 130, True, "silu", F32, "softmax", 1, F32, (E4, E4)),
+    (32, 40, 1, 256, 130, False, "relu2", F32, "sigmoid", 1, None, (E4, E4)),
+    (33, 40, 1, 256, 130, True, "relu2", F16, "softmax", 1, F16, (E4, E4)),
 ]
 
 
