@@ -26,7 +26,7 @@ enum { ASGD_ACT_RELU2 = 0 /* max(u, 0)^2 */, ASGD_ACT_SILU = 1 /* u / (1 + exp(-
 /*
  * For each token t with row x of X:
  *   logits   as given, or ((x . router[e]) - shift[e]) * temperature, fp32 (shift: 0 where there is none)
- *   e_j, w_j the choice and the weights of asgd_route
+ *   e_j, w_j the choice and the weights that asgd_route gives for these logits, bit by bit
  *   xq       x rounded to E4M3 in blocks of 128 (asgd_quantize)
  *   u        = W1[e_j] xq                          h or, gated, 2 h numbers
  *   a        = act(u), or act(u[i]) * u[h + i]     h numbers

@@ -12,6 +12,7 @@ struct Choice {
   asgd_route_config c;
   int group_lanes;                           // log2 of the lanes a group's keys are shared by
   unsigned group_magic;                      // e / (experts of a group) = umulhi(e, group_magic); 0: groups of one
+  int lanes;                                 // of a token: the softmax's sum is one of this many lanes' sums, whoever computes it
   const float* bias;
 };
 
@@ -289,6 +290,11 @@ inline bool config_ok(const asgd_route_config* c) {
 inline bool config_supported(const asgd_route_config* c) {
   return c->experts <= ASGD_MAX_EXPERTS && c->groups <= ASGD_MAX_EXPERT_GROUPS && c->top_k <= ASGD_MAX_TOP_K;
 }
+// Lanes of a token: 8 where they have room for the choices and the groups and hold eight numbers at most (see with_shape in asgd_route.cu).
+inline int lanes_of(const asgd_route_config& c) {
+  const int kept = c.groups_kept < c.groups ? c.groups : 1;
+  return c.experts <= 64 && c.top_k <= 8 && kept <= 8 ? 8 : 32;
+}
 inline Choice choice_of(const asgd_route_config& c, const float* bias) {
   Choice a;
   a.c = c;
@@ -296,6 +302,7 @@ inline Choice choice_of(const asgd_route_config& c, const float* bias) {
   while ((c.groups << (a.group_lanes + 1)) <= 32) ++a.group_lanes;
   const unsigned per = (unsigned)(c.experts / c.groups);
   a.group_magic = per > 1 ? (unsigned)((1ull << 32) / per + 1) : 0;    // exact for numbers below 2^16
+  a.lanes = lanes_of(c);
   a.bias = bias;
   return a;
 }

@@ -261,14 +261,16 @@ template <int kTok> __device__ inline void make_logits(const LayerArgs& a, float
 
 // ---- the choice and the plan, by the whole block ----
 
-// A warp chooses for one token, as asgd_route does, from logits and keys in shared memory: lane l has the experts l, l + 32, ...  A kernel
+// A warp chooses for one token from logits and keys in shared memory: lane l has the experts l, l + 32, ...  A kernel
 // that runs once for a few tokens meets its instructions cold, so this code is short: loops over what a lane has, where asgd_route's is unrolled
-// over registers (which took 10 us for a first token among 256 experts in groups, and 2 for every further one).
+// over registers (which took 10 us for a first token among 256 experts in groups, and 2 for every further one).  Choices and weights are asgd_route's to
+// the last bit: every sum runs in its order (choose() in asgd_choose.cuh), the softmax's over the same number of lanes, the renormalising one over choices
+// in the same places.  A lane returns a place among the top_k (-1: it has none), the expert there (-1: none) and its weight.
 template <typename T> __device__ __forceinline__ void read_logits(const T* row, int E, int lane, float* x) {
 #pragma unroll 4
   for (int e = lane; e < E; e += 32) x[e] = Elem<T>::to_f(__ldcg(row + e));
 }
-__device__ inline void choose_one(const LayerArgs& a, int t, const float* bias, float* x, unsigned* key, uint2* found, int* place, int lane, bool dry, int& id, float& weight) {
+__device__ inline void choose_one(const LayerArgs& a, int t, const float* bias, float* x, unsigned* key, uint2* found, int* place, int lane, bool dry, int& at, int& id, float& weight) {
   const asgd_route_config& c = a.c;
   const int E = c.experts, K = c.top_k;
   const bool by_logit = a.bias == nullptr && c.group_top == 1, sigmoid_scores = c.score == ASGD_SCORE_SIGMOID;
@@ -284,9 +286,10 @@ __device__ inline void choose_one(const LayerArgs& a, int t, const float* bias, 
     float m = -INFINITY, sum = 0.f;
     for (int e = lane; e < E; e += 32) m = e == lane ? x[e] : fmaxf(m, x[e]);
     f.m = lanes_max<32>(m);
+    __syncwarp();
 #pragma unroll 4
-    for (int e = lane; e < E; e += 32) sum += f.part(x[e]);
-    f.sum = lanes_sum<32>(sum);
+    for (int e = lane < a.lanes ? lane : E; e < E; e += a.lanes) sum += f.part(x[e]);
+    f.sum = lanes_sum<32>(sum);                      // (lanes from a.lanes on add zeros)
   }
   unsigned best = 0;                                 // the lane's largest key, and whose it is
   int whose = -1;
@@ -339,6 +342,7 @@ __device__ inline void choose_one(const LayerArgs& a, int t, const float* bias, 
   }
   // What reaches the top_k-th largest of the lanes' largest keys (top_k keys at least) is gathered and ranked by counting.
   id = -1;
+  at = lane < K ? lane : -1;
   unsigned top = best, bound = 1u;
   for (int i = 0; i < K; ++i) {
     const unsigned b = __reduce_max_sync(kAll, top);
@@ -351,8 +355,8 @@ __device__ inline void choose_one(const LayerArgs& a, int t, const float* bias, 
     const unsigned k = e0 + lane < E ? key[e0 + lane] : 0u;
     const bool there = k >= bound;
     const unsigned votes = __ballot_sync(kAll, there);
-    const int at = n + __popc(votes & ((1u << lane) - 1u));
-    if (there && at < 32) found[at] = make_uint2(k, (unsigned)(e0 + lane));
+    const int to = n + __popc(votes & ((1u << lane) - 1u));
+    if (there && to < 32) found[to] = make_uint2(k, (unsigned)(e0 + lane));
     n += __popc(votes);
   }
   if (n <= 32) {
@@ -364,9 +368,14 @@ __device__ inline void choose_one(const LayerArgs& a, int t, const float* bias, 
       const unsigned k = __shfl_sync(kAll, mine.x, i);
       rank += i < lane ? k >= mine.x : k > mine.x;
     }
-    if (lane < n && rank < K) place[rank] = (int)mine.y;
-    __syncwarp();
-    if (lane < min(n, K)) id = place[lane];
+    if (a.lanes == 32 && E <= 256) {                 // asgd_route leaves choices where they were found
+      if (lane < n) at = rank < K ? rank : -1;
+      if (lane < n && rank < K) id = (int)mine.y;
+    } else {
+      if (lane < n && rank < K) place[rank] = (int)mine.y;
+      __syncwarp();
+      if (lane < min(n, K)) id = place[lane];
+    }
   } else {                                           // one by one
     for (int i = 0; i < K; ++i) {
       const unsigned most = __reduce_max_sync(kAll, best);
@@ -399,16 +408,16 @@ __device__ __forceinline__ void choose_some(const LayerArgs& a, int first, int s
   const int K = a.c.top_k, end = dry ? 1 : a.T;
 #pragma unroll 1
   for (int t = first; t < end; t += step) {
-    int id;
+    int at, id;
     float w;
-    choose_one(a, t, dry ? m.x[wid] : m.bias, m.x[wid], m.key[wid], m.found[wid], m.place[wid], lane, dry, id, w);
-    if (lane >= K || dry) continue;
+    choose_one(a, t, dry ? m.x[wid] : m.bias, m.x[wid], m.key[wid], m.found[wid], m.place[wid], lane, dry, at, id, w);
+    if (at < 0 || dry) continue;
     if (share) {
-      a.made_ids[t * K + lane] = id;
-      a.made_weights[t * K + lane] = w;
+      a.made_ids[t * K + at] = id;
+      a.made_weights[t * K + at] = w;
     } else {
-      plan.ids[t * K + lane] = (short)id;
-      plan.weights[t * K + lane] = w;
+      plan.ids[t * K + at] = (short)id;
+      plan.weights[t * K + at] = w;
       if (id >= 0) atomicOr(&m.mask[id][t >> 5], 1u << (t & 31));
     }
   }

@@ -257,8 +257,8 @@ template <int S, int L, typename T> __global__ void __launch_bounds__(kThreads) 
 // lanes hold (gradient of 32768 x 64 logits: 13 us with 32 lanes a token, 9.6 with 8).
 template <int N> using Int = std::integral_constant<int, N>;
 template <typename F> void with_shape(const asgd_route_config& c, F&& f) {
-  const int E = c.experts, need = std::max(c.top_k, c.groups_kept < c.groups ? c.groups : 1);
-  if (E <= 64 && need <= 8) {
+  const int E = c.experts;
+  if (lanes_of(c) == 8) {
     if (E <= 16) f(Int<2>(), Int<8>());
     else if (E <= 32) f(Int<4>(), Int<8>());
     else f(Int<8>(), Int<8>());

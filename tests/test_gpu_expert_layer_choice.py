@@ -1,0 +1,94 @@
+"""The choice of experts in the whole layer's kernel is that of asgd_route, to the last bit.
+
+Both compute a score by the same operations in the same order (the softmax's sum over the lanes that asgd_route gives a token, the renormalising sum
+over the lanes that hold its choices), so ids and weights are equal bit by bit, whatever hangs on the last one.  The logits here differ by some
+steps of 2^-25 around a few levels: exponentials, their quotients and the sums with a bias then coincide or not by their last bits.
+"""
+import math
+
+import pytest
+import torch
+
+import paper_1505_04956_b200 as pkg
+
+from .test_gpu_expert_layer_serving import BF, F16, F32, _check, _gen, _matrices
+
+pytestmark = pytest.mark.gpu
+
+
+def _small_layer(g, E, d=16, h=16):
+    """Experts that are all the same one."""
+    w1, s1 = _matrices(g, 1, h, d)
+    w2, s2 = _matrices(g, 1, d, h)
+    many = lambda t: t.expand(E, *t.shape[1:]).contiguous() if t.dtype == F32 else t.view(torch.uint8).expand(E, *t.shape[1:]).contiguous().view(t.dtype)      # noqa: E731
+    return many(w1), many(s1), many(w2), many(s2)
+
+
+def _near(g, T, E, levels):
+    """Logits around a few levels, 2^-25 and more apart."""
+    level = torch.randint(0, levels, (T, E), generator=g, device="cuda").float() * 0.125
+    return level + torch.randint(-6, 7, (T, E), generator=g, device="cuda").float() * 2.0 ** -25
+
+
+@pytest.mark.parametrize("E, top_k, groups, kept, group_top", [
+    (16, 2, 1, 1, 1), (33, 8, 1, 1, 1), (48, 6, 1, 1, 1), (64, 8, 1, 1, 1), (64, 9, 1, 1, 1), (64, 8, 8, 4, 2), (40, 4, 4, 2, 2), (48, 5, 16, 8, 2), (60, 7, 6, 6, 2),
+    (12, 3, 3, 2, 1), (100, 8, 1, 1, 1), (256, 8, 8, 4, 2), (256, 32, 1, 1, 1), (300, 8, 1, 1, 1), (512, 16, 32, 8, 2)])
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("bias, renormalise", [("zeros", True), ("some", False), ("none", True)])
+def test_choices_that_hang_on_the_last_bit(E, top_k, groups, kept, group_top, score, bias, renormalise):
+    g = _gen(E + top_k + groups)
+    args = _small_layer(g, E)
+    b = dict(none=None, zeros=torch.zeros(E, device="cuda"), some=torch.randint(0, 3, (E,), generator=g, device="cuda").float() * 2.0 ** -9)[bias]
+    for T, levels in ((31, 3), (30, 1), (8, 2), (1, 1)):
+        logits = _near(g, T, E, levels)
+        x = torch.randn(T, 16, generator=g, device="cuda")
+        kw = dict(score=score, bias=b, groups=groups, groups_kept=kept, group_top=group_top, renormalise=renormalise, scale=1.5)
+        want_ids, want_weights = pkg.asgd_route(logits, top_k, plan=False, **kw)
+        y, ids, weights = pkg.asgd_expert_layer(x, *args, top_k, logits=logits, choice=True, **kw)
+        pkg.asgd_experts_sync()
+        assert torch.equal(ids, want_ids)
+        assert torch.equal(weights, want_weights)
+
+
+@pytest.mark.parametrize("T, E, top_k, groups, kept", [(5, 300, 8, 1, 1), (7, 1000, 32, 1, 1), (16, 64, 4, 1, 1), (8, 96, 7, 6, 3), (40, 512, 16, 8, 8), (100, 33, 3, 11, 5), (2, 32, 32, 1, 1)])
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("kind", ["ties", "gone", "all equal"])
+def test_weights_where_experts_are_unavailable(T, E, top_k, groups, kept, score, kind):
+    g = _gen(T + E)
+    logits = torch.randn(T, E, generator=g, device="cuda")
+    if kind == "ties":
+        logits = torch.round(logits * 2) / 2
+    elif kind == "all equal":
+        logits = torch.zeros(T, E, device="cuda")
+    else:
+        logits[torch.rand(T, E, generator=g, device="cuda") < 0.97] = -math.inf
+        logits[T // 2] = -math.inf
+    args = _small_layer(g, E)
+    x = torch.randn(T, 16, generator=g, device="cuda")
+    kw = dict(score=score, groups=groups, groups_kept=kept, group_top=1, scale=1.5)
+    want_ids, want_weights = pkg.asgd_route(logits, top_k, plan=False, **kw)
+    y, ids, weights = pkg.asgd_expert_layer(x, *args, top_k, logits=logits, choice=True, **kw)
+    pkg.asgd_experts_sync()
+    assert torch.equal(ids, want_ids) and torch.equal(weights, want_weights)
+    assert bool((weights[ids < 0] == 0).all()) and bool((y[(ids < 0).all(1)] == 0).all())
+    _check(x, *args, (y, ids, weights), "relu2", min_tight=False)
+
+
+@pytest.mark.parametrize("T, E, top_k, groups, group_top, score, bias, renormalise, logits, act", [
+    (8, 32, 4, 1, 1, "softmax", True, True, F32, "silu"), (40, 64, 8, 8, 2, "softmax", True, True, BF, "relu2"), (20, 96, 6, 6, 2, "softmax", False, False, F16, "silu"),
+    (5, 128, 8, 1, 1, "softmax", True, False, BF, "relu2"), (33, 24, 3, 4, 2, "sigmoid", True, False, F32, "silu"), (3, 300, 8, 1, 1, "sigmoid", False, False, F16, "relu2"),
+    (64, 16, 2, 1, 1, "softmax", False, False, BF, "silu")])
+def test_forms_of_the_choice(T, E, top_k, groups, group_top, score, bias, renormalise, logits, act):
+    g = _gen(3 * T + E)
+    d, h = 272, 144
+    x = torch.randn(T, d, generator=g, device="cuda").to(BF)
+    w1, s1 = _matrices(g, E, 2 * h, d)
+    w2, s2 = _matrices(g, E, d, h)
+    lg = (torch.randn(T, E, generator=g, device="cuda") * 1.5).to(logits)
+    kw = dict(score=score, bias=torch.randn(E, generator=g, device="cuda") * 0.1 if bias else None, groups=groups, groups_kept=(groups + 1) // 2,
+              group_top=group_top, renormalise=renormalise, scale=2.0)
+    want_ids, want_weights = pkg.asgd_route(lg, top_k, plan=False, **kw)
+    got = pkg.asgd_expert_layer(x, w1, s1, w2, s2, top_k, logits=lg, activation=act, choice=True, **kw)
+    pkg.asgd_experts_sync()
+    assert torch.equal(got[1], want_ids) and torch.equal(got[2], want_weights)
+    _check(x, w1, s1, w2, s2, got, act)
