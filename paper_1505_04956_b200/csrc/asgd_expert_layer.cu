@@ -974,7 +974,7 @@ expert_layer_kernel(const __grid_constant__ LayerArgs a, const __grid_constant__
     if (wid == 0 && lane == 0) {
       const unsigned issued = (unsigned)misc[2];
       for (unsigned q = 0; q < S && q < issued; ++q) wait_in_flight(bars + L::FULL + q, ((issued - 1 - q) / S) & 1, a.wait_limit);      // a slot's last use
-    } else if ((wid == 1 || wid == 3) && lane == 0) {
+    } else if ((wid == 1 || wid == 3) && elect_one()) {                     // the lane that issued the products: a commit is of its own thread's
       commit(bars + L::DRAIN + (wid >> 1));
       wait_in_flight(bars + L::DRAIN + (wid >> 1), 0, a.wait_limit);
     }

@@ -282,7 +282,7 @@ product4_few_kernel(const Params4 p, const __grid_constant__ CUtensorMap map_u, 
     if (wid == 0 && lane == 0) {
       const unsigned issued = (unsigned)misc[2];
       for (unsigned q = 0; q < S && q < issued; ++q) wait_in_flight(bars + F::FULL + q, ((issued - 1 - q) / S) & 1, p.wait_limit);      // a slot's last use
-    } else if (wid == 1 && lane == 0) {
+    } else if (wid == 1 && elect_one()) {            // the lane that issued the products: a commit is of its own thread's
       commit(bars + F::DRAIN);
       wait_in_flight(bars + F::DRAIN, 0, p.wait_limit);
     }

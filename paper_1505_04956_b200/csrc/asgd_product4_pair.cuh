@@ -280,7 +280,7 @@ product4_pair_kernel(const Params4 p, const __grid_constant__ CUtensorMap map_a,
         wait_in_flight(bars + Q_FULL + i % S, (i / S) & 1, p.wait_limit);
       atomicMin(p.status, ASGD_ETIMEOUT);
     }
-  } else if (gave_up && wid == 1 && lane == 0) {
+  } else if (gave_up && wid == 1 && elect_one()) {   // the lane that issued the products: a commit is of its own thread's
     if (rank == 0) commit_pair(bars + Q_DRAIN);
     wait_in_flight(bars + Q_DRAIN, 0, p.wait_limit);
   }

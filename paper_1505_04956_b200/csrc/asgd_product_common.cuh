@@ -48,7 +48,7 @@ __device__ inline void mma_f8(unsigned d_tmem, unsigned long long a, unsigned lo
   asm volatile("{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n}"
                ::"r"(d_tmem), "l"(a), "l"(b), "r"(idesc), "r"((unsigned)acc) : "memory");
 }
-// one lane of a whole warp, known as such to the compiler: what it issues takes its operands from uniform registers
+// one lane of a whole warp (the same one every time), known as such to the compiler: what it issues takes its operands from uniform registers
 __device__ inline bool elect_one() {
   unsigned me;
   asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.u32 %0, 1, 0, p;\n}" : "=r"(me));

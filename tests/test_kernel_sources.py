@@ -1,0 +1,22 @@
+"""Rules of the instruction set that no run can show to be kept: read off the kernels' sources."""
+import glob
+import os
+import re
+
+import pytest
+
+CSRC = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_1505_04956_b200", "csrc")
+FILES = sorted(glob.glob(os.path.join(CSRC, "*.cu*")))
+DRAIN = re.compile(r"commit(_pair)?\(bars \+ \w*:?:?\w*DRAIN")
+
+
+@pytest.mark.parametrize("path", [p for p in FILES if DRAIN.search(open(p).read())], ids=os.path.basename)
+def test_what_is_in_flight_is_committed_by_the_thread_that_issued_it(path):
+    """A tcgen05.commit covers what its own thread has issued.  Where an elected lane issues the products, that lane commits before a block that gave
+    up waits for them; where lane 0 does, lane 0."""
+    lines = open(path).read().split("\n")
+    elected = any("elect_one()" in line for line in lines)
+    for i, line in enumerate(lines):
+        if DRAIN.search(line):
+            branch = "\n".join(lines[i - 2:i + 1])
+            assert ("elect_one()" in branch) == elected and ("lane == 0" in branch) != elected, branch
