@@ -797,6 +797,7 @@ expert_layer_kernel(const __grid_constant__ LayerArgs a, const __grid_constant__
       bool met = true;
       if (lane == 0 && (f || !(a.router || share))) met = meet(a.shared, f ? MEET_HIDDEN : MEET_TOKENS, a.wait_limit, abort);      // (the block has met for the tokens already, or not)
       if (!(ok = __all_sync(kAll, met))) break;
+      __syncwarp();                                  // (a vote orders no memory: what lane 0 has met for is there for all lanes)
       const unsigned char* from = f ? a.hq : a.xq;
       const float* from_scales = f ? a.hs : a.xs;
       const int per_block = f ? a.T * a.c.top_k : a.T;
