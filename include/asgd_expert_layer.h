@@ -32,6 +32,7 @@ enum { ASGD_ACT_RELU2 = 0 /* max(u, 0)^2 */, ASGD_ACT_SILU = 1 /* u / (1 + exp(-
  *   a        = act(u), or act(u[i]) * u[h + i]     h numbers
  *   aq       a rounded to E4M3 in blocks of 128
  *   y        = sum_j w_j W2[e_j] aq                d numbers, over the choices in their order (those with an expert)
+ * A token without an expert has y = 0; but NaN where the logits are made here and x or one of its logits is not a number, or x infinite.
  * Everything between is fp32; the products' sums are those of asgd_product, K block by K block of 128, in stretches that depend
  * on the sizes and the loads of the experts alone; y is rounded once.
  *

@@ -624,6 +624,21 @@ __device__ __forceinline__ float activated(float u, bool silu) {
   return u != u ? u : r * r;                         // (the larger of a NaN and 0 would be 0)
 }
 
+// Whether a token has an infinity or a NaN, or a NaN among the logits made from it, by a warp.  Such a token gets no expert, and must not look like one
+// that was left out on purpose.  (Asked for tokens without an expert alone.  Where y is x in place, tiles of it may be written already: with NaNs, if so.)
+__device__ __noinline__ bool not_finite(const LayerArgs& a, int t, int lane) {
+  bool bad = false;
+  for (int e = lane; e < a.c.experts; e += 32) {
+    const float v = __ldcg(a.made_logits + (long long)t * a.c.experts + e);
+    bad = bad || v != v;
+  }
+  for (int k = lane * 4; k < a.d; k += 128) {
+    const float4 v = four(a.x, a.type, t * a.ldx, k, a.d, a.x_wide);
+    bad = bad || !(fabsf(v.x) < INFINITY && fabsf(v.y) < INFINITY && fabsf(v.z) < INFINITY && fabsf(v.w) < INFINITY);
+  }
+  return __any_sync(kAll, bad);
+}
+
 __device__ __forceinline__ void readers_sync() { asm volatile("bar.sync 1, %0;" ::"n"(kReaders * 32) : "memory"); }
 
 __device__ __forceinline__ void tmem_load8(unsigned taddr, float* v) {
@@ -942,6 +957,7 @@ expert_layer_kernel(const __grid_constant__ LayerArgs a, const __grid_constant__
           const int t = u / w.tiles, tile = u % w.tiles, c = tile * 128 + lane * 4;
           if (u != reader) choice = ChoiceAt<BN>(a, plan, t, tile, lane);
           float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
+          if (a.router && !__any_sync(kAll, choice.blocks != 0) && not_finite(a, t, lane)) y.x = y.y = y.z = y.w = __uint_as_float(0x7fffffffu);
           for (int j0 = 0; j0 < K; j0 += 8) {
             float4 z[8];
             const float* from[8];

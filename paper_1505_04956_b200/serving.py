@@ -62,8 +62,9 @@ def asgd_expert_layer(x, w1, w1_scale, w2, w2_scale, top_k, *, logits=None, rout
       w1 [E, h, d], or [E, 2 h, d] (gated: act(u[:h]) * u[h:]), and w2 [E, d, h], 8 bits, with w1_scale [E, ceil(rows / 128),
       ceil(d / 128)] and w2_scale [E, ceil(d / 128), ceil(h / 128)],
     summed with the weights of asgd_route.  The logits are given ([T, E]), or made here: (x @ router.T - shift) * temperature with
-    router [E, d] and shift [E].  `activation` is "relu2" (max(u, 0)^2) or "silu"; score, bias, groups, groups_kept, group_top, renormalise
-    and scale are those of asgd_route.  With `choice` returns y, ids [T, top_k] and weights [T, top_k]."""
+    router [E, d] and shift [E].  A token that no expert takes has zeros, but NaNs where a router made its logits and it is not finite.
+    `activation` is "relu2" (max(u, 0)^2) or "silu"; score, bias, groups, groups_kept, group_top, renormalise and scale are those of
+    asgd_route.  With `choice` returns y, ids [T, top_k] and weights [T, top_k]."""
     if stream is not None:
         return _on(stream, asgd_expert_layer, x, w1, w1_scale, w2, w2_scale, top_k, logits=logits, router=router, shift=shift, temperature=temperature,
                    activation=activation, score=score, bias=bias, groups=groups, groups_kept=groups_kept, group_top=group_top,

@@ -92,3 +92,56 @@ def test_forms_of_the_choice(T, E, top_k, groups, group_top, score, bias, renorm
     pkg.asgd_experts_sync()
     assert torch.equal(got[1], want_ids) and torch.equal(got[2], want_weights)
     _check(x, w1, s1, w2, s2, got, act)
+
+
+NAN_KW = [dict(score="softmax"), dict(score="sigmoid"), dict(score="sigmoid", groups=4, groups_kept=2, group_top=2)]
+
+
+@pytest.mark.parametrize("kw", NAN_KW, ids=["softmax", "sigmoid", "groups"])
+@pytest.mark.parametrize("T", [6, 40])
+@pytest.mark.parametrize("dtype, router, d", [(F32, F32, 256), (BF, F32, 333), (F16, BF, 1030)])
+def test_a_nan_and_an_infinity_reach_their_tokens_results_through_a_router(kw, T, dtype, router, d):
+    """A token that is not finite has no logit to choose by; its result is not one of a token without experts."""
+    g = _gen(T + d)
+    E, top_k, h = 8, 2, 128
+    x = torch.randn(T, d, generator=g, device="cuda").to(dtype)
+    args = (*_matrices(g, E, 2 * h, d), *_matrices(g, E, d, h), top_k)
+    matrix = torch.randn(E, d, generator=g, device="cuda") / d ** 0.5
+    matrix[:, 7] = -matrix[:, 7].abs() - 0.01                                      # an infinity there makes every logit -inf
+    kw = dict(kw, router=matrix.to(router), activation="silu", shift=torch.randn(E, generator=g, device="cuda") * 0.1)
+    want = pkg.asgd_expert_layer(x, *args, **kw)
+    bad = x.clone()
+    bad[1, 0], bad[2, d - 1], bad[3, 7], bad[4, 9] = math.nan, math.nan, math.inf, math.inf
+    got, ids, weights = pkg.asgd_expert_layer(bad, *args, choice=True, **kw)
+    pkg.asgd_experts_sync()
+    assert bool((ids[1:4] == -1).all()) and bool((weights[1:4] == 0).all())
+    assert bool(torch.isnan(got[1:4]).all())
+    assert not bool(torch.isfinite(got[4]).all())
+    keep = [t for t in range(T) if t not in (1, 2, 3, 4)]
+    assert torch.equal(got[keep], want[keep])
+
+
+def test_a_finite_token_whose_logits_overflow_is_not_passed_over():
+    g = _gen(12)
+    E, top_k, d, h = 4, 2, 256, 128
+    x = torch.randn(3, d, generator=g, device="cuda")
+    x[1, :128], x[1, 128:] = 3e38, -3e38                                           # sums of infinities of both signs
+    args = (*_matrices(g, E, 2 * h, d), *_matrices(g, E, d, h), top_k)
+    got, ids, _ = pkg.asgd_expert_layer(x, *args, router=torch.full((E, d), 1e3, device="cuda"), choice=True)
+    pkg.asgd_experts_sync()
+    assert bool((ids[1] == -1).all()) and bool(torch.isnan(got[1]).all())
+
+
+@pytest.mark.parametrize("dtype", [F32, BF])
+def test_finite_tokens_without_an_expert_are_zeros(dtype):
+    g = _gen(11)
+    E, top_k, d, h = 4, 2, 260, 128
+    x = torch.randn(5, d, generator=g, device="cuda").to(dtype)
+    args = (*_matrices(g, E, 2 * h, d), *_matrices(g, E, d, h), top_k)
+    matrix = torch.randn(E, d, generator=g, device="cuda")
+    away = torch.full((E,), math.inf, device="cuda")                               # every expert's shift takes it out
+    assert bool((pkg.asgd_expert_layer(x, *args, router=matrix, shift=away) == 0).all())
+    logits = torch.full((5, E), -math.inf, device="cuda")                          # given logits take the token out, whatever it holds
+    x[2] = math.nan
+    assert bool((pkg.asgd_expert_layer(x, *args, logits=logits) == 0).all())
+    pkg.asgd_experts_sync()
