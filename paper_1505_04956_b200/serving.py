@@ -13,7 +13,7 @@ import functools
 import torch
 
 from . import binding
-from .experts import (_EIGHT, _FLOAT, BLOCK, RouteConfig, SCORES, _chk, _first, _flat, _handle, _ld, _matrix, _need, _new, _on, _scale_of)
+from .experts import (_EIGHT, _FLOAT, BLOCK, RouteConfig, SCORES, _chk, _first, _flat, _handle, _ld, _matrix, _need, _new, _on, _scale_of, _values)
 
 LAYER_EXPORTS = ("asgd_expert_layer_workspace_bytes", "asgd_expert_layer")
 ACTIVATIONS = {"relu2": 0, "silu": 1}
@@ -44,12 +44,15 @@ def _load():
     return _lib
 
 
-@functools.lru_cache(maxsize=256)
 def _config(E, top_k, score, groups, groups_kept, group_top, renormalise, scale, T, d, h, gated, routed):
     """The configuration and the workspace's bytes."""
+    return _config_of(E, *_values(top_k, score, groups, groups_kept, group_top, renormalise, scale), T, d, h, gated, routed)
+
+
+@functools.lru_cache(maxsize=256)
+def _config_of(E, top_k, score, groups, groups_kept, group_top, renormalise, scale, T, d, h, gated, routed):
     _need(score in SCORES, "score must be one of %s", tuple(SCORES))
-    cfg = RouteConfig(E, int(top_k), SCORES[score], int(groups), int(groups if groups_kept is None else groups_kept), int(group_top),
-                      1 if renormalise else 0, 1, float(scale))
+    cfg = RouteConfig(E, top_k, SCORES[score], groups, groups_kept, group_top, renormalise, 1, scale)
     sizes = ExpertLayerArgs(T=T, d=d, h=h, gated=gated, router=1 if routed else None)          # sizes, and which pointers there are
     n = C.c_size_t(0)
     _chk(_load().asgd_expert_layer_workspace_bytes(C.byref(cfg), C.byref(sizes), C.byref(n)), "asgd_expert_layer_workspace_bytes")

@@ -145,3 +145,16 @@ def test_finite_tokens_without_an_expert_are_zeros(dtype):
     x[2] = math.nan
     assert bool((pkg.asgd_expert_layer(x, *args, logits=logits) == 0).all())
     pkg.asgd_experts_sync()
+
+
+def test_a_factor_that_changes_in_place_counts_as_it_is_at_the_call():
+    g = _gen(5)
+    args = _small_layer(g, 8)
+    x, logits = torch.randn(4, 16, generator=g, device="cuda"), torch.randn(4, 8, generator=g, device="cuda")
+    scale = torch.tensor(1.0)
+    for value in (1.0, 2.5):
+        scale.fill_(value)
+        _, _, weights = pkg.asgd_expert_layer(x, *args, 2, logits=logits, scale=scale, choice=True)
+        assert torch.equal(weights, pkg.asgd_expert_layer(x, *args, 2, logits=logits, scale=value, choice=True)[2])
+        assert torch.equal(pkg.asgd_route(logits, 2, scale=scale, plan=False)[1], pkg.asgd_route(logits, 2, scale=value, plan=False)[1])
+    pkg.asgd_experts_sync()
