@@ -148,21 +148,16 @@ def _on(stream, call, *args, **kw):
         return call(*args, **kw)
 
 
-def _values(top_k, score, groups, groups_kept, group_top, renormalise, scale):
-    """A choice's settings as plain values: configurations are kept by them, and a tensor would be known by its identity, whatever it holds by now."""
-    groups = int(groups)
-    return int(top_k), score, groups, groups if groups_kept is None else int(groups_kept), int(group_top), 1 if renormalise else 0, float(scale)
-
-
 def _route_config(E, top_k, score, groups, groups_kept, group_top, renormalise, scale, align, T):
     """The configuration and the workspace's bytes for T tokens."""
-    return _route_config_of(E, *_values(top_k, score, groups, groups_kept, group_top, renormalise, scale), int(align), T)
+    # by plain values: a tensor among them would be known by its identity, whatever it holds by now
+    return _route_config_of(E, int(top_k), score, int(groups), None if groups_kept is None else int(groups_kept), int(group_top), bool(renormalise), float(scale), int(align), T)
 
 
 @functools.lru_cache(maxsize=256)
 def _route_config_of(E, top_k, score, groups, groups_kept, group_top, renormalise, scale, align, T):
     _need(score in SCORES, "score must be one of %s", tuple(SCORES))
-    cfg = RouteConfig(E, top_k, SCORES[score], groups, groups_kept, group_top, renormalise, align, scale)
+    cfg = RouteConfig(E, top_k, SCORES[score], groups, groups if groups_kept is None else groups_kept, group_top, 1 if renormalise else 0, align, scale)
     n = C.c_size_t(0)
     _chk(_load().asgd_route_workspace_bytes(C.byref(cfg), T, C.byref(n)), "asgd_route_workspace_bytes")
     return C.pointer(cfg), n.value

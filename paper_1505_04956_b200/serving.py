@@ -13,7 +13,7 @@ import functools
 import torch
 
 from . import binding
-from .experts import (_EIGHT, _FLOAT, BLOCK, RouteConfig, SCORES, _chk, _first, _flat, _handle, _ld, _matrix, _need, _new, _on, _scale_of, _values)
+from .experts import (_EIGHT, _FLOAT, BLOCK, RouteConfig, SCORES, _chk, _first, _flat, _handle, _ld, _matrix, _need, _new, _on, _scale_of)
 
 LAYER_EXPORTS = ("asgd_expert_layer_workspace_bytes", "asgd_expert_layer")
 ACTIVATIONS = {"relu2": 0, "silu": 1}
@@ -46,13 +46,14 @@ def _load():
 
 def _config(E, top_k, score, groups, groups_kept, group_top, renormalise, scale, T, d, h, gated, routed):
     """The configuration and the workspace's bytes."""
-    return _config_of(E, *_values(top_k, score, groups, groups_kept, group_top, renormalise, scale), T, d, h, gated, routed)
+    return _config_of(E, int(top_k), score, int(groups), None if groups_kept is None else int(groups_kept), int(group_top), bool(renormalise), float(scale),
+                      T, d, h, gated, routed)                              # (by plain values, see _route_config)
 
 
 @functools.lru_cache(maxsize=256)
 def _config_of(E, top_k, score, groups, groups_kept, group_top, renormalise, scale, T, d, h, gated, routed):
     _need(score in SCORES, "score must be one of %s", tuple(SCORES))
-    cfg = RouteConfig(E, top_k, SCORES[score], groups, groups_kept, group_top, renormalise, 1, scale)
+    cfg = RouteConfig(E, top_k, SCORES[score], groups, groups if groups_kept is None else groups_kept, group_top, 1 if renormalise else 0, 1, scale)
     sizes = ExpertLayerArgs(T=T, d=d, h=h, gated=gated, router=1 if routed else None)          # sizes, and which pointers there are
     n = C.c_size_t(0)
     _chk(_load().asgd_expert_layer_workspace_bytes(C.byref(cfg), C.byref(sizes), C.byref(n)), "asgd_expert_layer_workspace_bytes")
