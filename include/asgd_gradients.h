@@ -33,7 +33,7 @@ typedef struct asgd_gradient {
 int asgd_gradients_workspace_bytes(int64_t count, size_t *bytes /* HOST out */);
 
 /* norm[0] = sqrt(sum of x^2 over all numbers of all tensors): sums in fp64, in an order that depends on the tensors'
- * sizes and types alone; rounded once to fp32.  0 without numbers; infinite or NaN where a number is, or where the norm passes fp32's
+ * sizes, types and addresses modulo 32 alone (other addresses may change the last bit); rounded once to fp32.  0 without numbers; infinite or NaN where a number is, or where the norm passes fp32's
  * range.  `workspace`: 16-byte aligned. */
 int asgd_grad_norm(const asgd_gradient *list, int64_t count, float *norm, void *workspace, size_t workspace_bytes,
                    void *stream);

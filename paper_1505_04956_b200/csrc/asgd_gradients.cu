@@ -35,7 +35,7 @@ template <int N> struct List {
   unsigned char type[N];
   int count;
 };
-constexpr int kFew = 64, kMany = 640;                // tensors that a launch's parameters hold (21.8 KB of 32 at most)
+constexpr int kFew = 64, kMany = 640;                // tensors that a launch's parameters hold (21.1 KB of 32 at most)
 static_assert(sizeof(List<kMany>) < 32000, "kernel parameters");
 
 __device__ __forceinline__ double block_sum(double v) {
@@ -59,7 +59,7 @@ template <typename T> __device__ __forceinline__ void unpack(const Piece& p, flo
   for (int i = 0; i < kPer<T>; ++i) v[i] = Elem<T>::to_f(e[i]);
 }
 // Pieces are those of memory, 32 bytes from a multiple of 32 on, so that a view that begins anywhere is read whole piece by whole piece;
-// its first and last ones may have numbers that are not its own.
+// its first and last ones may have numbers that are not its own.  (So which numbers a thread adds up depends on where the view begins in a piece.)
 template <typename T> __device__ __forceinline__ int skipped(const T* x) { return (int)(reinterpret_cast<unsigned long long>(x) & (kPiece - 1)) / (int)sizeof(T); }
 // Piece u of a tensor of n numbers behind `skip`; zeros for numbers that are not its own.
 template <typename T> __device__ __forceinline__ Piece load_piece(const T* x, long long n, long long u, int skip) {
@@ -145,7 +145,7 @@ template <int N> __device__ __forceinline__ int tensor_of(const List<N>& l, long
 }
 template <int N> __device__ __forceinline__ void stretch(const List<N>& l, long long& from, long long& to) {
   const long long all = l.first[l.count];
-  from = all * blockIdx.x / gridDim.x;               // at most 2^45 * 296
+  from = all * blockIdx.x / gridDim.x;               // below 2^55: 640 tensors of 2^37 pieces and one (2^40 numbers of fp32) by 296 blocks
   to = all * (blockIdx.x + 1ll) / gridDim.x;
 }
 
