@@ -1,4 +1,4 @@
-"""The choice of experts in the whole layer's kernel is that of asgd_route, to the last bit.
+"""The choice of experts in the whole layer's kernel is that of asgd_route, to the last bit; and forms of the call around it.
 
 Both compute a score by the same operations in the same order (the softmax's sum over the lanes that asgd_route gives a token, the renormalising sum
 over the lanes that hold its choices), so ids and weights are equal bit by bit, whatever hangs on the last one.  The logits here differ by some
@@ -92,6 +92,51 @@ def test_forms_of_the_choice(T, E, top_k, groups, group_top, score, bias, renorm
     pkg.asgd_experts_sync()
     assert torch.equal(got[1], want_ids) and torch.equal(got[2], want_weights)
     _check(x, w1, s1, w2, s2, got, act)
+
+
+@pytest.mark.parametrize("T, router", [(1, F32), (9, BF), (50, F16)])
+def test_a_router_without_shift(T, router):
+    g = _gen(T)
+    E, top_k, d, h = 24, 3, 300, 100
+    x = torch.randn(T, d, generator=g, device="cuda")
+    w1, s1 = _matrices(g, E, h, d)
+    w2, s2 = _matrices(g, E, d, h)
+    matrix = (torch.randn(E, d, generator=g, device="cuda") / d ** 0.5).to(router)
+    got = pkg.asgd_expert_layer(x, w1, s1, w2, s2, top_k, router=matrix, temperature=0.5, choice=True)
+    zero = pkg.asgd_expert_layer(x, w1, s1, w2, s2, top_k, router=matrix, shift=torch.zeros(E, device="cuda"), temperature=0.5, choice=True)
+    pkg.asgd_experts_sync()
+    assert all(torch.equal(a, b) for a, b in zip(got, zero))
+    _check(x, w1, s1, w2, s2, got, "relu2")
+    want_ids, _ = pkg.asgd_route(((x.double() @ matrix.double().t()) * 0.5).float(), top_k, plan=False)
+    assert int((got[1] != want_ids).any(1).sum()) <= 1                             # a token whose choice hangs on the last bits
+
+
+@pytest.mark.parametrize("T, E, top_k", [(128, 16, 2), (100, 64, 8), (70, 200, 1), (31, 3, 3), (16, 300, 2)])
+def test_one_expert_has_all_tokens(T, E, top_k):
+    """Several chunks of one expert, where the mean load is a small one."""
+    g = _gen(T * E)
+    d, h = 256, 200
+    x = torch.randn(T, d, generator=g, device="cuda").to(BF)
+    w1, s1 = _matrices(g, E, 2 * h, d)
+    w2, s2 = _matrices(g, E, d, h)
+    logits = torch.randn(T, E, generator=g, device="cuda")
+    logits[:, E // 2] = 9.0
+    got = pkg.asgd_expert_layer(x, w1, s1, w2, s2, top_k, logits=logits, activation="silu", choice=True)
+    pkg.asgd_experts_sync()
+    assert bool((got[1][:, 0] == E // 2).all())
+    _check(x, w1, s1, w2, s2, got, "silu")
+
+
+@pytest.mark.parametrize("E, top_k, d, h, gated, logits", [(2, 1, 65536, 16, True, True), (2, 2, 16, 65536, False, False), (1, 1, 4104, 32768, True, False)])
+def test_the_widest_layers(E, top_k, d, h, gated, logits):
+    g = _gen(d + h)
+    x = torch.randn(3, d, generator=g, device="cuda")
+    w1, s1 = _matrices(g, E, h * (2 if gated else 1), d)
+    w2, s2 = _matrices(g, E, d, h)
+    kw = dict(logits=torch.randn(3, E, generator=g, device="cuda")) if logits else dict(router=torch.randn(E, d, generator=g, device="cuda") / d ** 0.5)
+    got = pkg.asgd_expert_layer(x, w1, s1, w2, s2, top_k, activation="silu", choice=True, **kw)
+    pkg.asgd_experts_sync()
+    _check(x, w1, s1, w2, s2, got, "silu", min_tight=False)
 
 
 NAN_KW = [dict(score="softmax"), dict(score="sigmoid"), dict(score="sigmoid", groups=4, groups_kept=2, group_top=2)]
