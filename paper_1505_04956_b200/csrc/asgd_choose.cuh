@@ -1,5 +1,6 @@
-// The choice of a token's experts by the lanes of a warp, shared by the kernels that route.  The contract is that of asgd_route
-// in include/asgd_experts.h; how it works and what it costs stands in asgd_route.cu.
+// The choice of a token's experts by the lanes of a warp.  The contract is that of asgd_route in include/asgd_experts.h; how it works and what it
+// costs stands in asgd_route.cu.  The kernel of a whole layer (asgd_expert_layer.cu) takes the scores, the keys and the checks from here and has
+// shorter code of its own around them; an order of sums that changes here changes there.
 #pragma once
 
 #include "asgd_experts_common.cuh"

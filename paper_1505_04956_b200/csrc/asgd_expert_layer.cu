@@ -18,9 +18,9 @@
 // A tile is 128 rows of W (the MMA's M) by BN tokens of one expert (its N; an expert with more has several chunks); a
 // K block's products leave tensor memory and are added, scaled, in registers, as in asgd_product_few.cuh.
 //
-// What bounds it: one token of 128 experts (d 2048, h 768 gated, top 8) takes 28.4 us, of which its 39 MB need 6; the rest is a chain of
+// What bounds it: one token of 128 experts (d 2048, h 768 gated, top 8) takes 29 us, of which its 39 MB need 6; the rest is a chain of
 // steps that wait for one another (choice and plan 6, the meetings 5, activation 2, first bytes and last sums of either product 5, the launch 3).
-// Eight tokens of 256 experts take 44 us (181 MB, 28 of them), 60 tokens 55 (186 MB): the weights come at 5 to 7 TB/s once they are on their
+// Eight tokens of 256 experts take 44 to 47 us, by the drawn choices (181 MB, 28 of them), 60 tokens 55 (186 MB): the weights come at 5 to 7 TB/s once they are on their
 // way.  On the way there, 8 tokens: one warp that brings the tokens' rows 48, four 44.5; scales asked for before W1's copies are on their way
 // 53; the sums of a token's eight choices one after another 6 of them, together 2.
 //
@@ -1013,7 +1013,9 @@ __global__ void begin_kernel(Shared* sh) {
 
 constexpr size_t up256(size_t n) { return (n + 255) / 256 * 256; }
 
-// Tokens of a tile: an expert's as a rule fit into one chunk (its weights then are read once).
+// Tokens of a tile, by the mean load of an expert: with even loads an expert's tokens fit into one chunk, and its weights are read once.  Uneven loads
+// give popular experts several chunks, each of which reads the weights again: drawn loads with twice and three times the mean made the run of K blocks 10 % longer for
+// 60 tokens of 32 experts (top 4), 12 % for 128 of 64 and 16 % for 128 of 128 (top 8), a fifth at most; up to 16 tokens of 64 experts none.
 int tokens_of(long long assignments, int experts) {
   const double mean = (double)assignments / experts;
   return mean <= 8 ? 16 : mean <= 18 ? 32 : 64;

@@ -78,7 +78,9 @@ class Layer:
         return tuple(eight_bits(w)[0] for w in (self.w1, self.w2))
 
     def serve(self, x, weights=None):
-        """y of the few tokens of a serving step (128 at most), of x's type, in one call; `weights` as eight_bits() gives them."""
+        """y of the few tokens of a serving step (128 at most, 1024 choices of experts), of x's type; `weights` as eight_bits() gives them.
+        With them it is one call of the library; without, every matrix is rounded to 8 bits first, in every call.  Numbers between the two products are
+        fp32 here, while forward() rounds the first one's results to bf16, so the two differ by some per cent of y's norm."""
         (w1, s1), (w2, s2) = self.eight_bits() if weights is None else weights
         return asgd_expert_layer(x, w1, s1, w2, s2, self.top_k, router=self.router, shift=self.shift, temperature=self.temperature,
                                  activation="relu2", score="sigmoid", bias=self.bias)
